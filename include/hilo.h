@@ -63,8 +63,14 @@ enum {
  * separate low-frequency mode, shape.lf > 0). */
 enum { HILO_KEEP = 0, HILO_POOL2 = 1, HILO_POOL4 = 2, HILO_LF = 3 };
 
-/* Input dtypes of hilo_block_forward (HILO_F16: hilo_quantize_rows_e4m3). */
-enum { HILO_BF16 = 0, HILO_F32 = 1, HILO_F16 = 2 };
+/* Input dtypes of hilo_block_forward (HILO_F16: hilo_quantize_rows_e4m3;
+ * HILO_E4M3: an output of hilo_gate_norm). */
+enum { HILO_BF16 = 0, HILO_F32 = 1, HILO_F16 = 2, HILO_E4M3 = 3 };
+
+/* Norms of hilo_gate_norm and hilo_block_forward_mod, over a row's d channels:
+ * LAYER (x - mean) / sqrt(var + eps) with the biased variance, RMS
+ * x / sqrt(mean(x^2) + eps). */
+enum { HILO_NORM_NONE = 0, HILO_NORM_LAYER = 1, HILO_NORM_RMS = 2 };
 
 /*
  * Problem shape.
@@ -479,6 +485,226 @@ int hilo_block_forward_static_ws(const hilo_shape* shape, const hilo_block_weigh
  * once at load time (no counterpart in the paper).
  */
 int hilo_convert_bf16_to_f16(const void* src, void* dst, size_t n, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Positions, modulation and packed attention. The paper's block (Sec. 2.1) is
+ * conditioned on the time step and tells tokens apart by their place in the
+ * image, and its prompts come from a text encoder; the paper gives no formulas
+ * for these, so the ones below are this library's.
+ * ---------------------------------------------------------------------------
+ *
+ * hilo_row_positions -- where the rows of the row space are, for hilo_rope:
+ * three coordinates (time, height, width) per row.
+ *   split   outputs of hilo_split or hilo_split_regions
+ *   origin  the coordinates of the grid's token (0, 0) and of the text:
+ *           image rows (t_img, h0 + p, w0 + q), where (p, q) is the token of a
+ *           kept row, the mean of the class members of a pooled window, and
+ *           the middle of a low-frequency window; row j of an image's text
+ *           txt0 + j * txt_step on all three axes
+ *   pos     fp32 [B*T + cap, 3] device; the text rows and the first cu_img[B]
+ *           image rows (at most cap) are written, the rest is left as it was
+ * A mean is the exact sum divided once, correctly rounded; then h0 or w0 is
+ * added.
+ */
+typedef struct {
+  float t_img, h0, w0, txt0, txt_step;
+} hilo_positions_origin;
+
+int hilo_row_positions(const hilo_shape* shape, const hilo_split_out* split, const hilo_positions_origin* origin,
+                       float* pos, int32_t cap, void* stream);
+
+/*
+ * The rotation of hilo_rope. A head's first D = axis_dims[0] + ... +
+ * axis_dims[axes - 1] channels are D/2 pairs; the rest of the head is copied.
+ *   axes         1 to 4; axis_dims[a] even and >= 2; D a multiple of 16, at
+ *                most head_dim
+ *   interleaved  1: pair i is channels (2i, 2i + 1); 0: channels (i, i + D/2)
+ *   per_axis     which frequency pair i has, of axis a: its number j among the
+ *                pairs of its axis gives theta^(-2j / axis_dims[a]) (1), or its
+ *                number among all pairs theta^(-2i / D) (0). The axes own
+ *                consecutive pairs, in order.
+ *   theta        > 1, finite
+ */
+typedef struct {
+  int32_t axes;
+  int32_t axis_dims[4];
+  int32_t interleaved, per_axis;
+  double theta;
+} hilo_rotation;
+
+/*
+ * Rows of hilo_rope: x and y are [rows, heads, head_dim] with head_dim (a
+ * multiple of 8, at most 256) contiguous and strides in elements between rows
+ * and heads: positive multiples of 16 bytes. y's rows and heads must not
+ * overlap. dtype HILO_BF16, HILO_F16 or HILO_F32.
+ */
+typedef struct {
+  int32_t rows, heads, head_dim, dtype;
+  int64_t x_row, x_head, y_row, y_head;
+  hilo_rotation rot;
+} hilo_rope_shape;
+
+/*
+ * hilo_rope -- rotary positions with one to four axes: pair (a, b) of axis k
+ * of row r becomes (a cos t - b sin t, a sin t + b cos t), t = pos[r][k] times
+ * the pair's frequency.
+ *   x       device, 16-byte aligned
+ *   pos     fp32 [rows, axes] device, any finite values (pooled rows stand
+ *           between tokens); the angle is formed and reduced to one turn with
+ *           more than 32 bits, so far positions lose nothing
+ *   n_rows  device, or NULL for all: the first min(*n_rows, rows) rows are
+ *           rotated, y's others are left as they were
+ *   y       device, 16-byte aligned; y == x with x's strides rotates in place
+ *           (else the two must not overlap)
+ * Products and sums are fp32, rounded once to the dtype. Rotating by the
+ * negated positions undoes it and is its gradient.
+ */
+int hilo_rope(const hilo_rope_shape* shape, const void* x, const float* pos, const int32_t* n_rows, void* y,
+              void* stream);
+
+/*
+ * Vectors of one stream (text or image) for hilo_gate_norm, all 16-byte
+ * aligned device pointers of one dtype (hilo_norm_shape.vec_dtype), each may
+ * be NULL: gate (1), scale (0), shift (0) have a row of d elements per image,
+ * vec_row elements apart; w_branch (1), w_norm (1), b_norm (0) are [d], one
+ * for all images.
+ */
+typedef struct {
+  const void *gate, *scale, *shift, *w_branch, *w_norm, *b_norm;
+} hilo_norm_vectors;
+
+/*
+ *   B, T, cap        the row space: B*T text rows, then up to cap image rows
+ *   d                a multiple of 8 in [8, 4096]
+ *   norm             HILO_NORM_*: of the residual row, before the next sub-layer
+ *   norm_branch      HILO_NORM_*: of the branch row y, before its gate
+ *   u_dtype, y_dtype, u_out_dtype, vec_dtype   HILO_BF16 or HILO_F32
+ *   h_dtype          HILO_BF16, HILO_F16 (saturating), HILO_F32 or HILO_E4M3
+ *   eps              >= 0, of both norms; resid_scale finite
+ *   vec_row          elements between the images' gate, scale and shift rows,
+ *                    a multiple of 8 (>= 0; 0: all images share one)
+ */
+typedef struct {
+  int32_t B, T, cap, d;
+  int32_t norm, norm_branch;
+  int32_t u_dtype, y_dtype, u_out_dtype, h_dtype, vec_dtype;
+  float eps, resid_scale;
+  int64_t vec_row;
+} hilo_norm_shape;
+
+/*
+ * hilo_gate_norm -- what stands between two sub-layers of a conditioned block,
+ * in one pass over the rows of the row space:
+ *     z  = norm_branch(y) * w_branch
+ *     u' = resid_scale * u + gate * z
+ *     h  = (norm(u') * w_norm + b_norm) * (1 + scale) + shift
+ * each row with the vectors of its stream and image.
+ *   txt, img       the streams' vectors (txt may be NULL with T == 0)
+ *   cu_img         int32 [B+1] device, as in hilo_block_forward
+ *   u_txt, u_img   [B*T, d] and [cap, d], u_dtype (u_txt may be NULL with T == 0)
+ *   y              [B*T + cap, d], y_dtype, or NULL: u' = u, and u_out is NULL
+ *   u_out          [B*T + cap, d], u_out_dtype, or NULL: u' is not stored.
+ *                  In place (u_txt == u_out, u_img == u_out + B*T*d) is
+ *                  allowed where the dtypes are the same.
+ *   h              [B*T + cap, d], h_dtype, or NULL; with HILO_E4M3 each row is
+ *                  quantised as by hilo_quantize_rows_e4m3 and
+ *   h_scale        fp32 [B*T + cap] gets its scale (else may be NULL)
+ * All row pointers 16-byte aligned; buffers that are written overlap no other
+ * one, but for the in-place use. The norm takes u' before it is rounded to
+ * u_out_dtype. Sums, norms and products are fp32; the variance is a second
+ * pass over the row's registers. Rows from B*T + cu_img[B] on are left as they
+ * were.
+ */
+int hilo_gate_norm(const hilo_norm_shape* shape, const hilo_norm_vectors* txt, const hilo_norm_vectors* img,
+                   const int32_t* cu_img, const void* u_txt, const void* u_img, const void* y, void* u_out, void* h,
+                   float* h_scale, void* stream);
+
+/*
+ * Sequences of hilo_attention.
+ *   B                sequences (>= 1)
+ *   heads, kv_heads  heads of q and of k and v; kv_heads divides heads, query
+ *                    head i reads key head i / (heads / kv_heads), and heads /
+ *                    kv_heads is at most 128
+ *   head_dim         64 or 128
+ *   causal           1: the last query of a sequence sees all its keys, each
+ *                    one before it one key less; 0: every query sees every key
+ *   dtype            HILO_BF16 or HILO_F16 (q, k, v and out)
+ *   rows_q, rows_k   rows of q and out, of k and v
+ *   scale            of the logits, > 0 and finite; 0: 1 / sqrt(head_dim)
+ *   *_row, *_head    strides in elements between the rows and heads of q, k, v
+ *                    and out: positive multiples of 8, below 2^39 (of one head
+ *                    or one row the stride does not matter, but must be valid).
+ *                    out's rows and heads must not overlap.
+ */
+typedef struct {
+  int32_t B, heads, kv_heads, head_dim, causal, dtype, rows_q, rows_k;
+  float scale;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+} hilo_attn_shape;
+
+/* Workspace bytes hilo_attention needs (0 for an invalid shape). */
+size_t hilo_attention_workspace_bytes(const hilo_attn_shape* shape);
+
+/*
+ * hilo_attention -- softmax attention over packed sequences of different
+ * length, with grouped heads: whole prompts, chunks of new tokens over what is
+ * there already, and single tokens. The queries of sequence b are rows
+ * cu_q[b] .. cu_q[b+1] - 1 of q, its keys and values rows cu_k[b] ..
+ * cu_k[b+1] - 1 of k and v; with causal, query i of lq sees the keys up to
+ * i + lk - lq. A query that sees no key gives zeros.
+ *   cu_q, cu_k  int32 [B+1] device, non-decreasing; on the device they are cut
+ *               to [0, rows_q] and [0, rows_k], so no offset reads or writes
+ *               outside the buffers
+ *   q, k, v     device, 16-byte aligned. Rows outside the sequences are not
+ *               part of any result, nor are keys that a query does not see,
+ *               whatever their values.
+ *   out         device, 16-byte aligned, overlaps no input; rows outside the
+ *               sequences are left as they were
+ *   ws          hilo_attention_workspace_bytes of device memory, 16-byte
+ *               aligned; nothing in it has to be set. Calls that may overlap
+ *               on the device need workspaces of their own.
+ * Logits, maxima and sums are fp32; probabilities enter the product with v in
+ * the dtype; the result is rounded once. A call repeats itself bit for bit.
+ */
+int hilo_attention(const hilo_attn_shape* shape, const int32_t* cu_q, const int32_t* cu_k, const void* q,
+                   const void* k, const void* v, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Conditioning of hilo_block_forward_mod, for both sub-layers (attn, mlp) and
+ * both streams: scale, shift, w_norm and b_norm of the norm before the
+ * sub-layer, gate and w_branch of its output. norm, norm_branch, vec_dtype,
+ * vec_row, eps and resid_scale as in hilo_norm_shape (norm must not be
+ * HILO_NORM_NONE).
+ *   pos  fp32 [B*T + cap, rot.axes] device (e.g. hilo_row_positions), or NULL:
+ *        q and k are not rotated, and rot is not read
+ */
+typedef struct {
+  int32_t norm, norm_branch, vec_dtype;
+  float eps, resid_scale;
+  int64_t vec_row;
+  hilo_norm_vectors txt_attn, img_attn, txt_mlp, img_mlp;
+  const float* pos;
+  hilo_rotation rot;
+} hilo_block_mod;
+
+/*
+ * hilo_block_forward_mod -- hilo_block_forward conditioned on the time step
+ * and on positions: for each stream s
+ *     a  = Attn(rope(((norm(u) w + b) (1 + scale) + shift) W_qkv^s + b_qkv^s))
+ *     u  = resid_scale u + gate * norm_branch(a W_o^s + b_o^s)
+ *     u  = resid_scale u + gate * norm_branch(MLP((norm(u) w + b) (1 + scale) + shift))
+ * with the vectors of the sub-layer, the stream and the row's image, and the
+ * rotation on the q and k heads of every row. The sub-layers' outputs are
+ * rounded to bf16 before their norm and gate, as the attention's inputs are.
+ *   n_img  fp32 [cap] device: proportional attention as in
+ *          hilo_block_forward_prop; NULL: every key weighs 1
+ * Other arguments, layouts, in-place use and errors as hilo_block_forward,
+ * with hilo_block_workspace_bytes of workspace.
+ */
+int hilo_block_forward_mod(const hilo_shape* shape, const hilo_block_weights* weights, const hilo_block_mod* mod,
+                           const int32_t* cu_img, int32_t cap, const void* in_txt, const void* in_img, int in_dtype,
+                           const float* n_img, float* out, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Instrumentation (no counterpart in the paper; used by the benchmark).

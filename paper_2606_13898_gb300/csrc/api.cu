@@ -103,6 +103,60 @@ int check_split(const hilo_split_out* sp) {
   return HILO_OK;
 }
 
+// Whether every pointer is on a 16-byte boundary (NULL is).
+template <typename... P>
+bool aligned16(P... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & 15) == 0;
+}
+
+bool is_bf16_or_f32(int t) { return t == HILO_BF16 || t == HILO_F32; }
+bool is_norm(int n) { return n == HILO_NORM_NONE || n == HILO_NORM_LAYER || n == HILO_NORM_RMS; }
+bool is_finite(float v) { return v - v == 0.0f; }
+
+bool vectors_aligned(const hilo_norm_vectors& v) {
+  return aligned16(v.gate, v.scale, v.shift, v.w_branch, v.w_norm, v.b_norm);
+}
+
+// The norms and vectors that hilo_gate_norm and hilo_block_forward_mod share.
+int check_norm(const char* fn, int norm, int norm_branch, int vec_dtype, int64_t vec_row, float eps, float resid_scale) {
+  if (!is_norm(norm) || !is_norm(norm_branch)) return fail(HILO_ERR_ARG, "%s: norm=%d, norm_branch=%d", fn, norm, norm_branch);
+  if (!is_bf16_or_f32(vec_dtype)) return fail(HILO_ERR_ARG, "%s: vec_dtype=%d", fn, vec_dtype);
+  if (vec_row < 0 || vec_row % 8 || vec_row > (int64_t{1} << 39))
+    return fail(HILO_ERR_ARG, "%s: vec_row=%lld must be a multiple of 8, in [0, 2^39]", fn, static_cast<long long>(vec_row));
+  if (!(eps >= 0.0f) || !is_finite(eps) || !is_finite(resid_scale))
+    return fail(HILO_ERR_ARG, "%s: eps and resid_scale must be finite, eps >= 0", fn);
+  return HILO_OK;
+}
+
+int check_rotation(const char* fn, const hilo_rotation& r, int head_dim) {
+  if (r.axes < 1 || r.axes > 4) return fail(HILO_ERR_SHAPE, "%s: axes=%d must be 1 to 4", fn, r.axes);
+  int D = 0;
+  for (int k = 0; k < r.axes; ++k) {
+    if (r.axis_dims[k] < 2 || r.axis_dims[k] % 2 || r.axis_dims[k] > head_dim)
+      return fail(HILO_ERR_SHAPE, "%s: axis_dims[%d]=%d must be even, in [2, head_dim]", fn, k, r.axis_dims[k]);
+    D += r.axis_dims[k];
+  }
+  if (D % 16 || D > head_dim)
+    return fail(HILO_ERR_SHAPE, "%s: %d rotated channels must be a multiple of 16, at most head_dim=%d", fn, D, head_dim);
+  if ((r.interleaved & ~1) || (r.per_axis & ~1))
+    return fail(HILO_ERR_ARG, "%s: interleaved=%d and per_axis=%d must be 0 or 1", fn, r.interleaved, r.per_axis);
+  if (!(r.theta > 1.0) || !(r.theta < 1e300)) return fail(HILO_ERR_ARG, "%s: theta must be finite and > 1", fn);
+  return HILO_OK;
+}
+
+// Strides of a [rows, heads, head_dim] tensor: positive multiples of `step` elements, below 2^39.
+bool good_strides(int64_t row, int64_t head, int step) {
+  const int64_t most = int64_t{1} << 39;
+  return row > 0 && head > 0 && row % step == 0 && head % step == 0 && row < most && head < most;
+}
+
+// Whether no two (row, head) of the tensor share elements: heads within rows, or rows within heads.
+bool disjoint(int64_t rows, int64_t heads, int64_t dim, int64_t row, int64_t head) {
+  if (heads == 1) return rows == 1 || row >= dim;
+  if (rows == 1) return head >= dim;
+  return (head >= dim && row >= (heads - 1) * head + dim) || (row >= dim && head >= (rows - 1) * row + dim);
+}
+
 inline size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
 struct BlockWs {
@@ -188,6 +242,20 @@ bool encode_tmap_2d(CUtensorMap* map, TmapType type, const void* base, uint64_t 
   return r == CUDA_SUCCESS;
 }
 
+bool encode_tmap_16bit_3d(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, uint64_t n2, uint64_t stride1,
+                          uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {n0, n1, n2};
+  cuuint64_t strides[2] = {stride1 * 2, stride2 * 2};
+  cuuint32_t box[3] = {box0, box1, box2};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 bool encode_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                          uint64_t row_stride_elems, uint32_t box_inner, uint32_t box_outer) {
   return encode_tmap_2d(map, TMAP_BF16, base, inner, outer, row_stride_elems, box_inner, box_outer);
@@ -235,10 +303,11 @@ int hilo_sync_status(void* stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "hilo_sync_status: stream");
   const int g = hilo::gemm_take_device_error();
-  const int a = hilo::attn_take_device_error();
+  const int a1 = hilo::attn_take_device_error(), a2 = hilo::attn_var_take_device_error();
+  const int a = a1 ? a1 : a2;
   const int pr = hilo::probe_take_device_error();
   const int dc = hilo::dcheck_take_bw();
-  if (g < 0 || a < 0 || pr < 0 || dc < 0)
+  if (g < 0 || a1 < 0 || a2 < 0 || pr < 0 || dc < 0)
     return fail(HILO_ERR_CUDA, "hilo_sync_status: reading the device error word failed");
   if (g || a || pr)
     return fail(HILO_ERR_TIMEOUT, "device-side wait ran out (gemm=%d, attention=%d, probe=%d)", g, a, pr);
@@ -361,13 +430,28 @@ size_t hilo_block_workspace_bytes(const hilo_shape* shape, int32_t cap) {
   return block_ws_layout(shape, cap).total;
 }
 
+static int check_mod(const hilo_block_mod& m, const hilo_shape* shape) {
+  const char* fn = "hilo_block_forward_mod";
+  int st = check_norm(fn, m.norm, m.norm_branch, m.vec_dtype, m.vec_row, m.eps, m.resid_scale);
+  if (st) return st;
+  if (m.norm == HILO_NORM_NONE) return fail(HILO_ERR_ARG, "%s: norm must not be HILO_NORM_NONE", fn);
+  if (!vectors_aligned(m.img_attn) || (shape->mlp && !vectors_aligned(m.img_mlp)) ||
+      (shape->T > 0 && (!vectors_aligned(m.txt_attn) || (shape->mlp && !vectors_aligned(m.txt_mlp)))))
+    return fail(HILO_ERR_ARG, "%s: vectors must be 16-byte aligned", fn);
+  if (reinterpret_cast<uintptr_t>(m.pos) & 3) return fail(HILO_ERR_ARG, "%s: pos must be 4-byte aligned", fn);
+  return m.pos ? check_rotation(fn, m.rot, shape->d / shape->heads) : HILO_OK;
+}
+
 // The block of hilo_block_forward; n_img != NULL selects proportional
-// attention (hilo_block_forward_prop).
+// attention (hilo_block_forward_prop), mod != NULL the conditioned block
+// (hilo_block_forward_mod).
 static int block_forward_impl(const hilo_shape* shape, const hilo_block_weights* w, const int32_t* cu_img,
                               int32_t cap, const void* in_txt, const void* in_img, int in_dtype,
-                              const float* n_img, float* out, void* ws, size_t ws_bytes, void* stream) {
+                              const float* n_img, const hilo_block_mod* mod, float* out, void* ws, size_t ws_bytes,
+                              void* stream) {
   int st = check_shape(shape, true);
   if (st) return st;
+  if (mod && (st = check_mod(*mod, shape))) return st;
   if (!w || !cu_img || !in_img || !out) return fail(HILO_ERR_ARG, "hilo_block_forward: NULL pointer");
   if (shape->T > 0 && !in_txt) return fail(HILO_ERR_ARG, "hilo_block_forward: in_txt is NULL with T>0");
   if ((reinterpret_cast<uintptr_t>(in_txt) | reinterpret_cast<uintptr_t>(in_img) |
@@ -402,13 +486,44 @@ static int block_forward_impl(const hilo_shape* shape, const hilo_block_weights*
   const bool in_place = in_f32 && in_txt == out && in_img == out + static_cast<size_t>(BT) * d;
   const bool in_place_img = in_f32 && BT == 0 && in_img == out;
 
+  // The conditioned block's rows between two sub-layers: y (the first one's
+  // output, or NULL) gated into the residual with the vectors of `gate`, the
+  // norm of the next one with those of `norm`.
+  auto gate_norm = [&](const void* u_txt, const void* u_img, int u_dtype, const void* y, const hilo_norm_vectors* gate,
+                       const hilo_norm_vectors* norm, void* h, int h_dtype) {
+    hilo::NormArgs a = {};
+    a.s = {B, T, cap, d, mod->norm, mod->norm_branch, u_dtype, HILO_BF16, HILO_F32, h_dtype, mod->vec_dtype, mod->eps,
+           mod->resid_scale, mod->vec_row};
+    for (int i = 0; i < 2; ++i) {
+      if (norm) a.vec[i] = norm[i];
+      a.vec[i].gate = gate ? gate[i].gate : nullptr;
+      a.vec[i].w_branch = gate ? gate[i].w_branch : nullptr;
+    }
+    a.cu_img = cu_img;
+    a.u_txt = u_txt;
+    a.u_img = u_img;
+    a.y = y;
+    a.u_out = y ? out : nullptr;
+    a.h = h;
+    cudaError_t ge = hilo::launch_gate_norm(a, dev.num_sms, s);
+    if (ge == cudaSuccess) count(1);
+    return ge;
+  };
+  const hilo_norm_vectors none = {};
+  const hilo_norm_vectors mod_attn[2] = {mod ? mod->txt_attn : none, mod ? mod->img_attn : none};
+  const hilo_norm_vectors mod_mlp[2] = {mod ? mod->txt_mlp : none, mod ? mod->img_mlp : none};
+
   stage_mark(0, s);
   // the residual is read from the input by the out-projection epilogue (no
   // fp32 copy of it is made) unless the input already is the output buffer
-  cudaError_t e = hilo::launch_layernorm(in_txt, in_img, in_f32, ln, 0, nullptr, cu_img, B, BT, cap, d,
-                                         dev.num_sms, s);
+  cudaError_t e;
+  if (mod) {
+    e = gate_norm(in_txt, in_img, in_dtype, nullptr, nullptr, mod_attn, ln, HILO_BF16);
+  } else {
+    e = hilo::launch_layernorm(in_txt, in_img, in_f32, ln, 0, nullptr, cu_img, B, BT, cap, d, dev.num_sms, s);
+    if (e == cudaSuccess) count(1);
+  }
   if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: layernorm 1");
-  count(1);
   stage_mark(1, s);
 
   auto gemm = [&](const void* A, int op_f16, int N, int K, int epi, void* o,
@@ -434,6 +549,14 @@ static int block_forward_impl(const hilo_shape* shape, const hilo_block_weights*
   };
   e = gemm(ln, 0, 3 * d, d, hilo::EPI_BIAS_BF16, qkv, w->txt.w_qkv, w->txt.b_qkv, w->img.w_qkv, w->img.b_qkv);
   if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: qkv gemm");
+  if (mod && mod->pos) {
+    // the q and k heads of a row are neighbours: one rotation, in place
+    const int hd = d / shape->heads;
+    const hilo_rope_shape rs = {R, 2 * shape->heads, hd, HILO_BF16, 3 * d, hd, 3 * d, hd, mod->rot};
+    e = hilo::launch_rope(rs, qkv, mod->pos, BT, cu_img + B, qkv, dev.num_sms, s);
+    if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: rotary positions");
+    count(1);
+  }
   stage_mark(2, s);
 
   hilo::AttnArgs aa;
@@ -451,6 +574,30 @@ static int block_forward_impl(const hilo_shape* shape, const hilo_block_weights*
   if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: attention");
   count(1);
   stage_mark(3, s);
+
+  if (mod) {
+    // Each sub-layer's output goes to the buffer of the norm that is no longer
+    // needed, in bf16, as the attention's inputs are: its rounding is 2^-9 of the
+    // branch, which joins an fp32 residual once, gated. The norm's output then
+    // takes the attention's place.
+    void* y = ln;
+    e = gemm(attn, 0, d, d, hilo::EPI_BIAS_BF16, y, w->txt.w_o, w->txt.b_o, w->img.w_o, w->img.b_o);
+    if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: out-projection gemm");
+    stage_mark(4, s);
+    e = gate_norm(in_txt, in_img, in_dtype, y, mod_attn, mod_mlp, shape->mlp ? attn : nullptr, HILO_F16);
+    if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: gate and norm 2");
+    if (!shape->mlp) return HILO_OK;
+    stage_mark(5, s);
+    e = gemm(attn, 1, 4 * d, d, hilo::EPI_BIAS_GELU_F16, hid, w->txt.w_1, w->txt.b_1, w->img.w_1, w->img.b_1);
+    if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: mlp1 gemm");
+    stage_mark(6, s);
+    e = gemm(hid, 1, d, 4 * d, hilo::EPI_BIAS_BF16, y, w->txt.w_2, w->txt.b_2, w->img.w_2, w->img.b_2);
+    if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: mlp2 gemm");
+    e = gate_norm(out, out + static_cast<size_t>(BT) * d, HILO_F32, y, mod_mlp, nullptr, nullptr, HILO_F16);
+    if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: gate");
+    stage_mark(7, s);
+    return HILO_OK;
+  }
 
   e = gemm(attn, 0, d, d, (in_place || in_place_img) ? hilo::EPI_BIAS_RESID_F32 : hilo::EPI_BIAS_RESIDIN_F32, out, w->txt.w_o, w->txt.b_o, w->img.w_o, w->img.b_o);
   if (e != cudaSuccess) return cuda_fail(e, "hilo_block_forward: out-projection gemm");
@@ -474,8 +621,17 @@ static int block_forward_impl(const hilo_shape* shape, const hilo_block_weights*
 int hilo_block_forward(const hilo_shape* shape, const hilo_block_weights* w, const int32_t* cu_img,
                        int32_t cap, const void* in_txt, const void* in_img, int in_dtype,
                        float* out, void* ws, size_t ws_bytes, void* stream) {
-  return block_forward_impl(shape, w, cu_img, cap, in_txt, in_img, in_dtype, nullptr, out, ws, ws_bytes,
+  return block_forward_impl(shape, w, cu_img, cap, in_txt, in_img, in_dtype, nullptr, nullptr, out, ws, ws_bytes,
                             stream);
+}
+
+int hilo_block_forward_mod(const hilo_shape* shape, const hilo_block_weights* w, const hilo_block_mod* mod,
+                           const int32_t* cu_img, int32_t cap, const void* in_txt, const void* in_img, int in_dtype,
+                           const float* n_img, float* out, void* ws, size_t ws_bytes, void* stream) {
+  if (!mod) return fail(HILO_ERR_ARG, "hilo_block_forward_mod: mod is NULL");
+  if (reinterpret_cast<uintptr_t>(n_img) & 3)
+    return fail(HILO_ERR_ARG, "hilo_block_forward_mod: n_img must be 4-byte aligned");
+  return block_forward_impl(shape, w, cu_img, cap, in_txt, in_img, in_dtype, n_img, mod, out, ws, ws_bytes, stream);
 }
 
 int hilo_block_forward_prop(const hilo_shape* shape, const hilo_block_weights* w, const int32_t* cu_img,
@@ -484,7 +640,7 @@ int hilo_block_forward_prop(const hilo_shape* shape, const hilo_block_weights* w
   if (!n_img) return fail(HILO_ERR_ARG, "hilo_block_forward_prop: n_img is NULL");
   if (reinterpret_cast<uintptr_t>(n_img) & 3)
     return fail(HILO_ERR_ARG, "hilo_block_forward_prop: n_img must be 4-byte aligned");
-  return block_forward_impl(shape, w, cu_img, cap, in_txt, in_img, in_dtype, n_img, out, ws, ws_bytes,
+  return block_forward_impl(shape, w, cu_img, cap, in_txt, in_img, in_dtype, n_img, nullptr, out, ws, ws_bytes,
                             stream);
 }
 
@@ -669,6 +825,139 @@ int hilo_row_sizes(const hilo_shape* shape, const hilo_split_out* split, float* 
                                          static_cast<cudaStream_t>(stream));
   if (e == cudaSuccess && cap > 0) count(1);
   return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_row_sizes");
+}
+
+int hilo_row_positions(const hilo_shape* shape, const hilo_split_out* split, const hilo_positions_origin* origin,
+                       float* pos, int32_t cap, void* stream) {
+  int st = check_shape(shape, false);
+  if (st) return st;
+  if ((st = check_split(split))) return st;
+  if (!origin || !pos) return fail(HILO_ERR_ARG, "hilo_row_positions: NULL pointer");
+  if (shape->T < 0) return fail(HILO_ERR_SHAPE, "T=%d must be >= 0", shape->T);
+  if (cap < 0) return fail(HILO_ERR_ARG, "hilo_row_positions: cap=%d", cap);
+  if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(HILO_ERR_ARG, "hilo_row_positions: pos must be 4-byte aligned");
+  DevInfo dev;
+  if ((st = current_device(&dev))) return st;
+  if (static_cast<long long>(shape->B) * shape->T + cap == 0) return HILO_OK;
+  cudaError_t e = hilo::launch_row_positions(split->labels, split->row_src, split->counts, split->cu_img, *origin, pos,
+                                             shape->B, shape->T, shape->H, shape->W, cap, shape->lf, dev.num_sms,
+                                             static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess) count(1);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_row_positions");
+}
+
+int hilo_rope(const hilo_rope_shape* s, const void* x, const float* pos, const int32_t* n_rows, void* y,
+              void* stream) {
+  if (!s || !x || !pos || !y) return fail(HILO_ERR_ARG, "hilo_rope: NULL pointer");
+  if (s->dtype != HILO_BF16 && s->dtype != HILO_F16 && s->dtype != HILO_F32)
+    return fail(HILO_ERR_ARG, "hilo_rope: dtype=%d", s->dtype);
+  if (s->rows < 0 || s->heads < 1 || s->heads > 65536)
+    return fail(HILO_ERR_SHAPE, "hilo_rope: rows=%d must be >= 0, heads=%d in [1, 65536]", s->rows, s->heads);
+  if (s->head_dim < 8 || s->head_dim % 8 || s->head_dim > 256)
+    return fail(HILO_ERR_SHAPE, "hilo_rope: head_dim=%d must be a multiple of 8 in [8, 256]", s->head_dim);
+  int st = check_rotation("hilo_rope", s->rot, s->head_dim);
+  if (st) return st;
+  const int step = s->dtype == HILO_F32 ? 4 : 8;
+  if (!good_strides(s->x_row, s->x_head, step) || !good_strides(s->y_row, s->y_head, step))
+    return fail(HILO_ERR_ARG, "hilo_rope: strides must be positive multiples of 16 bytes, below 2^39 elements");
+  if (!disjoint(s->rows, s->heads, s->head_dim, s->y_row, s->y_head))
+    return fail(HILO_ERR_ARG, "hilo_rope: y's rows and heads overlap");
+  if (x == y && ((s->rows > 1 && s->x_row != s->y_row) || (s->heads > 1 && s->x_head != s->y_head)))
+    return fail(HILO_ERR_ARG, "hilo_rope: in place, x and y have the same strides");
+  if (!aligned16(x, y)) return fail(HILO_ERR_ARG, "hilo_rope: x and y must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(n_rows)) & 3)
+    return fail(HILO_ERR_ARG, "hilo_rope: pos and n_rows must be 4-byte aligned");
+  DevInfo dev;
+  if ((st = current_device(&dev))) return st;
+  if (s->rows == 0) return HILO_OK;
+  cudaError_t e = hilo::launch_rope(*s, x, pos, 0, n_rows, y, dev.num_sms, static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess) count(1);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_rope");
+}
+
+int hilo_gate_norm(const hilo_norm_shape* s, const hilo_norm_vectors* txt, const hilo_norm_vectors* img,
+                   const int32_t* cu_img, const void* u_txt, const void* u_img, const void* y, void* u_out, void* h,
+                   float* h_scale, void* stream) {
+  if (!s || !img || !cu_img || !u_img || (s->T > 0 && (!txt || !u_txt)))
+    return fail(HILO_ERR_ARG, "hilo_gate_norm: NULL pointer");
+  if (s->B < 1 || s->T < 0 || s->cap < 0 || static_cast<long long>(s->B) * s->T + s->cap > 0x7fffffffLL)
+    return fail(HILO_ERR_SHAPE, "hilo_gate_norm: B=%d, T=%d, cap=%d", s->B, s->T, s->cap);
+  if (s->d < 8 || s->d % 8 || s->d > 4096)
+    return fail(HILO_ERR_SHAPE, "hilo_gate_norm: d=%d must be a multiple of 8 in [8, 4096]", s->d);
+  int st = check_norm("hilo_gate_norm", s->norm, s->norm_branch, s->vec_dtype, s->vec_row, s->eps, s->resid_scale);
+  if (st) return st;
+  if (!is_bf16_or_f32(s->u_dtype) || (y && !is_bf16_or_f32(s->y_dtype)) || (u_out && !is_bf16_or_f32(s->u_out_dtype)) ||
+      (h && !is_bf16_or_f32(s->h_dtype) && s->h_dtype != HILO_F16 && s->h_dtype != HILO_E4M3))
+    return fail(HILO_ERR_ARG, "hilo_gate_norm: u_dtype=%d, y_dtype=%d, u_out_dtype=%d, h_dtype=%d", s->u_dtype, s->y_dtype,
+                s->u_out_dtype, s->h_dtype);
+  if (!h && !u_out) return fail(HILO_ERR_ARG, "hilo_gate_norm: neither u_out nor h");
+  if (u_out && !y) return fail(HILO_ERR_ARG, "hilo_gate_norm: u_out without y");
+  if (h && s->h_dtype == HILO_E4M3 && !h_scale) return fail(HILO_ERR_ARG, "hilo_gate_norm: h_scale is NULL with an e4m3 h");
+  if (reinterpret_cast<uintptr_t>(h_scale) & 3) return fail(HILO_ERR_ARG, "hilo_gate_norm: h_scale must be 4-byte aligned");
+  if (u_out && ((s->T > 0 && u_txt == u_out) || u_img == static_cast<char*>(u_out) + static_cast<size_t>(s->B) * s->T * s->d *
+                                                             (s->u_out_dtype == HILO_F32 ? 4 : 2)) &&
+      s->u_dtype != s->u_out_dtype)
+    return fail(HILO_ERR_ARG, "hilo_gate_norm: in place, u and u_out have the same dtype");
+  if (!aligned16(u_txt, u_img, y, u_out, h) || !vectors_aligned(*img) || (s->T > 0 && !vectors_aligned(*txt)))
+    return fail(HILO_ERR_ARG, "hilo_gate_norm: rows and vectors must be 16-byte aligned");
+  DevInfo dev;
+  if ((st = current_device(&dev))) return st;
+  if (static_cast<long long>(s->B) * s->T + s->cap == 0) return HILO_OK;
+  hilo::NormArgs a = {*s, {s->T > 0 ? *txt : *img, *img}, cu_img, u_txt, u_img, y, u_out, h, h_scale};
+  cudaError_t e = hilo::launch_gate_norm(a, dev.num_sms, static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess) count(1);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_gate_norm");
+}
+
+static int check_attn(const hilo_attn_shape* s) {
+  if (!s) return fail(HILO_ERR_ARG, "hilo_attention: shape is NULL");
+  if (s->B < 1 || s->B > hilo::ATTN_MAX_SEQUENCES)
+    return fail(HILO_ERR_SHAPE, "hilo_attention: B=%d must be in [1, %d]", s->B, hilo::ATTN_MAX_SEQUENCES);
+  if (s->heads < 1 || s->kv_heads < 1 || s->heads > 65536 || s->heads % s->kv_heads || s->heads / s->kv_heads > 128)
+    return fail(HILO_ERR_SHAPE, "hilo_attention: heads=%d must be a multiple of kv_heads=%d, at most 128 times it",
+                s->heads, s->kv_heads);
+  if (s->head_dim != 64 && s->head_dim != 128)
+    return fail(HILO_ERR_SHAPE, "hilo_attention: head_dim=%d must be 64 or 128", s->head_dim);
+  if (s->dtype != HILO_BF16 && s->dtype != HILO_F16) return fail(HILO_ERR_ARG, "hilo_attention: dtype=%d", s->dtype);
+  if (s->causal & ~1) return fail(HILO_ERR_ARG, "hilo_attention: causal=%d must be 0 or 1", s->causal);
+  if (!(s->scale >= 0.0f) || !is_finite(s->scale)) return fail(HILO_ERR_ARG, "hilo_attention: scale must be finite and >= 0");
+  const int most = 1 << 30;
+  if (s->rows_q < 0 || s->rows_k < 0 || s->rows_q > most || s->rows_k > most)
+    return fail(HILO_ERR_SHAPE, "hilo_attention: rows_q=%d and rows_k=%d must be in [0, 2^30]", s->rows_q, s->rows_k);
+  const int group = s->heads / s->kv_heads, tokens = 128 / group;
+  if ((static_cast<long long>(s->rows_q) / tokens + s->B) * s->kv_heads > most)
+    return fail(HILO_ERR_SHAPE, "hilo_attention: %d rows of %d heads make more than 2^30 tiles", s->rows_q, s->heads);
+  if (!good_strides(s->q_row, s->q_head, 8) || !good_strides(s->k_row, s->k_head, 8) ||
+      !good_strides(s->v_row, s->v_head, 8) || !good_strides(s->out_row, s->out_head, 8))
+    return fail(HILO_ERR_ARG, "hilo_attention: strides must be positive multiples of 8, below 2^39");
+  if (!disjoint(s->rows_q, s->heads, s->head_dim, s->out_row, s->out_head))
+    return fail(HILO_ERR_ARG, "hilo_attention: out's rows and heads overlap");
+  return HILO_OK;
+}
+
+size_t hilo_attention_workspace_bytes(const hilo_attn_shape* shape) {
+  return check_attn(shape) ? 0 : hilo::attn_var_workspace_bytes(*shape);
+}
+
+int hilo_attention(const hilo_attn_shape* s, const int32_t* cu_q, const int32_t* cu_k, const void* q, const void* k,
+                   const void* v, void* out, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_attn(s);
+  if (st) return st;
+  if (!cu_q || !cu_k || (s->rows_q > 0 && (!q || !out)) || (s->rows_k > 0 && (!k || !v)))
+    return fail(HILO_ERR_ARG, "hilo_attention: NULL pointer");
+  if (!aligned16(q, k, v, out, ws)) return fail(HILO_ERR_ARG, "hilo_attention: q, k, v, out and ws must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(cu_q) | reinterpret_cast<uintptr_t>(cu_k)) & 3)
+    return fail(HILO_ERR_ARG, "hilo_attention: cu_q and cu_k must be 4-byte aligned");
+  const size_t need = hilo::attn_var_workspace_bytes(*s);
+  if (!ws || ws_bytes < need) return fail(HILO_ERR_WORKSPACE, "hilo_attention: workspace %zu < %zu bytes", ws ? ws_bytes : 0, need);
+  DevInfo dev;
+  if ((st = current_device(&dev))) return st;
+  if (s->rows_q == 0) return HILO_OK;
+  int launches = 0;
+  cudaError_t e = hilo::launch_attention_var(*s, cu_q, cu_k, q, k, v, out, ws, dev.num_sms, &launches,
+                                             static_cast<cudaStream_t>(stream));
+  count(launches);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_attention");
 }
 
 int hilo_unpack(const hilo_shape* shape, const float* out_img, const hilo_split_out* split, float* y,

@@ -1,0 +1,1311 @@
+// Softmax attention of packed sequences with grouped heads on tcgen05: whole
+// prompts, chunks of new tokens over earlier ones, single tokens; causal or
+// not (hilo_attention, include/hilo.h). It serves the transformer that makes
+// the text rows of the block's joint attention (paper Sec. 2.1) and any other
+// attention over sequences whose lengths only the device knows.
+//
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i.k_j - m_i), over the keys j that query i sees,
+//
+// in one pass over the keys with the running maximum m_i and sum.
+//
+// Tiles. The g query heads of one key head share its keys, so a tile of 128
+// rows of the matrix product is floor(128 / g) neighbouring tokens with their
+// g heads each (row = token * g + head): one box of a three-axis tensor map.
+// A single token therefore costs one pass over the keys per key head, not per
+// query head, and a tile's rows see nearly the same keys.
+//
+// Jobs. Two neighbouring tiles of one key head are a job (pair): each softmax
+// warpgroup has one of them, and both share every K/V tile. A tile without a
+// partner is a job of its own (single), whose key tiles alternate between the
+// two warpgroups; the second then hands its maxima, sums and accumulator to
+// the first. A job whose steps are more than a CTA's fair share is cut along
+// the keys into pieces, each of which leaves unnormalised fp32 rows with their
+// maxima and sums in the workspace; a second kernel joins them. That is how a
+// few long sequences of single tokens get the whole device.
+//
+// Plan. Only the device knows the lengths, so every CTA makes the same plan
+// (plan_build): the jobs of all sequences, the fair share, the cuts, longest
+// first. CTA x of G takes items x, 2G-1-x, 2G+x, ..: the longest with the
+// shortest. One warp walks the CTA's items ahead of the others and hands them
+// on through a ring of four in shared memory.
+//
+// A CTA is three warpgroups, as in attn_tc.cu: two for the softmax (a row per
+// thread, S and P in tensor memory, P the A operand of the second product),
+// one for the Q/K copies, the V copies, the MMAs and the items.
+//
+// What a query does not see never reaches its result: masked logits are
+// replaced, not computed with, and a value tile that some row of the job sees
+// only in part is looked through for infinities and NaNs, whose product with
+// a probability of 0 would be NaN. They are taken out of the tile, and rows
+// that do see them get them back at the end (take_out, give_back).
+//
+// Every mbarrier wait is bounded (error latched, TMEM freed, CTA returns).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include <atomic>
+
+#include "attn_common.cuh"
+#include "common.cuh"
+#include "internal.h"
+
+namespace hilo {
+
+__device__ int g_attn_var_err;
+
+namespace {
+
+constexpr int BQ = 128;
+constexpr int BKV = 128;
+constexpr int THREADS = 384;
+constexpr int PRODUCER_WARP = 8;     // Q and K copies
+constexpr int MMA_WARP = 9;
+constexpr int V_PRODUCER_WARP = 10;  // V copies
+constexpr int ITEM_WARP = 11;
+constexpr uint32_t SOFTMAX_REGS = 216;
+constexpr uint32_t CONTROL_REGS = 72;
+constexpr uint32_t TMEM_COLS = 512;  // S0 | S1 | O0 | O1
+constexpr int BOX_BYTES = 128 * 128;  // 128 rows x 64 16-bit elements
+constexpr float RESCALE_LOG2 = 8.0f;
+
+struct VarParams {
+  const int32_t *cu_q, *cu_k;
+  const void* v;
+  void* out;
+  float* part;   // pieces' rows: [slot][tile 0, 1][row][HD]
+  float2* part_ml;  // their maxima and sums: [slot][tile][row]
+  long long v_row, v_head, out_row, out_head;
+  int B, kv_heads, group, tpt;  // tpt: tokens per tile
+  int causal, rows_q, rows_k;
+  int grid;  // CTAs of the main kernel
+  int may_cut;
+  float scale_log2;  // log2(e) * scale
+};
+
+// ---------------------------------------------------------------- sequences --
+
+struct Seq {
+  int q0, lq, k0, lk;
+  // Keys that token i sees.
+  __device__ __forceinline__ int seen(const VarParams& p, int i) const {
+    return p.causal ? min(lk, max(0, i + 1 + (lk - lq))) : lk;
+  }
+  __device__ __forceinline__ int tiles(const VarParams& p) const { return (lq + p.tpt - 1) / p.tpt; }
+  // Key tiles of query tile j: those its last token sees (one, all of it
+  // masked, where it sees none: the zeros of such rows are written too).
+  __device__ __forceinline__ int key_tiles(const VarParams& p, int j) const {
+    return max(1, (seen(p, min(lq, (j + 1) * p.tpt) - 1) + BKV - 1) / BKV);
+  }
+  // Steps of row job i: a pair's key tiles, half of a single's.
+  __device__ __forceinline__ int steps(const VarParams& p, int i) const {
+    const int nt = tiles(p);
+    return 2 * i + 1 < nt ? key_tiles(p, 2 * i + 1) : (key_tiles(p, nt - 1) + 1) / 2;
+  }
+};
+
+// (L2: before the kernel's own wait, when this SM's L1 may hold older offsets)
+template <bool L2>
+__device__ __forceinline__ Seq sequence(const VarParams& p, int b) {
+  auto at = [](const int32_t* cu, int rows) { return min(max(L2 ? ld_l2(cu) : *cu, 0), rows); };
+  const int q0 = at(p.cu_q + b, p.rows_q), q1 = at(p.cu_q + b + 1, p.rows_q);
+  const int k0 = at(p.cu_k + b, p.rows_k), k1 = at(p.cu_k + b + 1, p.rows_k);
+  return {q0, max(0, q1 - q0), k0, max(0, k1 - k0)};
+}
+
+// --------------------------------------------------------------------- plan --
+//
+// A row job is a job of one sequence for all its key heads. Up to MAX_TABLE
+// row jobs are listed, longest first to a sixteenth of the longest; the items of an
+// entry are its key heads' jobs, or their pieces. More row jobs than that are
+// taken as they come, the last of each sequence first, and never cut: every
+// CTA then has dozens.
+//
+// Cutting: with J jobs of T steps together on G CTAs, a piece has at most KS
+// steps. J >= G: KS = ceil(T / G), so only a job longer than a CTA's share is
+// cut, into fewer than 2G pieces (each cut job of c > KS steps into at most
+// c / KS + 1 < 2c / KS). J < G: the smaller of ceil(T / (G - J)), for which
+// sum(c / KS + 1) <= G, and the longest job in floor(G / J) pieces: at most G.
+// Pieces of less than MIN_STEPS would cost more in their epilogues than they save.
+
+constexpr int MAX_SEQ = ATTN_MAX_SEQUENCES;
+constexpr int MAX_TABLE = 1024;
+constexpr int MIN_STEPS = 2;
+constexpr int SLOTS_PER_CTA = 2;
+constexpr int BUCKETS = 32;  // 16 of cut jobs, 16 of whole ones
+
+struct Plan {
+  int first[MAX_SEQ + 1];  // row jobs before sequence b
+  int seq[MAX_TABLE];      // entry: sequence << 16 | row job of it
+  int steps[MAX_TABLE];
+  int items[MAX_TABLE];    // items before the entry
+  int jobs, n_items, n_cut, share;  // row jobs, items, cut entries, KS
+};
+static_assert(MAX_SEQ <= 1 << 15 && MAX_TABLE <= 1 << 16, "an entry's sequence and row job share a word");
+
+__device__ __forceinline__ int ceil_div(int a, int b) {
+  return static_cast<int>((static_cast<uint32_t>(a) + static_cast<uint32_t>(b) - 1u) / static_cast<uint32_t>(b));
+}
+__device__ __forceinline__ int pieces_of(int steps, int share) { return steps > share ? ceil_div(steps, share) : 1; }
+
+// Sum of v over the CTA's threads before this one, and of all: `tot` is a word per warp
+// that no other call is using.
+template <int NT>
+__device__ __forceinline__ int block_excl_scan(int v, int* tot, int& total) {
+  const int incl = warp_incl_scan(v), w = warp_id();
+  if (lane_id() == 31) tot[w] = incl;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < NT / 32; ++i) {
+    const int t = tot[i];
+    before += i < w ? t : 0;
+    total += t;
+  }
+  return before + incl - v;
+}
+
+// What plan_build needs for itself.
+template <int NT>
+struct PlanScratch {
+  static constexpr int PER = (MAX_TABLE + NT - 1) / NT;
+  int tot[4][NT / 32];
+  unsigned long long sum[NT / 32];
+  int most[NT / 32];
+  int hist[BUCKETS * PER * (NT / 32)];  // [bucket][round, warp]
+};
+
+template <int NT, bool L2>
+__device__ void plan_build(const VarParams& p, Plan& pl, PlanScratch<NT>& s) {
+  constexpr int PER = PlanScratch<NT>::PER, WARPS = NT / 32, ROWS = PER * WARPS;
+  const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
+  // row jobs before each sequence
+  int before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += NT) {
+    const int b = b0 + tid;
+    int n = 0;
+    if (b < p.B) n = (sequence<L2>(p, b).tiles(p) + 1) / 2;
+    int total;
+    const int at = block_excl_scan<NT>(n, s.tot[(b0 / NT) & 1], total);
+    if (b < p.B) pl.first[b] = before + at;
+    before += total;
+  }
+  const int U = before;
+  if (tid == 0) pl.first[p.B] = U;
+  for (int i = tid; i < BUCKETS * ROWS; i += NT) s.hist[i] = 0;
+  __syncthreads();
+  if (U > MAX_TABLE) {
+    if (tid == 0) {
+      pl.jobs = U;
+      pl.n_items = U * p.kv_heads;
+      pl.n_cut = 0;
+      pl.share = 0x7fffffff;
+    }
+    __syncthreads();
+    return;
+  }
+  // the row jobs' steps
+  int job[PER], c[PER];
+  unsigned long long sum = 0;
+  int most = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int u = k * NT + tid;
+    job[k] = c[k] = 0;
+    if (u >= U) continue;
+    int lo = 0, hi = p.B;  // the last sequence that begins at or before u
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pl.first[mid] <= u) lo = mid;
+      else hi = mid;
+    }
+    const int i = u - pl.first[lo];
+    job[k] = lo << 16 | i;
+    c[k] = sequence<L2>(p, lo).steps(p, i);
+    sum += static_cast<unsigned long long>(c[k]);
+    most = max(most, c[k]);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) {
+    s.sum[warp] = sum;
+    s.most[warp] = most;
+  }
+  __syncthreads();
+  sum = 0;
+  most = 0;
+#pragma unroll
+  for (int i = 0; i < WARPS; ++i) {
+    sum += s.sum[i];
+    most = max(most, s.most[i]);
+  }
+  const long long J = static_cast<long long>(U) * p.kv_heads, G = p.grid;
+  const long long T = static_cast<long long>(sum) * p.kv_heads;
+  int share = most;
+  if (p.may_cut && J > 0) {
+    long long ks;
+    if (J >= G) {
+      ks = (T + G - 1) / G;
+    } else {
+      const int each = static_cast<int>(G / J);
+      ks = min((T + G - J - 1) / (G - J), static_cast<long long>(ceil_div(most, each)));
+    }
+    share = static_cast<int>(min(max(ks, static_cast<long long>(MIN_STEPS)), static_cast<long long>(max(most, 1))));
+  }
+  // sorted by bucket, in order within one: the rank among the warp's lanes, then
+  // a scan over all warps' counts
+  int rank[PER], bucket[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const bool in = k * NT + tid < U;
+    bucket[k] = BUCKETS;
+    if (in) {
+      const int top = c[k] > share ? most : min(most, share);
+      bucket[k] = (c[k] > share ? 15 : 31) - min(15, static_cast<int>(static_cast<uint32_t>(c[k] - 1) * 16u /
+                                                                      static_cast<uint32_t>(top)));
+    }
+    const uint32_t same = __match_any_sync(0xffffffffu, bucket[k]);
+    rank[k] = __popc(same & ((1u << lane) - 1u));
+    if (in && rank[k] == 0) s.hist[bucket[k] * ROWS + k * WARPS + warp] = __popc(same);
+  }
+  __syncthreads();
+  constexpr int HPER = (BUCKETS * ROWS + NT - 1) / NT;
+  int h[HPER], mine = 0, total;
+#pragma unroll
+  for (int i = 0; i < HPER; ++i) {
+    const int at = tid * HPER + i;
+    h[i] = at < BUCKETS * ROWS ? s.hist[at] : 0;
+    mine += h[i];
+  }
+  int run = block_excl_scan<NT>(mine, s.tot[2], total);
+#pragma unroll
+  for (int i = 0; i < HPER; ++i) {
+    const int at = tid * HPER + i;
+    if (at < BUCKETS * ROWS) s.hist[at] = run;
+    run += h[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (bucket[k] == BUCKETS) continue;
+    const int at = s.hist[bucket[k] * ROWS + k * WARPS + warp] + rank[k];
+    pl.seq[at] = job[k];
+    pl.steps[at] = c[k];
+  }
+  __syncthreads();
+  // items before each entry
+  int n[PER], cut = 0;
+  mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int at = tid * PER + i;
+    n[i] = at < U ? pieces_of(pl.steps[at], share) * p.kv_heads : 0;
+    if (at < U) cut += pl.steps[at] > share;
+    mine += n[i];
+  }
+  run = block_excl_scan<NT>(mine, s.tot[3], total);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int at = tid * PER + i;
+    if (at < U) pl.items[at] = run;
+    run += n[i];
+  }
+  int n_cut;
+  block_excl_scan<NT>(cut, s.tot[0], n_cut);
+  if (tid == 0) {
+    pl.jobs = U;
+    pl.n_items = total;
+    pl.n_cut = n_cut;
+    pl.share = share;
+  }
+  __syncthreads();
+}
+
+// ------------------------------------------------------------------- items --
+
+// A CTA's unit of work: query tiles j0 (and j0 + 1 of a pair) of a sequence and
+// a key head over the key tiles [t0, t1).
+struct Item {
+  int more;  // 0: the CTA has no further item
+  int q0, lq, k0, lk;
+  int hk, j0, pair;
+  int t0, t1;
+  int n0, n1;  // steps of the two warpgroups
+  int slot;    // of a piece; -1: the whole job
+};
+
+// The key tile of step s of warpgroup i.
+__device__ __forceinline__ int item_tile(int pair, int t0, int i, int s) { return pair ? t0 + s : t0 + 2 * s + i; }
+
+__device__ Item item_at(const VarParams& p, const Plan& pl, int t) {
+  Item it;
+  it.more = 0;
+  if (t >= pl.n_items) return it;
+  int b, i, piece = 0, pieces = 1;
+  if (pl.jobs <= MAX_TABLE) {
+    int lo = 0, hi = pl.jobs;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pl.items[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    b = pl.seq[lo] >> 16;
+    i = pl.seq[lo] & 0xffff;
+    pieces = pieces_of(pl.steps[lo], pl.share);
+    const int r = t - pl.items[lo];
+    it.hk = r / pieces;
+    piece = r - it.hk * pieces;
+  } else {
+    const int v = t / p.kv_heads, u = pl.jobs - 1 - v;
+    it.hk = t - v * p.kv_heads;
+    int lo = 0, hi = p.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pl.first[mid] <= u) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    i = u - pl.first[lo];
+  }
+  const Seq s = sequence<false>(p, b);
+  it.more = 1;
+  it.q0 = s.q0;
+  it.lq = s.lq;
+  it.k0 = s.k0;
+  it.lk = s.lk;
+  it.j0 = 2 * i;
+  it.pair = 2 * i + 1 < s.tiles(p);
+  const uint32_t c = static_cast<uint32_t>(s.steps(p, i));
+  const int u0 = static_cast<int>(c * static_cast<uint32_t>(piece) / static_cast<uint32_t>(pieces));
+  const int u1 = static_cast<int>(c * static_cast<uint32_t>(piece + 1) / static_cast<uint32_t>(pieces));
+  const int nkv0 = s.key_tiles(p, it.j0);
+  if (it.pair) {
+    it.t0 = u0;
+    it.t1 = u1;
+    it.n0 = max(0, min(u1, nkv0) - u0);
+    it.n1 = u1 - u0;
+  } else {
+    it.t0 = 2 * u0;
+    it.t1 = min(nkv0, 2 * u1);
+    it.n1 = (it.t1 - it.t0) / 2;
+    it.n0 = it.t1 - it.t0 - it.n1;
+  }
+  it.slot = pieces > 1 ? t : -1;
+  return it;
+}
+
+// Item k of CTA x of G.
+__device__ __forceinline__ int item_index(int k, int x, int G) { return k & 1 ? (k + 1) * G - 1 - x : k * G + x; }
+
+// -------------------------------------------------------------- 16-bit types --
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  if (F16) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return pack_bf16x2(lo, hi);
+}
+
+// The exponent bits of both halves, and what carries an exponent of all ones (an
+// infinity or a NaN) into the half's sign bit.
+template <bool F16>
+__device__ __forceinline__ uint32_t special16(uint32_t w) {
+  return F16 ? ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u : ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+
+template <bool F16>
+__device__ __forceinline__ float widen16(uint32_t half) {
+  return F16 ? __half2float(__ushort_as_half(static_cast<unsigned short>(half))) : __uint_as_float(half << 16);
+}
+
+__device__ __forceinline__ void st_f32x8(float* p, const float* v) {
+  asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+               "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(p)
+               : "memory");
+}
+
+// The first key tile that some row of the item does not see whole.
+__device__ __forceinline__ int part_tile(const VarParams& p, const Item& it) {
+  return (p.causal ? min(it.lk, max(0, it.j0 * p.tpt + it.lk - it.lq + 1)) : it.lk) / BKV;
+}
+
+constexpr int RING = 4;
+
+// What the softmax warpgroups hand over, and the items.
+struct Shared {
+  float m1[BQ], l1[BQ];
+  Item ring[RING];
+  int special[2];  // an infinity or NaN was taken out of a value tile of the item (by its parity)
+};
+
+template <int HD>
+struct Cfg {
+  static constexpr int NBOX = HD / 64;
+  static constexpr int TILE_BYTES = NBOX * BOX_BYTES;  // 128 rows x HD
+  // Q0 | Q1 | K0 | K1 | V0 | V1 (the plan's scratch before the first copy)
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = 2 * TILE_BYTES;
+  static constexpr int OFF_V = 4 * TILE_BYTES;
+  static constexpr int DATA_BYTES = 6 * TILE_BYTES;
+  static constexpr int OFF_X = DATA_BYTES + 256;  // barriers before it
+  static constexpr int OFF_PLAN = OFF_X + static_cast<int>(sizeof(Shared));
+  static constexpr int SMEM_BYTES = OFF_PLAN + static_cast<int>(sizeof(Plan)) + 1024;  // + alignment of the base
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
+  static_assert(sizeof(PlanScratch<THREADS>) <= DATA_BYTES, "the plan's scratch");
+};
+
+template <int HD, bool F16>
+__global__ void __launch_bounds__(THREADS, 1)
+    attn_var_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ VarParams p) {
+  using C = Cfg<HD>;
+  extern __shared__ unsigned char smem_raw[];
+  // (an offset from smem_raw, so that accesses stay 32-bit shared-memory ones)
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::DATA_BYTES);
+  uint64_t* q_full = bars + 0;
+  uint64_t* k_full = bars + 1;    // [2]
+  uint64_t* k_empty = bars + 3;   // [2]
+  uint64_t* v_full = bars + 5;    // [2]
+  uint64_t* v_empty = bars + 7;   // [2]
+  uint64_t* s_full = bars + 9;    // [2] per softmax warpgroup
+  uint64_t* p_full = bars + 11;   // [2] per softmax warpgroup
+  uint64_t* o_done = bars + 13;   // [2] per softmax warpgroup
+  uint64_t* drain = bars + 15;
+  uint64_t* epi_done = bars + 16;  // an item's output rows are out: Q free
+  uint64_t* it_full = bars + 18;  // [RING]
+  uint64_t* it_empty = bars + 22; // [RING]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 26);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  Shared& shr = *reinterpret_cast<Shared*>(smem + C::OFF_X);
+  Plan& plan = *reinterpret_cast<Plan*>(smem + C::OFF_PLAN);
+  int* err = &g_attn_var_err;
+  auto sK = [&](int st) { return smem + C::OFF_K + st * C::TILE_BYTES; };
+  auto sV = [&](int st) { return smem + C::OFF_V + st * C::TILE_BYTES; };
+  auto sQ = [&](int i) { return smem + C::OFF_Q + i * C::TILE_BYTES; };
+
+  const int warp = warp_id(), lane = lane_id();
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 1);
+      mbar_init(&v_full[i], 1);
+      mbar_init(&v_empty[i], 1);
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 128);
+      mbar_init(&o_done[i], 1);
+    }
+    mbar_init(drain, 1);
+    mbar_init(epi_done, 1);
+    for (int i = 0; i < RING; ++i) {
+      mbar_init(&it_full[i], 1);
+      mbar_init(&it_empty[i], 3 + 8);  // two copy warps, the MMA warp, the softmax warps
+    }
+    *abort_flag = 0;
+    shr.special[0] = shr.special[1] = 0;
+    fence_mbar_init();
+  }
+  // the lengths may be the previous kernel's
+  pdl_wait();
+  pdl_trigger();
+  plan_build<THREADS, false>(p, plan, *reinterpret_cast<PlanScratch<THREADS>*>(smem));
+  if (static_cast<int>(blockIdx.x) >= plan.n_items) return;  // (uniform: nothing allocated yet)
+  if (warp == MMA_WARP) {
+    tmem_alloc(tmem_slot, TMEM_COLS);
+    tmem_relinquish();
+  }
+  // the plan's scratch (generic proxy) before the first copy over it (async proxy)
+  fence_proxy_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // key tile number kt of the CTA: its stage and the parity of that stage's use
+  auto kv_stage = [](uint32_t kt) { return static_cast<int>(kt & 1u); };
+  auto kv_phase = [](uint32_t kt) { return (kt >> 1) & 1u; };
+  auto it_wait = [&](uint32_t jn, int code) {
+    return mbar_wait(&it_full[jn & (RING - 1)], (jn / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * code);
+  };
+  if (warp >= 8) {
+    setmaxnreg_dec<CONTROL_REGS>();
+    if (warp == PRODUCER_WARP || warp == V_PRODUCER_WARP) {
+      if (lane == 0) {
+        // ---------------- TMA producers: Q and K tiles (warp 8), V tiles
+        // (warp 10). Two threads, so that a K copy never queues behind a V
+        // stage that is still being read, and the other way round.
+        const bool kq = warp == PRODUCER_WARP;
+        const CUtensorMap* tm = kq ? &tm_k : &tm_v;
+        tma_prefetch_desc(tm);
+        if (kq) tma_prefetch_desc(&tm_q);
+        // per stage (bit st): armed at least once, and the parity of the last arming
+        uint32_t armed = 0, par = 0;
+        bool q_armed = false;
+        uint32_t q_par = 0;
+        bool ok = true;
+        uint32_t kt = 0;
+        uint64_t* full = kq ? k_full : v_full;
+        uint64_t* empty = kq ? k_empty : v_empty;
+        const uint32_t q_bytes = static_cast<uint32_t>(C::NBOX * 128 * p.tpt * p.group);
+        for (uint32_t jn = 0;; ++jn) {
+          if (!it_wait(jn, 18)) {
+            ok = false;
+            break;
+          }
+          const Item& it = shr.ring[jn & (RING - 1)];
+          if (!it.more) break;
+          const int hk = it.hk, k0 = it.k0, t0 = it.t0, n = it.t1 - it.t0;
+          if (kq) {
+            const int pair = it.pair, row0 = it.q0 + it.j0 * p.tpt, h0 = hk * p.group;
+            // Q once the previous item's output rows (staged in its place) are out
+            if (jn > 0 && !mbar_wait(epi_done, (jn - 1) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 17)) {
+              ok = false;
+              break;
+            }
+            mbar_arrive_expect_tx(q_full, (pair ? 2 : 1) * q_bytes);
+#pragma unroll
+            for (int j = 0; j < C::NBOX; ++j) {
+              tma_load_3d(sQ(0) + j * BOX_BYTES, &tm_q, q_full, 64 * j, h0, row0);
+              if (pair) tma_load_3d(sQ(1) + j * BOX_BYTES, &tm_q, q_full, 64 * j, h0, row0 + p.tpt);
+            }
+            q_armed = true;
+            q_par = jn & 1u;
+          }
+          mbar_arrive(&it_empty[jn & (RING - 1)]);
+          for (int t = 0; t < n; ++t) {
+            const int st = kv_stage(kt + t);
+            const uint32_t ph = kv_phase(kt + t);
+            if (!mbar_wait(&empty[st], ph ^ 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * (kq ? 1 : 2))) {
+              ok = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
+            unsigned char* dst = kq ? sK(st) : sV(st);
+#pragma unroll
+            for (int j = 0; j < C::NBOX; ++j)
+              tma_load_3d(dst + j * BOX_BYTES, tm, &full[st], 64 * j, hk, k0 + (t0 + t) * BKV);
+            armed |= 1u << st;
+            par = (par & ~(1u << st)) | (ph << st);
+          }
+          if (!ok) break;
+          kt += static_cast<uint32_t>(n);
+        }
+        if (!ok) {
+          // wait (bounded) for this thread's bulk copies in flight before the
+          // CTA exits
+          const uint64_t g0 = globaltimer_ns();
+          const uint64_t lim = HILO_WAIT_LIMIT_NS / 4;
+          if (q_armed)
+            while (!mbar_try_wait(smem_u32(q_full), q_par) && globaltimer_ns() - g0 < lim) {
+            }
+          for (int st = 0; st < 2; ++st)
+            if ((armed >> st) & 1u)
+              while (!mbar_try_wait(smem_u32(&full[st]), (par >> st) & 1u) && globaltimer_ns() - g0 < lim) {
+              }
+        }
+      }
+    } else if (warp == MMA_WARP) {
+      // ---------------- MMA issuer: the whole warp walks the schedule and
+      // waits (descriptor words stay warp-uniform), one elected lane issues.
+      const bool leader = elect_one();
+      constexpr int FMT = F16 ? 0 : 1;
+      constexpr uint32_t idesc_s = idesc_kind_f16(BQ, BKV, 0, 0, FMT);
+      constexpr uint32_t idesc_o = idesc_kind_f16(BQ, HD, 0, 1, FMT);
+      constexpr uint32_t TILE16 = C::TILE_BYTES >> 4;
+      const uint32_t base16 = smem_u32(smem) >> 4;
+      const uint32_t q_lo = base16 + (C::OFF_Q >> 4) + sw128_lo_lbo(16);
+      const uint32_t k_lo = base16 + (C::OFF_K >> 4) + sw128_lo_lbo(16);
+      const uint32_t v_lo = base16 + (C::OFF_V >> 4) + sw128_lo_lbo(BOX_BYTES);
+      constexpr uint32_t hi = sw128_hi(1024);
+      // S_i = Q_qb K^T (K from stage kst)
+      auto issue_s = [&](int i, int qb, int kst) {
+        if (leader) {
+          const uint32_t a = q_lo + static_cast<uint32_t>(qb) * TILE16, b = k_lo + static_cast<uint32_t>(kst) * TILE16;
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint32_t off = static_cast<uint32_t>((k >> 2) * BOX_BYTES + (k & 3) * 32) >> 4;
+            umma_f16_w(tmem + 128u * i, a + off, b + off, hi, idesc_s, k > 0 ? 1u : 0u);
+          }
+          umma_commit(&s_full[i]);
+        }
+        __syncwarp();
+      };
+      // O_i (+)= P_i V: P_i from the first 64 TMEM columns of S_i, V from stage vst
+      auto issue_pv = [&](int i, int vst, bool acc, bool last) {
+        if (leader) {
+          const uint32_t b = v_lo + static_cast<uint32_t>(vst) * TILE16;
+#pragma unroll
+          for (int k = 0; k < BKV / 16; ++k)
+            umma_f16_tmem_a_w(tmem + 256u + 128u * i, tmem + 128u * i + 8u * k, b + ((k * 2048) >> 4), hi, idesc_o,
+                              (acc || k > 0) ? 1u : 0u);
+          if (last) umma_commit(&o_done[i]);
+        }
+        __syncwarp();
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (leader) umma_commit(bar);
+        __syncwarp();
+      };
+      bool ok = true;
+      uint32_t kt = 0, sc0 = 0, sc1 = 0;
+      for (uint32_t jn = 0;; ++jn) {
+        if (!__all_sync(0xffffffffu, it_wait(jn, 19))) {
+          ok = false;
+          break;
+        }
+        const Item& it = shr.ring[jn & (RING - 1)];
+        if (!it.more) break;
+        const bool pair = it.pair;
+        const int n0 = it.n0, n1 = it.n1, n = it.t1 - it.t0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&it_empty[jn & (RING - 1)]);
+        const int qb1 = pair ? 1 : 0;  // the Q buffer of warpgroup 1
+        // key tile of step s of warpgroup i, counted from the CTA's first
+        auto tile = [&](int i, int s) { return kt + static_cast<uint32_t>(pair ? s : 2 * s + i); };
+        auto wait_k = [&](uint32_t t) {
+          return mbar_wait_warp(&k_full[kv_stage(t)], kv_phase(t), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 4);
+        };
+        auto wait_v = [&](uint32_t t) {
+          return mbar_wait_warp(&v_full[kv_stage(t)], kv_phase(t), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 6);
+        };
+        if (!mbar_wait_warp(q_full, jn & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 3) || !wait_k(kt)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // the first S of each warpgroup; a pair shares its first key tile, a
+        // single gives warpgroup 1 the second one
+        if (n0 > 0) issue_s(0, 0, kv_stage(kt));
+        if (pair) {
+          issue_s(1, 1, kv_stage(kt));
+          commit(&k_empty[kv_stage(kt)]);
+        } else {
+          commit(&k_empty[kv_stage(kt)]);
+          if (n1 > 0) {
+            if (!wait_k(kt + 1)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            issue_s(1, 0, kv_stage(kt + 1));
+            commit(&k_empty[kv_stage(kt + 1)]);
+          }
+        }
+        // ping-pong: PV_0(s), S_0(s+1), PV_1(s), S_1(s+1); S_i(s+1)
+        // overwrites P_i(s) only after PV_i(s), in issue order
+        const int nmax = n0 > n1 ? n0 : n1;
+        for (int s = 0; s < nmax && ok; ++s) {
+          if (s < n0) {
+            const uint32_t t = tile(0, s);
+            if (!mbar_wait2_warp(&p_full[0], (sc0 + s) & 1u, &v_full[kv_stage(t)], kv_phase(t), abort_flag, err,
+                                 DEV_TIMEOUT_ATTN + 256 * 5, DEV_TIMEOUT_ATTN + 256 * 6)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            issue_pv(0, kv_stage(t), s > 0, s + 1 == n0);
+            if (!pair) commit(&v_empty[kv_stage(t)]);
+            if (s + 1 < n0) {
+              // no tcgen05 fence here: S reads only TMA-written Q and K (ordered
+              // by their mbarrier), and it follows the PV block above, whose
+              // fence already ordered the softmax's TMEM accesses, in issue order
+              const uint32_t t2 = tile(0, s + 1);
+              if (!wait_k(t2)) {
+                ok = false;
+                break;
+              }
+              issue_s(0, 0, kv_stage(t2));
+              if (!pair) commit(&k_empty[kv_stage(t2)]);
+            }
+          }
+          if (s < n1) {
+            // a pair's second tile has at least the first one's steps, and where both
+            // have one its key tiles are those that were waited for above
+            const uint32_t t = tile(1, s);
+            if (!mbar_wait_warp(&p_full[1], (sc1 + s) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 8) ||
+                ((!pair || s >= n0) && !wait_v(t))) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            issue_pv(1, kv_stage(t), s > 0, s + 1 == n1);
+            commit(&v_empty[kv_stage(t)]);
+            if (s + 1 < n1) {
+              const uint32_t t2 = tile(1, s + 1);
+              if ((!pair || s + 1 >= n0) && !wait_k(t2)) {
+                ok = false;
+                break;
+              }
+              issue_s(1, qb1, kv_stage(t2));
+              commit(&k_empty[kv_stage(t2)]);
+            }
+          }
+        }
+        if (!ok) break;
+        sc0 += static_cast<uint32_t>(n0);
+        sc1 += static_cast<uint32_t>(n1);
+        kt += static_cast<uint32_t>(n);
+      }
+      // every issued MMA has completed before TMEM is freed, also after an
+      // abort (so this wait ignores the abort flag; it is bounded by time)
+      commit(drain);
+      const uint64_t g0 = globaltimer_ns();
+      while (!mbar_try_wait(smem_u32(drain), 0u)) {
+        if (globaltimer_ns() - g0 > HILO_WAIT_LIMIT_NS) {
+          if (leader) atomicExch(err, DEV_TIMEOUT_ATTN + 256 * 9);
+          break;
+        }
+      }
+      __syncwarp();
+    } else if (warp == ITEM_WARP && lane == 0) {
+      // ---------------- warp 11, one lane: the CTA's items, ahead of their use
+      for (uint32_t jn = 0;; ++jn) {
+        const int slot = jn & (RING - 1);
+        if (jn >= RING &&
+            !mbar_wait(&it_empty[slot], ((jn - RING) / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 20))
+          break;
+        const Item it = item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x));
+        shr.ring[slot] = it;
+        mbar_arrive(&it_full[slot]);
+        if (!it.more) break;
+      }
+    }
+  } else {
+    setmaxnreg_inc<SOFTMAX_REGS>();
+    // ---------------- softmax: warpgroup i = warps 4i..4i+3, TMEM lane quarter warp % 4
+    const int i = warp >> 2;
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + 128u * i + lane_off;
+    const uint32_t tO = tmem + 256u + 128u * i + lane_off;
+    const uint32_t tO1 = tmem + 384u + lane_off;  // warpgroup 1's accumulator (single's merge)
+    const int row_tok = row / p.group;            // the row's token in its tile
+    bool ok = true;
+    // sc: S phases of this warpgroup so far (one per step); oc*: o_done phases so
+    // far (one per item in which a warpgroup has steps); kt: the running key tile
+    uint32_t kt = 0, sc = 0, oc0 = 0, oc1 = 0;
+    // All softmax warps go on to an item together or not at all: a warp that gave up
+    // a wait still meets the others at the barriers of its item.
+    bool go = !bar_red_or(2, 256, !it_wait(0, 21));
+    for (uint32_t jn = 0; go; ++jn) {
+      const Item& it = shr.ring[jn & (RING - 1)];
+      if (!it.more) break;
+      const bool pair = it.pair;
+      const int n = i ? it.n1 : it.n0, n1 = it.n1, t0 = it.t0, lk = it.lk;
+      const int tok0 = (it.j0 + (pair ? i : 0)) * p.tpt;  // the tile's first token
+      // keys that the row sees (rows without a token: as if all), the fewest that
+      // a row of the warp sees, and the first key that some row of the tile does not
+      int lim = lk, lim_warp, part0 = lk;
+      if (p.causal) {
+        const int off1 = lk - it.lq + 1;
+        if (row_tok < p.tpt && tok0 + row_tok < it.lq) lim = min(lk, max(0, tok0 + row_tok + off1));
+        part0 = min(lk, max(0, tok0 + off1));
+      }
+      lim_warp = __reduce_min_sync(0xffffffffu, lim);
+      // Steps below `owned` use a value tile that the other warpgroup takes care of.
+      const int owned = pair && i == 1 ? it.n0 : 0;
+      float m = -INFINITY, l = 0.f;
+      // Value tile t in shared memory, one row per thread: rows past the sequence
+      // (other tokens or stale data) become zero, so that their zero probabilities
+      // add exactly 0; so do infinities and NaNs of keys that some row of the tile
+      // does not see, and the item is marked. False when the wait for V gave up.
+      auto take_out = [&](int t, uint32_t ktile) -> bool {
+        if (!mbar_wait_warp(&v_full[kv_stage(ktile)], kv_phase(ktile), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 11))
+          return false;
+        unsigned char* vr = sV(kv_stage(ktile)) + row * 128;
+        if (t * BKV + row >= lk) {
+#pragma unroll
+          for (int j = 0; j < C::NBOX; ++j)
+#pragma unroll
+            for (int c16 = 0; c16 < 8; ++c16)
+              *reinterpret_cast<uint4*>(vr + j * BOX_BYTES + c16 * 16) = make_uint4(0, 0, 0, 0);
+        } else if (t * BKV + row >= part0) {
+#pragma unroll 1
+          for (int c16 = 0; c16 < 8 * C::NBOX; ++c16) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(vr + (c16 >> 3) * BOX_BYTES + (c16 & 7) * 16);
+            const uint4 q = *reinterpret_cast<const uint4*>(w);
+            if (special16<F16>(q.x) | special16<F16>(q.y) | special16<F16>(q.z) | special16<F16>(q.w)) {
+              const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t bad = special16<F16>(qs[e]);
+                w[e] = qs[e] & ~((bad & 0x8000u ? 0xFFFFu : 0u) | (bad & 0x80000000u ? 0xFFFF0000u : 0u));
+              }
+              shr.special[jn & 1u] = 1;
+            }
+          }
+        }
+        fence_proxy_async_smem();  // before the tensor core reads the tile
+        return true;
+      };
+      // S_i complete means every earlier MMA is too (PV_i of the previous
+      // step included), so O_i can be rescaled and P_i written over S_i
+      // without another wait. tcgen05.ld / tcgen05.st are warp-collective:
+      // the whole warp rescales when any of its rows needs it (rows that do
+      // not use alpha = 1)
+      auto rescale_o = [&](bool rescale, float m_use) {
+        if (__any_sync(0xffffffffu, rescale)) {
+          const float alpha = rescale ? ex2(m - m_use) : 1.0f;
+#pragma unroll 1
+          for (int c = 0; c < HD / 32; ++c) {
+            float o[32];
+            tmem_ld32(tO + c * 32, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] *= alpha;
+            tmem_st32(tO + c * 32, o);
+          }
+          l *= alpha;
+        }
+      };
+      for (int s = 0; s < n && ok; ++s) {
+        const int t = item_tile(pair, t0, i, s);
+        const uint32_t ktile = kt + static_cast<uint32_t>(t - t0);
+        if (!mbar_wait_warp(&s_full[i], (sc + s) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 10)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // row max and row sum with 8 independent partials combined by a tree; a
+        // tile that every row of the warp sees whole takes paired instructions
+        const bool full_tile = (t + 1) * BKV <= lim_warp;
+        const int valid = lim - t * BKV;
+        float sv[BKV];
+#pragma unroll
+        for (int c = 0; c < BKV / 32; ++c) tmem_ld32(tS + c * 32, sv + c * 32);
+        tmem_ld_wait();
+        float mx8[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) mx8[u] = -INFINITY;
+        if (full_tile) {
+#pragma unroll
+          for (int j = 0; j < BKV; j += 16)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) mx8[u] = fmax3(mx8[u], sv[j + u], sv[j + 8 + u]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < BKV; ++j)
+            if (j < valid) mx8[j & 7] = fmaxf(mx8[j & 7], sv[j]);
+        }
+        const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]),
+                               fmaxf(mx8[6], mx8[7]));
+        const float m_tile = mx * p.scale_log2;
+        bool rescale = false;
+        float m_use = m;
+        if (s == 0) {
+          m_use = m_tile;
+        } else if (m_tile > m + RESCALE_LOG2) {
+          m_use = m_tile;
+          rescale = true;
+        }
+        // a row that has seen nothing but -inf: its probabilities are exp(-inf) = 0
+        const float shift = m_use == -INFINITY ? 0.f : -m_use;
+        float ls8[8];
+        if (full_tile) {
+          const uint64_t sc2 = f2(p.scale_log2, p.scale_log2), nm2 = f2(shift, shift);
+          uint64_t ls4[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) ls4[u] = 0ull;
+#pragma unroll
+          for (int c = 0; c < BKV / 2; ++c) {
+            float a, a1;
+            f2_split(f2_fma(f2(sv[2 * c], sv[2 * c + 1]), sc2, nm2), a, a1);
+            a = ex2(a);
+            a1 = ex2(a1);
+            sv[2 * c] = a;
+            sv[2 * c + 1] = a1;
+            ls4[c & 3] = f2_add(ls4[c & 3], f2(a, a1));
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) f2_split(ls4[u], ls8[2 * u], ls8[2 * u + 1]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) ls8[u] = 0.f;
+#pragma unroll
+          for (int j = 0; j < BKV; ++j) {
+            const float pj = j < valid ? ex2(fmaf(sv[j], p.scale_log2, shift)) : 0.f;
+            sv[j] = pj;
+            ls8[j & 7] += pj;
+          }
+        }
+        const float lsum =
+            ((ls8[0] + ls8[1]) + (ls8[2] + ls8[3])) + ((ls8[4] + ls8[5]) + (ls8[6] + ls8[7]));
+        if (s >= owned && (t + 1) * BKV > part0 && !take_out(t, ktile)) {
+          ok = false;
+          break;
+        }
+        rescale_o(rescale, m_use);
+        m = m_use;
+        l += lsum;
+        // P_i as 16-bit pairs (keys 2c, 2c+1 in column c) over the first 64
+        // columns of S_i, the A operand of the PV product
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          float pk[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c)
+            pk[c] = __uint_as_float(pack16<F16>(sv[64 * h2 + 2 * c], sv[64 * h2 + 2 * c + 1]));
+          tmem_st32(tS + 32 * h2, pk);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&p_full[i]);
+      }
+      // ---- output rows. A pair: warpgroup i writes its tile. A single:
+      // warpgroup 1 hands its row maximum and sum to warpgroup 0, which merges
+      // the two accumulators (each relative to its own maximum) and writes.
+      const bool writer = pair || i == 0;
+      const bool merge = !pair && n1 > 0;
+      if (!pair) {
+        if (i == 1) {
+          shr.m1[row] = m;
+          shr.l1[row] = l;
+        }
+        named_bar_sync(1, 256);
+      }
+      if (ok && writer) {
+        bool done = n == 0 || mbar_wait_warp(&o_done[i], (i ? oc1 : oc0) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 14);
+        if (merge)
+          done = done && mbar_wait_warp(&o_done[1], oc1 & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 15);
+        ok = done;
+        if (ok) {
+          tc_fence_after();
+          float a0 = 1.f, a1 = 0.f;
+          if (merge) {
+            const float m1 = shr.m1[row], l1 = shr.l1[row];
+            const float mm = fmaxf(m, m1);
+            a0 = m == mm ? 1.f : ex2(m - mm);  // (both -inf: 1)
+            a1 = m1 == mm ? 1.f : ex2(m1 - mm);
+            l = l * a0 + l1 * a1;
+            m = mm;
+          }
+          const bool special = shr.special[jn & 1u] != 0;
+          // The infinities and NaNs that were taken out of the value tiles, added to
+          // 32 columns of the rows that see them.
+          auto give_back = [&](int c, float* o) {
+            const int first = max(t0, part_tile(p, it)) * BKV, last = min(lim, it.t1 * BKV);
+            const uint16_t* v = static_cast<const uint16_t*>(p.v) + static_cast<long long>(it.hk) * p.v_head + 32 * c;
+            for (int j = first; j < last; ++j) {
+              const uint4* src = reinterpret_cast<const uint4*>(v + static_cast<long long>(it.k0 + j) * p.v_row);
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const uint4 q = __ldg(src + u);
+                const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t bad = special16<F16>(qs[e]);
+                  if (bad & 0x8000u) o[8 * u + 2 * e] += widen16<F16>(qs[e] & 0xFFFFu);
+                  if (bad & 0x80000000u) o[8 * u + 2 * e + 1] += widen16<F16>(qs[e] >> 16);
+                }
+              }
+            }
+          };
+          if (it.slot >= 0) {
+            // a piece: unnormalised rows, their maxima and sums
+            const long long at = (static_cast<long long>(it.slot) * 2 + (pair ? i : 0)) * BQ + row;
+            p.part_ml[at] = make_float2(m, l);
+            if (n > 0) {
+#pragma unroll 1
+              for (int c = 0; c < HD / 32; ++c) {
+                float o[32];
+                tmem_ld32(tO + c * 32, o);
+                if (merge) {
+                  float o1[32];
+                  tmem_ld32(tO1 + c * 32, o1);
+                  tmem_ld_wait_regs(o);
+                  tmem_ld_wait_regs(o1);
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) o[j] = o[j] * a0 + o1[j] * a1;
+                } else {
+                  tmem_ld_wait_regs(o);
+                }
+                if (special) give_back(c, o);
+                float* dst = p.part + at * HD + 32 * c;
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) st_f32x8(dst + j, o + j);
+              }
+            }
+          } else {
+            const float inv = lim == 0 ? 0.f : 1.0f / l;
+            // normalised rows to 16 bits, staged through shared memory so that
+            // the global stores leave as whole lines. Each warp owns a slice of its
+            // tile's Q: every S product of the tile, the last reader of Q,
+            // completed before O did, and the next item's Q is loaded only after
+            // this item's epi_done. (Not of the K stages: the other tile of a
+            // pair may have more steps.) The 16-byte units of a row are XOR-swizzled
+            // by the row, so neither the writes (one row per lane) nor the
+            // reads (consecutive units of a row) collide in the banks.
+            constexpr int UNITS = HD / 8;    // 16-byte units per row
+            constexpr int RPI = 32 / UNITS;  // rows per store instruction
+            uint4* stage = reinterpret_cast<uint4*>(smem + C::OFF_Q) + warp * 32 * UNITS;
+            auto stage_chunk = [&](int c, const float* o) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint4 v;
+                v.x = pack16<F16>(o[8 * j] * inv, o[8 * j + 1] * inv);
+                v.y = pack16<F16>(o[8 * j + 2] * inv, o[8 * j + 3] * inv);
+                v.z = pack16<F16>(o[8 * j + 4] * inv, o[8 * j + 5] * inv);
+                v.w = pack16<F16>(o[8 * j + 6] * inv, o[8 * j + 7] * inv);
+                stage[lane * UNITS + ((4 * c + j) ^ (lane & (UNITS - 1)))] = v;
+              }
+            };
+            if (!merge && !special) {
+              // all of O's columns in flight before one wait (the softmax's
+              // registers are free here)
+              float o[HD];
+#pragma unroll
+              for (int c = 0; c < HD / 32; ++c) tmem_ld32(tO + c * 32, o + c * 32);
+#pragma unroll
+              for (int c = 0; c < HD / 32; ++c) tmem_ld_wait_regs(o + c * 32);
+#pragma unroll
+              for (int c = 0; c < HD / 32; ++c) stage_chunk(c, o + c * 32);
+            } else {
+#pragma unroll 1
+              for (int c = 0; c < HD / 32; ++c) {
+                float o[32];
+                tmem_ld32(tO + c * 32, o);
+                if (merge) {
+                  float o1[32];
+                  tmem_ld32(tO1 + c * 32, o1);
+                  tmem_ld_wait_regs(o);
+                  tmem_ld_wait_regs(o1);
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) o[j] = o[j] * a0 + o1[j] * a1;
+                } else {
+                  tmem_ld_wait_regs(o);
+                }
+                if (special) give_back(c, o);
+                stage_chunk(c, o);
+              }
+            }
+            __syncwarp();
+            // rows of the tile that are a token's: row r is head r % group of token r / group
+            const int rows = min(p.tpt, it.lq - tok0) * p.group;
+            const uint32_t inv_g = (65536u + static_cast<uint32_t>(p.group) - 1u) / static_cast<uint32_t>(p.group);
+            const long long out0 = static_cast<long long>(it.q0 + tok0) * p.out_row +
+                                   static_cast<long long>(it.hk) * p.group * p.out_head;
+            const int u = lane % UNITS;
+#pragma unroll 4
+            for (int k = 0; k < 32 / RPI; ++k) {
+              const int rr = k * RPI + lane / UNITS;  // row within the warp's 32
+              const int r = (warp & 3) * 32 + rr;     // row within the tile
+              if (r < rows) {
+                const int tok = static_cast<int>((static_cast<uint32_t>(r) * inv_g) >> 16), h = r - tok * p.group;
+                reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + out0 + tok * p.out_row + h * p.out_head)[u] =
+                    stage[rr * UNITS + (u ^ (rr & (UNITS - 1)))];
+              }
+            }
+          }
+        }
+      }
+      // end of the item: the staging reads are done (generic proxy) before
+      // the producer's next Q copies (async proxy) overwrite them;
+      // in a single warpgroup 1's accumulator has been read before its
+      // next PV may overwrite it
+      const int n0_all = it.n0, len = it.t1 - t0;
+      if (threadIdx.x == 0) shr.special[(jn + 1) & 1u] = 0;  // (last read before the previous item's end)
+      fence_proxy_async_smem();
+      tc_fence_before();
+      ok = ok && it_wait(jn + 1, 21);
+      go = !bar_red_or(2, 256, !ok);
+      if (!go) break;
+      if (threadIdx.x == 0) mbar_arrive(epi_done);
+      if (lane == 0) mbar_arrive(&it_empty[jn & (RING - 1)]);
+      sc += static_cast<uint32_t>(n);
+      oc0 += n0_all > 0 ? 1u : 0u;
+      oc1 += n1 > 0 ? 1u : 0u;
+      kt += static_cast<uint32_t>(len);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// -------------------------------------------------------------------- join --
+//
+// The pieces of the cut jobs, joined: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p with
+// M the largest m_p. A warp per row, a lane per four (two) columns; the
+// pieces' maxima and sums are read 32 at a time, a lane each. Bound by the
+// L2 reads of the pieces' rows. The plan is made before the wait for the main
+// kernel: the offsets were there before that began.
+
+constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_ROWS = JOIN_THREADS / 32;  // rows per unit of work
+
+struct JoinShared {
+  Plan plan;
+  PlanScratch<JOIN_THREADS> scratch;
+};
+
+template <int HD, bool F16>
+__global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ VarParams p) {
+  extern __shared__ __align__(16) unsigned char join_raw[];
+  JoinShared& sh = *reinterpret_cast<JoinShared*>(join_raw);
+  plan_build<JOIN_THREADS, true>(p, sh.plan, sh.scratch);
+  pdl_wait();
+  pdl_trigger();
+  constexpr int COLS = HD / 32;
+  constexpr int UNITS = BQ / JOIN_ROWS;  // of a tile
+  const int warp = warp_id(), lane = lane_id();
+  const long long units = static_cast<long long>(sh.plan.n_cut) * p.kv_heads * 2 * UNITS;
+  for (long long w = blockIdx.x; w < units; w += gridDim.x) {
+    const int r = static_cast<int>(w % UNITS) * JOIN_ROWS + warp;
+    const int tile = static_cast<int>(w / UNITS) & 1;
+    const int job = static_cast<int>(w / (2 * UNITS));
+    const int e = job / p.kv_heads, hk = job - e * p.kv_heads;
+    const Seq s = sequence<false>(p, sh.plan.seq[e] >> 16);
+    const int j = 2 * (sh.plan.seq[e] & 0xffff) + tile, tok = j * p.tpt + r / p.group;
+    if (r / p.group >= p.tpt || tok >= s.lq) continue;
+    const int n = pieces_of(sh.plan.steps[e], sh.plan.share);
+    const long long slot = static_cast<long long>(sh.plan.items[e]) + hk * n;
+    auto row_of = [&](int q) { return ((slot + q) * 2 + tile) * BQ + r; };
+    float M = -INFINITY;
+    for (int q = lane; q < n; q += 32) M = fmaxf(M, p.part_ml[row_of(q)].x);
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    float o[COLS] = {}, total = 0.f;
+    for (int q0 = 0; q0 < n; q0 += 32) {
+      float a = 0.f;
+      if (q0 + lane < n) {
+        const float2 ml = p.part_ml[row_of(q0 + lane)];
+        // a piece in which the row saw nothing has no rows to read
+        a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.x == M ? 1.f : ex2(ml.x - M);
+        total = fmaf(a, ml.y, total);
+      }
+      const int most = min(32, n - q0);
+#pragma unroll 4
+      for (int q = 0; q < most; ++q) {
+        const float f = __shfl_sync(0xffffffffu, a, q);
+        if (f == 0.f) continue;
+        const float* src = p.part + row_of(q0 + q) * HD + COLS * lane;
+        if (COLS == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(src);
+          o[0] = fmaf(f, v.x, o[0]);
+          o[1] = fmaf(f, v.y, o[1]);
+          o[COLS - 2] = fmaf(f, v.z, o[COLS - 2]);
+          o[COLS - 1] = fmaf(f, v.w, o[COLS - 1]);
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(src);
+          o[0] = fmaf(f, v.x, o[0]);
+          o[1] = fmaf(f, v.y, o[1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+    const float inv = s.seen(p, tok) == 0 ? 0.f : 1.0f / total;
+    uint16_t* dst = static_cast<uint16_t*>(p.out) + static_cast<long long>(s.q0 + tok) * p.out_row +
+                    static_cast<long long>(hk * p.group + r % p.group) * p.out_head + COLS * lane;
+    if (COLS == 4)
+      *reinterpret_cast<uint2*>(dst) =
+          make_uint2(pack16<F16>(o[0] * inv, o[1] * inv), pack16<F16>(o[COLS - 2] * inv, o[COLS - 1] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(dst) = pack16<F16>(o[0] * inv, o[1] * inv);
+  }
+}
+
+template <int HD, bool F16>
+cudaError_t launch_hd(const hilo_attn_shape& s, const VarParams& p, const void* q, const void* k, const void* v,
+                      int* launches, cudaStream_t st) {
+  // k and v of no rows: any address will do, all keys are masked
+  const bool none = s.rows_k == 0;
+  const uint64_t rows_k = none ? 1 : s.rows_k;
+  CUtensorMap tm_q, tm_k, tm_v;
+  const uint64_t hd = HD;
+  if (!encode_tmap_16bit_3d(&tm_q, q, hd, s.heads, s.rows_q, s.q_head, s.q_row, 64, p.group, p.tpt) ||
+      !encode_tmap_16bit_3d(&tm_k, none ? q : k, hd, none ? 1 : s.kv_heads, rows_k, s.k_head, s.k_row, 64, 1, BKV) ||
+      !encode_tmap_16bit_3d(&tm_v, none ? q : v, hd, none ? 1 : s.kv_heads, rows_k, s.v_head, s.v_row, 64, 1, BKV))
+    return cudaErrorInvalidValue;
+  auto* kern = attn_var_kernel<HD, F16>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<HD>::SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  // the register split must fit what the CTA is launched with, or the
+  // softmax warpgroups' setmaxnreg.inc would wait for registers forever
+  // (one number for every device: the library holds one binary)
+  static std::atomic<int> known{0};
+  int regs = known.load(std::memory_order_relaxed);
+  if (regs == 0) {
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, kern);
+    if (e != cudaSuccess) return e;
+    regs = fa.numRegs;
+    known.store(regs, std::memory_order_relaxed);
+  }
+  if (static_cast<long long>(regs) * THREADS < 256LL * SOFTMAX_REGS + 128LL * CONTROL_REGS)
+    return cudaErrorInvalidConfiguration;
+  e = launch_pdl(kern, dim3(p.grid), dim3(THREADS), Cfg<HD>::SMEM_BYTES, st, tm_q, tm_k, tm_v, p);
+  if (e != cudaSuccess) return e;
+  *launches = 1;
+  if (!p.may_cut) return cudaSuccess;
+  auto* join = attn_join_kernel<HD, F16>;
+  e = cudaFuncSetAttribute(join, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(JoinShared));
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(join, dim3(p.grid), dim3(JOIN_THREADS), sizeof(JoinShared), st, p);
+  if (e == cudaSuccess) *launches = 2;
+  return e;
+}
+
+// Whether a job could have more steps than the smallest piece.
+bool may_cut(const hilo_attn_shape& s) { return (s.rows_k + BKV - 1) / BKV > MIN_STEPS; }
+
+constexpr size_t SLOTS = static_cast<size_t>(SLOTS_PER_CTA) * ATTN_MAX_CTAS;
+
+}  // namespace
+
+size_t attn_var_workspace_bytes(const hilo_attn_shape& s) {
+  // (32 bytes to bring the rows onto the boundary that they are stored from)
+  return may_cut(s) ? SLOTS * 2 * BQ * (static_cast<size_t>(s.head_dim) * sizeof(float) + sizeof(float2)) + 32 : 32;
+}
+
+cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, const int32_t* cu_k, const void* q,
+                                 const void* k, const void* v, void* out, void* ws, int num_sms, int* launches,
+                                 cudaStream_t st) {
+  *launches = 0;
+  VarParams p;
+  p.cu_q = cu_q;
+  p.cu_k = cu_k;
+  p.v = v;
+  p.out = out;
+  p.part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ws) + 31) & ~static_cast<uintptr_t>(31));
+  p.part_ml = reinterpret_cast<float2*>(p.part + SLOTS * 2 * BQ * s.head_dim);
+  p.v_row = s.v_row;
+  p.v_head = s.v_head;
+  p.out_row = s.out_row;
+  p.out_head = s.out_head;
+  p.B = s.B;
+  p.kv_heads = s.kv_heads;
+  p.group = s.heads / s.kv_heads;
+  p.tpt = BQ / p.group;
+  p.causal = s.causal;
+  p.rows_q = s.rows_q;
+  p.rows_k = s.rows_k;
+  // a persistent grid: one CTA per SM; each takes its share of the items, whose
+  // number is known on the device only
+  p.grid = num_sms < 1 ? 1 : num_sms < ATTN_MAX_CTAS ? num_sms : ATTN_MAX_CTAS;
+  p.may_cut = may_cut(s);
+  const double scale = s.scale > 0.f ? s.scale : 1.0 / sqrt(static_cast<double>(s.head_dim));
+  p.scale_log2 = static_cast<float>(1.4426950408889634 * scale);
+  const bool f16 = s.dtype == HILO_F16;
+  if (s.head_dim == 128)
+    return f16 ? launch_hd<128, true>(s, p, q, k, v, launches, st) : launch_hd<128, false>(s, p, q, k, v, launches, st);
+  return f16 ? launch_hd<64, true>(s, p, q, k, v, launches, st) : launch_hd<64, false>(s, p, q, k, v, launches, st);
+}
+
+int attn_var_take_device_error() {
+  int v = 0, z = 0;
+  if (cudaMemcpyFromSymbol(&v, g_attn_var_err, sizeof(int)) != cudaSuccess) return -1;
+  if (v) cudaMemcpyToSymbol(g_attn_var_err, &z, sizeof(int));
+  return v;
+}
+
+}  // namespace hilo

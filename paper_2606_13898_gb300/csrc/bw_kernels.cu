@@ -941,6 +941,73 @@ __global__ void __launch_bounds__(256) row_sizes_kernel(const uint8_t* __restric
   }
 }
 
+// The rows' places: (t_img, h0 + p, w0 + q) of each image row, (p, q) the token of a
+// kept row, the mean of the class members of a pooled window (the sum of their whole
+// coordinates is exact, one division), the middle of a low-frequency window; txt0 + j
+// txt_step three times for text row j. One thread per row of the row space; bound by the
+// chain of dependent reads (offsets, counts, row source, labels).
+__global__ void __launch_bounds__(256) row_positions_kernel(const uint8_t* __restrict__ labels,
+                                                            const int32_t* __restrict__ row_src,
+                                                            const int32_t* __restrict__ counts,
+                                                            const int32_t* __restrict__ cu_img,
+                                                            const hilo_positions_origin o,
+                                                            float* __restrict__ pos, int B, int T, int H, int W,
+                                                            int cap, int lf) {
+  pdl_wait();
+  pdl_trigger();
+  const int N = H * W, n_txt = B * T;
+  const long long total = static_cast<long long>(n_txt) + max(0, min(cu_img[B], cap));
+  const long long step = static_cast<long long>(gridDim.x) * blockDim.x;
+  for (long long i = blockIdx.x * static_cast<long long>(blockDim.x) + threadIdx.x; i < total; i += step) {
+    float t, h, w;
+    if (i < n_txt) {
+      t = h = w = fmaf(static_cast<float>(static_cast<int>(i) % T), o.txt_step, o.txt0);
+    } else {
+      const int r = static_cast<int>(i - n_txt);
+      int b = 0;
+      for (int hi = B; hi - b > 1;) {
+        const int mid = (b + hi) >> 1;
+        if (__ldg(cu_img + mid) <= r) b = mid;
+        else hi = mid;
+      }
+      const int local = r - __ldg(cu_img + b);
+      const int nk = counts[3 * b], n2 = counts[3 * b + 1];
+      const int size = local < nk ? 1 : lf ? lf : local < nk + n2 ? 2 : 4;
+      const int src = row_src[r], Wn = W / size;
+      if (!HILO_DCHECK(local >= 0 && src >= 0 && src < (H / size) * Wn, DCHECK_ROW_POSITIONS_SRC)) continue;
+      const int p0 = size * (src / Wn), q0 = size * (src % Wn);
+      h = static_cast<float>(p0);
+      w = static_cast<float>(q0);
+      if (local >= nk) {
+        if (lf) {
+          h += 0.5f * static_cast<float>(lf - 1);
+          w += 0.5f * static_cast<float>(lf - 1);
+        } else {
+          const uint8_t cls = size == 2 ? HILO_LABEL_POOL2 : HILO_LABEL_POOL4;
+          const uint8_t* lab = labels + static_cast<long long>(b) * N + p0 * W + q0;
+          int n = 0, sp = 0, sq = 0;
+          for (int y = 0; y < size; ++y)
+            for (int x = 0; x < size; ++x)
+              if (lab[y * W + x] == cls) {
+                ++n;
+                sp += p0 + y;
+                sq += q0 + x;
+              }
+          h = __fdiv_rn(static_cast<float>(sp), static_cast<float>(n));
+          w = __fdiv_rn(static_cast<float>(sq), static_cast<float>(n));
+        }
+      }
+      t = o.t_img;
+      h += o.h0;
+      w += o.w0;
+    }
+    float* dst = pos + 3 * i;
+    dst[0] = t;
+    dst[1] = h;
+    dst[2] = w;
+  }
+}
+
 // ============================================================= unpack =====
 //
 // One warp per token, bound by HBM. Where the fp32 arrays begin on 32 bytes (WIDE) a
@@ -1584,6 +1651,14 @@ cudaError_t launch_row_sizes(const uint8_t* labels, const int32_t* row_src, cons
   if (cap <= 0) return cudaSuccess;
   return launch_pdl(row_sizes_kernel, dim3(grid_for(cap, 256, num_sms, 4)), dim3(256), 0, st, labels, row_src,
                     counts, cu_img, n_img, B, H, W, cap, lf);
+}
+
+cudaError_t launch_row_positions(const uint8_t* labels, const int32_t* row_src, const int32_t* counts,
+                                 const int32_t* cu_img, const hilo_positions_origin& o, float* pos, int B, int T,
+                                 int H, int W, int cap, int lf, int num_sms, cudaStream_t st) {
+  const long long rows = static_cast<long long>(B) * T + cap;
+  return launch_pdl(row_positions_kernel, dim3(grid_for(rows, 256, num_sms, 4)), dim3(256), 0, st, labels, row_src,
+                    counts, cu_img, o, pos, B, T, H, W, cap, lf);
 }
 
 cudaError_t launch_unpack_delta(const float* out_img, const void* packed, const void* x,

@@ -65,6 +65,24 @@ cudaError_t launch_quant_rows(const void* src, int type, int cols, int rows_stat
 cudaError_t launch_bf16_to_f16(const void* src, void* dst, long long n, int num_sms,
                                cudaStream_t st);
 
+// ---- rows of the conditioned block (rows.cu)
+// What hilo_gate_norm does to the row space: hilo_norm_shape with its vectors and buffers.
+struct NormArgs {
+  hilo_norm_shape s;
+  hilo_norm_vectors vec[2];  // text, image
+  const int32_t* cu_img;
+  const void *u_txt, *u_img, *y;
+  void *u_out, *h;
+  float* h_scale;
+};
+cudaError_t launch_gate_norm(const NormArgs& a, int num_sms, cudaStream_t st);
+// Rows 0 .. min(row_base + *n_rows, s.rows) - 1 (all where n_rows is null).
+cudaError_t launch_rope(const hilo_rope_shape& s, const void* x, const float* pos, int row_base,
+                        const int32_t* n_rows, void* y, int num_sms, cudaStream_t st);
+cudaError_t launch_row_positions(const uint8_t* labels, const int32_t* row_src, const int32_t* counts,
+                                 const int32_t* cu_img, const hilo_positions_origin& o, float* pos, int B, int T,
+                                 int H, int W, int cap, int lf, int num_sms, cudaStream_t st);
+
 // ---- the paper's Sobel selector (select.cu)
 size_t sobel_workspace_bytes(int B, int H, int W);
 cudaError_t launch_sobel_select(const float* img, int B, int H, int W, int C, int patch,
@@ -122,6 +140,15 @@ struct AttnArgs {
 };
 cudaError_t launch_attention(const AttnArgs& a, int num_sms, cudaStream_t st);
 int attn_take_device_error();
+// ---- tcgen05 attention of packed sequences (attn_var.cu)
+constexpr int ATTN_MAX_SEQUENCES = 4096;  // their offsets are kept in shared memory
+constexpr int ATTN_MAX_CTAS = 160;        // sizes the workspace (a GB300 has 152 SMs)
+size_t attn_var_workspace_bytes(const hilo_attn_shape& s);
+// *launches: kernels launched, also where one of them fails
+cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, const int32_t* cu_k, const void* q,
+                                 const void* k, const void* v, void* out, void* ws, int num_sms, int* launches,
+                                 cudaStream_t st);
+int attn_var_take_device_error();
 // The wait-timeout probe: one bounded mbarrier wait that runs out; its code
 // is read (and cleared) like the kernels' device error words.
 cudaError_t launch_wait_probe(cudaStream_t st);
@@ -139,6 +166,9 @@ int check_block_shape(const hilo_shape* shape);
 enum TmapType : int { TMAP_BF16 = 0, TMAP_U8 = 1 };  // 16-bit elements (bf16 and fp16 alike), bytes
 bool encode_tmap_2d(CUtensorMap* map, TmapType type, const void* base, uint64_t inner, uint64_t outer,
                     uint64_t row_stride_elems, uint32_t box_inner, uint32_t box_outer);
+// 16-bit elements over three axes: [n2][n1][n0], strides in elements
+bool encode_tmap_16bit_3d(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, uint64_t n2, uint64_t stride1,
+                          uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2);
 bool encode_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                          uint64_t row_stride_elems, uint32_t box_inner, uint32_t box_outer);
 

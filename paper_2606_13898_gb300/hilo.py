@@ -26,6 +26,8 @@ HILO_ERR_SHAPE = -2
 HILO_ERR_TIMEOUT, HILO_ERR_CHECK = -5, -7
 HILO_KEEP, HILO_POOL2, HILO_POOL4 = 0, 1, 2
 HILO_BF16, HILO_F32 = 0, 1
+HILO_E4M3 = 3
+HILO_NORM_NONE, HILO_NORM_LAYER, HILO_NORM_RMS = 0, 1, 2
 
 
 class HiloError(RuntimeError):
@@ -61,6 +63,49 @@ class hilo_block_weights_fp8(ctypes.Structure):
     _fields_ = [("txt", hilo_stream_weights_fp8), ("img", hilo_stream_weights_fp8)]
 
 
+class hilo_positions_origin(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("t_img", "h0", "w0", "txt0", "txt_step")]
+
+
+class hilo_rotation(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int32), ("axis_dims", ctypes.c_int32 * 4), ("interleaved", ctypes.c_int32),
+                ("per_axis", ctypes.c_int32), ("theta", ctypes.c_double)]
+
+
+class hilo_rope_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("rows", "heads", "head_dim", "dtype")]
+                + [(n, ctypes.c_int64) for n in ("x_row", "x_head", "y_row", "y_head")] + [("rot", hilo_rotation)])
+
+
+_VECTORS = ("gate", "scale", "shift", "w_branch", "w_norm", "b_norm")
+
+
+class hilo_norm_vectors(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in _VECTORS]
+
+
+class hilo_norm_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "T", "cap", "d", "norm", "norm_branch", "u_dtype", "y_dtype",
+                                               "u_out_dtype", "h_dtype", "vec_dtype")]
+                + [("eps", ctypes.c_float), ("resid_scale", ctypes.c_float), ("vec_row", ctypes.c_int64)])
+
+
+_ATTN_STRIDES = ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row", "out_head")
+
+
+class hilo_attn_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "head_dim", "causal", "dtype", "rows_q",
+                                               "rows_k")]
+                + [("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in _ATTN_STRIDES])
+
+
+class hilo_block_mod(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("norm", "norm_branch", "vec_dtype")]
+                + [("eps", ctypes.c_float), ("resid_scale", ctypes.c_float), ("vec_row", ctypes.c_int64)]
+                + [(n, hilo_norm_vectors) for n in ("txt_attn", "img_attn", "txt_mlp", "img_mlp")]
+                + [("pos", ctypes.c_void_p), ("rot", hilo_rotation)])
+
+
 EXPORTS = ("hilo_status_string", "hilo_last_error", "hilo_sync_status", "hilo_device_info",
            "hilo_score", "hilo_split_workspace_bytes", "hilo_split", "hilo_pack",
            "hilo_block_workspace_bytes", "hilo_block_forward", "hilo_unpack", "hilo_unpack_update",
@@ -68,7 +113,9 @@ EXPORTS = ("hilo_status_string", "hilo_last_error", "hilo_sync_status", "hilo_de
            "hilo_block_forward_static_ws", "hilo_sobel_workspace_bytes", "hilo_sobel_select",
            "hilo_split_regions", "hilo_unpack_delta", "hilo_row_sizes", "hilo_block_forward_prop",
            "hilo_row_capacity", "hilo_quantize_rows_e4m3", "hilo_block_fp8_workspace_bytes",
-           "hilo_block_forward_fp8", "hilo_block_forward_fp8_prop", "hilo_debug_wait_timeout")
+           "hilo_block_forward_fp8", "hilo_block_forward_fp8_prop", "hilo_debug_wait_timeout",
+           "hilo_row_positions", "hilo_rope", "hilo_gate_norm", "hilo_attention_workspace_bytes", "hilo_attention",
+           "hilo_block_forward_mod")
 
 _lib = None
 
@@ -124,6 +171,14 @@ def lib() -> ctypes.CDLL:
                                             I, P, P, P, S, P]),
         "hilo_block_forward_prop": (I, [shp, ctypes.POINTER(hilo_block_weights), P, ctypes.c_int32, P, P, I,
                                         P, P, P, S, P]),
+        "hilo_row_positions": (I, [shp, spo, ctypes.POINTER(hilo_positions_origin), P, ctypes.c_int32, P]),
+        "hilo_rope": (I, [ctypes.POINTER(hilo_rope_shape), P, P, P, P, P]),
+        "hilo_gate_norm": (I, [ctypes.POINTER(hilo_norm_shape), ctypes.POINTER(hilo_norm_vectors),
+                               ctypes.POINTER(hilo_norm_vectors), P, P, P, P, P, P, P, P]),
+        "hilo_attention_workspace_bytes": (S, [ctypes.POINTER(hilo_attn_shape)]),
+        "hilo_attention": (I, [ctypes.POINTER(hilo_attn_shape), P, P, P, P, P, P, P, S, P]),
+        "hilo_block_forward_mod": (I, [shp, ctypes.POINTER(hilo_block_weights), ctypes.POINTER(hilo_block_mod), P,
+                                       ctypes.c_int32, P, P, I, P, P, P, S, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -311,6 +366,178 @@ class DeviceWeightsFP8:
         return st
 
 
+def _kept(obj, build):
+    """obj's C struct, built once: the object is frozen and the C entry points only read it."""
+    st = obj.__dict__.get("_c")
+    if st is None:
+        st = build()
+        obj.__dict__["_c"] = st
+    return st
+
+
+@dataclasses.dataclass(frozen=True)
+class RowPositions:
+    """Where the grid and the text begin (hilo_row_positions)."""
+
+    t_img: float = 0.0
+    h0: float = 0.0
+    w0: float = 0.0
+    txt0: float = 0.0
+    txt_step: float = 0.0
+
+    def c(self) -> hilo_positions_origin:
+        return _kept(self, lambda: hilo_positions_origin(self.t_img, self.h0, self.w0, self.txt0, self.txt_step))
+
+
+def _rotation(axis_dims, theta, interleaved, per_axis) -> hilo_rotation:
+    dims = tuple(axis_dims)
+    if not 1 <= len(dims) <= 4:
+        raise ValueError(f"one to four axes: axis_dims={dims}")
+    return hilo_rotation(len(dims), (ctypes.c_int32 * 4)(*dims), int(interleaved), int(per_axis), theta)
+
+
+@dataclasses.dataclass(frozen=True)
+class RopeShape:
+    """Rows and rotation of hilo_rope. Strides in elements; None: dense rows of dense heads."""
+
+    rows: int
+    heads: int
+    head_dim: int
+    dtype: int
+    axis_dims: tuple
+    theta: float = 10000.0
+    interleaved: int = 1
+    per_axis: int = 1
+    x_row: int | None = None
+    x_head: int | None = None
+    y_row: int | None = None
+    y_head: int | None = None
+
+    def c(self) -> hilo_rope_shape:
+        def build():
+            row, head = self.heads * self.head_dim, self.head_dim
+            given = (self.x_row, self.x_head, self.y_row, self.y_head)
+            strides = (d if s is None else s for s, d in zip(given, (row, head, row, head)))
+            return hilo_rope_shape(self.rows, self.heads, self.head_dim, self.dtype, *strides,
+                                   _rotation(self.axis_dims, self.theta, self.interleaved, self.per_axis))
+        return _kept(self, build)
+
+
+@dataclasses.dataclass
+class NormVectors:
+    """One stream's vectors of hilo_gate_norm: device tensors (or addresses), None where there is none."""
+
+    gate: object = None
+    scale: object = None
+    shift: object = None
+    w_branch: object = None
+    w_norm: object = None
+    b_norm: object = None
+
+    def c(self) -> hilo_norm_vectors:
+        """The C struct of the device pointers, rebuilt only when one of the vectors is replaced."""
+        ts = (self.gate, self.scale, self.shift, self.w_branch, self.w_norm, self.b_norm)
+        cached = self.__dict__.get("_c")
+        if cached is None or any(a is not b for a, b in zip(cached[1], ts)):
+            cached = (hilo_norm_vectors(*(_ptr(t) for t in ts)), ts)
+            self.__dict__["_c"] = cached
+        return cached[0]
+
+
+@dataclasses.dataclass(frozen=True)
+class NormShape:
+    """Rows, norms and dtypes of hilo_gate_norm. vec_row None: dense vectors, a row of d per image."""
+
+    B: int
+    T: int
+    cap: int
+    d: int
+    norm: int = HILO_NORM_LAYER
+    norm_branch: int = HILO_NORM_NONE
+    eps: float = 1e-6
+    resid_scale: float = 1.0
+    u_dtype: int = HILO_F32
+    y_dtype: int = HILO_BF16
+    u_out_dtype: int = HILO_F32
+    h_dtype: int = HILO_BF16
+    vec_dtype: int = HILO_BF16
+    vec_row: int | None = None
+
+    def c(self) -> hilo_norm_shape:
+        return _kept(self, lambda: hilo_norm_shape(
+            self.B, self.T, self.cap, self.d, self.norm, self.norm_branch, self.u_dtype, self.y_dtype,
+            self.u_out_dtype, self.h_dtype, self.vec_dtype, self.eps, self.resid_scale,
+            self.d if self.vec_row is None else self.vec_row))
+
+
+@dataclasses.dataclass(frozen=True)
+class AttnShape:
+    """Sequences and heads of hilo_attention. Strides in elements; None: dense rows of dense heads.
+    scale 0: 1 / sqrt(head_dim)."""
+
+    B: int
+    heads: int
+    kv_heads: int
+    head_dim: int
+    rows_q: int
+    rows_k: int
+    causal: int = 1
+    dtype: int = HILO_BF16
+    scale: float = 0.0
+    q_row: int | None = None
+    q_head: int | None = None
+    k_row: int | None = None
+    k_head: int | None = None
+    v_row: int | None = None
+    v_head: int | None = None
+    out_row: int | None = None
+    out_head: int | None = None
+
+    def c(self) -> hilo_attn_shape:
+        def build():
+            q, kv = self.heads * self.head_dim, self.kv_heads * self.head_dim
+            dense = (q, self.head_dim, kv, self.head_dim, kv, self.head_dim, q, self.head_dim)
+            given = (getattr(self, n) for n in _ATTN_STRIDES)
+            return hilo_attn_shape(self.B, self.heads, self.kv_heads, self.head_dim, int(self.causal), self.dtype,
+                                   self.rows_q, self.rows_k, self.scale,
+                                   *(d if s is None else s for s, d in zip(given, dense)))
+        return _kept(self, build)
+
+
+@dataclasses.dataclass
+class BlockMod:
+    """Conditioning of one block (hilo_block_forward_mod). axis_dims None: no rotary positions. The
+    NormVectors and their tensors are fixed after construction (their values may change)."""
+
+    txt_attn: NormVectors
+    img_attn: NormVectors
+    txt_mlp: NormVectors
+    img_mlp: NormVectors
+    vec_row: int
+    norm: int = HILO_NORM_LAYER
+    norm_branch: int = HILO_NORM_NONE
+    vec_dtype: int = HILO_BF16
+    eps: float = 1e-6
+    resid_scale: float = 1.0
+    axis_dims: tuple | None = None
+    theta: float = 10000.0
+    interleaved: int = 1
+    per_axis: int = 1
+
+    def c(self, pos) -> hilo_block_mod:
+        """The C struct, built once, with the positions of this call (None without rotary positions)."""
+        def build():
+            rot = hilo_rotation() if self.axis_dims is None else _rotation(self.axis_dims, self.theta,
+                                                                           self.interleaved, self.per_axis)
+            return hilo_block_mod(self.norm, self.norm_branch, self.vec_dtype, self.eps, self.resid_scale, self.vec_row,
+                                  self.txt_attn.c(), self.img_attn.c(), self.txt_mlp.c(), self.img_mlp.c(), None, rot)
+        if (pos is None) != (self.axis_dims is None):
+            raise ValueError("positions and axis_dims go together")
+        st = hilo_block_mod.from_buffer_copy(_kept(self, build))  # calls of other threads have their own
+        st.pos = _ptr(pos)
+        return st
+
+
 # ---------------------------------------------------------------------------
 # The C entry points
 # ---------------------------------------------------------------------------
@@ -444,6 +671,50 @@ def hilo_row_sizes(shape: Shape, split: SplitBuffers, n_img, cap: int, stream=No
                                                   _stream(stream)))
 
 
+def hilo_row_positions(shape: Shape, split: SplitBuffers, origin: RowPositions, pos, cap: int, stream=None) -> None:
+    s, o, g = shape.c(), split.c(), origin.c()
+    _check("hilo_row_positions", lib().hilo_row_positions(ctypes.byref(s), ctypes.byref(o), ctypes.byref(g), _ptr(pos),
+                                                          cap, _stream(stream)))
+
+
+def hilo_rope(shape: RopeShape, x, pos, n_rows, y, stream=None) -> None:
+    s = shape.c()
+    _check("hilo_rope", lib().hilo_rope(ctypes.byref(s), _ptr(x), _ptr(pos), _ptr(n_rows), _ptr(y), _stream(stream)))
+
+
+def hilo_gate_norm(shape: NormShape, txt: NormVectors | None, img: NormVectors, cu_img, u_txt, u_img, y, u_out, h,
+                   h_scale, stream=None) -> None:
+    s, i = shape.c(), img.c()
+    x = None if txt is None else ctypes.byref(txt.c())
+    _check("hilo_gate_norm", lib().hilo_gate_norm(ctypes.byref(s), x, ctypes.byref(i), _ptr(cu_img), _ptr(u_txt),
+                                                  _ptr(u_img), _ptr(y), _ptr(u_out), _ptr(h), _ptr(h_scale),
+                                                  _stream(stream)))
+
+
+def hilo_attention_workspace_bytes(shape: AttnShape) -> int:
+    s = shape.c()
+    n = int(lib().hilo_attention_workspace_bytes(ctypes.byref(s)))
+    if n == 0:
+        raise HiloError("hilo_attention_workspace_bytes", HILO_ERR_SHAPE, lib().hilo_last_error().decode())
+    return n
+
+
+def hilo_attention(shape: AttnShape, cu_q, cu_k, q, k, v, out, ws, ws_bytes: int, stream=None) -> None:
+    s = shape.c()
+    _check("hilo_attention", lib().hilo_attention(ctypes.byref(s), _ptr(cu_q), _ptr(cu_k), _ptr(q), _ptr(k), _ptr(v),
+                                                  _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def hilo_block_forward_mod(shape: Shape, weights: DeviceWeights, mod: BlockMod, pos, cu_img, cap: int, in_txt, in_img,
+                           in_dtype: int, n_img, out, ws, ws_bytes: int, stream=None) -> None:
+    s = shape.c()
+    w = weights.c()
+    m = mod.c(pos)
+    _check("hilo_block_forward_mod", lib().hilo_block_forward_mod(
+        ctypes.byref(s), ctypes.byref(w), ctypes.byref(m), _ptr(cu_img), cap, _ptr(in_txt), _ptr(in_img), in_dtype,
+        _ptr(n_img), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
 def hilo_block_forward_static_ws(shape: Shape, weights: DeviceWeights, cu_img, cap: int, in_txt, in_img,
                                  in_dtype: int, out, stream=None) -> None:
     """hilo_block_forward with the library's built-in scratch (no workspace argument)."""
@@ -517,6 +788,20 @@ class HotPath:
         self.ws_bytes = hilo_block_workspace_bytes(shape, self.cap)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         self.weights_fp8 = None
+        self.mods = self.origin = self.pos = None
+
+    def enable_mod(self, mods: list, origin: RowPositions | None = None) -> None:
+        """Makes run(..., mod=True) available: one BlockMod per block, and where
+        the positions of their rotations begin (needed if any block rotates)."""
+        rotated = [m.axis_dims for m in mods if m.axis_dims is not None]
+        if rotated and origin is None:
+            raise ValueError("rotary positions need an origin")
+        if any(len(dims) != 3 for dims in rotated):
+            raise ValueError("rows have three coordinates: a block that rotates has three axes")
+        self.mods, self.origin = mods, origin
+        if origin is not None:
+            rows = self.shape.B * self.shape.T + self.cap
+            self.pos = torch.empty(rows, 3, dtype=torch.float32, device=self.out.device)
 
     def enable_fp8(self, weights_fp8: list) -> None:
         """Makes run(..., fp8=True) available: one DeviceWeightsFP8 per block
@@ -536,13 +821,17 @@ class HotPath:
         return self.out.data_ptr() + self.shape.B * self.shape.T * self.shape.d * self.out.element_size()
 
     def run(self, x, text, mask, k_keep, k_mid, stream=None, unpack: bool = True, regions: bool = False,
-            prop: bool = False, fp8: bool = False) -> None:
+            prop: bool = False, fp8: bool = False, mod: bool = False) -> None:
         """One pass. regions=True takes the window-granular split and the
         delta unpool instead of the token-granular split and the nearest
         unpool; prop=True weights each packed row's attention by its row size
         (proportional attention). A shape with lf > 0 runs the separate
         low-frequency token set (with the delta unpool). fp8=True runs the
-        blocks with e4m3 GEMM operands (enable_fp8 first)."""
+        blocks with e4m3 GEMM operands (enable_fp8 first). mod=True runs the
+        blocks conditioned on the time step and on the rows' positions
+        (enable_mod first)."""
+        if fp8 and mod:
+            raise ValueError("the conditioned block has no e4m3 form")
         sh = self.shape
         stream = _stream(stream)  # looked up once for the whole pass
         hilo_score(sh, x, self.score, stream)
@@ -551,7 +840,11 @@ class HotPath:
         hilo_pack(sh, x, self.split, self.packed, self.cap, stream)
         if prop:
             hilo_row_sizes(sh, self.split, self.n_img, self.cap, stream)
-        if fp8:
+        if mod:
+            if self.origin is not None:
+                hilo_row_positions(sh, self.split, self.origin, self.pos, self.cap, stream)
+            self.blocks_mod(text, self.packed, HILO_BF16, stream, self.n_img if prop else None)
+        elif fp8:
             self.blocks_fp8(text, self.packed, HILO_BF16, stream, self.n_img if prop else None)
         else:
             self.blocks(text, self.packed, HILO_BF16, stream, self.n_img if prop else None)
@@ -574,6 +867,14 @@ class HotPath:
             else:
                 hilo_block_forward_fp8_prop(sh, w, self.split.cu_img, self.cap, *args, n_img, self.out, self.ws,
                                             self.ws_bytes, stream)
+
+    def blocks_mod(self, in_txt, in_img, in_dtype, stream=None, n_img=None) -> None:
+        sh = self.shape
+        stream = _stream(stream)
+        for i, (w, m) in enumerate(zip(self.weights, self.mods, strict=True)):
+            args = (in_txt, in_img, in_dtype) if i == 0 else (self.out, self._out_img_ptr(), HILO_F32)
+            hilo_block_forward_mod(sh, w, m, None if m.axis_dims is None else self.pos, self.split.cu_img, self.cap, *args,
+                                   n_img, self.out, self.ws, self.ws_bytes, stream)
 
     def blocks(self, in_txt, in_img, in_dtype, stream=None, n_img=None) -> None:
         sh = self.shape

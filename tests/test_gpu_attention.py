@@ -1,0 +1,267 @@
+"""hilo_attention against softmax attention in 64 bits on the same 16-bit inputs.
+
+Tolerance, per element (u = half a step of the dtype, p and v of the row's sum
+o = sum p v / sum p): each probability is rounded once before the product
+(u sum p |v|), the result once (u |o|); the fp32 logits of up to a few tens are
+off by less than 2^-14, as are the exponentials, maxima and sums together
+(2^-13 sum p |v|). fp16 probabilities below its normal range round to a
+multiple of 2^-24 (half of it per key, against a largest probability of 1 or
+more).
+"""
+import math
+
+import pytest
+import torch
+
+from .gpu_helpers import lib_ready
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": (torch.bfloat16, 0), "f16": (torch.float16, 2)}
+
+
+@pytest.fixture(scope="module")
+def H():
+    return lib_ready()
+
+
+def offsets(lens, first=0):
+    o = [first]
+    for n in lens:
+        o.append(o[-1] + n)
+    return torch.tensor(o, dtype=torch.int32, device="cuda")
+
+
+def make(lq, lk, heads, kv, hd, dtype="bf16", first=0, spare=0, seed=0, sharp=2.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    t = TYPES[dtype][0]
+    nq, nk = first + sum(lq) + spare, first + sum(lk) + spare
+    q = (sharp * torch.randn(nq, heads, hd, generator=g, device="cuda")).to(t)
+    k = torch.randn(nk, kv, hd, generator=g, device="cuda").to(t)
+    v = torch.randn(nk, kv, hd, generator=g, device="cuda").to(t)
+    return q, k, v, offsets(lq, first), offsets(lk, first)
+
+
+def call(H, q, k, v, cu_q, cu_k, causal=1, out=None, scale=0.0, ws=None, stream=None, fill=float("nan")):
+    heads, kv, hd = q.shape[1], k.shape[1], q.shape[2]
+    if out is None:
+        out = torch.full(q.shape, fill, dtype=q.dtype, device="cuda")
+    sh = H.AttnShape(B=cu_q.numel() - 1, heads=heads, kv_heads=kv, head_dim=hd, rows_q=q.shape[0], rows_k=k.shape[0],
+                     causal=causal, dtype=0 if q.dtype == torch.bfloat16 else 2, scale=scale, q_row=q.stride(0),
+                     q_head=q.stride(1), k_row=k.stride(0), k_head=k.stride(1), v_row=v.stride(0), v_head=v.stride(1),
+                     out_row=out.stride(0), out_head=out.stride(1))
+    n = H.hilo_attention_workspace_bytes(sh)
+    if ws is None:
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    H.hilo_attention(sh, cu_q, cu_k, q, k, v, out, ws, n, stream)
+    return out
+
+
+def reference(q, k, v, cu_q, cu_k, causal, scale=0.0):
+    """(o, sum p |v| / sum p, keys) in 64 bits; rows outside the sequences NaN."""
+    hd, g = q.shape[2], q.shape[1] // k.shape[1]
+    scale = scale or 1 / math.sqrt(hd)
+    o = torch.full(q.shape, math.nan, dtype=torch.float64, device="cuda")
+    mag = torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    cq, ck = cu_q.tolist(), cu_k.tolist()
+    for b in range(len(cq) - 1):
+        q0, q1, k0, k1 = cq[b], cq[b + 1], ck[b], ck[b + 1]
+        if q1 == q0:
+            continue
+        kk = k[k0:k1].double().repeat_interleave(g, 1).transpose(0, 1)
+        vv = v[k0:k1].double().repeat_interleave(g, 1).transpose(0, 1)
+        s = (q[q0:q1].double().transpose(0, 1) @ kk.transpose(1, 2)) * scale
+        if causal:
+            i = torch.arange(q1 - q0, device="cuda")[:, None] + (k1 - k0) - (q1 - q0)
+            s = s.masked_fill(torch.arange(k1 - k0, device="cuda") > i, -math.inf)
+        if k1 > k0:
+            p = torch.exp(s - s.amax(-1, keepdim=True).clamp(min=-1e300))
+            n = p.sum(-1, keepdim=True).clamp(min=1e-300)
+            o[q0:q1] = (p @ vv / n).transpose(0, 1)
+            mag[q0:q1] = (p @ vv.abs() / n).transpose(0, 1)
+        else:
+            o[q0:q1] = 0
+    return o, mag, k.shape[0]
+
+
+def check(got, ref, dtype):
+    o, mag, keys = ref
+    t = TYPES[dtype][0]
+    u = torch.finfo(t).eps / 2
+    tol = (u + 2.0 ** -13) * mag + u * o.abs() + (keys * 2.0 ** -25 * 8 if dtype == "f16" else 0.0) + 1e-30
+    inside = ~o.isnan()
+    assert bool(got[inside].isfinite().all())
+    off = ((got.double() - o).abs() / tol)[inside]
+    worst = float(off.max()) if off.numel() else 0.0
+    assert worst <= 1.0, worst
+    assert bool(got[~inside].isnan().all()), "rows outside the sequences were written"
+
+
+CASES = [
+    # lq, lk (None: the same), heads, kv heads, head_dim, causal, dtype
+    ([1], None, 1, 1, 64, 1, "bf16"),
+    ([1, 2, 127, 128, 129], None, 2, 2, 128, 1, "bf16"),
+    ([255, 256, 257, 0, 1, 300], None, 2, 1, 64, 1, "f16"),
+    ([333], None, 3, 1, 128, 1, "bf16"),
+    ([200, 513], None, 10, 2, 64, 0, "bf16"),
+    ([77, 0, 131], None, 14, 2, 128, 1, "f16"),
+    ([640], None, 16, 1, 64, 1, "bf16"),
+    ([5, 1, 40], None, 128, 1, 128, 1, "bf16"),
+    ([9], None, 100, 1, 64, 0, "f16"),
+    # chunks over earlier tokens, single tokens, sequences without keys or queries
+    ([1, 1, 1, 1], [1, 129, 5000, 64], 8, 2, 128, 1, "bf16"),
+    ([1, 0, 3], [0, 17, 0], 4, 4, 64, 0, "bf16"),
+    ([100, 17, 1], [1100, 4000, 2], 6, 2, 64, 1, "f16"),
+    ([64], [20000], 4, 1, 128, 0, "bf16"),
+    ([300, 7], [2048, 2048], 4, 4, 128, 1, "bf16"),
+    # more queries than keys: the first ones see none
+    ([200, 5, 300], [70, 0, 299], 4, 2, 128, 1, "bf16"),
+    # many sequences, in the plan's table and beyond it
+    ([3] * 300, [1 + 7 * (i % 40) for i in range(300)], 4, 2, 64, 1, "bf16"),
+    ([1 + i % 3 for i in range(1300)], [4 + i % 300 for i in range(1300)], 2, 1, 128, 1, "bf16"),
+    # a long sequence among short ones: cut where more jobs than CTAs are there
+    ([1] * 100 + [260], [60] * 100 + [9000], 8, 4, 64, 1, "bf16"),
+    ([2500], None, 4, 4, 64, 1, "bf16"),
+    ([1500, 700], None, 16, 8, 128, 1, "f16"),
+    ([1024, 2048], None, 24, 24, 128, 0, "bf16"),
+]
+
+
+@pytest.mark.parametrize("lq,lk,heads,kv,hd,causal,dtype", CASES)
+def test_against_64_bits(H, lq, lk, heads, kv, hd, causal, dtype):
+    lk = lq if lk is None else lk
+    q, k, v, cu_q, cu_k = make(lq, lk, heads, kv, hd, dtype, first=3, spare=5, seed=len(lq) + sum(lk))
+    got = call(H, q, k, v, cu_q, cu_k, causal)
+    H.hilo_sync_status()
+    check(got, reference(q, k, v, cu_q, cu_k, causal), dtype)
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+def test_growing_logits_rescale(H, causal):
+    """Keys whose logits rise along the sequence: the running maximum moves at every tile."""
+    q, k, v, cu_q, cu_k = make([400], [1500], 4, 2, 128, "bf16", seed=3, sharp=1.0)
+    q[:] = q.abs()
+    k[:] = k.abs() * torch.linspace(0.05, 1.5, 1500, device="cuda")[:, None, None].to(k.dtype)
+    ref = reference(q, k, v, cu_q, cu_k, causal)
+    got = call(H, q, k, v, cu_q, cu_k, causal)
+    # logits of up to 150: fp32 products of 128 terms are off by up to 150 * 2^-17
+    o, mag, n = ref
+    check(got, (o, mag * (1 + 150 * 2.0 ** -17 / 2.0 ** -8), n), "bf16")
+
+
+def test_scale_and_strides(H):
+    """q, k and v as columns of one product, a cache ordered by head, out ordered by head; a scale of its own."""
+    lq, hd = [130, 61], 64
+    q, k, v, cu_q, cu_k = make(lq, lq, 6, 2, hd, "bf16", spare=2, seed=9)
+    n = q.shape[0]
+    rows = torch.cat([x.reshape(n, -1) for x in (q, k, v)], 1)
+    pad = torch.cat([rows, torch.full((n, 8), math.nan, dtype=rows.dtype, device="cuda")], 1)
+    fq, fk, fv = (x.unflatten(1, (-1, hd)) for x in pad[:, :-8].split([6 * hd, 2 * hd, 2 * hd], 1))
+    ref = reference(q, k, v, cu_q, cu_k, 1, scale=0.3)
+    check(call(H, fq, fk, fv, cu_q, cu_k, 1, scale=0.3), ref, "bf16")
+    hk, hv = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (k, v))
+    store = torch.full((6, n + 1, hd + 8), math.nan, dtype=q.dtype, device="cuda")
+    out = store[:, :n, :hd].transpose(0, 1)
+    check(call(H, q, hk, hv, cu_q, cu_k, 1, out=out, scale=0.3), ref, "bf16")
+    assert bool(store[:, n].isnan().all()) and bool(store[:, :, hd:].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("lq,lk,heads", [([300], [300], 2), ([90], [1400], 4), ([200], [450], 12)])
+def test_infinities_and_nans_of_unseen_keys(H, dtype, lq, lk, heads):
+    """Keys past a query, behind the sequence and of other sequences may hold anything; a query that does see
+    an infinite value gets it, and only in its column."""
+    q, k, v, cu_q, cu_k = make(lq, lk, heads, 2, 128, dtype, first=2, spare=6, seed=5)
+    clean = reference(q, k, v, cu_q, cu_k, 1)
+    k[:2], v[:2], k[-6:], v[-6:] = math.nan, math.inf, math.nan, math.nan
+    base = call(H, q, k, v, cu_q, cu_k, 1)
+    check(base, clean, dtype)
+    # the last keys hold infinities and NaNs in a few columns
+    n_q, n_k = lq[0], lk[0]
+    for back, col, value in ((0, 5, math.inf), (1, 70, math.nan), (37, 9, -math.inf), (64, 127, math.inf)):
+        row = 2 + n_k - 1 - back
+        v[row, :, col] = value
+    k[2 + n_k - 1] = math.nan  # seen by the last query alone
+    got = call(H, q, k, v, cu_q, cu_k, 1)
+    H.hilo_sync_status()
+    for i in range(n_q):
+        back = n_q - 1 - i  # keys from the end that query i does not see
+        row = got[2 + i].float()
+        if back == 0:
+            assert bool(row.isnan().all())
+            continue
+        want = base[2 + i].float().clone()
+        for b, col, value in ((1, 70, math.nan), (37, 9, -math.inf), (64, 127, math.inf)):
+            if b >= back:
+                want[:, col] = value
+        assert torch.equal(row.nan_to_num(7e4, 8e4, 9e4), want.nan_to_num(7e4, 8e4, 9e4)), (i, back)
+
+
+def test_infinite_logits(H):
+    """-inf logits weigh nothing, also where a query's first tile holds nothing else; all -inf gives NaN, as 0/0."""
+    q, k, v, cu_q, cu_k = make([3, 40], [400, 300], 2, 1, 64, "bf16", seed=8)
+    q[:, :, 0] = 1
+    k[:200, :, 0] = -math.inf
+    k[400:, :, 0] = -math.inf
+    got = call(H, q, k, v, cu_q, cu_k, 0)
+    cu2 = torch.tensor([200, 400], dtype=torch.int32, device="cuda")
+    ref = reference(q[:3], k[:400], v[:400], cu_q[:2], cu2, 0)
+    check(got[:3], ref, "bf16")
+    assert bool(got[3:].isnan().all())
+
+
+def test_calls_repeat_and_overlap(H):
+    """The same bits again, on another stream, from a captured graph, and next to a call with a workspace of its own."""
+    q, k, v, cu_q, cu_k = make([1, 1, 200], [3000, 900, 2500], 8, 2, 128, "bf16", seed=4)
+    first = call(H, q, k, v, cu_q, cu_k)
+    assert torch.equal(first, call(H, q, k, v, cu_q, cu_k))
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(3):
+        for s in (s1, s2):
+            with torch.cuda.stream(s):
+                outs.append(call(H, q, k, v, cu_q, cu_k))
+    torch.cuda.synchronize()
+    assert all(torch.equal(first, o) for o in outs)
+    out = torch.zeros_like(q)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    call(H, q, k, v, cu_q, cu_k, out=out, ws=ws)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(H, q, k, v, cu_q, cu_k, out=out, ws=ws)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(first, out)
+    # the lengths are read at replay
+    cu_q.copy_(torch.tensor([0, 1, 1, 150], dtype=torch.int32))
+    cu_k.copy_(torch.tensor([0, 2000, 2000, 2900], dtype=torch.int32))
+    out.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    check(out, reference(q, k, v, cu_q, cu_k, 1), "bf16")
+
+
+def test_offsets_past_the_buffers_are_cut(H):
+    """Offsets beyond the rows that the shape names (and falling ones) address nothing outside them."""
+    q, k, v, cu_q, cu_k = make([100], [100], 2, 2, 64, "bf16", seed=6)
+    store = torch.full((160, 2, 64), math.nan, dtype=q.dtype, device="cuda")
+    cu_q = torch.tensor([-5, 90, 40, 150], dtype=torch.int32, device="cuda")
+    cu_k = torch.tensor([0, 90, 95, 1 << 30], dtype=torch.int32, device="cuda")
+    call(H, q, k, v, cu_q, cu_k, out=store[:100])
+    H.hilo_sync_status()
+    assert bool(store[100:].isnan().all())
+    one = torch.tensor([0, 90], dtype=torch.int32, device="cuda")
+    ref = reference(q[:90], k[:90], v[:90], one, one, 1)
+    # (the third sequence, rows 40 to 99, overwrites the first one's later rows)
+    check(store[:40], tuple(x[:40] if hasattr(x, "shape") else x for x in ref), "bf16")
+
+
+def test_no_keys_at_all(H):
+    q, k, v, _, _ = make([4], [1], 2, 2, 64, "bf16")
+    cu_q = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    zero = torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert bool((call(H, q, k[:0], v[:0], cu_q, zero, 0) == 0).all())
+    assert bool(call(H, q, k, v, zero, zero, 0).isnan().all())
