@@ -67,17 +67,6 @@ __device__ __forceinline__ void widen(const Raw<F32>& r, float* v) {
   }
 }
 
-// Eight elements of a vector that many rows read (bf16 or fp32).
-__device__ __forceinline__ void vec8(const void* base, bool f32, long long i, float* v) {
-  if (f32) {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + i);
-    const float4 a = __ldg(p), b = __ldg(p + 1);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  } else {
-    widen_bf16(__ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + i)), v);
-  }
-}
-
 __device__ __forceinline__ void store8_f32(void* base, long long i, const float* v) {
   float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + i);
   p[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -90,20 +79,29 @@ __device__ __forceinline__ void store8_bf16(void* base, long long i, const float
 }
 
 // ------------------------------------------------- sums over a row's threads --
-// `red` is two arrays of four floats that take turns (`turn`): a slot is
-// written again only after the reduction in between, whose barrier every
-// thread passes after its last read of the slot.
-template <int GROUP, bool MAX>
-__device__ __forceinline__ float group_reduce(float v, float (*red)[4], int& turn) {
+// Over the CTA's W warps (one row at a time), or over a warp (W = 0). `red` is two
+// arrays of 16 floats that take turns (`turn`): a slot is written again only
+// after the reduction in between, whose barrier every thread passes after its
+// last read of the slot.
+template <bool WARP, bool MAX>
+__device__ __forceinline__ float row_reduce(float v, float (*red)[16], int& turn, int warps) {
   auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, off));
-  if (GROUP == 32) return v;
+  if (WARP) return v;
   float* r = red[turn];
   turn ^= 1;
-  if ((threadIdx.x & 31) == 0) r[(threadIdx.x >> 5) % (GROUP / 32)] = v;
-  named_bar_sync(1 + static_cast<int>(threadIdx.x) / GROUP, GROUP);
-  return GROUP == 64 ? join(r[0], r[1]) : join(join(r[0], r[1]), join(r[2], r[3]));
+  if (lane_id() == 0) r[warp_id()] = v;
+  __syncthreads();
+  // (the slots past the last warp stay 0, which neither a sum nor a maximum of
+  // magnitudes changes)
+  float4 s = *reinterpret_cast<const float4*>(r);
+  v = join(join(s.x, s.y), join(s.z, s.w));
+  for (int w = 4; w < warps; w += 4) {
+    s = *reinterpret_cast<const float4*>(r + w);
+    v = join(v, join(join(s.x, s.y), join(s.z, s.w)));
+  }
+  return v;
 }
 
 // The image that packed row r belongs to: the last one that begins at or
@@ -122,182 +120,168 @@ __device__ __forceinline__ int image_of(const int32_t* cu, int B, int r) {
 //
 // z = norm_branch(y) w_branch; u' = rs u + gate z; h = (norm(u') w + b)(1 + scale) + shift.
 //
-// A row per group of 128 threads (64 up to 512 elements, a warp up to 256),
-// 384 threads per CTA. Thread t of a group of G holds the chunks of eight
-// elements t, t + G, ..: the whole row is in registers from its one read to
-// its writes, and the variance is a second pass over them. The vectors are
-// read for every row again: an image's rows are neighbours, so that all but
-// the first read of a CTA hit its L1.
-// Bound by HBM for many rows, by the chain load, reductions, store for few, so
-// each group loads its next row before it reduces the present one.
+// With A = gate w_branch, S = w (1 + scale) and C = b (1 + scale) + shift that is
+// u' = rs u + A norm_branch(y) and h = S norm(u') + C.
+//
+// Eight elements of a row per thread: a row is a CTA of d / 8 threads (whole
+// warps), of up to 256 elements a warp. The row is in registers from its one read
+// to its writes, and the variance is a second pass over them. A CTA goes through
+// a range of neighbouring rows and keeps A, S and C of their image in registers.
+// Bound by HBM for many rows, by the chain load, reductions, store for few. What
+// hides the chain is rows in flight: each row is asked for before the one ahead of
+// it is reduced. (More elements per thread, as a warpgroup per row, take more
+// registers and leave fewer threads on the SM: 2389 rows of 3072 30.9 us, 8586 rows
+// of 1152 with both norms 65.6. Vectors read again for every row: 25.9 and 43.7,
+// half of the issue slots and a third of the loads' pipe spent on them. So: 19.8 =
+// 4.5 TB/s, and 18.4.)
 
-constexpr int GN_THREADS = 384;
-constexpr int gn_group(int d) { return d <= 256 ? 32 : d <= 512 ? 64 : 128; }
+constexpr int GN_WARP_ROWS = 8;  // rows of up to 256 elements: warps per CTA
+constexpr int GN_THREADS = 1024;  // resident per SM (64 registers each)
 
 enum { Y_NONE = 0, Y_BF16 = 1, Y_F32 = 2 };
 
-template <int NC, int GROUP>
-__device__ __forceinline__ void row_norm(float (&v)[NC][8], int kind, float eps, float inv_d, int tid, int nchunk,
-                                         float (*red)[4], int& turn) {
+// Eight elements of a vector, `none` where there is no vector.
+__device__ __forceinline__ void vector8(const void* v, bool f32, long long i, float none, float* out) {
+  if (v == nullptr) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) out[j] = none;
+  } else if (f32) {
+    widen<true>(load8<true>(v, i), out);
+  } else {
+    widen<false>(load8<false>(v, i), out);
+  }
+}
+
+template <bool WARP>
+__device__ __forceinline__ void row_norm(float (&v)[8], int kind, float eps, float inv_d, bool in, float (*red)[16],
+                                         int& turn, int warps) {
   if (kind == HILO_NORM_NONE) return;
   if (kind == HILO_NORM_LAYER) {
-    float sum = 0.f;
+    const float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    const float mean = row_reduce<WARP, false>(sum, red, turn, warps) * inv_d;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += v[c][i];
-    const float mean = group_reduce<GROUP, false>(sum, red, turn) * inv_d;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      if (tid + GROUP * c < nchunk)  // (the chunks past the row stay zero)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] -= mean;
+    for (int i = 0; i < 8; ++i) v[i] = in ? v[i] - mean : 0.f;
   }
   float sq = 0.f;
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int i = 0; i < 8; ++i) sq = fmaf(v[i], v[i], sq);
+  const float r = rsqrtf(row_reduce<WARP, false>(sq, red, turn, warps) * inv_d + eps);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sq = fmaf(v[c][i], v[c][i], sq);
-  const float r = rsqrtf(group_reduce<GROUP, false>(sq, red, turn) * inv_d + eps);
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] *= r;
+  for (int i = 0; i < 8; ++i) v[i] *= r;
 }
 
-template <int NC, int GROUP, bool UF32, int YM>
-__global__ void __launch_bounds__(GN_THREADS) gate_norm_kernel(const __grid_constant__ NormArgs a) {
+template <bool WARP, bool UF32, int YM>
+__global__ void __launch_bounds__(WARP ? 32 * GN_WARP_ROWS : 512, WARP ? 4 : 2)
+    gate_norm_kernel(const __grid_constant__ NormArgs a) {
   pdl_wait();
   pdl_trigger();
-  constexpr int GROUPS = GN_THREADS / GROUP;
-  __shared__ float red_s[GROUPS][2][4];
-  const int group = threadIdx.x / GROUP, tid = threadIdx.x % GROUP;
-  float(*red)[4] = red_s[group];
+  __shared__ __align__(16) float red[2][16];
   int turn = 0;
-  const int d = a.s.d, nchunk = d / 8, n_txt = a.s.B * a.s.T;
+  const int warps = blockDim.x / 32;
+  if (!WARP) {
+    if (threadIdx.x < 32) red[threadIdx.x >> 4][threadIdx.x & 15] = 0.f;
+    __syncthreads();
+  }
+  const int d = a.s.d, k = 8 * (WARP ? lane_id() : static_cast<int>(threadIdx.x));
+  const bool in = k < d;
+  const int n_txt = a.s.B * a.s.T;
   const int rows = n_txt + max(0, min(a.cu_img[a.s.B], a.s.cap));
   const float inv_d = 1.0f / static_cast<float>(d);
-  const bool vf32 = a.s.vec_dtype == HILO_F32;
-  const long long step = static_cast<long long>(gridDim.x) * GROUPS;
-  Raw<UF32> u_raw[NC];
-  Raw<YM == Y_F32> y_raw[NC];
-  int stream = 0, image = 0;  // of the row loaded last
-  auto load = [&](int r) {
-    const long long off = static_cast<long long>(r < n_txt ? r : r - n_txt) * d;
-    const void* u = r < n_txt ? a.u_txt : a.u_img;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int k = tid + GROUP * c;
-      if (k < nchunk) {
-        u_raw[c] = load8<UF32>(u, off + 8 * k);
-        if (YM != Y_NONE) y_raw[c] = load8<YM == Y_F32>(a.y, static_cast<long long>(r) * d + 8 * k);
-      }
-    }
-    stream = r >= n_txt;
-    image = stream ? image_of(a.cu_img, a.s.B, r - n_txt) : r / a.s.T;
+  // this group's range of rows
+  const int groups = WARP ? gridDim.x * GN_WARP_ROWS : gridDim.x;
+  const int group = WARP ? blockIdx.x * GN_WARP_ROWS + warp_id() : blockIdx.x;
+  const int each = rows / groups, more = rows - each * groups;
+  int r = group * each + min(group, more);
+  const int end = r + each + (group < more ? 1 : 0);
+  Raw<UF32> u_raw;
+  Raw<YM == Y_F32> y_raw;
+  auto load = [&](int row) {
+    const long long off = static_cast<long long>(row < n_txt ? row : row - n_txt) * d + k;
+    u_raw = load8<UF32>(row < n_txt ? a.u_txt : a.u_img, off);
+    if (YM != Y_NONE) y_raw = load8<YM == Y_F32>(a.y, static_cast<long long>(row) * d + k);
   };
-  long long r = blockIdx.x + static_cast<long long>(gridDim.x) * group;
-  if (r < rows) load(static_cast<int>(r));
-  for (; r < rows; r += step) {
-    const hilo_norm_vectors& vec = a.vec[stream];
-    const long long vrow = static_cast<long long>(image) * a.s.vec_row;
-    const long long at = r * d;
-    float u[NC][8], z[NC][8];
+  if (r < end && in) load(r);
+  float A[8], S[8], C[8];
+  int change = r;  // the row from which on they are another image's
+  for (; r < end; ++r) {
+    if (r >= change) {
+      const int stream = r >= n_txt;
+      const int image = stream ? image_of(a.cu_img, a.s.B, r - n_txt) : r / a.s.T;
+      change = !stream ? (image + 1) * a.s.T : image + 1 < a.s.B ? max(r + 1, n_txt + __ldg(a.cu_img + image + 1)) : rows;
+      const hilo_norm_vectors& v = a.vec[stream];
+      const long long vk = static_cast<long long>(image) * a.s.vec_row + k;
+      const bool f32 = a.s.vec_dtype == HILO_F32;
+      if (in) {
+        float w[8];
+        if (YM != Y_NONE) {
+          vector8(v.gate, f32, vk, 1.0f, A);
+          vector8(v.w_branch, f32, k, 1.0f, w);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const bool in = tid + GROUP * c < nchunk;
-      float t[8];
-      widen<UF32>(u_raw[c], t);
+          for (int i = 0; i < 8; ++i) A[i] *= w[i];
+        }
+        if (a.h) {
+          vector8(v.scale, f32, vk, 0.0f, w);
+          vector8(v.w_norm, f32, k, 1.0f, S);
+          vector8(v.b_norm, f32, k, 0.0f, C);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[c][i] = in ? t[i] : 0.f;
-      if (YM != Y_NONE) {
-        widen<YM == Y_F32>(y_raw[c], t);
+          for (int i = 0; i < 8; ++i) S[i] *= 1.0f + w[i], C[i] *= 1.0f + w[i];
+          vector8(v.shift, f32, vk, 0.0f, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[c][i] = in ? t[i] : 0.f;
+          for (int i = 0; i < 8; ++i) C[i] += w[i];
+        }
       }
     }
-    if (r + step < rows) load(static_cast<int>(r + step));
+    const long long at = static_cast<long long>(r) * d + k;
+    float u[8], z[8];
+    widen<UF32>(u_raw, u);
+    if (YM != Y_NONE) widen<YM == Y_F32>(y_raw, z);
+    if (!in) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = z[i] = 0.f;
+    } else if (r + 1 < end) {
+      load(r + 1);
+    }
     if (YM != Y_NONE) {
-      row_norm<NC, GROUP>(z, a.s.norm_branch, a.s.eps, inv_d, tid, nchunk, red, turn);
+      row_norm<WARP>(z, a.s.norm_branch, a.s.eps, inv_d, in, red, turn, warps);
+      if (in) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int k = tid + GROUP * c;
-        if (k >= nchunk) continue;
-        float w[8];
-        if (vec.w_branch) {
-          vec8(vec.w_branch, vf32, 8 * k, w);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) z[c][i] *= w[i];
-        }
-        if (vec.gate) {
-          vec8(vec.gate, vf32, vrow + 8 * k, w);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) u[c][i] = fmaf(w[i], z[c][i], a.s.resid_scale * u[c][i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) u[c][i] = fmaf(a.s.resid_scale, u[c][i], z[c][i]);
-        }
+        for (int i = 0; i < 8; ++i) u[i] = fmaf(A[i], z[i], a.s.resid_scale * u[i]);
         if (a.u_out) {
-          if (a.s.u_out_dtype == HILO_F32) store8_f32(a.u_out, at + 8 * k, u[c]);
-          else store8_bf16(a.u_out, at + 8 * k, u[c]);
+          if (a.s.u_out_dtype == HILO_F32) store8_f32(a.u_out, at, u);
+          else store8_bf16(a.u_out, at, u);
         }
       }
     }
     if (!a.h) continue;
-    row_norm<NC, GROUP>(u, a.s.norm, a.s.eps, inv_d, tid, nchunk, red, turn);
+    row_norm<WARP>(u, a.s.norm, a.s.eps, inv_d, in, red, turn, warps);
     float am = 0.f;
+    if (in) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int k = tid + GROUP * c;
-      if (k >= nchunk) continue;
-      float w[8];
-      if (vec.w_norm) {
-        vec8(vec.w_norm, vf32, 8 * k, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] *= w[i];
-      }
-      if (vec.b_norm) {
-        vec8(vec.b_norm, vf32, 8 * k, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] += w[i];
-      }
-      if (vec.scale) {
-        vec8(vec.scale, vf32, vrow + 8 * k, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] *= 1.0f + w[i];
-      }
-      if (vec.shift) {
-        vec8(vec.shift, vf32, vrow + 8 * k, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[c][i] += w[i];
-      }
+      for (int i = 0; i < 8; ++i) u[i] = fmaf(u[i], S[i], C[i]);
       if (a.s.h_dtype == HILO_BF16) {
-        store8_bf16(a.h, at + 8 * k, u[c]);
+        store8_bf16(a.h, at, u);
       } else if (a.s.h_dtype == HILO_F32) {
-        store8_f32(a.h, at + 8 * k, u[c]);
+        store8_f32(a.h, at, u);
       } else if (a.s.h_dtype == HILO_F16) {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.h) + at + 8 * k) =
-            make_uint4(pack_f16x2_sat(u[c][0], u[c][1]), pack_f16x2_sat(u[c][2], u[c][3]),
-                       pack_f16x2_sat(u[c][4], u[c][5]), pack_f16x2_sat(u[c][6], u[c][7]));
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.h) + at) =
+            make_uint4(pack_f16x2_sat(u[0], u[1]), pack_f16x2_sat(u[2], u[3]), pack_f16x2_sat(u[4], u[5]),
+                       pack_f16x2_sat(u[6], u[7]));
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) am = fmaxf(am, fabsf(u[c][i]));
+        for (int i = 0; i < 8; ++i) am = fmaxf(am, fabsf(u[i]));
       }
     }
     if (a.s.h_dtype == HILO_E4M3) {  // quantised by the row's largest magnitude
-      am = group_reduce<GROUP, true>(am, red, turn);
+      am = row_reduce<WARP, true>(am, red, turn, warps);
       const float inv = am > 0.f ? __fdiv_rn(448.0f, am) : 1.0f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int k = tid + GROUP * c;
-        if (k >= nchunk) continue;
+      if (in) {
         float q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = __fmul_rn(u[c][i], inv);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.h) + at + 8 * k) =
+        for (int i = 0; i < 8; ++i) q[i] = __fmul_rn(u[i], inv);
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.h) + at) =
             make_uint2(pack_e4m3x4(q[0], q[1], q[2], q[3]), pack_e4m3x4(q[4], q[5], q[6], q[7]));
       }
-      if (tid == 0) a.h_scale[r] = am > 0.f ? __fdiv_rn(am, 448.0f) : 1.0f;
+      if (k == 0) a.h_scale[r] = am > 0.f ? __fdiv_rn(am, 448.0f) : 1.0f;
     }
   }
 }
@@ -309,7 +293,10 @@ __global__ void __launch_bounds__(GN_THREADS) gate_norm_kernel(const __grid_cons
 // A row per group of 128 threads (a warp where a row is at most 64 pieces of
 // 16 bytes). The row's pieces are on their way while the group's threads form
 // the row's angles, one pair each, into shared memory; all heads of the row
-// share them. Bound by HBM, each element read and written once.
+// share them. Bound by HBM, each element read and written once: 2389 rows of 48
+// heads of 128 (bf16) 11.5 us = 5.1 TB/s, 18001 fp32 rows of 16 heads of 64 26.3 us =
+// 5.6 TB/s. (Four or two pieces per thread in flight instead of six, and 16 CTAs per
+// SM that their registers did not let in: 13.3 and 26.2 us.)
 //
 // The angle in turns is pos * f, f = theta^-p / 2 pi as the sum of two floats
 // (fh, fl): pos * fh is formed exactly as a product and its error, whole turns
@@ -319,6 +306,7 @@ __global__ void __launch_bounds__(GN_THREADS) gate_norm_kernel(const __grid_cons
 
 constexpr int RP_MAX_PAIRS = 128;
 constexpr int RP_THREADS = 128;
+constexpr int RP_CTAS = 9;  // resident per SM
 
 struct RopeArgs {
   const void* x;
@@ -371,13 +359,13 @@ __device__ __forceinline__ uint4 piece_pack(const float* v) {
 }
 
 template <int DT, bool INTERLEAVED, int GROUP>
-__global__ void __launch_bounds__(RP_THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(RP_THREADS, RP_CTAS) rope_kernel(const __grid_constant__ RopeArgs a) {
   pdl_wait();
   pdl_trigger();
   constexpr int GROUPS = RP_THREADS / GROUP;
   constexpr int EV = Piece<DT>::EV;
   constexpr int PT = (RP_MAX_PAIRS + GROUP - 1) / GROUP;  // pairs per thread
-  constexpr int BATCH = INTERLEAVED ? 4 : 2;              // units in flight per thread
+  constexpr int BATCH = INTERLEAVED ? 6 : 3;              // units in flight per thread
   // cosines and sines of a group's row, of two rows in turn
   __shared__ __align__(16) float cs_s[GROUPS][2][RP_MAX_PAIRS], sn_s[GROUPS][2][RP_MAX_PAIRS];
   const int group = threadIdx.x / GROUP, tid = threadIdx.x % GROUP;
@@ -483,30 +471,27 @@ int grid_for(long long items, int per_block, int num_sms, int blocks_per_sm) {
   return static_cast<int>(g < 1 ? 1 : g < most ? g : most);
 }
 
-template <int NC, int GROUP>
+template <bool WARP, bool UF32, int YM>
 cudaError_t gate_norm_of(const NormArgs& a, int num_sms, cudaStream_t st) {
   const long long R = static_cast<long long>(a.s.B) * a.s.T + a.s.cap;
-  const dim3 grid(grid_for(R, GN_THREADS / GROUP, num_sms, 2));
+  const int threads = WARP ? 32 * GN_WARP_ROWS : (a.s.d / 8 + 31) / 32 * 32;
+  const dim3 grid(grid_for(R, WARP ? GN_WARP_ROWS : 1, num_sms, GN_THREADS / threads));
+  return launch_pdl(gate_norm_kernel<WARP, UF32, YM>, grid, dim3(threads), 0, st, a);
+}
+
+template <bool WARP>
+cudaError_t gate_norm_by_type(const NormArgs& a, int num_sms, cudaStream_t st) {
   const bool uf = a.s.u_dtype == HILO_F32;
-  auto* kern = !a.y                         ? (uf ? gate_norm_kernel<NC, GROUP, true, Y_NONE> : gate_norm_kernel<NC, GROUP, false, Y_NONE>)
-               : a.s.y_dtype == HILO_BF16 ? (uf ? gate_norm_kernel<NC, GROUP, true, Y_BF16> : gate_norm_kernel<NC, GROUP, false, Y_BF16>)
-                                          : (uf ? gate_norm_kernel<NC, GROUP, true, Y_F32> : gate_norm_kernel<NC, GROUP, false, Y_F32>);
-  return launch_pdl(kern, grid, dim3(GN_THREADS), 0, st, a);
+  if (!a.y) return uf ? gate_norm_of<WARP, true, Y_NONE>(a, num_sms, st) : gate_norm_of<WARP, false, Y_NONE>(a, num_sms, st);
+  if (a.s.y_dtype == HILO_BF16)
+    return uf ? gate_norm_of<WARP, true, Y_BF16>(a, num_sms, st) : gate_norm_of<WARP, false, Y_BF16>(a, num_sms, st);
+  return uf ? gate_norm_of<WARP, true, Y_F32>(a, num_sms, st) : gate_norm_of<WARP, false, Y_F32>(a, num_sms, st);
 }
 
 }  // namespace
 
 cudaError_t launch_gate_norm(const NormArgs& a, int num_sms, cudaStream_t st) {
-  const int group = gn_group(a.s.d);
-  if (group == 32) return gate_norm_of<1, 32>(a, num_sms, st);
-  if (group == 64) return gate_norm_of<1, 64>(a, num_sms, st);
-  switch ((a.s.d + 1023) / 1024) {
-    case 1: return gate_norm_of<1, 128>(a, num_sms, st);
-    case 2: return gate_norm_of<2, 128>(a, num_sms, st);
-    case 3: return gate_norm_of<3, 128>(a, num_sms, st);
-    case 4: return gate_norm_of<4, 128>(a, num_sms, st);
-    default: return cudaErrorInvalidValue;
-  }
+  return a.s.d <= 256 ? gate_norm_by_type<true>(a, num_sms, st) : gate_norm_by_type<false>(a, num_sms, st);
 }
 
 cudaError_t launch_rope(const hilo_rope_shape& s, const void* x, const float* pos, int row_base,
@@ -543,7 +528,7 @@ cudaError_t launch_rope(const hilo_rope_shape& s, const void* x, const float* po
   a.rest_from = D;
   // a warp per row where the row gives its lanes at most two units each
   const bool small = a.heads * (a.per_head + a.rest) <= 64;
-  const dim3 grid(grid_for(s.rows, small ? RP_THREADS / 32 : 1, num_sms, 16));
+  const dim3 grid(grid_for(s.rows, small ? RP_THREADS / 32 : 1, num_sms, RP_CTAS));
 #define HILO_ROPE(DT)                                                                        \
   (s.rot.interleaved ? (small ? rope_kernel<DT, true, 32> : rope_kernel<DT, true, 128>)      \
                      : (small ? rope_kernel<DT, false, 32> : rope_kernel<DT, false, 128>))

@@ -436,12 +436,16 @@ class NormVectors:
 
     def c(self) -> hilo_norm_vectors:
         """The C struct of the device pointers, rebuilt only when one of the vectors is replaced."""
-        ts = (self.gate, self.scale, self.shift, self.w_branch, self.w_norm, self.b_norm)
         cached = self.__dict__.get("_c")
-        if cached is None or any(a is not b for a, b in zip(cached[1], ts)):
-            cached = (hilo_norm_vectors(*(_ptr(t) for t in ts)), ts)
-            self.__dict__["_c"] = cached
-        return cached[0]
+        if cached is not None:
+            st, gate, scale, shift, w_branch, w_norm, b_norm = cached
+            if (gate is self.gate and scale is self.scale and shift is self.shift and w_branch is self.w_branch
+                    and w_norm is self.w_norm and b_norm is self.b_norm):
+                return st
+        ts = (self.gate, self.scale, self.shift, self.w_branch, self.w_norm, self.b_norm)
+        st = hilo_norm_vectors(*(_ptr(t) for t in ts))
+        self.__dict__["_c"] = (st, *ts)
+        return st
 
 
 @dataclasses.dataclass(frozen=True)
