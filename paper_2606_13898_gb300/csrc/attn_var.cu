@@ -66,18 +66,18 @@ constexpr int V_PRODUCER_WARP = 10;  // V copies
 constexpr int ITEM_WARP = 11;
 constexpr uint32_t SOFTMAX_REGS = 216;
 constexpr uint32_t CONTROL_REGS = 72;
-constexpr uint32_t TMEM_COLS = 512;  // S0 | S1 | O0 | O1
-constexpr int BOX_BYTES = 128 * 128;  // 128 rows x 64 16-bit elements
 constexpr float RESCALE_LOG2 = 8.0f;
 
 struct VarParams {
   const int32_t *cu_q, *cu_k;
   const void* v;
   void* out;
-  float* part;   // pieces' rows: [slot][tile 0, 1][row][HD]
+  float* part;      // pieces' rows: [slot][tile 0, 1][HD / 8][row][8], so that a warp's stores join up
   float2* part_ml;  // their maxima and sums: [slot][tile][row]
   long long v_row, v_head, out_row, out_head;
   int B, kv_heads, group, tpt;  // tpt: tokens per tile
+  unsigned long long tpt_mul;   // n / tpt = n * tpt_mul >> tpt_shift, n < 2^31
+  int tpt_shift;
   int causal, rows_q, rows_k;
   int grid;  // CTAs of the main kernel
   int may_cut;
@@ -92,15 +92,16 @@ struct Seq {
   __device__ __forceinline__ int seen(const VarParams& p, int i) const {
     return p.causal ? min(lk, max(0, i + 1 + (lk - lq))) : lk;
   }
-  __device__ __forceinline__ int tiles(const VarParams& p) const { return (lq + p.tpt - 1) / p.tpt; }
+  __device__ __forceinline__ int tiles(const VarParams& p) const {
+    return static_cast<int>(static_cast<unsigned long long>(lq + p.tpt - 1) * p.tpt_mul >> p.tpt_shift);
+  }
   // Key tiles of query tile j: those its last token sees (one, all of it
   // masked, where it sees none: the zeros of such rows are written too).
   __device__ __forceinline__ int key_tiles(const VarParams& p, int j) const {
     return max(1, (seen(p, min(lq, (j + 1) * p.tpt) - 1) + BKV - 1) / BKV);
   }
-  // Steps of row job i: a pair's key tiles, half of a single's.
-  __device__ __forceinline__ int steps(const VarParams& p, int i) const {
-    const int nt = tiles(p);
+  // Steps of row job i of a sequence of nt tiles: a pair's key tiles, half of a single's.
+  __device__ __forceinline__ int steps(const VarParams& p, int nt, int i) const {
     return 2 * i + 1 < nt ? key_tiles(p, 2 * i + 1) : (key_tiles(p, nt - 1) + 1) / 2;
   }
 };
@@ -117,21 +118,27 @@ __device__ __forceinline__ Seq sequence(const VarParams& p, int b) {
 // --------------------------------------------------------------------- plan --
 //
 // A row job is a job of one sequence for all its key heads. Up to MAX_TABLE
-// row jobs are listed, longest first to a sixteenth of the longest; the items of an
-// entry are its key heads' jobs, or their pieces. More row jobs than that are
-// taken as they come, the last of each sequence first, and never cut: every
-// CTA then has dozens.
+// row jobs are listed; the items of an entry are its key heads' jobs, or their
+// pieces. More row jobs than that are taken as they come, the last of each
+// sequence first, and never cut: every CTA then has dozens.
 //
-// Cutting: with J jobs of T steps together on G CTAs, a piece has at most KS
-// steps. J >= G: KS = ceil(T / G), so only a job longer than a CTA's share is
-// cut, into fewer than 2G pieces (each cut job of c > KS steps into at most
-// c / KS + 1 < 2c / KS). J < G: the smaller of ceil(T / (G - J)), for which
-// sum(c / KS + 1) <= G, and the longest job in floor(G / J) pieces: at most G.
+// Cutting: J jobs of T steps together on G CTAs, pieces of at most `share`
+// steps. An item costs about ITEM_STEPS more than its steps (copies to wait for,
+// the last product, the output rows).
+//   J < G   the smallest share, of one per warp between ceil(T / G) and the smaller
+//           of ceil(T / (G - J)) and the longest job in floor(G / J) pieces, that makes at
+//           most G items: one for each CTA. (The last two do: sum(c / share + 1)
+//           <= G, and each job of at most floor(G / J) pieces.)
+//   J >= G  ceil((T + J ITEM_STEPS) / G) - ITEM_STEPS, and only jobs that are
+//           longer by more than ITEM_STEPS are cut. Listed longest first, to a
+//           sixteenth of the longest, the cut ones ahead of the others: fewer than
+//           2G pieces, as a job of c > share + 1 steps has at most (c - 1) / share + 1.
 // Pieces of less than MIN_STEPS would cost more in their epilogues than they save.
 
 constexpr int MAX_SEQ = ATTN_MAX_SEQUENCES;
 constexpr int MAX_TABLE = 1024;
-constexpr int MIN_STEPS = 2;
+constexpr int MIN_STEPS = 4;
+constexpr int ITEM_STEPS = 2;
 constexpr int SLOTS_PER_CTA = 2;
 constexpr int BUCKETS = 32;  // 16 of cut jobs, 16 of whole ones
 
@@ -140,14 +147,64 @@ struct Plan {
   int seq[MAX_TABLE];      // entry: sequence << 16 | row job of it
   int steps[MAX_TABLE];
   int items[MAX_TABLE];    // items before the entry
-  int jobs, n_items, n_cut, share;  // row jobs, items, cut entries, KS
+  int jobs, n_items, n_cut, share, cut_above;  // row jobs, items, entries that may be cut (the first ones)
 };
 static_assert(MAX_SEQ <= 1 << 15 && MAX_TABLE <= 1 << 16, "an entry's sequence and row job share a word");
 
 __device__ __forceinline__ int ceil_div(int a, int b) {
   return static_cast<int>((static_cast<uint32_t>(a) + static_cast<uint32_t>(b) - 1u) / static_cast<uint32_t>(b));
 }
-__device__ __forceinline__ int pieces_of(int steps, int share) { return steps > share ? ceil_div(steps, share) : 1; }
+__device__ __forceinline__ int pieces_of(const Plan& pl, int steps) {
+  return steps > pl.cut_above ? ceil_div(steps, pl.share) : 1;
+}
+
+// A CTA's unit of work: query tiles j0 (and j0 + 1 of a pair) of a sequence and
+// a key head over the key tiles [t0, t1).
+struct Item {
+  int more;  // 0: the CTA has no further item
+  int q0, lq, k0, lk;
+  int hk, j0, pair;
+  int t0, t1;
+  int n0, n1;  // steps of the two warpgroups
+  int slot;    // of a piece; -1: the whole job
+};
+
+// The key tile of step s of warpgroup i.
+__device__ __forceinline__ int item_tile(int pair, int t0, int i, int s) { return pair ? t0 + s : t0 + 2 * s + i; }
+
+// Item t: of the items of row job `job` (c steps, `pieces` pieces), number r.
+__device__ __forceinline__ Item make_item(const VarParams& p, int job, int i, int c, int pieces, int r, int t) {
+  const Seq s = sequence<false>(p, job);
+  Item it;
+  it.hk = pieces == 1 ? r : static_cast<int>(static_cast<uint32_t>(r) / static_cast<uint32_t>(pieces));
+  const int piece = r - it.hk * pieces;
+  it.more = 1;
+  it.q0 = s.q0;
+  it.lq = s.lq;
+  it.k0 = s.k0;
+  it.lk = s.lk;
+  it.j0 = 2 * i;
+  it.pair = 2 * i + 1 < s.tiles(p);
+  int u0 = 0, u1 = c;
+  if (pieces > 1) {
+    u0 = static_cast<int>(static_cast<uint32_t>(c) * static_cast<uint32_t>(piece) / static_cast<uint32_t>(pieces));
+    u1 = static_cast<int>(static_cast<uint32_t>(c) * static_cast<uint32_t>(piece + 1) / static_cast<uint32_t>(pieces));
+  }
+  const int nkv0 = s.key_tiles(p, it.j0);
+  if (it.pair) {
+    it.t0 = u0;
+    it.t1 = u1;
+    it.n0 = max(0, min(u1, nkv0) - u0);
+    it.n1 = u1 - u0;
+  } else {
+    it.t0 = 2 * u0;
+    it.t1 = min(nkv0, 2 * u1);
+    it.n1 = (it.t1 - it.t0) / 2;
+    it.n0 = it.t1 - it.t0 - it.n1;
+  }
+  it.slot = pieces > 1 ? t : -1;
+  return it;
+}
 
 // Sum of v over the CTA's threads before this one, and of all: `tot` is a word per warp
 // that no other call is using.
@@ -172,13 +229,14 @@ template <int NT>
 struct PlanScratch {
   static constexpr int PER = (MAX_TABLE + NT - 1) / NT;
   int tot[4][NT / 32];
-  unsigned long long sum[NT / 32];
-  int most[NT / 32];
+  int sum[NT / 32], most[NT / 32], least[NT / 32], count[NT / 32], cut[NT / 32];
   int hist[BUCKETS * PER * (NT / 32)];  // [bucket][round, warp]
 };
 
+// By all NT threads; ends with a barrier. Where `own` is not null, item t_own of the
+// listed ones is written there by the thread that finds it.
 template <int NT, bool L2>
-__device__ void plan_build(const VarParams& p, Plan& pl, PlanScratch<NT>& s) {
+__device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScratch<NT>& s, Item* own, int t_own) {
   constexpr int PER = PlanScratch<NT>::PER, WARPS = NT / 32, ROWS = PER * WARPS;
   const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
   // row jobs before each sequence
@@ -194,22 +252,19 @@ __device__ void plan_build(const VarParams& p, Plan& pl, PlanScratch<NT>& s) {
   }
   const int U = before;
   if (tid == 0) pl.first[p.B] = U;
-  for (int i = tid; i < BUCKETS * ROWS; i += NT) s.hist[i] = 0;
   __syncthreads();
-  if (U > MAX_TABLE) {
+  if (U > MAX_TABLE || U == 0) {
     if (tid == 0) {
       pl.jobs = U;
       pl.n_items = U * p.kv_heads;
       pl.n_cut = 0;
-      pl.share = 0x7fffffff;
+      pl.share = pl.cut_above = 0x7fffffff;
     }
     __syncthreads();
     return;
   }
   // the row jobs' steps
-  int job[PER], c[PER];
-  unsigned long long sum = 0;
-  int most = 0;
+  int job[PER], c[PER], sum = 0, most = 0, least = 0x7fffffff;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int u = k * NT + tid;
@@ -222,129 +277,155 @@ __device__ void plan_build(const VarParams& p, Plan& pl, PlanScratch<NT>& s) {
       else hi = mid;
     }
     const int i = u - pl.first[lo];
+    const Seq q = sequence<L2>(p, lo);
     job[k] = lo << 16 | i;
-    c[k] = sequence<L2>(p, lo).steps(p, i);
-    sum += static_cast<unsigned long long>(c[k]);
+    c[k] = q.steps(p, q.tiles(p), i);
+    pl.seq[u] = job[k];
+    pl.steps[u] = c[k];
+    sum += c[k];
     most = max(most, c[k]);
+    least = min(least, c[k]);
   }
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  sum = __reduce_add_sync(0xffffffffu, sum);  // (steps are below 2^25)
   most = __reduce_max_sync(0xffffffffu, most);
+  least = __reduce_min_sync(0xffffffffu, least);
   if (lane == 0) {
     s.sum[warp] = sum;
     s.most[warp] = most;
+    s.least[warp] = least;
   }
   __syncthreads();
-  sum = 0;
-  most = 0;
+  float T = 0.f;
 #pragma unroll
   for (int i = 0; i < WARPS; ++i) {
-    sum += s.sum[i];
+    T += static_cast<float>(s.sum[i]);
     most = max(most, s.most[i]);
+    least = min(least, s.least[i]);
   }
-  const long long J = static_cast<long long>(U) * p.kv_heads, G = p.grid;
-  const long long T = static_cast<long long>(sum) * p.kv_heads;
-  int share = most;
-  if (p.may_cut && J > 0) {
-    long long ks;
-    if (J >= G) {
-      ks = (T + G - 1) / G;
-    } else {
-      const int each = static_cast<int>(G / J);
-      ks = min((T + G - J - 1) / (G - J), static_cast<long long>(ceil_div(most, each)));
+  // (fp32: a share that is off by its rounding is as good)
+  T *= static_cast<float>(p.kv_heads);
+  const int G = p.grid;
+  const bool few = U * static_cast<long long>(p.kv_heads) < G;
+  int share = most, cut_above = most;
+  if (p.may_cut && few) {
+    const int J = U * p.kv_heads;
+    const int each = static_cast<int>(__fdividef(static_cast<float>(G), static_cast<float>(J)) + 1e-3f);  // floor(G / J)
+    const int hi = max(MIN_STEPS, min(static_cast<int>(__fdividef(T, static_cast<float>(G - J))) + 1,
+                                      static_cast<int>(__fdividef(static_cast<float>(most), static_cast<float>(each))) + 1));
+    const int lo = max(MIN_STEPS, min(hi, static_cast<int>(__fdividef(T, static_cast<float>(G))) + 1));
+    auto tried = [&](int w) { return lo + (hi - lo) * w / (WARPS - 1); };  // (the last one is hi)
+    const float inv = __fdividef(1.0f, static_cast<float>(tried(warp)));
+    int n = 0;
+    for (int u = lane; u < U; u += 32) n += static_cast<int>(ceilf(static_cast<float>(pl.steps[u]) * inv - 1e-3f));
+    n = __reduce_add_sync(0xffffffffu, n) * p.kv_heads;
+    if (lane == 0) s.count[warp] = n;
+    __syncthreads();
+    share = hi;
+#pragma unroll
+    for (int w = WARPS - 1; w >= 0; --w)
+      if (s.count[w] <= G) share = min(share, tried(w));
+    share = min(share, most);
+    cut_above = share;
+  } else if (p.may_cut) {
+    const float J = static_cast<float>(U) * static_cast<float>(p.kv_heads);
+    share = max(MIN_STEPS, static_cast<int>((T + J * ITEM_STEPS) / static_cast<float>(G)) + 1 - ITEM_STEPS);
+    share = min(share, most);
+    cut_above = min(most, share + ITEM_STEPS);
+  }
+  const bool sorted = !few && most > least;
+  if (sorted) {
+    // by bucket, in order within one: the rank among the warp's lanes, then a scan over
+    // all warps' counts
+    for (int i = tid; i < BUCKETS * ROWS; i += NT) s.hist[i] = 0;
+    __syncthreads();
+    int rank[PER], bucket[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      bucket[k] = BUCKETS;
+      if (k * NT >= U) continue;  // (uniform)
+      const bool in = k * NT + tid < U;
+      if (in) {
+        const bool cut = c[k] > cut_above;
+        const float top = static_cast<float>(cut ? most : cut_above);
+        bucket[k] = (cut ? 15 : 31) - min(15, static_cast<int>(static_cast<float>(c[k] - 1) * 16.0f / top));
+      }
+      const uint32_t same = __match_any_sync(0xffffffffu, bucket[k]);
+      rank[k] = __popc(same & ((1u << lane) - 1u));
+      if (in && rank[k] == 0) s.hist[bucket[k] * ROWS + k * WARPS + warp] = __popc(same);
     }
-    share = static_cast<int>(min(max(ks, static_cast<long long>(MIN_STEPS)), static_cast<long long>(max(most, 1))));
-  }
-  // sorted by bucket, in order within one: the rank among the warp's lanes, then
-  // a scan over all warps' counts
-  int rank[PER], bucket[PER];
+    __syncthreads();
+    constexpr int HPER = (BUCKETS * ROWS + NT - 1) / NT;
+    int h[HPER], mine = 0, total;
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const bool in = k * NT + tid < U;
-    bucket[k] = BUCKETS;
-    if (in) {
-      const int top = c[k] > share ? most : min(most, share);
-      bucket[k] = (c[k] > share ? 15 : 31) - min(15, static_cast<int>(static_cast<uint32_t>(c[k] - 1) * 16u /
-                                                                      static_cast<uint32_t>(top)));
+    for (int i = 0; i < HPER; ++i) {
+      const int at = tid * HPER + i;
+      h[i] = at < BUCKETS * ROWS ? s.hist[at] : 0;
+      mine += h[i];
     }
-    const uint32_t same = __match_any_sync(0xffffffffu, bucket[k]);
-    rank[k] = __popc(same & ((1u << lane) - 1u));
-    if (in && rank[k] == 0) s.hist[bucket[k] * ROWS + k * WARPS + warp] = __popc(same);
-  }
-  __syncthreads();
-  constexpr int HPER = (BUCKETS * ROWS + NT - 1) / NT;
-  int h[HPER], mine = 0, total;
+    int run = block_excl_scan<NT>(mine, s.tot[2], total);
 #pragma unroll
-  for (int i = 0; i < HPER; ++i) {
-    const int at = tid * HPER + i;
-    h[i] = at < BUCKETS * ROWS ? s.hist[at] : 0;
-    mine += h[i];
-  }
-  int run = block_excl_scan<NT>(mine, s.tot[2], total);
+    for (int i = 0; i < HPER; ++i) {
+      const int at = tid * HPER + i;
+      if (at < BUCKETS * ROWS) s.hist[at] = run;
+      run += h[i];
+    }
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < HPER; ++i) {
-    const int at = tid * HPER + i;
-    if (at < BUCKETS * ROWS) s.hist[at] = run;
-    run += h[i];
+    for (int k = 0; k < PER; ++k) {
+      if (bucket[k] == BUCKETS) continue;
+      const int at = s.hist[bucket[k] * ROWS + k * WARPS + warp] + rank[k];
+      pl.seq[at] = job[k];
+      pl.steps[at] = c[k];
+    }
+    __syncthreads();
   }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    if (bucket[k] == BUCKETS) continue;
-    const int at = s.hist[bucket[k] * ROWS + k * WARPS + warp] + rank[k];
-    pl.seq[at] = job[k];
-    pl.steps[at] = c[k];
-  }
-  __syncthreads();
   // items before each entry
-  int n[PER], cut = 0;
-  mine = 0;
+  int n[PER], mine = 0, cut = 0, total;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int at = tid * PER + i;
-    n[i] = at < U ? pieces_of(pl.steps[at], share) * p.kv_heads : 0;
-    if (at < U) cut += pl.steps[at] > share;
-    mine += n[i];
+    n[i] = 0;
+    if (at < U) {
+      const int steps = pl.steps[at];
+      n[i] = steps > cut_above ? ceil_div(steps, share) : 1;
+      if (n[i] > 1) cut = at + 1;
+      mine += n[i] * p.kv_heads;
+    }
   }
-  run = block_excl_scan<NT>(mine, s.tot[3], total);
+  cut = __reduce_max_sync(0xffffffffu, cut);
+  if (lane == 0) s.cut[warp] = cut;
+  int run = block_excl_scan<NT>(mine, s.tot[3], total);
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int at = tid * PER + i;
-    if (at < U) pl.items[at] = run;
-    run += n[i];
+    if (at >= U) continue;
+    pl.items[at] = run;
+    const int more = n[i] * p.kv_heads;
+    if (own && t_own >= run && t_own < run + more)
+      *own = make_item(p, pl.seq[at] >> 16, pl.seq[at] & 0xffff, pl.steps[at], n[i], t_own - run, t_own);
+    run += more;
   }
-  int n_cut;
-  block_excl_scan<NT>(cut, s.tot[0], n_cut);
   if (tid == 0) {
+    cut = 0;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) cut = max(cut, s.cut[i]);
     pl.jobs = U;
     pl.n_items = total;
-    pl.n_cut = n_cut;
+    pl.n_cut = cut;
     pl.share = share;
+    pl.cut_above = cut_above;
   }
   __syncthreads();
 }
 
 // ------------------------------------------------------------------- items --
 
-// A CTA's unit of work: query tiles j0 (and j0 + 1 of a pair) of a sequence and
-// a key head over the key tiles [t0, t1).
-struct Item {
-  int more;  // 0: the CTA has no further item
-  int q0, lq, k0, lk;
-  int hk, j0, pair;
-  int t0, t1;
-  int n0, n1;  // steps of the two warpgroups
-  int slot;    // of a piece; -1: the whole job
-};
-
-// The key tile of step s of warpgroup i.
-__device__ __forceinline__ int item_tile(int pair, int t0, int i, int s) { return pair ? t0 + s : t0 + 2 * s + i; }
-
 __device__ Item item_at(const VarParams& p, const Plan& pl, int t) {
-  Item it;
-  it.more = 0;
-  if (t >= pl.n_items) return it;
-  int b, i, piece = 0, pieces = 1;
+  if (t >= pl.n_items) {
+    Item none;
+    none.more = 0;
+    return none;
+  }
   if (pl.jobs <= MAX_TABLE) {
     int lo = 0, hi = pl.jobs;
     while (hi - lo > 1) {
@@ -352,49 +433,19 @@ __device__ Item item_at(const VarParams& p, const Plan& pl, int t) {
       if (pl.items[mid] <= t) lo = mid;
       else hi = mid;
     }
-    b = pl.seq[lo] >> 16;
-    i = pl.seq[lo] & 0xffff;
-    pieces = pieces_of(pl.steps[lo], pl.share);
-    const int r = t - pl.items[lo];
-    it.hk = r / pieces;
-    piece = r - it.hk * pieces;
-  } else {
-    const int v = t / p.kv_heads, u = pl.jobs - 1 - v;
-    it.hk = t - v * p.kv_heads;
-    int lo = 0, hi = p.B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (pl.first[mid] <= u) lo = mid;
-      else hi = mid;
-    }
-    b = lo;
-    i = u - pl.first[lo];
+    const int steps = pl.steps[lo];
+    return make_item(p, pl.seq[lo] >> 16, pl.seq[lo] & 0xffff, steps, pieces_of(pl, steps), t - pl.items[lo], t);
   }
-  const Seq s = sequence<false>(p, b);
-  it.more = 1;
-  it.q0 = s.q0;
-  it.lq = s.lq;
-  it.k0 = s.k0;
-  it.lk = s.lk;
-  it.j0 = 2 * i;
-  it.pair = 2 * i + 1 < s.tiles(p);
-  const uint32_t c = static_cast<uint32_t>(s.steps(p, i));
-  const int u0 = static_cast<int>(c * static_cast<uint32_t>(piece) / static_cast<uint32_t>(pieces));
-  const int u1 = static_cast<int>(c * static_cast<uint32_t>(piece + 1) / static_cast<uint32_t>(pieces));
-  const int nkv0 = s.key_tiles(p, it.j0);
-  if (it.pair) {
-    it.t0 = u0;
-    it.t1 = u1;
-    it.n0 = max(0, min(u1, nkv0) - u0);
-    it.n1 = u1 - u0;
-  } else {
-    it.t0 = 2 * u0;
-    it.t1 = min(nkv0, 2 * u1);
-    it.n1 = (it.t1 - it.t0) / 2;
-    it.n0 = it.t1 - it.t0 - it.n1;
+  const int v = t / p.kv_heads, u = pl.jobs - 1 - v;
+  int lo = 0, hi = p.B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (pl.first[mid] <= u) lo = mid;
+    else hi = mid;
   }
-  it.slot = pieces > 1 ? t : -1;
-  return it;
+  const int i = u - pl.first[lo];
+  const Seq s = sequence<false>(p, lo);
+  return make_item(p, lo, i, s.steps(p, s.tiles(p), i), 1, t - v * p.kv_heads, t);
 }
 
 // Item k of CTA x of G.
@@ -445,16 +496,24 @@ struct Shared {
 
 template <int HD>
 struct Cfg {
-  static constexpr int NBOX = HD / 64;
-  static constexpr int TILE_BYTES = NBOX * BOX_BYTES;  // 128 rows x HD
+  static constexpr int NBOX = HD / 64;               // boxes of 64 columns
+  static constexpr int Q_BOX = BQ * 128, KV_BOX = BKV * 128;
+  static constexpr int Q_BYTES = NBOX * Q_BOX, KV_BYTES = NBOX * KV_BOX;
   // Q0 | Q1 | K0 | K1 | V0 | V1 (the plan's scratch before the first copy)
   static constexpr int OFF_Q = 0;
-  static constexpr int OFF_K = 2 * TILE_BYTES;
-  static constexpr int OFF_V = 4 * TILE_BYTES;
-  static constexpr int DATA_BYTES = 6 * TILE_BYTES;
+  static constexpr int OFF_K = 2 * Q_BYTES;
+  static constexpr int OFF_V = OFF_K + 2 * KV_BYTES;
+  static constexpr int DATA_BYTES = OFF_V + 2 * KV_BYTES;
   static constexpr int OFF_X = DATA_BYTES + 256;  // barriers before it
   static constexpr int OFF_PLAN = OFF_X + static_cast<int>(sizeof(Shared));
   static constexpr int SMEM_BYTES = OFF_PLAN + static_cast<int>(sizeof(Plan)) + 1024;  // + alignment of the base
+  // Tensor memory: S0 | S1 | O0 | O1, P_i over the first half of S_i; of heads of 64
+  // there is room for a P_i of its own (S0 | S1 | P0 | P1 | O0 | O1).
+  static constexpr bool OWN_P = HD == 64;
+  static constexpr uint32_t COL_P = OWN_P ? 2 * BKV : 0, P_STEP = OWN_P ? BKV / 2 : BKV;
+  static constexpr uint32_t COL_O = 2 * BKV + (OWN_P ? BKV : 0);
+  static constexpr uint32_t TMEM_COLS = 512;
+  static_assert(COL_O + 2 * HD <= TMEM_COLS, "tensor memory");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
   static_assert(sizeof(PlanScratch<THREADS>) <= DATA_BYTES, "the plan's scratch");
 };
@@ -480,14 +539,15 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* epi_done = bars + 16;  // an item's output rows are out: Q free
   uint64_t* it_full = bars + 18;  // [RING]
   uint64_t* it_empty = bars + 22; // [RING]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 26);
+  uint64_t* s_free = bars + 26;   // [2] OWN_P: S_i is in registers, the next one may be formed
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 28);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   Shared& shr = *reinterpret_cast<Shared*>(smem + C::OFF_X);
   Plan& plan = *reinterpret_cast<Plan*>(smem + C::OFF_PLAN);
   int* err = &g_attn_var_err;
-  auto sK = [&](int st) { return smem + C::OFF_K + st * C::TILE_BYTES; };
-  auto sV = [&](int st) { return smem + C::OFF_V + st * C::TILE_BYTES; };
-  auto sQ = [&](int i) { return smem + C::OFF_Q + i * C::TILE_BYTES; };
+  auto sK = [&](int st) { return smem + C::OFF_K + st * C::KV_BYTES; };
+  auto sV = [&](int st) { return smem + C::OFF_V + st * C::KV_BYTES; };
+  auto sQ = [&](int i) { return smem + C::OFF_Q + i * C::Q_BYTES; };
 
   const int warp = warp_id(), lane = lane_id();
   if (threadIdx.x == 0) {
@@ -500,6 +560,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[i], 128);
       mbar_init(&o_done[i], 1);
+      mbar_init(&s_free[i], 128);
     }
     mbar_init(drain, 1);
     mbar_init(epi_done, 1);
@@ -514,18 +575,24 @@ __global__ void __launch_bounds__(THREADS, 1)
   // the lengths may be the previous kernel's
   pdl_wait();
   pdl_trigger();
-  plan_build<THREADS, false>(p, plan, *reinterpret_cast<PlanScratch<THREADS>*>(smem));
-  if (static_cast<int>(blockIdx.x) >= plan.n_items) return;  // (uniform: nothing allocated yet)
-  if (warp == MMA_WARP) {
-    tmem_alloc(tmem_slot, TMEM_COLS);
+  if (warp == MMA_WARP) {  // (the others go on to the plan)
+    tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
   }
+  plan_build<THREADS, false>(p, plan, *reinterpret_cast<PlanScratch<THREADS>*>(smem), &shr.ring[0], blockIdx.x);
+  const bool idle = static_cast<int>(blockIdx.x) >= plan.n_items;  // (uniform)
+  // the plan has left the first item in the ring
+  if (threadIdx.x == 0 && plan.jobs <= MAX_TABLE) mbar_arrive(&it_full[0]);
   // the plan's scratch (generic proxy) before the first copy over it (async proxy)
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  if (idle) {
+    if (warp == MMA_WARP) tmem_dealloc(tmem, C::TMEM_COLS);
+    return;
+  }
   // key tile number kt of the CTA: its stage and the parity of that stage's use
   auto kv_stage = [](uint32_t kt) { return static_cast<int>(kt & 1u); };
   auto kv_phase = [](uint32_t kt) { return (kt >> 1) & 1u; };
@@ -570,8 +637,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_arrive_expect_tx(q_full, (pair ? 2 : 1) * q_bytes);
 #pragma unroll
             for (int j = 0; j < C::NBOX; ++j) {
-              tma_load_3d(sQ(0) + j * BOX_BYTES, &tm_q, q_full, 64 * j, h0, row0);
-              if (pair) tma_load_3d(sQ(1) + j * BOX_BYTES, &tm_q, q_full, 64 * j, h0, row0 + p.tpt);
+              tma_load_3d(sQ(0) + j * C::Q_BOX, &tm_q, q_full, 64 * j, h0, row0);
+              if (pair) tma_load_3d(sQ(1) + j * C::Q_BOX, &tm_q, q_full, 64 * j, h0, row0 + p.tpt);
             }
             q_armed = true;
             q_par = jn & 1u;
@@ -584,11 +651,11 @@ __global__ void __launch_bounds__(THREADS, 1)
               ok = false;
               break;
             }
-            mbar_arrive_expect_tx(&full[st], C::TILE_BYTES);
+            mbar_arrive_expect_tx(&full[st], C::KV_BYTES);
             unsigned char* dst = kq ? sK(st) : sV(st);
 #pragma unroll
             for (int j = 0; j < C::NBOX; ++j)
-              tma_load_3d(dst + j * BOX_BYTES, tm, &full[st], 64 * j, hk, k0 + (t0 + t) * BKV);
+              tma_load_3d(dst + j * C::KV_BOX, tm, &full[st], 64 * j, hk, k0 + (t0 + t) * BKV);
             armed |= 1u << st;
             par = (par & ~(1u << st)) | (ph << st);
           }
@@ -616,34 +683,35 @@ __global__ void __launch_bounds__(THREADS, 1)
       constexpr int FMT = F16 ? 0 : 1;
       constexpr uint32_t idesc_s = idesc_kind_f16(BQ, BKV, 0, 0, FMT);
       constexpr uint32_t idesc_o = idesc_kind_f16(BQ, HD, 0, 1, FMT);
-      constexpr uint32_t TILE16 = C::TILE_BYTES >> 4;
+      constexpr uint32_t Q16 = C::Q_BYTES >> 4, KV16 = C::KV_BYTES >> 4;
       const uint32_t base16 = smem_u32(smem) >> 4;
       const uint32_t q_lo = base16 + (C::OFF_Q >> 4) + sw128_lo_lbo(16);
       const uint32_t k_lo = base16 + (C::OFF_K >> 4) + sw128_lo_lbo(16);
-      const uint32_t v_lo = base16 + (C::OFF_V >> 4) + sw128_lo_lbo(BOX_BYTES);
+      const uint32_t v_lo = base16 + (C::OFF_V >> 4) + sw128_lo_lbo(C::KV_BOX);
       constexpr uint32_t hi = sw128_hi(1024);
       // S_i = Q_qb K^T (K from stage kst)
       auto issue_s = [&](int i, int qb, int kst) {
         if (leader) {
-          const uint32_t a = q_lo + static_cast<uint32_t>(qb) * TILE16, b = k_lo + static_cast<uint32_t>(kst) * TILE16;
+          const uint32_t a = q_lo + static_cast<uint32_t>(qb) * Q16, b = k_lo + static_cast<uint32_t>(kst) * KV16;
 #pragma unroll
           for (int k = 0; k < HD / 16; ++k) {
-            const uint32_t off = static_cast<uint32_t>((k >> 2) * BOX_BYTES + (k & 3) * 32) >> 4;
-            umma_f16_w(tmem + 128u * i, a + off, b + off, hi, idesc_s, k > 0 ? 1u : 0u);
+            const uint32_t qo = static_cast<uint32_t>((k >> 2) * C::Q_BOX + (k & 3) * 32) >> 4;
+            const uint32_t ko = static_cast<uint32_t>((k >> 2) * C::KV_BOX + (k & 3) * 32) >> 4;
+            umma_f16_w(tmem + BKV * i, a + qo, b + ko, hi, idesc_s, k > 0 ? 1u : 0u);
           }
           umma_commit(&s_full[i]);
         }
         __syncwarp();
       };
-      // O_i (+)= P_i V: P_i from the first 64 TMEM columns of S_i, V from stage vst
+      // O_i (+)= P_i V: P_i from the first half of S_i's columns, V from stage vst
       auto issue_pv = [&](int i, int vst, bool acc, bool last) {
         if (leader) {
-          const uint32_t b = v_lo + static_cast<uint32_t>(vst) * TILE16;
+          const uint32_t b = v_lo + static_cast<uint32_t>(vst) * KV16;
 #pragma unroll
           for (int k = 0; k < BKV / 16; ++k)
-            umma_f16_tmem_a_w(tmem + 256u + 128u * i, tmem + 128u * i + 8u * k, b + ((k * 2048) >> 4), hi, idesc_o,
+            umma_f16_tmem_a_w(tmem + C::COL_O + HD * i, tmem + C::COL_P + C::P_STEP * i + 8u * k, b + ((k * 2048) >> 4), hi, idesc_o,
                               (acc || k > 0) ? 1u : 0u);
-          if (last) umma_commit(&o_done[i]);
+          if (C::OWN_P || last) umma_commit(&o_done[i]);
         }
         __syncwarp();
       };
@@ -696,11 +764,34 @@ __global__ void __launch_bounds__(THREADS, 1)
             commit(&k_empty[kv_stage(kt + 1)]);
           }
         }
-        // ping-pong: PV_0(s), S_0(s+1), PV_1(s), S_1(s+1); S_i(s+1)
-        // overwrites P_i(s) only after PV_i(s), in issue order
+        // S_i(s + 1) of a step whose S_i(s) has been taken
+        auto next_s = [&](int i, int qb, int s, int n, uint32_t sc, bool waited) {
+          if (s + 1 >= n) return true;
+          const uint32_t t2 = tile(i, s + 1);
+          if (!waited && !wait_k(t2)) return false;
+          if (C::OWN_P) {
+            if (!mbar_wait_warp(&s_free[i], (sc + s) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 7)) return false;
+            tc_fence_after();
+          }
+          // (without OWN_P no tcgen05 fence here: S reads only TMA-written Q and K, ordered
+          // by their mbarrier, and it follows the PV block before it, whose fence
+          // already ordered the softmax's TMEM accesses, in issue order)
+          issue_s(i, qb, kv_stage(t2));
+          if (!pair || i == 1) commit(&k_empty[kv_stage(t2)]);
+          return true;
+        };
+        // P_i over S_i: PV_0(s), S_0(s+1), PV_1(s), S_1(s+1), where S_i(s+1) overwrites
+        // P_i(s) only after PV_i(s), in issue order. P_i of its own: S_i(s+1) before
+        // PV_i(s), as soon as S_i(s) is in registers, so that the softmax never waits
+        // for two products in a row (images of 1111 to 4096 tokens, 16 heads of 64:
+        // 132 us with P over S).
         const int nmax = n0 > n1 ? n0 : n1;
         for (int s = 0; s < nmax && ok; ++s) {
           if (s < n0) {
+            if (C::OWN_P && !next_s(0, 0, s, n0, sc0, false)) {
+              ok = false;
+              break;
+            }
             const uint32_t t = tile(0, s);
             if (!mbar_wait2_warp(&p_full[0], (sc0 + s) & 1u, &v_full[kv_stage(t)], kv_phase(t), abort_flag, err,
                                  DEV_TIMEOUT_ATTN + 256 * 5, DEV_TIMEOUT_ATTN + 256 * 6)) {
@@ -710,22 +801,18 @@ __global__ void __launch_bounds__(THREADS, 1)
             tc_fence_after();
             issue_pv(0, kv_stage(t), s > 0, s + 1 == n0);
             if (!pair) commit(&v_empty[kv_stage(t)]);
-            if (s + 1 < n0) {
-              // no tcgen05 fence here: S reads only TMA-written Q and K (ordered
-              // by their mbarrier), and it follows the PV block above, whose
-              // fence already ordered the softmax's TMEM accesses, in issue order
-              const uint32_t t2 = tile(0, s + 1);
-              if (!wait_k(t2)) {
-                ok = false;
-                break;
-              }
-              issue_s(0, 0, kv_stage(t2));
-              if (!pair) commit(&k_empty[kv_stage(t2)]);
+            if (!C::OWN_P && !next_s(0, 0, s, n0, sc0, false)) {
+              ok = false;
+              break;
             }
           }
           if (s < n1) {
             // a pair's second tile has at least the first one's steps, and where both
             // have one its key tiles are those that were waited for above
+            if (C::OWN_P && !next_s(1, qb1, s, n1, sc1, pair && s + 1 < n0)) {
+              ok = false;
+              break;
+            }
             const uint32_t t = tile(1, s);
             if (!mbar_wait_warp(&p_full[1], (sc1 + s) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 8) ||
                 ((!pair || s >= n0) && !wait_v(t))) {
@@ -735,14 +822,9 @@ __global__ void __launch_bounds__(THREADS, 1)
             tc_fence_after();
             issue_pv(1, kv_stage(t), s > 0, s + 1 == n1);
             commit(&v_empty[kv_stage(t)]);
-            if (s + 1 < n1) {
-              const uint32_t t2 = tile(1, s + 1);
-              if ((!pair || s + 1 >= n0) && !wait_k(t2)) {
-                ok = false;
-                break;
-              }
-              issue_s(1, qb1, kv_stage(t2));
-              commit(&k_empty[kv_stage(t2)]);
+            if (!C::OWN_P && !next_s(1, qb1, s, n1, sc1, pair && s + 1 < n0)) {
+              ok = false;
+              break;
             }
           }
         }
@@ -769,10 +851,10 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (jn >= RING &&
             !mbar_wait(&it_empty[slot], ((jn - RING) / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 20))
           break;
-        const Item it = item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x));
-        shr.ring[slot] = it;
+        if (jn == 0 && plan.jobs <= MAX_TABLE) continue;  // there already
+        shr.ring[slot] = item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x));
         mbar_arrive(&it_full[slot]);
-        if (!it.more) break;
+        if (!shr.ring[slot].more) break;
       }
     }
   } else {
@@ -781,14 +863,18 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int i = warp >> 2;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t tS = tmem + 128u * i + lane_off;
-    const uint32_t tO = tmem + 256u + 128u * i + lane_off;
-    const uint32_t tO1 = tmem + 384u + lane_off;  // warpgroup 1's accumulator (single's merge)
+    const uint32_t tS = tmem + BKV * i + lane_off;
+    const uint32_t tP = tmem + C::COL_P + C::P_STEP * i + lane_off;
+    const uint32_t tO = tmem + C::COL_O + HD * i + lane_off;
+    const uint32_t tO1 = tmem + C::COL_O + HD + lane_off;  // warpgroup 1's accumulator (single's merge)
     const int row_tok = row / p.group;            // the row's token in its tile
     bool ok = true;
     // sc: S phases of this warpgroup so far (one per step); oc*: o_done phases so
-    // far (one per item in which a warpgroup has steps); kt: the running key tile
+    // far (one per item in which a warpgroup has steps, or with OWN_P one per step);
+    // kt: the running key tile
     uint32_t kt = 0, sc = 0, oc0 = 0, oc1 = 0;
+    // the phase of o_done after a warpgroup's n steps of the item
+    auto o_phase = [](uint32_t oc, int n) { return (C::OWN_P ? oc + static_cast<uint32_t>(n) - 1u : oc) & 1u; };
     // All softmax warps go on to an item together or not at all: a warp that gave up
     // a wait still meets the others at the barriers of its item.
     bool go = !bar_red_or(2, 256, !it_wait(0, 21));
@@ -823,11 +909,11 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int j = 0; j < C::NBOX; ++j)
 #pragma unroll
             for (int c16 = 0; c16 < 8; ++c16)
-              *reinterpret_cast<uint4*>(vr + j * BOX_BYTES + c16 * 16) = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(vr + j * C::KV_BOX + c16 * 16) = make_uint4(0, 0, 0, 0);
         } else if (t * BKV + row >= part0) {
 #pragma unroll 1
           for (int c16 = 0; c16 < 8 * C::NBOX; ++c16) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(vr + (c16 >> 3) * BOX_BYTES + (c16 & 7) * 16);
+            uint32_t* w = reinterpret_cast<uint32_t*>(vr + (c16 >> 3) * C::KV_BOX + (c16 & 7) * 16);
             const uint4 q = *reinterpret_cast<const uint4*>(w);
             if (special16<F16>(q.x) | special16<F16>(q.y) | special16<F16>(q.z) | special16<F16>(q.w)) {
               const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
@@ -843,8 +929,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         fence_proxy_async_smem();  // before the tensor core reads the tile
         return true;
       };
-      // S_i complete means every earlier MMA is too (PV_i of the previous
-      // step included), so O_i can be rescaled and P_i written over S_i
+      // With P_i over S_i, S_i complete means every earlier MMA is too (PV_i of the
+      // previous step included), so O_i can be rescaled and P_i written
       // without another wait. tcgen05.ld / tcgen05.st are warp-collective:
       // the whole warp rescales when any of its rows needs it (rows that do
       // not use alpha = 1)
@@ -879,6 +965,10 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int c = 0; c < BKV / 32; ++c) tmem_ld32(tS + c * 32, sv + c * 32);
         tmem_ld_wait();
+        if (C::OWN_P) {
+          tc_fence_before();
+          mbar_arrive(&s_free[i]);
+        }
         float mx8[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) mx8[u] = -INFINITY;
@@ -939,18 +1029,25 @@ __global__ void __launch_bounds__(THREADS, 1)
           ok = false;
           break;
         }
+        // (OWN_P: the previous step's PV may still read P_i and write O_i)
+        if (C::OWN_P && s > 0) {
+          if (!mbar_wait_warp(&o_done[i], o_phase(i ? oc1 : oc0, s), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 12)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+        }
         rescale_o(rescale, m_use);
         m = m_use;
         l += lsum;
-        // P_i as 16-bit pairs (keys 2c, 2c+1 in column c) over the first 64
-        // columns of S_i, the A operand of the PV product
+        // P_i as 16-bit pairs (keys 2c, 2c+1 in column c), the A operand of the PV product
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
+        for (int h2 = 0; h2 < BKV / 64; ++h2) {
           float pk[32];
 #pragma unroll
           for (int c = 0; c < 32; ++c)
             pk[c] = __uint_as_float(pack16<F16>(sv[64 * h2 + 2 * c], sv[64 * h2 + 2 * c + 1]));
-          tmem_st32(tS + 32 * h2, pk);
+          tmem_st32(tP + 32 * h2, pk);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -969,9 +1066,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         named_bar_sync(1, 256);
       }
       if (ok && writer) {
-        bool done = n == 0 || mbar_wait_warp(&o_done[i], (i ? oc1 : oc0) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 14);
+        bool done = n == 0 || mbar_wait_warp(&o_done[i], o_phase(i ? oc1 : oc0, n), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 14);
         if (merge)
-          done = done && mbar_wait_warp(&o_done[1], oc1 & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 15);
+          done = done && mbar_wait_warp(&o_done[1], o_phase(oc1, n1), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 15);
         ok = done;
         if (ok) {
           tc_fence_after();
@@ -1025,9 +1122,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                   tmem_ld_wait_regs(o);
                 }
                 if (special) give_back(c, o);
-                float* dst = p.part + at * HD + 32 * c;
+                float* dst = p.part + ((at - row) * HD + (32 * c * BQ + 8 * row));
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) st_f32x8(dst + j, o + j);
+                for (int j = 0; j < 32; j += 8) st_f32x8(dst + j * BQ, o + j);
               }
             }
           } else {
@@ -1117,8 +1214,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (threadIdx.x == 0) mbar_arrive(epi_done);
       if (lane == 0) mbar_arrive(&it_empty[jn & (RING - 1)]);
       sc += static_cast<uint32_t>(n);
-      oc0 += n0_all > 0 ? 1u : 0u;
-      oc1 += n1 > 0 ? 1u : 0u;
+      oc0 += C::OWN_P ? static_cast<uint32_t>(n0_all) : n0_all > 0 ? 1u : 0u;
+      oc1 += C::OWN_P ? static_cast<uint32_t>(n1) : n1 > 0 ? 1u : 0u;
       kt += static_cast<uint32_t>(len);
     }
   }
@@ -1127,7 +1224,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   __syncthreads();
   if (warp == MMA_WARP) {
     tc_fence_after();
-    tmem_dealloc(tmem, TMEM_COLS);
+    tmem_dealloc(tmem, C::TMEM_COLS);
   }
 }
 
@@ -1151,7 +1248,7 @@ template <int HD, bool F16>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ VarParams p) {
   extern __shared__ __align__(16) unsigned char join_raw[];
   JoinShared& sh = *reinterpret_cast<JoinShared*>(join_raw);
-  plan_build<JOIN_THREADS, true>(p, sh.plan, sh.scratch);
+  plan_build<JOIN_THREADS, true>(p, sh.plan, sh.scratch, nullptr, 0);
   pdl_wait();
   pdl_trigger();
   constexpr int COLS = HD / 32;
@@ -1166,7 +1263,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     const Seq s = sequence<false>(p, sh.plan.seq[e] >> 16);
     const int j = 2 * (sh.plan.seq[e] & 0xffff) + tile, tok = j * p.tpt + r / p.group;
     if (r / p.group >= p.tpt || tok >= s.lq) continue;
-    const int n = pieces_of(sh.plan.steps[e], sh.plan.share);
+    const int n = pieces_of(sh.plan, sh.plan.steps[e]);
+    if (n == 1) continue;
     const long long slot = static_cast<long long>(sh.plan.items[e]) + hk * n;
     auto row_of = [&](int q) { return ((slot + q) * 2 + tile) * BQ + r; };
     float M = -INFINITY;
@@ -1187,7 +1285,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
       for (int q = 0; q < most; ++q) {
         const float f = __shfl_sync(0xffffffffu, a, q);
         if (f == 0.f) continue;
-        const float* src = p.part + row_of(q0 + q) * HD + COLS * lane;
+        const float* src = p.part + (row_of(q0 + q) - r) * HD + (lane * COLS / 8 * (8 * BQ) + 8 * r + lane * COLS % 8);
         if (COLS == 4) {
           const float4 v = *reinterpret_cast<const float4*>(src);
           o[0] = fmaf(f, v.x, o[0]);
@@ -1257,7 +1355,6 @@ cudaError_t launch_hd(const hilo_attn_shape& s, const VarParams& p, const void* 
 
 // Whether a job could have more steps than the smallest piece.
 bool may_cut(const hilo_attn_shape& s) { return (s.rows_k + BKV - 1) / BKV > MIN_STEPS; }
-
 constexpr size_t SLOTS = static_cast<size_t>(SLOTS_PER_CTA) * ATTN_MAX_CTAS;
 
 }  // namespace
@@ -1289,6 +1386,10 @@ cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, 
   p.causal = s.causal;
   p.rows_q = s.rows_q;
   p.rows_k = s.rows_k;
+  int log2 = 0;
+  while ((1 << log2) < p.tpt) ++log2;
+  p.tpt_shift = 31 + log2;  // 2^31 / 2^shift <= 1 / tpt: exact below 2^31
+  p.tpt_mul = ((1ull << p.tpt_shift) + p.tpt - 1) / p.tpt;
   // a persistent grid: one CTA per SM; each takes its share of the items, whose
   // number is known on the device only
   p.grid = num_sms < 1 ? 1 : num_sms < ATTN_MAX_CTAS ? num_sms : ATTN_MAX_CTAS;
