@@ -74,6 +74,7 @@ struct VarParams {
   void* out;
   float* part;      // pieces' rows: [slot][tile 0, 1][HD / 8][row][8], so that a warp's stores join up
   float2* part_ml;  // their maxima and sums: [slot][tile][row]
+  struct Joints* joints;  // the cut jobs
   long long v_row, v_head, out_row, out_head;
   int B, kv_heads, group, tpt;  // tpt: tokens per tile
   unsigned long long tpt_mul;   // n / tpt = n * tpt_mul >> tpt_shift, n < 2^31
@@ -106,10 +107,8 @@ struct Seq {
   }
 };
 
-// (L2: before the kernel's own wait, when this SM's L1 may hold older offsets)
-template <bool L2>
 __device__ __forceinline__ Seq sequence(const VarParams& p, int b) {
-  auto at = [](const int32_t* cu, int rows) { return min(max(L2 ? ld_l2(cu) : *cu, 0), rows); };
+  auto at = [](const int32_t* cu, int rows) { return min(max(*cu, 0), rows); };
   const int q0 = at(p.cu_q + b, p.rows_q), q1 = at(p.cu_q + b + 1, p.rows_q);
   const int k0 = at(p.cu_k + b, p.rows_k), k1 = at(p.cu_k + b + 1, p.rows_k);
   return {q0, max(0, q1 - q0), k0, max(0, k1 - k0)};
@@ -158,6 +157,10 @@ __device__ __forceinline__ int pieces_of(const Plan& pl, int steps) {
   return steps > pl.cut_above ? ceil_div(steps, pl.share) : 1;
 }
 
+// The plan's larger parts (block_excl_scan, plan_sort, list_joints) are calls of their own,
+// made before the warpgroups share out their registers only: setmaxnreg does not know
+// a callee's need.
+
 // A CTA's unit of work: query tiles j0 (and j0 + 1 of a pair) of a sequence and
 // a key head over the key tiles [t0, t1).
 struct Item {
@@ -172,9 +175,9 @@ struct Item {
 // The key tile of step s of warpgroup i.
 __device__ __forceinline__ int item_tile(int pair, int t0, int i, int s) { return pair ? t0 + s : t0 + 2 * s + i; }
 
-// Item t: of the items of row job `job` (c steps, `pieces` pieces), number r.
-__device__ __forceinline__ Item make_item(const VarParams& p, int job, int i, int c, int pieces, int r, int t) {
-  const Seq s = sequence<false>(p, job);
+// Item t: of the items of row job i of a sequence (c steps, `pieces` pieces), number r.
+__device__ __forceinline__ void make_item(const VarParams& p, Item* out, const Seq& s, int i, int c, int pieces, int r,
+                                          int t) {
   Item it;
   it.hk = pieces == 1 ? r : static_cast<int>(static_cast<uint32_t>(r) / static_cast<uint32_t>(pieces));
   const int piece = r - it.hk * pieces;
@@ -203,73 +206,199 @@ __device__ __forceinline__ Item make_item(const VarParams& p, int job, int i, in
     it.n0 = it.t1 - it.t0 - it.n1;
   }
   it.slot = pieces > 1 ? t : -1;
-  return it;
+  *out = it;
 }
 
-// Sum of v over the CTA's threads before this one, and of all: `tot` is a word per warp
-// that no other call is using.
-template <int NT>
-__device__ __forceinline__ int block_excl_scan(int v, int* tot, int& total) {
+// Sum of v over the CTA's threads before this one, and of all (*total): `tot` is a word per
+// warp that no other call is using.
+__device__ __noinline__ int block_excl_scan(int v, int* tot, int* total) {
   const int incl = warp_incl_scan(v), w = warp_id();
   if (lane_id() == 31) tot[w] = incl;
   __syncthreads();
-  int before = 0;
-  total = 0;
+  int before = 0, all = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 32; ++i) {
+  for (int i = 0; i < THREADS / 32; ++i) {
     const int t = tot[i];
     before += i < w ? t : 0;
-    total += t;
+    all += t;
   }
+  *total = all;
   return before + incl - v;
 }
 
+// Between which shares of few jobs (J < G) the one is looked for; the share of many.
+struct Shares {
+  int lo, hi;
+};
+__device__ __forceinline__ Shares shares_of_few(float T, int most, int J, int G) {
+  const int each = static_cast<int>(__fdividef(static_cast<float>(G), static_cast<float>(J)) + 1e-3f);  // floor(G / J)
+  const int hi = max(MIN_STEPS, min(static_cast<int>(__fdividef(T, static_cast<float>(G - J))) + 1,
+                                    static_cast<int>(__fdividef(static_cast<float>(most), static_cast<float>(each))) + 1));
+  return {max(MIN_STEPS, min(hi, static_cast<int>(__fdividef(T, static_cast<float>(G))) + 1)), hi};
+}
+__device__ __forceinline__ int share_of_many(float T, float J, int G) {
+  return max(MIN_STEPS, static_cast<int>(__fdividef(T + J * ITEM_STEPS, static_cast<float>(G))) + 1 - ITEM_STEPS);
+}
+
+// The plan of up to 32 row jobs of up to 32 sequences, by one warp without a barrier: a lane per
+// sequence, then per row job. (The CTA's way to the same plan takes 4000 to 5000
+// cycles of barriers and shared memory, a third of the shortest calls.) Returns whether it
+// was made; pl.jobs is set either way.
+__device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* own, int t_own) {
+  constexpr uint32_t ALL = 0xffffffffu;
+  const int lane = lane_id();
+  Seq s = {0, 0, 0, 0};
+  if (lane < p.B) s = sequence(p, lane);
+  const int mine = (s.tiles(p) + 1) / 2, incl = warp_incl_scan(mine), first = incl - mine;
+  const int U = __shfl_sync(ALL, incl, 31);
+  if (lane == 0) pl.jobs = U;
+  if (U > 32) return false;
+  int b = 0;  // the sequence of row job `lane`: the sequences that end at or before it
+#pragma unroll
+  for (int step = 16; step >= 1; step >>= 1)
+    if (__shfl_sync(ALL, incl, b + step - 1) <= lane) b += step;
+  b = min(b, 31);
+  const int i = lane - __shfl_sync(ALL, first, b);
+  const Seq q = {__shfl_sync(ALL, s.q0, b), __shfl_sync(ALL, s.lq, b), __shfl_sync(ALL, s.k0, b),
+                 __shfl_sync(ALL, s.lk, b)};
+  const bool in = lane < U;
+  const int c = in ? q.steps(p, q.tiles(p), i) : 0;
+  const float T = static_cast<float>(__reduce_add_sync(ALL, c)) * static_cast<float>(p.kv_heads);
+  const int most = __reduce_max_sync(ALL, c), least = __reduce_min_sync(ALL, in ? c : 0x7fffffff);
+  const int G = p.grid;
+  const bool few = U * static_cast<long long>(p.kv_heads) < G;
+  int share = most, cut_above = most;
+  if (p.may_cut && few && most > MIN_STEPS) {
+    const Shares r = shares_of_few(T, most, U * p.kv_heads, G);
+    const int tried = r.lo + (r.hi - r.lo) * lane / 31;
+    const float inv = __fdividef(1.0f, static_cast<float>(tried));
+    int n = 0;
+    for (int j = 0; j < U; ++j) n += static_cast<int>(ceilf(static_cast<float>(__shfl_sync(ALL, c, j)) * inv - 1e-3f));
+    share = cut_above = min(most, __reduce_min_sync(ALL, n * p.kv_heads <= G ? tried : r.hi));
+  } else if (p.may_cut && !few) {
+    share = min(most, share_of_many(T, static_cast<float>(U) * static_cast<float>(p.kv_heads), G));
+    cut_above = min(most, share + ITEM_STEPS);
+  }
+  const int pieces = c > cut_above ? ceil_div(c, share) : 1, n = in ? pieces * p.kv_heads : 0;
+  int at = lane, run = 0;  // the entry, and the items before it
+  if (!few && most > least) {
+    at = 0;
+    for (int j = 0; j < U; ++j) {
+      const int cj = __shfl_sync(ALL, c, j), nj = __shfl_sync(ALL, n, j);
+      const bool before = cj > c || (cj == c && j < lane);
+      at += before;
+      run += before ? nj : 0;
+    }
+  } else {
+    run = warp_incl_scan(n) - n;
+  }
+  if (in) {
+    pl.seq[at] = b << 16 | i;
+    pl.steps[at] = c;
+    pl.items[at] = run;
+    if (t_own >= run && t_own < run + n) make_item(p, own, q, i, c, pieces, t_own - run, t_own);
+  }
+  const int total = __reduce_add_sync(ALL, n), cut = __reduce_max_sync(ALL, pieces > 1 ? at + 1 : 0);
+  if (lane == 0) {
+    pl.n_items = total;
+    pl.n_cut = cut;
+    pl.share = share;
+    pl.cut_above = cut_above;
+  }
+  return true;
+}
+
 // What plan_build needs for itself.
-template <int NT>
+constexpr int PLAN_PER = (MAX_TABLE + THREADS - 1) / THREADS;
 struct PlanScratch {
-  static constexpr int PER = (MAX_TABLE + NT - 1) / NT;
-  int tot[4][NT / 32];
-  int sum[NT / 32], most[NT / 32], least[NT / 32], count[NT / 32], cut[NT / 32];
-  int hist[BUCKETS * PER * (NT / 32)];  // [bucket][round, warp]
+  int tot[4][THREADS / 32];
+  int sum[THREADS / 32], most[THREADS / 32], least[THREADS / 32], count[THREADS / 32], cut[THREADS / 32];
+  int seq[MAX_TABLE], steps[MAX_TABLE], rank[MAX_TABLE];  // in the order of the sequences
+  int hist[BUCKETS * PLAN_PER * (THREADS / 32)];          // [bucket][round, warp]
 };
 
-// By all NT threads; ends with a barrier. Where `own` is not null, item t_own of the
-// listed ones is written there by the thread that finds it.
-template <int NT, bool L2>
-__device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScratch<NT>& s, Item* own, int t_own) {
-  constexpr int PER = PlanScratch<NT>::PER, WARPS = NT / 32, ROWS = PER * WARPS;
+// Longest first by bucket, in the sequences' order within one: the rank among a
+// warp's lanes, then a scan over all warps' counts.
+__device__ __noinline__ void plan_sort(Plan& pl, PlanScratch& s, int U, int most, int cut_above) {
+  constexpr int WARPS = THREADS / 32, ROWS = PLAN_PER * WARPS;
   const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
+  for (int i = tid; i < BUCKETS * ROWS; i += THREADS) s.hist[i] = 0;
+  __syncthreads();
+  auto bucket_of = [&](int c) {
+    const bool cut = c > cut_above;
+    const float top = static_cast<float>(cut ? most : cut_above);
+    return (cut ? 15 : 31) - min(15, static_cast<int>(static_cast<float>(c - 1) * __fdividef(16.0f, top)));
+  };
+#pragma unroll 1
+  for (int k = 0; k * THREADS < U; ++k) {
+    const int u = k * THREADS + tid;
+    const int bucket = u < U ? bucket_of(s.steps[u]) : BUCKETS;
+    const uint32_t same = __match_any_sync(0xffffffffu, bucket);
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    if (u < U) s.rank[u] = rank;
+    if (u < U && rank == 0) s.hist[bucket * ROWS + k * WARPS + warp] = __popc(same);
+  }
+  __syncthreads();
+  constexpr int HPER = (BUCKETS * ROWS + THREADS - 1) / THREADS;
+  int mine = 0, total;
+  for (int i = 0; i < HPER; ++i)
+    if (tid * HPER + i < BUCKETS * ROWS) mine += s.hist[tid * HPER + i];
+  int run = block_excl_scan(mine, s.tot[2], &total);
+  for (int i = 0; i < HPER; ++i) {
+    const int at = tid * HPER + i;
+    if (at >= BUCKETS * ROWS) break;
+    const int h = s.hist[at];
+    s.hist[at] = run;
+    run += h;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k * THREADS < U; ++k) {
+    const int u = k * THREADS + tid;
+    if (u >= U) break;
+    const int at = s.hist[bucket_of(s.steps[u]) * ROWS + k * WARPS + warp] + s.rank[u];
+    pl.seq[at] = s.seq[u];
+    pl.steps[at] = s.steps[u];
+  }
+  __syncthreads();
+}
+
+// By all threads; ends with a barrier. The thread that finds item t_own among the listed
+// ones writes it to *own.
+__device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScratch& s, Item* own, int t_own) {
+  constexpr int WARPS = THREADS / 32;
+  const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
+  if (p.B <= 32) {
+    if (warp == 0) plan_small(p, pl, own, t_own);
+    __syncthreads();
+    if (pl.jobs <= 32) return;
+    __syncthreads();  // (pl.jobs is written again)
+  }
   // row jobs before each sequence
-  int before = 0;
-  for (int b0 = 0; b0 < p.B; b0 += NT) {
+  int before = 0, total;
+#pragma unroll 1
+  for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int b = b0 + tid;
     int n = 0;
-    if (b < p.B) n = (sequence<L2>(p, b).tiles(p) + 1) / 2;
-    int total;
-    const int at = block_excl_scan<NT>(n, s.tot[(b0 / NT) & 1], total);
+    if (b < p.B) n = (sequence(p, b).tiles(p) + 1) / 2;
+    const int at = block_excl_scan(n, s.tot[(b0 / THREADS) & 1], &total);
     if (b < p.B) pl.first[b] = before + at;
     before += total;
   }
   const int U = before;
-  if (tid == 0) pl.first[p.B] = U;
-  __syncthreads();
-  if (U > MAX_TABLE || U == 0) {
-    if (tid == 0) {
-      pl.jobs = U;
-      pl.n_items = U * p.kv_heads;
-      pl.n_cut = 0;
-      pl.share = pl.cut_above = 0x7fffffff;
-    }
-    __syncthreads();
-    return;
+  if (tid == 0) {
+    pl.first[p.B] = U;
+    pl.jobs = U;
+    pl.n_items = U * p.kv_heads;  // (of a plan without a table)
+    pl.n_cut = 0;
+    pl.share = pl.cut_above = 0x7fffffff;
   }
+  __syncthreads();
+  if (U > MAX_TABLE || U == 0) return;
   // the row jobs' steps
-  int job[PER], c[PER], sum = 0, most = 0, least = 0x7fffffff;
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int u = k * NT + tid;
-    job[k] = c[k] = 0;
-    if (u >= U) continue;
+  int sum = 0, most = 0, least = 0x7fffffff;
+#pragma unroll 1
+  for (int u = tid; u < U; u += THREADS) {
     int lo = 0, hi = p.B;  // the last sequence that begins at or before u
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -277,16 +406,15 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
       else hi = mid;
     }
     const int i = u - pl.first[lo];
-    const Seq q = sequence<L2>(p, lo);
-    job[k] = lo << 16 | i;
-    c[k] = q.steps(p, q.tiles(p), i);
-    pl.seq[u] = job[k];
-    pl.steps[u] = c[k];
-    sum += c[k];
-    most = max(most, c[k]);
-    least = min(least, c[k]);
+    const Seq q = sequence(p, lo);
+    const int c = q.steps(p, q.tiles(p), i);
+    s.seq[u] = lo << 16 | i;
+    s.steps[u] = c;
+    sum += c;
+    most = max(most, c);
+    least = min(least, c);
   }
-  sum = __reduce_add_sync(0xffffffffu, sum);  // (steps are below 2^25)
+  sum = __reduce_add_sync(0xffffffffu, sum);  // (steps are below 2^24)
   most = __reduce_max_sync(0xffffffffu, most);
   least = __reduce_min_sync(0xffffffffu, least);
   if (lane == 0) {
@@ -295,121 +423,65 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     s.least[warp] = least;
   }
   __syncthreads();
-  float T = 0.f;
+  // (lane w of each warp has warp w's: fp32, a share that is off by its rounding is as good)
+  float T = lane < WARPS ? static_cast<float>(s.sum[lane]) : 0.f;
 #pragma unroll
-  for (int i = 0; i < WARPS; ++i) {
-    T += static_cast<float>(s.sum[i]);
-    most = max(most, s.most[i]);
-    least = min(least, s.least[i]);
-  }
-  // (fp32: a share that is off by its rounding is as good)
-  T *= static_cast<float>(p.kv_heads);
+  for (int off = 8; off >= 1; off >>= 1) T += __shfl_xor_sync(0xffffffffu, T, off);
+  T = __shfl_sync(0xffffffffu, T, 0) * static_cast<float>(p.kv_heads);
+  most = __reduce_max_sync(0xffffffffu, lane < WARPS ? s.most[lane] : 0);
+  least = __reduce_min_sync(0xffffffffu, lane < WARPS ? s.least[lane] : 0x7fffffff);
   const int G = p.grid;
   const bool few = U * static_cast<long long>(p.kv_heads) < G;
   int share = most, cut_above = most;
-  if (p.may_cut && few) {
+  if (p.may_cut && few && most > MIN_STEPS) {
     const int J = U * p.kv_heads;
-    const int each = static_cast<int>(__fdividef(static_cast<float>(G), static_cast<float>(J)) + 1e-3f);  // floor(G / J)
-    const int hi = max(MIN_STEPS, min(static_cast<int>(__fdividef(T, static_cast<float>(G - J))) + 1,
-                                      static_cast<int>(__fdividef(static_cast<float>(most), static_cast<float>(each))) + 1));
-    const int lo = max(MIN_STEPS, min(hi, static_cast<int>(__fdividef(T, static_cast<float>(G))) + 1));
-    auto tried = [&](int w) { return lo + (hi - lo) * w / (WARPS - 1); };  // (the last one is hi)
-    const float inv = __fdividef(1.0f, static_cast<float>(tried(warp)));
+    const Shares r = shares_of_few(T, most, J, G);
+    const int lo = r.lo, hi = r.hi;
+    const int tried = lo + (hi - lo) * warp / (WARPS - 1);  // (the last one is hi)
+    const float inv = __fdividef(1.0f, static_cast<float>(tried));
     int n = 0;
-    for (int u = lane; u < U; u += 32) n += static_cast<int>(ceilf(static_cast<float>(pl.steps[u]) * inv - 1e-3f));
+    for (int u = lane; u < U; u += 32) n += static_cast<int>(ceilf(static_cast<float>(s.steps[u]) * inv - 1e-3f));
     n = __reduce_add_sync(0xffffffffu, n) * p.kv_heads;
-    if (lane == 0) s.count[warp] = n;
+    if (lane == 0) s.count[warp] = n <= G ? tried : hi;
     __syncthreads();
-    share = hi;
-#pragma unroll
-    for (int w = WARPS - 1; w >= 0; --w)
-      if (s.count[w] <= G) share = min(share, tried(w));
+    share = __reduce_min_sync(0xffffffffu, lane < WARPS ? s.count[lane] : hi);
     share = min(share, most);
     cut_above = share;
-  } else if (p.may_cut) {
+  } else if (p.may_cut && !few) {
     const float J = static_cast<float>(U) * static_cast<float>(p.kv_heads);
-    share = max(MIN_STEPS, static_cast<int>((T + J * ITEM_STEPS) / static_cast<float>(G)) + 1 - ITEM_STEPS);
-    share = min(share, most);
+    share = min(most, share_of_many(T, J, G));
     cut_above = min(most, share + ITEM_STEPS);
   }
   const bool sorted = !few && most > least;
-  if (sorted) {
-    // by bucket, in order within one: the rank among the warp's lanes, then a scan over
-    // all warps' counts
-    for (int i = tid; i < BUCKETS * ROWS; i += NT) s.hist[i] = 0;
-    __syncthreads();
-    int rank[PER], bucket[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      bucket[k] = BUCKETS;
-      if (k * NT >= U) continue;  // (uniform)
-      const bool in = k * NT + tid < U;
-      if (in) {
-        const bool cut = c[k] > cut_above;
-        const float top = static_cast<float>(cut ? most : cut_above);
-        bucket[k] = (cut ? 15 : 31) - min(15, static_cast<int>(static_cast<float>(c[k] - 1) * 16.0f / top));
-      }
-      const uint32_t same = __match_any_sync(0xffffffffu, bucket[k]);
-      rank[k] = __popc(same & ((1u << lane) - 1u));
-      if (in && rank[k] == 0) s.hist[bucket[k] * ROWS + k * WARPS + warp] = __popc(same);
-    }
-    __syncthreads();
-    constexpr int HPER = (BUCKETS * ROWS + NT - 1) / NT;
-    int h[HPER], mine = 0, total;
-#pragma unroll
-    for (int i = 0; i < HPER; ++i) {
-      const int at = tid * HPER + i;
-      h[i] = at < BUCKETS * ROWS ? s.hist[at] : 0;
-      mine += h[i];
-    }
-    int run = block_excl_scan<NT>(mine, s.tot[2], total);
-#pragma unroll
-    for (int i = 0; i < HPER; ++i) {
-      const int at = tid * HPER + i;
-      if (at < BUCKETS * ROWS) s.hist[at] = run;
-      run += h[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      if (bucket[k] == BUCKETS) continue;
-      const int at = s.hist[bucket[k] * ROWS + k * WARPS + warp] + rank[k];
-      pl.seq[at] = job[k];
-      pl.steps[at] = c[k];
-    }
-    __syncthreads();
-  }
+  if (sorted) plan_sort(pl, s, U, most, cut_above);
   // items before each entry
-  int n[PER], mine = 0, cut = 0, total;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int at = tid * PER + i;
-    n[i] = 0;
-    if (at < U) {
-      const int steps = pl.steps[at];
-      n[i] = steps > cut_above ? ceil_div(steps, share) : 1;
-      if (n[i] > 1) cut = at + 1;
-      mine += n[i] * p.kv_heads;
-    }
+  const int* steps = sorted ? pl.steps : s.steps;
+  int mine = 0, cut = 0;
+  const int at0 = tid * PLAN_PER, at1 = min(U, at0 + PLAN_PER);
+#pragma unroll 1
+  for (int at = at0; at < at1; ++at) {
+    const int c = steps[at], n = c > cut_above ? ceil_div(c, share) : 1;
+    if (n > 1) cut = at + 1;
+    mine += n * p.kv_heads;
   }
   cut = __reduce_max_sync(0xffffffffu, cut);
   if (lane == 0) s.cut[warp] = cut;
-  int run = block_excl_scan<NT>(mine, s.tot[3], total);
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int at = tid * PER + i;
-    if (at >= U) continue;
+  int run = block_excl_scan(mine, s.tot[3], &total);
+#pragma unroll 1
+  for (int at = at0; at < at1; ++at) {
+    const int c = steps[at], n = c > cut_above ? ceil_div(c, share) : 1;
+    const int job = sorted ? pl.seq[at] : s.seq[at];
     pl.items[at] = run;
-    const int more = n[i] * p.kv_heads;
-    if (own && t_own >= run && t_own < run + more)
-      *own = make_item(p, pl.seq[at] >> 16, pl.seq[at] & 0xffff, pl.steps[at], n[i], t_own - run, t_own);
-    run += more;
+    if (!sorted) {
+      pl.seq[at] = job;
+      pl.steps[at] = c;
+    }
+    if (t_own >= run && t_own < run + n * p.kv_heads) 
+      make_item(p, own, sequence(p, job >> 16), job & 0xffff, c, n, t_own - run, t_own);
+    run += n * p.kv_heads;
   }
+  cut = __reduce_max_sync(0xffffffffu, lane < WARPS ? s.cut[lane] : 0);
   if (tid == 0) {
-    cut = 0;
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) cut = max(cut, s.cut[i]);
-    pl.jobs = U;
     pl.n_items = total;
     pl.n_cut = cut;
     pl.share = share;
@@ -418,13 +490,38 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   __syncthreads();
 }
 
+// A cut job for the second kernel.
+struct Joint {
+  int q0, lq, lk, hk, tok0;  // tok0: the job's first token
+  int slot, pieces;          // of the first piece
+  int unused;
+};
+struct Joints {
+  int n;
+  int unused[7];
+  Joint job[SLOTS_PER_CTA * ATTN_MAX_CTAS];
+};
+
+// The cut jobs, listed for the second kernel by one CTA. (Each has at least two pieces.)
+__device__ __noinline__ void list_joints(const VarParams& p, const Plan& pl) {
+  if (threadIdx.x == 0) p.joints->n = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int e = threadIdx.x; e < pl.n_cut * p.kv_heads; e += THREADS) {
+    const int at = e / p.kv_heads, hk = e - at * p.kv_heads, n = pieces_of(pl, pl.steps[at]);
+    if (n == 1) continue;
+    const Seq s = sequence(p, pl.seq[at] >> 16);
+    p.joints->job[atomicAdd(&p.joints->n, 1)] = {s.q0, s.lq, s.lk, hk, 2 * (pl.seq[at] & 0xffff) * p.tpt,
+                                                 pl.items[at] + hk * n, n, 0};
+  }
+}
+
 // ------------------------------------------------------------------- items --
 
-__device__ Item item_at(const VarParams& p, const Plan& pl, int t) {
+__device__ __forceinline__ void item_at(const VarParams& p, const Plan& pl, int t, Item* out) {
   if (t >= pl.n_items) {
-    Item none;
-    none.more = 0;
-    return none;
+    out->more = 0;
+    return;
   }
   if (pl.jobs <= MAX_TABLE) {
     int lo = 0, hi = pl.jobs;
@@ -434,7 +531,8 @@ __device__ Item item_at(const VarParams& p, const Plan& pl, int t) {
       else hi = mid;
     }
     const int steps = pl.steps[lo];
-    return make_item(p, pl.seq[lo] >> 16, pl.seq[lo] & 0xffff, steps, pieces_of(pl, steps), t - pl.items[lo], t);
+    make_item(p, out, sequence(p, pl.seq[lo] >> 16), pl.seq[lo] & 0xffff, steps, pieces_of(pl, steps), t - pl.items[lo], t);
+    return;
   }
   const int v = t / p.kv_heads, u = pl.jobs - 1 - v;
   int lo = 0, hi = p.B;
@@ -444,8 +542,8 @@ __device__ Item item_at(const VarParams& p, const Plan& pl, int t) {
     else hi = mid;
   }
   const int i = u - pl.first[lo];
-  const Seq s = sequence<false>(p, lo);
-  return make_item(p, lo, i, s.steps(p, s.tiles(p), i), 1, t - v * p.kv_heads, t);
+  const Seq s = sequence(p, lo);
+  make_item(p, out, s, i, s.steps(p, s.tiles(p), i), 1, t - v * p.kv_heads, t);
 }
 
 // Item k of CTA x of G.
@@ -515,7 +613,7 @@ struct Cfg {
   static constexpr uint32_t TMEM_COLS = 512;
   static_assert(COL_O + 2 * HD <= TMEM_COLS, "tensor memory");
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
-  static_assert(sizeof(PlanScratch<THREADS>) <= DATA_BYTES, "the plan's scratch");
+  static_assert(sizeof(PlanScratch) <= DATA_BYTES, "the plan's scratch");
 };
 
 template <int HD, bool F16>
@@ -550,6 +648,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   auto sQ = [&](int i) { return smem + C::OFF_Q + i * C::Q_BYTES; };
 
   const int warp = warp_id(), lane = lane_id();
+  if (threadIdx.x == 32) {
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
     for (int i = 0; i < 2; ++i) {
@@ -579,7 +682,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
   }
-  plan_build<THREADS, false>(p, plan, *reinterpret_cast<PlanScratch<THREADS>*>(smem), &shr.ring[0], blockIdx.x);
+  plan_build(p, plan, *reinterpret_cast<PlanScratch*>(smem), &shr.ring[0], blockIdx.x);
+  if (p.may_cut && blockIdx.x == gridDim.x - 1) list_joints(p, plan);  // (the CTA that is idle or has the least)
   const bool idle = static_cast<int>(blockIdx.x) >= plan.n_items;  // (uniform)
   // the plan has left the first item in the ring
   if (threadIdx.x == 0 && plan.jobs <= MAX_TABLE) mbar_arrive(&it_full[0]);
@@ -608,8 +712,6 @@ __global__ void __launch_bounds__(THREADS, 1)
         // stage that is still being read, and the other way round.
         const bool kq = warp == PRODUCER_WARP;
         const CUtensorMap* tm = kq ? &tm_k : &tm_v;
-        tma_prefetch_desc(tm);
-        if (kq) tma_prefetch_desc(&tm_q);
         // per stage (bit st): armed at least once, and the parity of the last arming
         uint32_t armed = 0, par = 0;
         bool q_armed = false;
@@ -852,7 +954,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             !mbar_wait(&it_empty[slot], ((jn - RING) / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 20))
           break;
         if (jn == 0 && plan.jobs <= MAX_TABLE) continue;  // there already
-        shr.ring[slot] = item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x));
+        item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x), &shr.ring[slot]);
         mbar_arrive(&it_full[slot]);
         if (!shr.ring[slot].more) break;
       }
@@ -911,18 +1013,25 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int c16 = 0; c16 < 8; ++c16)
               *reinterpret_cast<uint4*>(vr + j * C::KV_BOX + c16 * 16) = make_uint4(0, 0, 0, 0);
         } else if (t * BKV + row >= part0) {
-#pragma unroll 1
+          auto word = [&](int c16) { return reinterpret_cast<uint4*>(vr + (c16 >> 3) * C::KV_BOX + (c16 & 7) * 16); };
+          uint32_t any = 0;
+#pragma unroll 4
           for (int c16 = 0; c16 < 8 * C::NBOX; ++c16) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(vr + (c16 >> 3) * C::KV_BOX + (c16 & 7) * 16);
-            const uint4 q = *reinterpret_cast<const uint4*>(w);
-            if (special16<F16>(q.x) | special16<F16>(q.y) | special16<F16>(q.z) | special16<F16>(q.w)) {
-              const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
+            const uint4 q = *word(c16);
+            any |= (special16<F16>(q.x) | special16<F16>(q.y)) | (special16<F16>(q.z) | special16<F16>(q.w));
+          }
+          if (any) {
+            shr.special[jn & 1u] = 1;
+#pragma unroll 1
+            for (int c16 = 0; c16 < 8 * C::NBOX; ++c16) {
+              uint4 q = *word(c16);
+              uint32_t* w = &q.x;
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const uint32_t bad = special16<F16>(qs[e]);
-                w[e] = qs[e] & ~((bad & 0x8000u ? 0xFFFFu : 0u) | (bad & 0x80000000u ? 0xFFFF0000u : 0u));
+                const uint32_t bad = special16<F16>(w[e]);
+                w[e] &= ~((bad & 0x8000u ? 0xFFFFu : 0u) | (bad & 0x80000000u ? 0xFFFF0000u : 0u));
               }
-              shr.special[jn & 1u] = 1;
+              *word(c16) = q;
             }
           }
         }
@@ -957,10 +1066,6 @@ __global__ void __launch_bounds__(THREADS, 1)
           break;
         }
         tc_fence_after();
-        // row max and row sum with 8 independent partials combined by a tree; a
-        // tile that every row of the warp sees whole takes paired instructions
-        const bool full_tile = (t + 1) * BKV <= lim_warp;
-        const int valid = lim - t * BKV;
         float sv[BKV];
 #pragma unroll
         for (int c = 0; c < BKV / 32; ++c) tmem_ld32(tS + c * 32, sv + c * 32);
@@ -969,19 +1074,20 @@ __global__ void __launch_bounds__(THREADS, 1)
           tc_fence_before();
           mbar_arrive(&s_free[i]);
         }
+        // the keys that the row does not see, whatever their logits
+        if ((t + 1) * BKV > lim_warp) {
+          const int valid = lim - t * BKV;
+#pragma unroll
+          for (int j = 0; j < BKV; ++j) sv[j] = j < valid ? sv[j] : -INFINITY;
+        }
+        // row max and row sum with 8 independent partials combined by a tree
         float mx8[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) mx8[u] = -INFINITY;
-        if (full_tile) {
 #pragma unroll
-          for (int j = 0; j < BKV; j += 16)
+        for (int j = 0; j < BKV; j += 16)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) mx8[u] = fmax3(mx8[u], sv[j + u], sv[j + 8 + u]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < BKV; ++j)
-            if (j < valid) mx8[j & 7] = fmaxf(mx8[j & 7], sv[j]);
-        }
+          for (int u = 0; u < 8; ++u) mx8[u] = fmax3(mx8[u], sv[j + u], sv[j + 8 + u]);
         const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]),
                                fmaxf(mx8[6], mx8[7]));
         const float m_tile = mx * p.scale_log2;
@@ -996,33 +1102,22 @@ __global__ void __launch_bounds__(THREADS, 1)
         // a row that has seen nothing but -inf: its probabilities are exp(-inf) = 0
         const float shift = m_use == -INFINITY ? 0.f : -m_use;
         float ls8[8];
-        if (full_tile) {
-          const uint64_t sc2 = f2(p.scale_log2, p.scale_log2), nm2 = f2(shift, shift);
-          uint64_t ls4[4];
+        const uint64_t sc2 = f2(p.scale_log2, p.scale_log2), nm2 = f2(shift, shift);
+        uint64_t ls4[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) ls4[u] = 0ull;
+        for (int u = 0; u < 4; ++u) ls4[u] = 0ull;
 #pragma unroll
-          for (int c = 0; c < BKV / 2; ++c) {
-            float a, a1;
-            f2_split(f2_fma(f2(sv[2 * c], sv[2 * c + 1]), sc2, nm2), a, a1);
-            a = ex2(a);
-            a1 = ex2(a1);
-            sv[2 * c] = a;
-            sv[2 * c + 1] = a1;
-            ls4[c & 3] = f2_add(ls4[c & 3], f2(a, a1));
-          }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) f2_split(ls4[u], ls8[2 * u], ls8[2 * u + 1]);
-        } else {
-#pragma unroll
-          for (int u = 0; u < 8; ++u) ls8[u] = 0.f;
-#pragma unroll
-          for (int j = 0; j < BKV; ++j) {
-            const float pj = j < valid ? ex2(fmaf(sv[j], p.scale_log2, shift)) : 0.f;
-            sv[j] = pj;
-            ls8[j & 7] += pj;
-          }
+        for (int c = 0; c < BKV / 2; ++c) {
+          float a, a1;
+          f2_split(f2_fma(f2(sv[2 * c], sv[2 * c + 1]), sc2, nm2), a, a1);
+          a = ex2(a);
+          a1 = ex2(a1);
+          sv[2 * c] = a;
+          sv[2 * c + 1] = a1;
+          ls4[c & 3] = f2_add(ls4[c & 3], f2(a, a1));
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f2_split(ls4[u], ls8[2 * u], ls8[2 * u + 1]);
         const float lsum =
             ((ls8[0] + ls8[1]) + (ls8[2] + ls8[3])) + ((ls8[4] + ls8[5]) + (ls8[6] + ls8[7]));
         if (s >= owned && (t + 1) * BKV > part0 && !take_out(t, ktile)) {
@@ -1231,84 +1326,74 @@ __global__ void __launch_bounds__(THREADS, 1)
 // -------------------------------------------------------------------- join --
 //
 // The pieces of the cut jobs, joined: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p with
-// M the largest m_p. A warp per row, a lane per four (two) columns; the
-// pieces' maxima and sums are read 32 at a time, a lane each. Bound by the
-// L2 reads of the pieces' rows. The plan is made before the wait for the main
-// kernel: the offsets were there before that began.
+// M the largest m_p. As many CTAs per job as there are, a warp per row, a lane
+// per four (two) columns; the pieces' maxima and sums are read 32 at a time, a
+// lane each. Bound by the chain job, maxima, rows for single tokens, by L2 for whole tiles.
 
 constexpr int JOIN_THREADS = 256;
-constexpr int JOIN_ROWS = JOIN_THREADS / 32;  // rows per unit of work
-
-struct JoinShared {
-  Plan plan;
-  PlanScratch<JOIN_THREADS> scratch;
-};
 
 template <int HD, bool F16>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ VarParams p) {
-  extern __shared__ __align__(16) unsigned char join_raw[];
-  JoinShared& sh = *reinterpret_cast<JoinShared*>(join_raw);
-  plan_build<JOIN_THREADS, true>(p, sh.plan, sh.scratch, nullptr, 0);
   pdl_wait();
   pdl_trigger();
   constexpr int COLS = HD / 32;
-  constexpr int UNITS = BQ / JOIN_ROWS;  // of a tile
+  constexpr int WARPS = JOIN_THREADS / 32;
   const int warp = warp_id(), lane = lane_id();
-  const long long units = static_cast<long long>(sh.plan.n_cut) * p.kv_heads * 2 * UNITS;
-  for (long long w = blockIdx.x; w < units; w += gridDim.x) {
-    const int r = static_cast<int>(w % UNITS) * JOIN_ROWS + warp;
-    const int tile = static_cast<int>(w / UNITS) & 1;
-    const int job = static_cast<int>(w / (2 * UNITS));
-    const int e = job / p.kv_heads, hk = job - e * p.kv_heads;
-    const Seq s = sequence<false>(p, sh.plan.seq[e] >> 16);
-    const int j = 2 * (sh.plan.seq[e] & 0xffff) + tile, tok = j * p.tpt + r / p.group;
-    if (r / p.group >= p.tpt || tok >= s.lq) continue;
-    const int n = pieces_of(sh.plan, sh.plan.steps[e]);
-    if (n == 1) continue;
-    const long long slot = static_cast<long long>(sh.plan.items[e]) + hk * n;
-    auto row_of = [&](int q) { return ((slot + q) * 2 + tile) * BQ + r; };
-    float M = -INFINITY;
-    for (int q = lane; q < n; q += 32) M = fmaxf(M, p.part_ml[row_of(q)].x);
+  const int jobs = p.joints->n;
+  if (jobs == 0) return;
+  const int slices = max(1, static_cast<int>(gridDim.x) / jobs);
+  for (int w = blockIdx.x; w < jobs * slices; w += gridDim.x) {
+    const int job = w / slices, slice = w - job * slices;
+    const Joint j = p.joints->job[job];
+    const int rows = min(j.lq - j.tok0, 2 * p.tpt) * p.group;  // tokens with their heads
+    for (int g = slice * WARPS + warp; g < rows; g += slices * WARPS) {
+      const int tok = j.tok0 + g / p.group, h = g % p.group;
+      const int tile = tok >= j.tok0 + p.tpt, r = g - tile * p.tpt * p.group;
+      auto row_of = [&](int q) { return (static_cast<long long>(j.slot + q) * 2 + tile) * BQ + r; };
+      float M = -INFINITY;
+      for (int q = lane; q < j.pieces; q += 32) M = fmaxf(M, p.part_ml[row_of(q)].x);
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-    float o[COLS] = {}, total = 0.f;
-    for (int q0 = 0; q0 < n; q0 += 32) {
-      float a = 0.f;
-      if (q0 + lane < n) {
-        const float2 ml = p.part_ml[row_of(q0 + lane)];
-        // a piece in which the row saw nothing has no rows to read
-        a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.x == M ? 1.f : ex2(ml.x - M);
-        total = fmaf(a, ml.y, total);
-      }
-      const int most = min(32, n - q0);
+      for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+      float o[COLS] = {}, total = 0.f;
+      for (int q0 = 0; q0 < j.pieces; q0 += 32) {
+        float a = 0.f;
+        if (q0 + lane < j.pieces) {
+          const float2 ml = p.part_ml[row_of(q0 + lane)];
+          // a piece in which the row saw nothing has no rows to read
+          a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.x == M ? 1.f : ex2(ml.x - M);
+          total = fmaf(a, ml.y, total);
+        }
+        const int most = min(32, j.pieces - q0);
 #pragma unroll 4
-      for (int q = 0; q < most; ++q) {
-        const float f = __shfl_sync(0xffffffffu, a, q);
-        if (f == 0.f) continue;
-        const float* src = p.part + (row_of(q0 + q) - r) * HD + (lane * COLS / 8 * (8 * BQ) + 8 * r + lane * COLS % 8);
-        if (COLS == 4) {
-          const float4 v = *reinterpret_cast<const float4*>(src);
-          o[0] = fmaf(f, v.x, o[0]);
-          o[1] = fmaf(f, v.y, o[1]);
-          o[COLS - 2] = fmaf(f, v.z, o[COLS - 2]);
-          o[COLS - 1] = fmaf(f, v.w, o[COLS - 1]);
-        } else {
-          const float2 v = *reinterpret_cast<const float2*>(src);
-          o[0] = fmaf(f, v.x, o[0]);
-          o[1] = fmaf(f, v.y, o[1]);
+        for (int q = 0; q < most; ++q) {
+          const float f = __shfl_sync(0xffffffffu, a, q);
+          if (f == 0.f) continue;
+          const float* src = p.part + (row_of(q0 + q) - r) * HD + (lane * COLS / 8 * (8 * BQ) + 8 * r + lane * COLS % 8);
+          if (COLS == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(src);
+            o[0] = fmaf(f, v.x, o[0]);
+            o[1] = fmaf(f, v.y, o[1]);
+            o[COLS - 2] = fmaf(f, v.z, o[COLS - 2]);
+            o[COLS - 1] = fmaf(f, v.w, o[COLS - 1]);
+          } else {
+            const float2 v = *reinterpret_cast<const float2*>(src);
+            o[0] = fmaf(f, v.x, o[0]);
+            o[1] = fmaf(f, v.y, o[1]);
+          }
         }
       }
-    }
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
-    const float inv = s.seen(p, tok) == 0 ? 0.f : 1.0f / total;
-    uint16_t* dst = static_cast<uint16_t*>(p.out) + static_cast<long long>(s.q0 + tok) * p.out_row +
-                    static_cast<long long>(hk * p.group + r % p.group) * p.out_head + COLS * lane;
-    if (COLS == 4)
-      *reinterpret_cast<uint2*>(dst) =
-          make_uint2(pack16<F16>(o[0] * inv, o[1] * inv), pack16<F16>(o[COLS - 2] * inv, o[COLS - 1] * inv));
-    else
-      *reinterpret_cast<uint32_t*>(dst) = pack16<F16>(o[0] * inv, o[1] * inv);
+      for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+      const Seq s = {j.q0, j.lq, 0, j.lk};
+      const float inv = s.seen(p, tok) == 0 ? 0.f : 1.0f / total;
+      uint16_t* dst = static_cast<uint16_t*>(p.out) + static_cast<long long>(j.q0 + tok) * p.out_row +
+                      static_cast<long long>(j.hk * p.group + h) * p.out_head + COLS * lane;
+      if (COLS == 4)
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(pack16<F16>(o[0] * inv, o[1] * inv), pack16<F16>(o[COLS - 2] * inv, o[COLS - 1] * inv));
+      else
+        *reinterpret_cast<uint32_t*>(dst) = pack16<F16>(o[0] * inv, o[1] * inv);
+    }
   }
 }
 
@@ -1346,9 +1431,7 @@ cudaError_t launch_hd(const hilo_attn_shape& s, const VarParams& p, const void* 
   *launches = 1;
   if (!p.may_cut) return cudaSuccess;
   auto* join = attn_join_kernel<HD, F16>;
-  e = cudaFuncSetAttribute(join, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(JoinShared));
-  if (e != cudaSuccess) return e;
-  e = launch_pdl(join, dim3(p.grid), dim3(JOIN_THREADS), sizeof(JoinShared), st, p);
+  e = launch_pdl(join, dim3(p.grid), dim3(JOIN_THREADS), 0, st, p);
   if (e == cudaSuccess) *launches = 2;
   return e;
 }
@@ -1361,7 +1444,9 @@ constexpr size_t SLOTS = static_cast<size_t>(SLOTS_PER_CTA) * ATTN_MAX_CTAS;
 
 size_t attn_var_workspace_bytes(const hilo_attn_shape& s) {
   // (32 bytes to bring the rows onto the boundary that they are stored from)
-  return may_cut(s) ? SLOTS * 2 * BQ * (static_cast<size_t>(s.head_dim) * sizeof(float) + sizeof(float2)) + 32 : 32;
+  return may_cut(s) ? SLOTS * 2 * BQ * (static_cast<size_t>(s.head_dim) * sizeof(float) + sizeof(float2)) +
+                          sizeof(Joints) + 32
+                    : 32;
 }
 
 cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, const int32_t* cu_k, const void* q,
@@ -1375,6 +1460,7 @@ cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, 
   p.out = out;
   p.part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ws) + 31) & ~static_cast<uintptr_t>(31));
   p.part_ml = reinterpret_cast<float2*>(p.part + SLOTS * 2 * BQ * s.head_dim);
+  p.joints = reinterpret_cast<Joints*>(p.part_ml + SLOTS * 2 * BQ);
   p.v_row = s.v_row;
   p.v_head = s.v_head;
   p.out_row = s.out_row;
