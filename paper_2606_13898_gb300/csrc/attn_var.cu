@@ -82,6 +82,7 @@ struct VarParams {
   int causal, rows_q, rows_k;
   int grid;  // CTAs of the main kernel
   int may_cut;
+  int out_wide;  // out's rows and heads begin on 32 bytes
   float scale_log2;  // log2(e) * scale
 };
 
@@ -578,6 +579,12 @@ __device__ __forceinline__ void st_f32x8(float* p, const float* v) {
                : "memory");
 }
 
+__device__ __forceinline__ void st_b32x8(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p)
+               : "memory");
+}
+
 // The first key tile that some row of the item does not see whole.
 __device__ __forceinline__ int part_tile(const VarParams& p, const Item& it) {
   return (p.causal ? min(it.lk, max(0, it.j0 * p.tpt + it.lk - it.lq + 1)) : it.lk) / BKV;
@@ -634,7 +641,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* p_full = bars + 11;   // [2] per softmax warpgroup
   uint64_t* o_done = bars + 13;   // [2] per softmax warpgroup
   uint64_t* drain = bars + 15;
-  uint64_t* epi_done = bars + 16;  // an item's output rows are out: Q free
+  uint64_t* q_empty = bars + 16;  // every S product of an item done: Q may be reloaded
   uint64_t* it_full = bars + 18;  // [RING]
   uint64_t* it_empty = bars + 22; // [RING]
   uint64_t* s_free = bars + 26;   // [2] OWN_P: S_i is in registers, the next one may be formed
@@ -666,7 +673,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&s_free[i], 128);
     }
     mbar_init(drain, 1);
-    mbar_init(epi_done, 1);
+    mbar_init(q_empty, 1);
     for (int i = 0; i < RING; ++i) {
       mbar_init(&it_full[i], 1);
       mbar_init(&it_empty[i], 3 + 8);  // two copy warps, the MMA warp, the softmax warps
@@ -731,8 +738,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           const int hk = it.hk, k0 = it.k0, t0 = it.t0, n = it.t1 - it.t0;
           if (kq) {
             const int pair = it.pair, row0 = it.q0 + it.j0 * p.tpt, h0 = hk * p.group;
-            // Q once the previous item's output rows (staged in its place) are out
-            if (jn > 0 && !mbar_wait(epi_done, (jn - 1) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 17)) {
+            // Q once the previous item's S products are done with it
+            if (jn > 0 && !mbar_wait(q_empty, (jn - 1) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 17)) {
               ok = false;
               break;
             }
@@ -888,6 +895,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         // for two products in a row (images of 1111 to 4096 tokens, 16 heads of 64:
         // 132 us with P over S).
         const int nmax = n0 > n1 ? n0 : n1;
+        if (nmax == 1) commit(q_empty);
         for (int s = 0; s < nmax && ok; ++s) {
           if (s < n0) {
             if (C::OWN_P && !next_s(0, 0, s, n0, sc0, false)) {
@@ -929,6 +937,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               break;
             }
           }
+          if (s + 2 == nmax) commit(q_empty);  // the item's last S products are issued
         }
         if (!ok) break;
         sc0 += static_cast<uint32_t>(n0);
@@ -1012,6 +1021,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int c16 = 0; c16 < 8; ++c16)
               *reinterpret_cast<uint4*>(vr + j * C::KV_BOX + c16 * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();  // before the tensor core reads the tile
         } else if (t * BKV + row >= part0) {
           auto word = [&](int c16) { return reinterpret_cast<uint4*>(vr + (c16 >> 3) * C::KV_BOX + (c16 & 7) * 16); };
           uint32_t any = 0;
@@ -1033,9 +1043,9 @@ __global__ void __launch_bounds__(THREADS, 1)
               }
               *word(c16) = q;
             }
+            fence_proxy_async_smem();
           }
         }
-        fence_proxy_async_smem();  // before the tensor core reads the tile
         return true;
       };
       // With P_i over S_i, S_i complete means every earlier MMA is too (PV_i of the
@@ -1061,6 +1071,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int s = 0; s < n && ok; ++s) {
         const int t = item_tile(pair, t0, i, s);
         const uint32_t ktile = kt + static_cast<uint32_t>(t - t0);
+        // (while the tensor core forms S)
+        if (s >= owned && (t + 1) * BKV > part0 && !take_out(t, ktile)) {
+          ok = false;
+          break;
+        }
         if (!mbar_wait_warp(&s_full[i], (sc + s) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 10)) {
           ok = false;
           break;
@@ -1120,10 +1135,6 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int u = 0; u < 4; ++u) f2_split(ls4[u], ls8[2 * u], ls8[2 * u + 1]);
         const float lsum =
             ((ls8[0] + ls8[1]) + (ls8[2] + ls8[3])) + ((ls8[4] + ls8[5]) + (ls8[6] + ls8[7]));
-        if (s >= owned && (t + 1) * BKV > part0 && !take_out(t, ktile)) {
-          ok = false;
-          break;
-        }
         // (OWN_P: the previous step's PV may still read P_i and write O_i)
         if (C::OWN_P && s > 0) {
           if (!mbar_wait_warp(&o_done[i], o_phase(i ? oc1 : oc0, s), abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 12)) {
@@ -1224,26 +1235,25 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
           } else {
             const float inv = lim == 0 ? 0.f : 1.0f / l;
-            // normalised rows to 16 bits, staged through shared memory so that
-            // the global stores leave as whole lines. Each warp owns a slice of its
-            // tile's Q: every S product of the tile, the last reader of Q,
-            // completed before O did, and the next item's Q is loaded only after
-            // this item's epi_done. (Not of the K stages: the other tile of a
-            // pair may have more steps.) The 16-byte units of a row are XOR-swizzled
-            // by the row, so neither the writes (one row per lane) nor the
-            // reads (consecutive units of a row) collide in the banks.
-            constexpr int UNITS = HD / 8;    // 16-byte units per row
-            constexpr int RPI = 32 / UNITS;  // rows per store instruction
-            uint4* stage = reinterpret_cast<uint4*>(smem + C::OFF_Q) + warp * 32 * UNITS;
-            auto stage_chunk = [&](int c, const float* o) {
+            // normalised rows to 16 bits, each lane its own row, 32 bytes (whole sectors)
+            // at a time. (Staged through shared memory for whole lines the rows left no
+            // sooner, and Q, in whose place they were staged, could not be
+            // loaded for the next item meanwhile: 2000 to 3000 cycles an item.)
+            const bool token = row_tok < p.tpt && tok0 + row_tok < it.lq;
+            uint16_t* dst = static_cast<uint16_t*>(p.out) + static_cast<long long>(it.q0 + tok0 + row_tok) * p.out_row +
+                            static_cast<long long>(it.hk * p.group + (row - row_tok * p.group)) * p.out_head;
+            auto store_chunk = [&](int c, const float* o) {
+              uint32_t w[16];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                uint4 v;
-                v.x = pack16<F16>(o[8 * j] * inv, o[8 * j + 1] * inv);
-                v.y = pack16<F16>(o[8 * j + 2] * inv, o[8 * j + 3] * inv);
-                v.z = pack16<F16>(o[8 * j + 4] * inv, o[8 * j + 5] * inv);
-                v.w = pack16<F16>(o[8 * j + 6] * inv, o[8 * j + 7] * inv);
-                stage[lane * UNITS + ((4 * c + j) ^ (lane & (UNITS - 1)))] = v;
+              for (int j = 0; j < 16; ++j) w[j] = pack16<F16>(o[2 * j] * inv, o[2 * j + 1] * inv);
+              if (!token) return;
+              if (p.out_wide) {
+                st_b32x8(dst + 32 * c, w);
+                st_b32x8(dst + 32 * c + 16, w + 8);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  reinterpret_cast<uint4*>(dst + 32 * c)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
               }
             };
             if (!merge && !special) {
@@ -1255,7 +1265,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
               for (int c = 0; c < HD / 32; ++c) tmem_ld_wait_regs(o + c * 32);
 #pragma unroll
-              for (int c = 0; c < HD / 32; ++c) stage_chunk(c, o + c * 32);
+              for (int c = 0; c < HD / 32; ++c) store_chunk(c, o + c * 32);
             } else {
 #pragma unroll 1
               for (int c = 0; c < HD / 32; ++c) {
@@ -1272,41 +1282,20 @@ __global__ void __launch_bounds__(THREADS, 1)
                   tmem_ld_wait_regs(o);
                 }
                 if (special) give_back(c, o);
-                stage_chunk(c, o);
-              }
-            }
-            __syncwarp();
-            // rows of the tile that are a token's: row r is head r % group of token r / group
-            const int rows = min(p.tpt, it.lq - tok0) * p.group;
-            const uint32_t inv_g = (65536u + static_cast<uint32_t>(p.group) - 1u) / static_cast<uint32_t>(p.group);
-            const long long out0 = static_cast<long long>(it.q0 + tok0) * p.out_row +
-                                   static_cast<long long>(it.hk) * p.group * p.out_head;
-            const int u = lane % UNITS;
-#pragma unroll 4
-            for (int k = 0; k < 32 / RPI; ++k) {
-              const int rr = k * RPI + lane / UNITS;  // row within the warp's 32
-              const int r = (warp & 3) * 32 + rr;     // row within the tile
-              if (r < rows) {
-                const int tok = static_cast<int>((static_cast<uint32_t>(r) * inv_g) >> 16), h = r - tok * p.group;
-                reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + out0 + tok * p.out_row + h * p.out_head)[u] =
-                    stage[rr * UNITS + (u ^ (rr & (UNITS - 1)))];
+                store_chunk(c, o);
               }
             }
           }
         }
       }
-      // end of the item: the staging reads are done (generic proxy) before
-      // the producer's next Q copies (async proxy) overwrite them;
-      // in a single warpgroup 1's accumulator has been read before its
-      // next PV may overwrite it
+      // end of the item: in a single, warpgroup 1's accumulator has been read before
+      // its next PV may overwrite it
       const int n0_all = it.n0, len = it.t1 - t0;
       if (threadIdx.x == 0) shr.special[(jn + 1) & 1u] = 0;  // (last read before the previous item's end)
-      fence_proxy_async_smem();
       tc_fence_before();
       ok = ok && it_wait(jn + 1, 21);
       go = !bar_red_or(2, 256, !ok);
       if (!go) break;
-      if (threadIdx.x == 0) mbar_arrive(epi_done);
       if (lane == 0) mbar_arrive(&it_empty[jn & (RING - 1)]);
       sc += static_cast<uint32_t>(n);
       oc0 += C::OWN_P ? static_cast<uint32_t>(n0_all) : n0_all > 0 ? 1u : 0u;
@@ -1480,6 +1469,7 @@ cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, 
   // number is known on the device only
   p.grid = num_sms < 1 ? 1 : num_sms < ATTN_MAX_CTAS ? num_sms : ATTN_MAX_CTAS;
   p.may_cut = may_cut(s);
+  p.out_wide = reinterpret_cast<uintptr_t>(out) % 32 == 0 && s.out_row % 16 == 0 && s.out_head % 16 == 0;
   const double scale = s.scale > 0.f ? s.scale : 1.0 / sqrt(static_cast<double>(s.head_dim));
   p.scale_log2 = static_cast<float>(1.4426950408889634 * scale);
   const bool f16 = s.dtype == HILO_F16;
