@@ -1079,8 +1079,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int s = 0; s < n && ok; ++s) {
         const int t = item_tile(pair, t0, i, s);
         const uint32_t ktile = kt + static_cast<uint32_t>(t - t0);
-        // (while the tensor core forms S)
-        if (s >= owned && (t + 1) * BKV > part0 && !take_out(t, ktile)) {
+        // The wait for a value tile tells its arrival from the next but one only: the one
+        // before it in its stage has to be there already. In a pair that is the tile
+        // of two steps ago, whose PV is done: while the tensor core forms S. In a single
+        // it is the step before's: once that PV is done.
+        const bool take = s >= owned && (t + 1) * BKV > part0, early = pair || s == 0;
+        if (take && early && !take_out(t, ktile)) {
           ok = false;
           break;
         }
@@ -1150,6 +1154,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             break;
           }
           tc_fence_after();
+        }
+        // (P over S: S_i(s) is formed after the PV of the step before)
+        if (take && !early && !take_out(t, ktile)) {
+          ok = false;
+          break;
         }
         rescale_o(rescale, m_use);
         m = m_use;

@@ -197,6 +197,26 @@ def test_infinities_and_nans_of_unseen_keys(H, dtype, lq, lk, heads):
         assert torch.equal(row.nan_to_num(7e4, 8e4, 9e4), want.nan_to_num(7e4, 8e4, 9e4)), (i, back)
 
 
+@pytest.mark.parametrize("hd,heads,kv", [(128, 24, 4), (64, 32, 8)])
+def test_rows_behind_a_long_cache(H, hd, heads, kv):
+    """The last tile of a cache that keeps every SM loading: its rows behind the sequence are taken out after they
+    have arrived, also where values come long after keys."""
+    lk = [777, 20000, 64, 9001, 12345, 30001, 16000, 32700]
+    q, k, v, cu_q, cu_k = make([1] * 8, lk, heads, kv, hd, "bf16", spare=200, seed=hd)
+    k[sum(lk):], v[sum(lk):] = math.nan, math.nan
+    ref = reference(q, k, v, cu_q, cu_k, 1)
+    for _ in range(10):
+        check(call(H, q, k, v, cu_q, cu_k, 1), ref, "bf16")
+    # a last sequence of a single row of tiles too, at every remainder
+    for n in (31997, 32001, 32100):
+        cu = cu_k.clone()
+        cu[-1] = cu[-2] + n
+        k[int(cu[-1]):], v[int(cu[-1]):] = math.nan, math.nan
+        got = call(H, q, k, v, cu_q, cu, 1)
+        check(got[7:8], tuple(x[7:8] if hasattr(x, "shape") else x for x in reference(q[:8], k, v, cu_q, cu, 1)), "bf16")
+        k.nan_to_num_(0.5), v.nan_to_num_(0.5)
+
+
 def test_infinite_logits(H):
     """-inf logits weigh nothing, also where a query's first tile holds nothing else; all -inf gives NaN, as 0/0."""
     q, k, v, cu_q, cu_k = make([3, 40], [400, 300], 2, 1, 64, "bf16", seed=8)
