@@ -150,11 +150,13 @@ bool good_strides(int64_t row, int64_t head, int step) {
   return row > 0 && head > 0 && row % step == 0 && head % step == 0 && row < most && head < most;
 }
 
-// Whether no two (row, head) of the tensor share elements: heads within rows, or rows within heads.
+// Whether no two (row, head) of the tensor share elements: heads within rows, or rows within
+// heads. (Positive strides; divided, as the products may pass 63 bits.)
 bool disjoint(int64_t rows, int64_t heads, int64_t dim, int64_t row, int64_t head) {
-  if (heads == 1) return rows == 1 || row >= dim;
-  if (rows == 1) return head >= dim;
-  return (head >= dim && row >= (heads - 1) * head + dim) || (row >= dim && head >= (rows - 1) * row + dim);
+  if (heads == 1) return rows <= 1 || row >= dim;
+  if (rows <= 1) return head >= dim;
+  return (head >= dim && row >= dim && (row - dim) / head >= heads - 1) ||
+         (row >= dim && head >= dim && (head - dim) / row >= rows - 1);
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }

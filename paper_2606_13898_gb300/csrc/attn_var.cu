@@ -558,6 +558,23 @@ __device__ __forceinline__ void item_at(const VarParams& p, const Plan& pl, int 
 // Item k of CTA x of G.
 __device__ __forceinline__ int item_index(int k, int x, int G) { return k & 1 ? (k + 1) * G - 1 - x : k * G + x; }
 
+// mbar_wait for what may take as long as whole items (up to 2^23 steps of 2 us each, of
+// a sequence of 2^30 keys): the other roles' waits are of single steps, and raise `abort`
+// within a second where something is wrong.
+__device__ __forceinline__ bool mbar_wait_items(uint64_t* bar, uint32_t parity, volatile int* abort, int* err, int code) {
+  const uint32_t a = smem_u32(bar);
+  const uint64_t g0 = globaltimer_ns();
+  while (!mbar_try_wait(a, parity)) {
+    if (*abort) return false;
+    if (globaltimer_ns() - g0 > 100 * HILO_WAIT_LIMIT_NS) {
+      atomicExch(err, code);
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
 // -------------------------------------------------------------- 16-bit types --
 
 template <bool F16>
@@ -747,7 +764,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (kq) {
             const int pair = it.pair, row0 = it.q0 + it.j0 * p.tpt, h0 = hk * p.group;
             // Q once the previous item's S products are done with it
-            if (jn > 0 && !mbar_wait(q_empty, (jn - 1) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 17)) {
+            if (jn > 0 && !mbar_wait_items(q_empty, (jn - 1) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 17)) {
               ok = false;
               break;
             }
@@ -968,7 +985,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (uint32_t jn = 0;; ++jn) {
         const int slot = jn & (RING - 1);
         if (jn >= RING &&
-            !mbar_wait(&it_empty[slot], ((jn - RING) / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 20))
+            !mbar_wait_items(&it_empty[slot], ((jn - RING) / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 20))
           break;
         if (jn == 0 && plan.jobs <= MAX_TABLE) continue;  // there already
         item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x), &shr.ring[slot]);

@@ -7,6 +7,9 @@ by as much; its tolerance is that of the other block tests (max-abs 2e-2,
 rel-L2 1e-2).
 """
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -262,3 +265,45 @@ def test_prompt_layer(H):
     assert rel <= 1e-2, rel
     h_r = norm(u_r, 2) * gain[1].double()
     assert float((h2.double() - h_r).norm() / h_r.norm()) <= 1e-2 + 2.0 ** -8
+
+
+CAPTURED = r"""
+import torch
+from paper_2606_13898_gb300 import hilo as H
+n, d = 300, 512
+u = torch.randn(n, d, device="cuda")
+h = torch.empty(n, d, dtype=torch.bfloat16, device="cuda")
+out = torch.empty_like(h)
+pos = torch.arange(n, device="cuda").float()[:, None].contiguous()
+cu = torch.tensor([0, 100, n], dtype=torch.int32, device="cuda")
+ns = H.NormShape(B=2, T=0, cap=n, d=d, norm=H.HILO_NORM_RMS)
+rs = H.RopeShape(rows=n, heads=8, head_dim=64, dtype=H.HILO_BF16, axis_dims=(64,))
+sh = H.AttnShape(B=2, heads=8, kv_heads=8, head_dim=64, rows_q=n, rows_k=n)
+nb = H.hilo_attention_workspace_bytes(sh)
+ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+torch.cuda.synchronize()
+
+
+def layer():
+    H.hilo_gate_norm(ns, None, H.NormVectors(), cu, None, u, None, None, h, None)
+    H.hilo_rope(rs, h, pos, None, h)
+    H.hilo_attention(sh, cu, cu, h, h, h, out, ws, nb)
+
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):  # the process's first calls of these kernels
+    layer()
+out.zero_()
+graph.replay()
+torch.cuda.synchronize()
+got = out.clone()
+layer()
+H.hilo_sync_status()
+assert torch.equal(got, out) and bool(out.isfinite().all()) and float(out.float().abs().max()) > 0.1
+"""
+
+
+def test_first_calls_in_a_capture(H):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", CAPTURED], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr

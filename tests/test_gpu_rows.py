@@ -8,6 +8,9 @@ Tolerances (u = half a step of the output's dtype, 2^-24 of fp32):
              of the sum of its terms' magnitudes and a norm of n values x by 2^-18 (|xhat| + r mean|x|)
 """
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -18,6 +21,7 @@ from .gpu_helpers import lib_ready
 pytestmark = pytest.mark.gpu
 TYPES = {0: torch.bfloat16, 1: torch.float32, 2: torch.float16}
 BF16, F32, F16, E4M3 = 0, 1, 2, 3
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -79,6 +83,39 @@ def test_row_positions(H, B, Hh, W, T, levels, lf, regions):
     pos.fill_(math.nan)
     H.hilo_row_positions(sh, sp, org, pos, 3)
     assert np.array_equal(pos.cpu().numpy()[:B * T + 3], got[:B * T + 3]) and bool(pos[B * T + 3:].isnan().all())
+
+
+CHECKED = r"""
+import torch
+from paper_2606_13898_gb300 import hilo as H
+assert H.library_path().endswith("_build_checks/libhilo.so"), H.library_path()
+sh = H.Shape(B=1, H=8, W=8, d=128, T=2)
+sp = H.SplitBuffers.alloc(sh)
+sp.labels.zero_()
+sp.row_src.copy_(torch.arange(64))
+sp.counts.copy_(torch.tensor([64, 0, 0]))
+sp.cu_img.copy_(torch.tensor([0, 64]))
+sp.row_src[9] = 64  # one past the grid: its labels would be another image's
+pos = torch.full((66, 3), -7.0, device="cuda")
+H.hilo_row_positions(sh, sp, H.RowPositions(t_img=1.0), pos, 64)
+try:
+    H.hilo_sync_status()
+    raise SystemExit("no check fired")
+except H.HiloError as e:
+    assert e.status == H.HILO_ERR_CHECK and "check 7" in str(e), str(e)
+assert bool((pos[11] == -7).all()) and bool((pos[10] == torch.tensor([1.0, 1.0, 0.0], device="cuda")).all())
+"""
+
+
+def test_positions_on_the_checks_build():
+    """A row source outside the grid is caught before anything is addressed with it, and its row skipped."""
+    from paper_2606_13898_gb300 import build
+    env = dict(os.environ, HILO_LIBRARY=build.build(variant="checks"))
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "-p", "no:cacheprovider", "-k", "row_positions",
+                        "tests/test_gpu_rows.py"], cwd=ROOT, env=env, capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0 and " passed" in r.stdout, r.stdout[-3000:] + r.stderr[-2000:]
+    r = subprocess.run([sys.executable, "-c", CHECKED], cwd=ROOT, env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
 
 
 # ------------------------------------------------------------------- rope --
