@@ -132,13 +132,19 @@ __device__ __forceinline__ int image_of(const int32_t* cu, int B, int r) {
 // it is reduced. (More elements per thread, as a warpgroup per row, take more
 // registers and leave fewer threads on the SM: 2389 rows of 3072 30.9 us, 8586 rows
 // of 1152 with both norms 65.6. Vectors read again for every row: 25.9 and 43.7,
-// half of the issue slots and a third of the loads' pipe spent on them. So: 19.8 =
-// 4.5 TB/s, and 18.4.)
+// half of the issue slots and a third of the loads' pipe spent on them. So: 19.3 =
+// 4.6 TB/s, and 17.5. Rows copied two to four ahead into shared memory or registers, sixteen
+// elements per thread, or rows dealt one by one to the CTAs: 20 to 28 and 18 to 30.)
 
 constexpr int GN_WARP_ROWS = 8;  // rows of up to 256 elements: warps per CTA
-constexpr int GN_THREADS = 1024;  // resident per SM (64 registers each)
 
 enum { Y_NONE = 0, Y_BF16 = 1, Y_F32 = 2 };
+
+// Registers per thread, and with them the threads on an SM: three rows of 3072 at 56, two
+// at 64 (with gate and norm, 15000 rows 111 us, 120 at 64); fp32 branch rows spill at 56
+// (6000 rows of 2048: 35.4 us, 31.8 at 64), rows of a warp gain nothing (30000 of 256:
+// 19.7 and 19.1).
+__host__ __device__ constexpr int gn_regs(bool warp, int y) { return warp || y == Y_F32 ? 64 : 56; }
 
 // Eight elements of a vector, `none` where there is no vector.
 __device__ __forceinline__ void vector8(const void* v, bool f32, long long i, float none, float* out) {
@@ -171,7 +177,7 @@ __device__ __forceinline__ void row_norm(float (&v)[8], int kind, float eps, flo
 }
 
 template <bool WARP, bool UF32, int YM>
-__global__ void __launch_bounds__(WARP ? 32 * GN_WARP_ROWS : 512, WARP ? 4 : 2)
+__global__ void __maxnreg__((gn_regs(WARP, YM)))
     gate_norm_kernel(const __grid_constant__ NormArgs a) {
   pdl_wait();
   pdl_trigger();
@@ -475,7 +481,7 @@ template <bool WARP, bool UF32, int YM>
 cudaError_t gate_norm_of(const NormArgs& a, int num_sms, cudaStream_t st) {
   const long long R = static_cast<long long>(a.s.B) * a.s.T + a.s.cap;
   const int threads = WARP ? 32 * GN_WARP_ROWS : (a.s.d / 8 + 31) / 32 * 32;
-  const dim3 grid(grid_for(R, WARP ? GN_WARP_ROWS : 1, num_sms, GN_THREADS / threads));
+  const dim3 grid(grid_for(R, WARP ? GN_WARP_ROWS : 1, num_sms, 65536 / gn_regs(WARP, YM) / threads));
   return launch_pdl(gate_norm_kernel<WARP, UF32, YM>, grid, dim3(threads), 0, st, a);
 }
 
