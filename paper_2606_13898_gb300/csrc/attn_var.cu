@@ -104,9 +104,15 @@ struct Seq {
   __device__ __forceinline__ int key_tiles(const VarParams& p, int j) const {
     return max(1, (seen(p, min(lq, (j + 1) * p.tpt) - 1) + BKV - 1) / BKV);
   }
-  // Steps of row job i of a sequence of nt tiles: a pair's key tiles, half of a single's.
-  __device__ __forceinline__ int steps(const VarParams& p, int nt, int i) const {
-    return 2 * i + 1 < nt ? key_tiles(p, 2 * i + 1) : (key_tiles(p, nt - 1) + 1) / 2;
+  // Row jobs of up to `width` tiles, and the steps of job i of a sequence of nt tiles: a
+  // pair's key tiles, half of a single's.
+  __device__ __forceinline__ int row_jobs(const VarParams& p, int width) const {
+    const int nt = tiles(p);
+    return width == 1 ? nt : (nt + 1) / 2;
+  }
+  __device__ __forceinline__ int steps(const VarParams& p, int width, int nt, int i) const {
+    const int last = width * (i + 1) - 1;
+    return width == 2 && last < nt ? key_tiles(p, last) : (key_tiles(p, min(last, nt - 1)) + 1) / 2;
   }
 };
 
@@ -135,11 +141,19 @@ __device__ __forceinline__ Seq sequence(const VarParams& p, int b) {
 //           longer by more than ITEM_STEPS are cut. Listed longest first, to a
 //           sixteenth of the longest, the cut ones ahead of the others: fewer than
 //           2G pieces, as a job of c > share + 1 steps has at most (c - 1) / share + 1.
-// Pieces of less than MIN_STEPS would cost more in their epilogues than they save.
+// Pieces of fewer steps than min_steps would cost more in their epilogues and in the second
+// kernel than they save.
+//
+// Singles or pairs: both take two tiles' products per step, a pair reads the keys once
+// for both. Every tile is a job of its own where that makes shorter jobs for idle CTAs or
+// evens out a causal triangle (job_width): one prompt of 985 tokens, 8 heads, 23.4 us
+// in pairs and 15.3 in singles; prompts of up to 2235 tokens, 6 heads on one, 49.3 and 25.7.
 
 constexpr int MAX_SEQ = ATTN_MAX_SEQUENCES;
 constexpr int MAX_TABLE = 1024;
-constexpr int MIN_STEPS = 4;
+constexpr int MIN_STEPS = 4;       // of a piece
+constexpr int MIN_STEPS_ROWS = 2;  // of jobs of up to FEW_ROWS rows, which are joined at once
+constexpr int FEW_ROWS = 32;
 constexpr int ITEM_STEPS = 2;
 constexpr int SLOTS_PER_CTA = 2;
 constexpr int BUCKETS = 32;  // 16 of cut jobs, 16 of whole ones
@@ -149,8 +163,10 @@ struct Plan {
   int seq[MAX_TABLE];      // entry: sequence << 16 | row job of it
   int steps[MAX_TABLE];
   int items[MAX_TABLE];    // items before the entry
+  int width;  // tiles of a job at most
   int jobs, n_items, n_cut, share, cut_above;  // row jobs, items, entries that may be cut (the first ones)
 };
+static_assert(2 * MIN_STEPS_ROWS >= MIN_STEPS, "may_cut goes by the key tiles of a pair");
 static_assert(MAX_SEQ <= 1 << 15 && MAX_TABLE <= 1 << 16, "an entry's sequence and row job share a word");
 
 // Pieces of a job of so many steps, at most `share` each but for a rounding: in fp32, a
@@ -181,8 +197,8 @@ struct Item {
 __device__ __forceinline__ int item_tile(int pair, int t0, int i, int s) { return pair ? t0 + s : t0 + 2 * s + i; }
 
 // Item t: of the items of row job i of a sequence (c steps, `pieces` pieces), number r.
-__device__ __forceinline__ void make_item(const VarParams& p, Item* out, const Seq& s, int i, int c, int pieces, int r,
-                                          int t) {
+__device__ __forceinline__ void make_item(const VarParams& p, Item* out, const Seq& s, int width, int i, int c, int pieces,
+                                          int r, int t) {
   Item it;
   it.hk = pieces == 1 ? r : static_cast<int>(static_cast<uint32_t>(r) / static_cast<uint32_t>(pieces));
   const int piece = r - it.hk * pieces;
@@ -191,8 +207,8 @@ __device__ __forceinline__ void make_item(const VarParams& p, Item* out, const S
   it.lq = s.lq;
   it.k0 = s.k0;
   it.lk = s.lk;
-  it.j0 = 2 * i;
-  it.pair = 2 * i + 1 < s.tiles(p);
+  it.j0 = width * i;
+  it.pair = width == 2 && 2 * i + 1 < s.tiles(p);
   int u0 = 0, u1 = c;
   if (pieces > 1) {  // (a piece begins where the one before it ends: the same product)
     const float each = __fdividef(static_cast<float>(c), static_cast<float>(pieces));
@@ -236,14 +252,28 @@ __device__ __noinline__ int block_excl_scan(int v, int* tot, int* total) {
 struct Shares {
   int lo, hi;
 };
-__device__ __forceinline__ Shares shares_of_few(float T, int most, int J, int G) {
+__device__ __forceinline__ Shares shares_of_few(float T, int most, int J, int G, int least_piece) {
   const int each = static_cast<int>(__fdividef(static_cast<float>(G), static_cast<float>(J)) + 1e-3f);  // floor(G / J)
-  const int hi = max(MIN_STEPS, min(static_cast<int>(__fdividef(T, static_cast<float>(G - J))) + 1,
+  const int hi = max(least_piece, min(static_cast<int>(__fdividef(T, static_cast<float>(G - J))) + 1,
                                     static_cast<int>(__fdividef(static_cast<float>(most), static_cast<float>(each))) + 1));
-  return {max(MIN_STEPS, min(hi, static_cast<int>(__fdividef(T, static_cast<float>(G))) + 1)), hi};
+  return {max(least_piece, min(hi, static_cast<int>(__fdividef(T, static_cast<float>(G))) + 1)), hi};
 }
-__device__ __forceinline__ int share_of_many(float T, float J, int G) {
-  return max(MIN_STEPS, static_cast<int>(__fdividef(T + J * ITEM_STEPS, static_cast<float>(G))) + 1 - ITEM_STEPS);
+__device__ __forceinline__ int share_of_many(float T, float J, int G, int least_piece) {
+  return max(least_piece, static_cast<int>(__fdividef(T + J * ITEM_STEPS, static_cast<float>(G))) + 1 - ITEM_STEPS);
+}
+
+// Tiles per job at most, for so many tiles (of one head; counted up to MANY_TILES per
+// sequence or thread) whose longest sequence has lk keys. Jobs without a causal order
+// are of one length: singles only fill idle CTAs there. (Up to four tiles per CTA: prompts
+// of up to 2251 tokens 55 us in pairs and 51 in singles, but of up to 1021, where the
+// items' own time counts, 24 and 31.)
+constexpr int MANY_TILES = 1 << 16;
+__device__ __forceinline__ int job_width(const VarParams& p, int tiles, int lk) {
+  const int per_cta = !p.causal ? 1 : lk >= 16 * BKV ? 4 : 2;
+  return static_cast<long long>(tiles) * p.kv_heads <= per_cta * p.grid ? 1 : 2;
+}
+__device__ __forceinline__ int min_steps(const VarParams& p, int lq) {
+  return lq * static_cast<long long>(p.group) <= FEW_ROWS ? MIN_STEPS_ROWS : MIN_STEPS;
 }
 
 // The plan of up to 32 row jobs of up to 32 sequences, by one warp without a barrier: a lane per
@@ -255,9 +285,14 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
   const int lane = lane_id();
   Seq s = {0, 0, 0, 0};
   if (lane < p.B) s = sequence(p, lane);
-  const int mine = (s.tiles(p) + 1) / 2, incl = warp_incl_scan(mine), first = incl - mine;
+  const int width = job_width(p, __reduce_add_sync(ALL, min(s.tiles(p), MANY_TILES)), __reduce_max_sync(ALL, s.lk));
+  const int least_piece = min_steps(p, __reduce_max_sync(ALL, s.lq));
+  const int mine = s.row_jobs(p, width), incl = warp_incl_scan(mine), first = incl - mine;
   const int U = __shfl_sync(ALL, incl, 31);
-  if (lane == 0) pl.jobs = U;
+  if (lane == 0) {
+    pl.jobs = U;
+    pl.width = width;
+  }
   if (U > 32) return false;
   int b = 0;  // the sequence of row job `lane`: the sequences that end at or before it
 #pragma unroll
@@ -268,14 +303,14 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
   const Seq q = {__shfl_sync(ALL, s.q0, b), __shfl_sync(ALL, s.lq, b), __shfl_sync(ALL, s.k0, b),
                  __shfl_sync(ALL, s.lk, b)};
   const bool in = lane < U;
-  const int c = in ? q.steps(p, q.tiles(p), i) : 0;
+  const int c = in ? q.steps(p, width, q.tiles(p), i) : 0;
   const float T = static_cast<float>(__reduce_add_sync(ALL, c)) * static_cast<float>(p.kv_heads);
   const int most = __reduce_max_sync(ALL, c), least = __reduce_min_sync(ALL, in ? c : 0x7fffffff);
   const int G = p.grid;
   const bool few = U * static_cast<long long>(p.kv_heads) < G;
   int share = most, cut_above = most;
-  if (p.may_cut && few && most > MIN_STEPS) {
-    const Shares r = shares_of_few(T, most, U * p.kv_heads, G);
+  if (p.may_cut && few && most > least_piece) {
+    const Shares r = shares_of_few(T, most, U * p.kv_heads, G, least_piece);
     const int tried = r.lo + (r.hi - r.lo) * lane / 31;
     const float inv = __fdividef(1.0f, static_cast<float>(tried));
     const float cf = static_cast<float>(c);
@@ -284,7 +319,7 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
     for (int j = 0; j < U; ++j) n += ceilf(fmaf(__shfl_sync(ALL, cf, j), inv, -1e-3f));
     share = cut_above = min(most, __reduce_min_sync(ALL, n * static_cast<float>(p.kv_heads) <= static_cast<float>(G) ? tried : r.hi));
   } else if (p.may_cut && !few) {
-    share = min(most, share_of_many(T, static_cast<float>(U) * static_cast<float>(p.kv_heads), G));
+    share = min(most, share_of_many(T, static_cast<float>(U) * static_cast<float>(p.kv_heads), G, least_piece));
     cut_above = min(most, share + ITEM_STEPS);
   }
   const int pieces = pieces_of(c, share, cut_above), n = in ? pieces * p.kv_heads : 0;
@@ -305,7 +340,7 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
     pl.seq[at] = b << 16 | i;
     pl.steps[at] = c;
     pl.items[at] = run;
-    if (t_own >= run && t_own < run + n) make_item(p, own, q, i, c, pieces, t_own - run, t_own);
+    if (t_own >= run && t_own < run + n) make_item(p, own, q, width, i, c, pieces, t_own - run, t_own);
   }
   const int total = __reduce_add_sync(ALL, n), cut = __reduce_max_sync(ALL, pieces > 1 ? at + 1 : 0);
   if (lane == 0) {
@@ -384,12 +419,28 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     __syncthreads();  // (pl.jobs is written again)
   }
   // row jobs before each sequence
-  int before = 0, total;
+  int before = 0, total, tiles = 0, lk = 0, lq = 0;
+#pragma unroll 1
+  for (int b = tid; b < p.B; b += THREADS) {
+    const Seq q = sequence(p, b);
+    tiles = min(tiles + min(q.tiles(p), MANY_TILES), MANY_TILES);
+    lk = max(lk, q.lk);
+    lq = max(lq, q.lq);
+  }
+  lk = __reduce_max_sync(0xffffffffu, lk);
+  lq = __reduce_max_sync(0xffffffffu, lq);
+  if (lane == 0) {
+    s.sum[warp] = lk;
+    s.most[warp] = lq;
+  }
+  block_excl_scan(tiles, s.tot[2], &tiles);
+  const int width = job_width(p, tiles, __reduce_max_sync(0xffffffffu, lane < WARPS ? s.sum[lane] : 0));
+  const int least_piece = min_steps(p, __reduce_max_sync(0xffffffffu, lane < WARPS ? s.most[lane] : 0));
 #pragma unroll 1
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int b = b0 + tid;
     int n = 0;
-    if (b < p.B) n = (sequence(p, b).tiles(p) + 1) / 2;
+    if (b < p.B) n = sequence(p, b).row_jobs(p, width);
     const int at = block_excl_scan(n, s.tot[(b0 / THREADS) & 1], &total);
     if (b < p.B) pl.first[b] = before + at;
     before += total;
@@ -398,6 +449,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   if (tid == 0) {
     pl.first[p.B] = U;
     pl.jobs = U;
+    pl.width = width;
     pl.n_items = U * p.kv_heads;  // (of a plan without a table)
     pl.n_cut = 0;
     pl.share = pl.cut_above = 0x7fffffff;
@@ -416,7 +468,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     }
     const int i = u - pl.first[lo];
     const Seq q = sequence(p, lo);
-    const int c = q.steps(p, q.tiles(p), i);
+    const int c = q.steps(p, width, q.tiles(p), i);
     s.seq[u] = lo << 16 | i;
     s.steps[u] = c;
     sum += c;
@@ -442,9 +494,9 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   const int G = p.grid;
   const bool few = U * static_cast<long long>(p.kv_heads) < G;
   int share = most, cut_above = most;
-  if (p.may_cut && few && most > MIN_STEPS) {
+  if (p.may_cut && few && most > least_piece) {
     const int J = U * p.kv_heads;
-    const Shares r = shares_of_few(T, most, J, G);
+    const Shares r = shares_of_few(T, most, J, G, least_piece);
     const int lo = r.lo, hi = r.hi;
     const int tried = lo + (hi - lo) * warp / (WARPS - 1);  // (the last one is hi)
     const float inv = __fdividef(1.0f, static_cast<float>(tried));
@@ -458,7 +510,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     cut_above = share;
   } else if (p.may_cut && !few) {
     const float J = static_cast<float>(U) * static_cast<float>(p.kv_heads);
-    share = min(most, share_of_many(T, J, G));
+    share = min(most, share_of_many(T, J, G, least_piece));
     cut_above = min(most, share + ITEM_STEPS);
   }
   const bool sorted = !few && most > least;
@@ -486,7 +538,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
       pl.steps[at] = c;
     }
     if (t_own >= run && t_own < run + n * p.kv_heads) 
-      make_item(p, own, sequence(p, job >> 16), job & 0xffff, c, n, t_own - run, t_own);
+      make_item(p, own, sequence(p, job >> 16), width, job & 0xffff, c, n, t_own - run, t_own);
     run += n * p.kv_heads;
   }
   cut = __reduce_max_sync(0xffffffffu, lane < WARPS ? s.cut[lane] : 0);
@@ -503,7 +555,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
 struct Joint {
   int q0, lq, lk, hk, tok0;  // tok0: the job's first token
   int slot, pieces;          // of the first piece
-  int unused;
+  int width;                 // tiles at most
 };
 struct Joints {
   int n;
@@ -520,8 +572,8 @@ __device__ __noinline__ void list_joints(const VarParams& p, const Plan& pl) {
     const int at = e / p.kv_heads, hk = e - at * p.kv_heads, n = pieces_of(pl, pl.steps[at]);
     if (n == 1) continue;
     const Seq s = sequence(p, pl.seq[at] >> 16);
-    p.joints->job[atomicAdd(&p.joints->n, 1)] = {s.q0, s.lq, s.lk, hk, 2 * (pl.seq[at] & 0xffff) * p.tpt,
-                                                 pl.items[at] + hk * n, n, 0};
+    p.joints->job[atomicAdd(&p.joints->n, 1)] = {s.q0, s.lq, s.lk, hk, pl.width * (pl.seq[at] & 0xffff) * p.tpt,
+                                                 pl.items[at] + hk * n, n, pl.width};
   }
 }
 
@@ -540,7 +592,7 @@ __device__ __forceinline__ void item_at(const VarParams& p, const Plan& pl, int 
       else hi = mid;
     }
     const int steps = pl.steps[lo];
-    make_item(p, out, sequence(p, pl.seq[lo] >> 16), pl.seq[lo] & 0xffff, steps, pieces_of(pl, steps), t - pl.items[lo], t);
+    make_item(p, out, sequence(p, pl.seq[lo] >> 16), pl.width, pl.seq[lo] & 0xffff, steps, pieces_of(pl, steps), t - pl.items[lo], t);
     return;
   }
   const int v = t / p.kv_heads, u = pl.jobs - 1 - v;
@@ -552,7 +604,7 @@ __device__ __forceinline__ void item_at(const VarParams& p, const Plan& pl, int 
   }
   const int i = u - pl.first[lo];
   const Seq s = sequence(p, lo);
-  make_item(p, out, s, i, s.steps(p, s.tiles(p), i), 1, t - v * p.kv_heads, t);
+  make_item(p, out, s, pl.width, i, s.steps(p, pl.width, s.tiles(p), i), 1, t - v * p.kv_heads, t);
 }
 
 // Item k of CTA x of G.
@@ -1368,7 +1420,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
   for (int w = blockIdx.x; w < jobs * slices; w += gridDim.x) {
     const int job = w / slices, slice = w - job * slices;
     const Joint j = p.joints->job[job];
-    const int rows = min(j.lq - j.tok0, 2 * p.tpt) * p.group;  // tokens with their heads
+    const int rows = min(j.lq - j.tok0, j.width * p.tpt) * p.group;  // tokens with their heads
     for (int g = slice * WARPS + warp; g < rows; g += slices * WARPS) {
       const int tok = j.tok0 + g / p.group, h = g % p.group;
       const int tile = tok >= j.tok0 + p.tpt, r = g - tile * p.tpt * p.group;
@@ -1459,7 +1511,8 @@ cudaError_t launch_hd(const hilo_attn_shape& s, const VarParams& p, const void* 
   return e;
 }
 
-// Whether a job could have more steps than the smallest piece.
+// Whether a job could have more steps than the smallest piece: a pair a step per key tile, a
+// single half of that.
 bool may_cut(const hilo_attn_shape& s) { return (s.rows_k + BKV - 1) / BKV > MIN_STEPS; }
 constexpr size_t SLOTS = static_cast<size_t>(SLOTS_PER_CTA) * ATTN_MAX_CTAS;
 
