@@ -299,10 +299,17 @@ __global__ void __maxnreg__((gn_regs(WARP, YM)))
 // A row per group of 128 threads (a warp where a row is at most 64 pieces of
 // 16 bytes). The row's pieces are on their way while the group's threads form
 // the row's angles, one pair each, into shared memory; all heads of the row
-// share them. Bound by HBM, each element read and written once: 2389 rows of 48
-// heads of 128 (bf16) 11.5 us = 5.1 TB/s, 18001 fp32 rows of 16 heads of 64 26.3 us =
-// 5.6 TB/s. (Four or two pieces per thread in flight instead of six, and 16 CTAs per
-// SM that their registers did not let in: 13.3 and 26.2 us.)
+// share them. Bound by HBM, each element read and written once: 2389 interleaved
+// rows of 48 heads of 128 (bf16) 10.6 us = 5.5 TB/s, 18001 split fp32 rows of 16 heads
+// of 64 24.8 us = 5.9 TB/s.
+//
+// How many pieces a thread has in flight decides with how many CTAs an SM holds:
+// interleaved, six pieces and 8 CTAs (four and 10 take 12.4 us for the first rows above);
+// split, two pieces of each half and 9 CTAs (three of each half take 27.4 us for the
+// second rows, one and 16 CTAs 26.4; two and 12 spill, and 1415 rows of 16 heads of 128
+// take 5.3 us instead of 4.7). A thread steps through heads and pieces by addition: one
+// division per row and piece took 11.5 us for the first rows, and 5.1 us instead of 2.9
+// for 16 rows of 48 heads of 256.
 //
 // The angle in turns is pos * f, f = theta^-p / 2 pi as the sum of two floats
 // (fh, fl): pos * fh is formed exactly as a product and its error, whole turns
@@ -312,7 +319,7 @@ __global__ void __maxnreg__((gn_regs(WARP, YM)))
 
 constexpr int RP_MAX_PAIRS = 128;
 constexpr int RP_THREADS = 128;
-constexpr int RP_CTAS = 9;  // resident per SM
+constexpr int rp_ctas(bool interleaved) { return interleaved ? 8 : 9; }  // resident per SM
 
 struct RopeArgs {
   const void* x;
@@ -365,13 +372,13 @@ __device__ __forceinline__ uint4 piece_pack(const float* v) {
 }
 
 template <int DT, bool INTERLEAVED, int GROUP>
-__global__ void __launch_bounds__(RP_THREADS, RP_CTAS) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(RP_THREADS, rp_ctas(INTERLEAVED)) rope_kernel(const __grid_constant__ RopeArgs a) {
   pdl_wait();
   pdl_trigger();
   constexpr int GROUPS = RP_THREADS / GROUP;
   constexpr int EV = Piece<DT>::EV;
   constexpr int PT = (RP_MAX_PAIRS + GROUP - 1) / GROUP;  // pairs per thread
-  constexpr int BATCH = INTERLEAVED ? 6 : 3;              // units in flight per thread
+  constexpr int BATCH = INTERLEAVED ? 6 : 2;              // units in flight per thread
   // cosines and sines of a group's row, of two rows in turn
   __shared__ __align__(16) float cs_s[GROUPS][2][RP_MAX_PAIRS], sn_s[GROUPS][2][RP_MAX_PAIRS];
   const int group = threadIdx.x / GROUP, tid = threadIdx.x % GROUP;
@@ -388,6 +395,7 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) rope_kernel(const __grid_
                                                    static_cast<long long>(a.row_base) + max(0, *a.n_rows)))
                             : a.rows;
   const int per = a.per_head, units = a.heads * per, rest = a.heads * a.rest;
+  const int head0 = tid / per, piece0 = tid - head0 * per, step_h = GROUP / per, step_e = GROUP - step_h * per;
   const char* x = static_cast<const char*>(a.x);
   char* y = static_cast<char*>(a.y);
   constexpr int ES = Piece<DT>::ES;
@@ -396,18 +404,26 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) rope_kernel(const __grid_
   for (long long r = blockIdx.x + static_cast<long long>(gridDim.x) * group; r < rows; r += step) {
     const char* xr = x + r * a.x_row * ES;
     char* yr = y + r * a.y_row * ES;
-    // unit u: piece u % per of head u / per
-    auto head_of = [&](int u) { return static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(per)); };
+    // unit u: piece u % per of head u / per; the thread's next unit is step_h heads and
+    // step_e pieces on
     uint4 lo[BATCH], hi[BATCH];
+    int hl = head0, el = piece0, hs = head0, es = piece0;  // of the loads, of the stores
+    auto next = [&](int& h, int& e) {
+      h += step_h;
+      e += step_e;
+      if (e >= per) {
+        e -= per;
+        ++h;
+      }
+    };
     auto load = [&](int u0) {
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
-        const int u = u0 + GROUP * i;
-        if (u < units) {
-          const int h = head_of(u), e = (u - h * per) * EV;
-          const char* p = xr + (h * a.x_head + e) * ES;
+        if (u0 + GROUP * i < units) {
+          const char* p = xr + (hl * a.x_head + el * EV) * ES;
           lo[i] = *reinterpret_cast<const uint4*>(p);
           if (!INTERLEAVED) hi[i] = *reinterpret_cast<const uint4*>(p + a.pairs * ES);
+          next(hl, el);
         }
       }
     };
@@ -435,10 +451,10 @@ __global__ void __launch_bounds__(RP_THREADS, RP_CTAS) rope_kernel(const __grid_
       if (u0 != tid) load(u0);
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
-        const int u = u0 + GROUP * i;
-        if (u >= units) break;
-        const int h = head_of(u), e = (u - h * per) * EV;
-        char* p = yr + (h * a.y_head + e) * ES;
+        if (u0 + GROUP * i >= units) break;
+        const int e = es * EV;
+        char* p = yr + (hs * a.y_head + e) * ES;
+        next(hs, es);
         float v[EV], w[EV];
         piece_widen<DT>(lo[i], v);
         if constexpr (INTERLEAVED) {
@@ -540,7 +556,7 @@ cudaError_t launch_rope(const hilo_rope_shape& s, const void* x, const float* po
   a.rest_from = D;
   // a warp per row where the row gives its lanes at most two units each
   const bool small = a.heads * (a.per_head + a.rest) <= 64;
-  const dim3 grid(grid_for(s.rows, small ? RP_THREADS / 32 : 1, num_sms, RP_CTAS));
+  const dim3 grid(grid_for(s.rows, small ? RP_THREADS / 32 : 1, num_sms, rp_ctas(s.rot.interleaved)));
 #define HILO_ROPE(DT)                                                                        \
   (s.rot.interleaved ? (small ? rope_kernel<DT, true, 32> : rope_kernel<DT, true, 128>)      \
                      : (small ? rope_kernel<DT, false, 32> : rope_kernel<DT, false, 128>))
