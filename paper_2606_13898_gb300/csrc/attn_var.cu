@@ -681,12 +681,13 @@ struct Cfg {
   static constexpr int NBOX = HD / 64;               // boxes of 64 columns
   static constexpr int Q_BOX = BQ * 128, KV_BOX = BKV * 128;
   static constexpr int Q_BYTES = NBOX * Q_BOX, KV_BYTES = NBOX * KV_BOX;
-  // Q0 | Q1 | K0 | K1 | V0 | V1 (the plan's scratch before the first copy)
+  static constexpr int STAGES = HD == 64 ? 4 : 2;    // of K and of V
+  // Q0 | Q1 | K.. | V.. (the plan's scratch before the first copy)
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = 2 * Q_BYTES;
-  static constexpr int OFF_V = OFF_K + 2 * KV_BYTES;
-  static constexpr int DATA_BYTES = OFF_V + 2 * KV_BYTES;
-  static constexpr int OFF_X = DATA_BYTES + 256;  // barriers before it
+  static constexpr int OFF_V = OFF_K + STAGES * KV_BYTES;
+  static constexpr int DATA_BYTES = OFF_V + STAGES * KV_BYTES;
+  static constexpr int OFF_X = DATA_BYTES + 384;  // barriers before it
   static constexpr int OFF_PLAN = OFF_X + static_cast<int>(sizeof(Shared));
   static constexpr int SMEM_BYTES = OFF_PLAN + static_cast<int>(sizeof(Plan)) + 1024;  // + alignment of the base
   // Tensor memory: S0 | S1 | O0 | O1, P_i over the first half of S_i; of heads of 64
@@ -710,19 +711,20 @@ __global__ void __launch_bounds__(THREADS, 1)
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::DATA_BYTES);
   uint64_t* q_full = bars + 0;
-  uint64_t* k_full = bars + 1;    // [2]
-  uint64_t* k_empty = bars + 3;   // [2]
-  uint64_t* v_full = bars + 5;    // [2]
-  uint64_t* v_empty = bars + 7;   // [2]
-  uint64_t* s_full = bars + 9;    // [2] per softmax warpgroup
-  uint64_t* p_full = bars + 11;   // [2] per softmax warpgroup
-  uint64_t* o_done = bars + 13;   // [2] per softmax warpgroup
-  uint64_t* drain = bars + 15;
-  uint64_t* q_empty = bars + 16;  // every S product of an item done: Q may be reloaded
-  uint64_t* it_full = bars + 18;  // [RING]
-  uint64_t* it_empty = bars + 22; // [RING]
-  uint64_t* s_free = bars + 26;   // [2] OWN_P: S_i is in registers, the next one may be formed
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 28);
+  uint64_t* s_full = bars + 1;    // [2] per softmax warpgroup
+  uint64_t* p_full = bars + 3;    // [2] per softmax warpgroup
+  uint64_t* o_done = bars + 5;    // [2] per softmax warpgroup
+  uint64_t* s_free = bars + 7;    // [2] OWN_P: S_i is in registers, the next one may be formed
+  uint64_t* drain = bars + 9;
+  uint64_t* q_empty = bars + 10;  // every S product of an item done: Q may be reloaded
+  uint64_t* it_full = bars + 11;  // [RING]
+  uint64_t* it_empty = it_full + RING;
+  uint64_t* k_full = it_empty + RING;
+  uint64_t* k_empty = k_full + C::STAGES;
+  uint64_t* v_full = k_empty + C::STAGES;
+  uint64_t* v_empty = v_full + C::STAGES;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_empty + C::STAGES);
+  static_assert((11 + 2 * RING + 4 * C::STAGES + 1) * 8 <= C::OFF_X - C::DATA_BYTES, "room for the barriers");
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   Shared& shr = *reinterpret_cast<Shared*>(smem + C::OFF_X);
   Plan& plan = *reinterpret_cast<Plan*>(smem + C::OFF_PLAN);
@@ -739,15 +741,17 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(&k_full[i], 1);
       mbar_init(&k_empty[i], 1);
       mbar_init(&v_full[i], 1);
       mbar_init(&v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 128);
+      mbar_init(&p_full[i], 4);
       mbar_init(&o_done[i], 1);
-      mbar_init(&s_free[i], 128);
+      mbar_init(&s_free[i], 4);
     }
     mbar_init(drain, 1);
     mbar_init(q_empty, 1);
@@ -782,8 +786,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     return;
   }
   // key tile number kt of the CTA: its stage and the parity of that stage's use
-  auto kv_stage = [](uint32_t kt) { return static_cast<int>(kt & 1u); };
-  auto kv_phase = [](uint32_t kt) { return (kt >> 1) & 1u; };
+  auto kv_stage = [](uint32_t kt) { return static_cast<int>(kt & (C::STAGES - 1u)); };
+  auto kv_phase = [](uint32_t kt) { return (kt / C::STAGES) & 1u; };
   auto it_wait = [&](uint32_t jn, int code) {
     return mbar_wait(&it_full[jn & (RING - 1)], (jn / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * code);
   };
@@ -856,7 +860,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (q_armed)
             while (!mbar_try_wait(smem_u32(q_full), q_par) && globaltimer_ns() - g0 < lim) {
             }
-          for (int st = 0; st < 2; ++st)
+          for (int st = 0; st < C::STAGES; ++st)
             if ((armed >> st) & 1u)
               while (!mbar_try_wait(smem_u32(&full[st]), (par >> st) & 1u) && globaltimer_ns() - g0 < lim) {
               }
@@ -1168,7 +1172,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         tmem_ld_wait();
         if (C::OWN_P) {
           tc_fence_before();
-          mbar_arrive(&s_free[i]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_free[i]);
         }
         // the keys that the row does not see, whatever their logits
         if ((t + 1) * BKV > lim_warp) {
@@ -1243,7 +1248,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&p_full[i]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[i]);
       }
       // ---- output rows. A pair: warpgroup i writes its tile. A single:
       // warpgroup 1 hands its row maximum and sum to warpgroup 0, which merges
