@@ -137,10 +137,12 @@ __device__ __forceinline__ Seq sequence(const VarParams& p, int b) {
 //           of ceil(T / (G - J)) and the longest job in floor(G / J) pieces, that makes at
 //           most G items: one for each CTA. (The last two do: sum(c / share + 1)
 //           <= G, and each job of at most floor(G / J) pieces.)
+//           Not so single tokens whose jobs are too many for that (deal_few).
 //   J >= G  ceil((T + J ITEM_STEPS) / G) - ITEM_STEPS, and only jobs that are
 //           longer by more than ITEM_STEPS are cut. Listed longest first, to a
 //           sixteenth of the longest, the cut ones ahead of the others: fewer than
-//           2G pieces, as a job of c > share + 1 steps has at most (c - 1) / share + 1.
+//           2G pieces. (One of k pieces has more than (k - 1) share steps, of two at least
+//           share + 3, and T < G (share + 2) - 2J: so too with J >= G / 2.)
 // Pieces of fewer steps than min_steps would cost more in their epilogues and in the second
 // kernel than they save.
 //
@@ -262,6 +264,15 @@ __device__ __forceinline__ int share_of_many(float T, float J, int G, int least_
   return max(least_piece, static_cast<int>(__fdividef(T + J * ITEM_STEPS, static_cast<float>(G))) + 1 - ITEM_STEPS);
 }
 
+// Whether few jobs (J < G) are dealt out like many: where they are at least half of the CTAs, one
+// item for each may leave too few pieces for the longest. Of single tokens only, whose
+// items cost little beside their steps: 16 of them over 1 to 32768 keys, 8 key heads of 64,
+// 97 us and 69 so, 10 over 64 to 16000 keys, whose share is near the even one,
+// 39 us and 49; prompts of 8 to 2500 tokens 24 us and 39.
+__device__ __forceinline__ bool deal_few(float T, int share, int J, int G, int least_piece) {
+  return least_piece == MIN_STEPS_ROWS && 2 * J >= G && static_cast<float>(share) * static_cast<float>(G) > 1.2f * T + static_cast<float>(2 * ITEM_STEPS * G);
+}
+
 // Tiles per job at most, for so many tiles (of one head; counted up to MANY_TILES per
 // sequence or thread) whose longest sequence has lk keys. Jobs without a causal order
 // are of one length: singles only fill idle CTAs there. (Up to four tiles per CTA: prompts
@@ -307,7 +318,7 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
   const float T = static_cast<float>(__reduce_add_sync(ALL, c)) * static_cast<float>(p.kv_heads);
   const int most = __reduce_max_sync(ALL, c), least = __reduce_min_sync(ALL, in ? c : 0x7fffffff);
   const int G = p.grid;
-  const bool few = U * static_cast<long long>(p.kv_heads) < G;
+  bool few = U * static_cast<long long>(p.kv_heads) < G;
   int share = most, cut_above = most;
   if (p.may_cut && few && most > least_piece) {
     const Shares r = shares_of_few(T, most, U * p.kv_heads, G, least_piece);
@@ -318,7 +329,9 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
 #pragma unroll 8
     for (int j = 0; j < U; ++j) n += ceilf(fmaf(__shfl_sync(ALL, cf, j), inv, -1e-3f));
     share = cut_above = min(most, __reduce_min_sync(ALL, n * static_cast<float>(p.kv_heads) <= static_cast<float>(G) ? tried : r.hi));
-  } else if (p.may_cut && !few) {
+    few = !deal_few(T, share, U * p.kv_heads, G, least_piece);
+  }
+  if (p.may_cut && !few) {
     share = min(most, share_of_many(T, static_cast<float>(U) * static_cast<float>(p.kv_heads), G, least_piece));
     cut_above = min(most, share + ITEM_STEPS);
   }
@@ -492,7 +505,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   most = __reduce_max_sync(0xffffffffu, lane < WARPS ? s.most[lane] : 0);
   least = __reduce_min_sync(0xffffffffu, lane < WARPS ? s.least[lane] : 0x7fffffff);
   const int G = p.grid;
-  const bool few = U * static_cast<long long>(p.kv_heads) < G;
+  bool few = U * static_cast<long long>(p.kv_heads) < G;
   int share = most, cut_above = most;
   if (p.may_cut && few && most > least_piece) {
     const int J = U * p.kv_heads;
@@ -508,7 +521,9 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     share = __reduce_min_sync(0xffffffffu, lane < WARPS ? s.count[lane] : hi);
     share = min(share, most);
     cut_above = share;
-  } else if (p.may_cut && !few) {
+    few = !deal_few(T, share, J, G, least_piece);
+  }
+  if (p.may_cut && !few) {
     const float J = static_cast<float>(U) * static_cast<float>(p.kv_heads);
     share = min(most, share_of_many(T, J, G, least_piece));
     cut_above = min(most, share + ITEM_STEPS);

@@ -121,6 +121,9 @@ CASES = [
     ([1 + i % 3 for i in range(1300)], [4 + i % 300 for i in range(1300)], 2, 1, 128, 1, "bf16"),
     # a long sequence among short ones: cut where more jobs than CTAs are there
     ([1] * 100 + [260], [60] * 100 + [9000], 8, 4, 64, 1, "bf16"),
+    # fewer jobs than CTAs, dealt out like many: single tokens, one of them over a long cache
+    ([1] * 16, [64, 16000, 1, 300] + [70 + 90 * i for i in range(12)], 16, 8, 64, 1, "bf16"),
+    ([1] * 45, [12000] + [1 + 13 * i for i in range(44)], 6, 3, 128, 0, "f16"),
     ([2500], None, 4, 4, 64, 1, "bf16"),
     ([1500, 700], None, 16, 8, 128, 1, "f16"),
     ([1024, 2048], None, 24, 24, 128, 0, "bf16"),
