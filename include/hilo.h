@@ -655,7 +655,8 @@ size_t hilo_attention_workspace_bytes(const hilo_attn_shape* shape);
  * i + lk - lq. A query that sees no key gives zeros.
  *   cu_q, cu_k  int32 [B+1] device, non-decreasing; on the device they are cut
  *               to [0, rows_q] and [0, rows_k], so no offset reads or writes
- *               outside the buffers
+ *               outside the buffers. Offsets that fall leave rows in the
+ *               sequences unspecified.
  *   q, k, v     device, 16-byte aligned. Rows outside the sequences are not
  *               part of any result, nor are keys that a query does not see,
  *               whatever their values.

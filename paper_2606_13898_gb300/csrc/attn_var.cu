@@ -298,7 +298,7 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
   if (lane < p.B) s = sequence(p, lane);
   const int width = job_width(p, __reduce_add_sync(ALL, min(s.tiles(p), MANY_TILES)), __reduce_max_sync(ALL, s.lk));
   const int least_piece = min_steps(p, __reduce_max_sync(ALL, s.lq));
-  const int mine = s.row_jobs(p, width), incl = warp_incl_scan(mine), first = incl - mine;
+  const int mine = min(s.row_jobs(p, width), 1 << 25), incl = warp_incl_scan(mine), first = incl - mine;
   const int U = __shfl_sync(ALL, incl, 31);
   if (lane == 0) {
     pl.jobs = U;
@@ -433,9 +433,11 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   }
   // row jobs before each sequence
   int before = 0, total, tiles = 0, lk = 0, lq = 0;
+  long long all = 0;
 #pragma unroll 1
   for (int b = tid; b < p.B; b += THREADS) {
     const Seq q = sequence(p, b);
+    all += q.tiles(p);
     tiles = min(tiles + min(q.tiles(p), MANY_TILES), MANY_TILES);
     lk = max(lk, q.lk);
     lq = max(lq, q.lq);
@@ -445,6 +447,16 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   if (lane == 0) {
     s.sum[warp] = lk;
     s.most[warp] = lq;
+  }
+  // Offsets that fall and rise again can name every row thousands of times, more jobs than an
+  // int counts: then there are none. (In order they make at most a tile per row and one per
+  // sequence. Counted in 4096s: the threads' sums are below 2^34, what is let through below 2^31.)
+  int many;
+  block_excl_scan(static_cast<int>(all >> 12), s.tot[3], &many);
+  if (many > static_cast<int>((static_cast<long long>(p.rows_q) + p.B) >> 12)) {
+    if (tid == 0) pl.jobs = pl.n_items = pl.n_cut = 0;
+    __syncthreads();
+    return;
   }
   block_excl_scan(tiles, s.tot[2], &tiles);
   const int width = job_width(p, tiles, __reduce_max_sync(0xffffffffu, lane < WARPS ? s.sum[lane] : 0));

@@ -282,6 +282,21 @@ def test_offsets_past_the_buffers_are_cut(H):
     check(store[:40], tuple(x[:40] if hasattr(x, "shape") else x for x in ref), "bf16")
 
 
+def test_falling_offsets_that_name_rows_again_and_again(H):
+    """More query tiles than rows and sequences can have: no row is written, and the next call is whole."""
+    rows = 40000
+    q = torch.randn(rows, 128, 64, device="cuda", dtype=torch.bfloat16)
+    k = torch.randn(64, 1, 64, device="cuda", dtype=torch.bfloat16)
+    cu_q = torch.tensor([0, rows] * 500, dtype=torch.int32, device="cuda")
+    cu_k = torch.tensor([0, 64] * 500, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, math.nan)
+    call(H, q, k, k, cu_q, cu_k, 0, out=out)
+    H.hilo_sync_status()
+    assert bool(out.isnan().all())
+    one = [torch.tensor([0, n], dtype=torch.int32, device="cuda") for n in (200, 64)]
+    check(call(H, q[:200], k, k, *one, 0), reference(q[:200], k, k, *one, 0), "bf16")
+
+
 def test_no_keys_at_all(H):
     q, k, v, _, _ = make([4], [1], 2, 2, 64, "bf16")
     cu_q = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
