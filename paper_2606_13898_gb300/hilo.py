@@ -435,17 +435,13 @@ class NormVectors:
     b_norm: object = None
 
     def c(self) -> hilo_norm_vectors:
-        """The C struct of the device pointers, rebuilt only when one of the vectors is replaced."""
-        cached = self.__dict__.get("_c")
-        if cached is not None:
-            st, gate, scale, shift, w_branch, w_norm, b_norm = cached
-            if (gate is self.gate and scale is self.scale and shift is self.shift and w_branch is self.w_branch
-                    and w_norm is self.w_norm and b_norm is self.b_norm):
-                return st
-        ts = (self.gate, self.scale, self.shift, self.w_branch, self.w_norm, self.b_norm)
-        st = hilo_norm_vectors(*(_ptr(t) for t in ts))
-        self.__dict__["_c"] = (st, *ts)
-        return st
+        """The C struct of the vectors' present addresses."""
+        at = (_ptr(self.gate), _ptr(self.scale), _ptr(self.shift), _ptr(self.w_branch), _ptr(self.w_norm),
+              _ptr(self.b_norm))
+        kept = self.__dict__.get("_c")  # (a struct of the same addresses is the same struct)
+        if kept is None or kept[0] != at:
+            kept = self.__dict__["_c"] = (at, hilo_norm_vectors(*at))
+        return kept[1]
 
 
 @dataclasses.dataclass(frozen=True)
@@ -510,8 +506,7 @@ class AttnShape:
 
 @dataclasses.dataclass
 class BlockMod:
-    """Conditioning of one block (hilo_block_forward_mod). axis_dims None: no rotary positions. The
-    NormVectors and their tensors are fixed after construction (their values may change)."""
+    """Conditioning of one block (hilo_block_forward_mod). axis_dims None: no rotary positions."""
 
     txt_attn: NormVectors
     img_attn: NormVectors
@@ -529,17 +524,13 @@ class BlockMod:
     per_axis: int = 1
 
     def c(self, pos) -> hilo_block_mod:
-        """The C struct, built once, with the positions of this call (None without rotary positions)."""
-        def build():
-            rot = hilo_rotation() if self.axis_dims is None else _rotation(self.axis_dims, self.theta,
-                                                                           self.interleaved, self.per_axis)
-            return hilo_block_mod(self.norm, self.norm_branch, self.vec_dtype, self.eps, self.resid_scale, self.vec_row,
-                                  self.txt_attn.c(), self.img_attn.c(), self.txt_mlp.c(), self.img_mlp.c(), None, rot)
+        """The C struct with the positions of this call (None without rotary positions)."""
         if (pos is None) != (self.axis_dims is None):
             raise ValueError("positions and axis_dims go together")
-        st = hilo_block_mod.from_buffer_copy(_kept(self, build))  # calls of other threads have their own
-        st.pos = _ptr(pos)
-        return st
+        rot = hilo_rotation() if self.axis_dims is None else _rotation(self.axis_dims, self.theta, self.interleaved,
+                                                                       self.per_axis)
+        return hilo_block_mod(self.norm, self.norm_branch, self.vec_dtype, self.eps, self.resid_scale, self.vec_row,
+                              self.txt_attn.c(), self.img_attn.c(), self.txt_mlp.c(), self.img_mlp.c(), _ptr(pos), rot)
 
 
 # ---------------------------------------------------------------------------

@@ -219,8 +219,8 @@ def test_conditioned_block(H):
 
 
 def test_structs_follow_their_vectors(H):
-    """The cached structs carry the present addresses: a replaced vector gives a rebuilt struct, and two calls with the
-    same conditioning have structs of their own."""
+    """The structs carry the present addresses: a replaced vector or its replaced memory gives a rebuilt struct, and two
+    calls with the same conditioning have structs of their own."""
     import torch
 
     v = H.NormVectors(gate=torch.empty(8), scale=torch.empty(8))
@@ -231,6 +231,10 @@ def test_structs_follow_their_vectors(H):
     m = H.BlockMod(v, v, v, v, vec_row=64, axis_dims=(16, 16))
     a, b = m.c(A), m.c(2 * A)
     assert a.pos == A and b.pos == 2 * A and a.rot.axes == 2 and b.img_mlp.gate == v.gate.data_ptr()
+    v.gate.data = torch.empty(8)  # the same tensor object over other memory
+    assert v.c().gate == v.gate.data_ptr() and m.c(A).txt_attn.gate == v.gate.data_ptr()
+    m.txt_attn = H.NormVectors(shift=torch.empty(8))
+    assert m.c(A).txt_attn.gate is None and m.c(A).txt_attn.shift == m.txt_attn.shift.data_ptr()
 
 
 SANITIZED = r"""
