@@ -788,13 +788,15 @@ class HotPath:
     def enable_mod(self, mods: list, origin: RowPositions | None = None) -> None:
         """Makes run(..., mod=True) available: one BlockMod per block, and where
         the positions of their rotations begin (needed if any block rotates)."""
+        if len(mods) != len(self.weights):
+            raise ValueError(f"{len(mods)} BlockMods for {len(self.weights)} blocks")
         rotated = [m.axis_dims for m in mods if m.axis_dims is not None]
         if rotated and origin is None:
             raise ValueError("rotary positions need an origin")
         if any(len(dims) != 3 for dims in rotated):
             raise ValueError("rows have three coordinates: a block that rotates has three axes")
         self.mods, self.origin = mods, origin
-        if origin is not None:
+        if origin is not None and self.pos is None:  # (a captured graph keeps writing to it)
             rows = self.shape.B * self.shape.T + self.cap
             self.pos = torch.empty(rows, 3, dtype=torch.float32, device=self.out.device)
 
@@ -827,6 +829,8 @@ class HotPath:
         (enable_mod first)."""
         if fp8 and mod:
             raise ValueError("the conditioned block has no e4m3 form")
+        if mod and self.mods is None:
+            raise ValueError("enable_mod first")
         sh = self.shape
         stream = _stream(stream)  # looked up once for the whole pass
         hilo_score(sh, x, self.score, stream)

@@ -213,6 +213,14 @@ def test_hot_path_with_conditioning(H):
     assert torch.equal(hp.y, want)
     with pytest.raises(ValueError):
         hp.run(x, text, mask, kk, km, mod=True, fp8=True)
+    # enabled again, the path keeps the positions that the graph writes
+    pos = hp.pos
+    hp.enable_mod(hp.mods, H.RowPositions(t_img=2.0))
+    assert hp.pos is pos
+    with pytest.raises(ValueError):
+        hp.enable_mod(hp.mods[:1], origin)
+    with pytest.raises(ValueError):
+        H.HotPath(sh, hp.weights).run(x, text, mask, kk, km, mod=True)
 
 
 def test_prompt_layer(H):
