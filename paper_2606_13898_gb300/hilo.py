@@ -436,8 +436,8 @@ class NormVectors:
 
     def c(self) -> hilo_norm_vectors:
         """The C struct of the vectors' present addresses."""
-        at = (_ptr(self.gate), _ptr(self.scale), _ptr(self.shift), _ptr(self.w_branch), _ptr(self.w_norm),
-              _ptr(self.b_norm))
+        at = [t if t is None or isinstance(t, int) else t.data_ptr()  # (_ptr; 12 calls of it are a microsecond)
+              for t in (self.gate, self.scale, self.shift, self.w_branch, self.w_norm, self.b_norm)]
         kept = self.__dict__.get("_c")  # (a struct of the same addresses is the same struct)
         if kept is None or kept[0] != at:
             kept = self.__dict__["_c"] = (at, hilo_norm_vectors(*at))
@@ -464,7 +464,7 @@ class NormShape:
     vec_row: int | None = None
 
     def c(self) -> hilo_norm_shape:
-        return _kept(self, lambda: hilo_norm_shape(
+        return self.__dict__.get("_c") or _kept(self, lambda: hilo_norm_shape(
             self.B, self.T, self.cap, self.d, self.norm, self.norm_branch, self.u_dtype, self.y_dtype,
             self.u_out_dtype, self.h_dtype, self.vec_dtype, self.eps, self.resid_scale,
             self.d if self.vec_row is None else self.vec_row))
@@ -679,11 +679,10 @@ def hilo_rope(shape: RopeShape, x, pos, n_rows, y, stream=None) -> None:
 
 def hilo_gate_norm(shape: NormShape, txt: NormVectors | None, img: NormVectors, cu_img, u_txt, u_img, y, u_out, h,
                    h_scale, stream=None) -> None:
-    s, i = shape.c(), img.c()
-    x = None if txt is None else ctypes.byref(txt.c())
-    _check("hilo_gate_norm", lib().hilo_gate_norm(ctypes.byref(s), x, ctypes.byref(i), _ptr(cu_img), _ptr(u_txt),
-                                                  _ptr(u_img), _ptr(y), _ptr(u_out), _ptr(h), _ptr(h_scale),
-                                                  _stream(stream)))
+    _check("hilo_gate_norm", lib().hilo_gate_norm(shape.c(), None if txt is None else txt.c(), img.c(), _ptr(cu_img),
+                                                  _ptr(u_txt), _ptr(u_img), None if y is None else _ptr(y),
+                                                  None if u_out is None else _ptr(u_out), None if h is None else _ptr(h),
+                                                  None if h_scale is None else _ptr(h_scale), _stream(stream)))
 
 
 def hilo_attention_workspace_bytes(shape: AttnShape) -> int:
