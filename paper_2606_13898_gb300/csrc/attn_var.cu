@@ -180,7 +180,7 @@ __device__ __forceinline__ int pieces_of(int steps, int share, int cut_above) {
 }
 __device__ __forceinline__ int pieces_of(const Plan& pl, int steps) { return pieces_of(steps, pl.share, pl.cut_above); }
 
-// The plan's larger parts (block_excl_scan, plan_sort, list_joints) are calls of their own,
+// The plan's larger parts (block_excl_scan, count_jobs, plan_sort, list_joints) are calls of their own,
 // made before the warpgroups share out their registers only: setmaxnreg does not know
 // a callee's need.
 
@@ -287,24 +287,49 @@ __device__ __forceinline__ int min_steps(const VarParams& p, int lq) {
   return lq * static_cast<long long>(p.group) <= FEW_ROWS ? MIN_STEPS_ROWS : MIN_STEPS;
 }
 
+// What plan_build needs for itself.
+constexpr int PLAN_PER = (MAX_TABLE + THREADS - 1) / THREADS;
+struct PlanScratch {
+  Seq of[32];       // up to 32 sequences
+  int least_piece;  // of theirs
+  int tot[4][THREADS / 32];
+  int sum[THREADS / 32], most[THREADS / 32], least[THREADS / 32], count[THREADS / 32], cut[THREADS / 32];
+  int seq[MAX_TABLE], steps[MAX_TABLE], rank[MAX_TABLE];  // in the order of the sequences
+  int hist[BUCKETS * PLAN_PER * (THREADS / 32)];          // [bucket][round, warp]
+};
+
 // The plan of up to 32 row jobs of up to 32 sequences, by one warp without a barrier: a lane per
 // sequence, then per row job. (The CTA's way to the same plan takes 4000 to 5000
-// cycles of barriers and shared memory, a third of the shortest calls.) Returns whether it
-// was made; pl.jobs is set either way.
-__device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* own, int t_own) {
+// cycles of barriers and shared memory, a third of the shortest calls.) More row jobs than
+// that: it leaves what it knows of the sequences.
+constexpr int MANY_JOBS = 1 << 25;  // of a sequence: not counted exactly here
+__device__ __forceinline__ void plan_small(const VarParams& p, Plan& pl, PlanScratch& sc, Item* own, int t_own) {
   constexpr uint32_t ALL = 0xffffffffu;
   const int lane = lane_id();
   Seq s = {0, 0, 0, 0};
   if (lane < p.B) s = sequence(p, lane);
   const int width = job_width(p, __reduce_add_sync(ALL, min(s.tiles(p), MANY_TILES)), __reduce_max_sync(ALL, s.lk));
   const int least_piece = min_steps(p, __reduce_max_sync(ALL, s.lq));
-  const int mine = min(s.row_jobs(p, width), 1 << 25), incl = warp_incl_scan(mine), first = incl - mine;
+  const int mine = min(s.row_jobs(p, width), MANY_JOBS), incl = warp_incl_scan(mine), first = incl - mine;
   const int U = __shfl_sync(ALL, incl, 31);
   if (lane == 0) {
     pl.jobs = U;
     pl.width = width;
   }
-  if (U > 32) return false;
+  if (U > 32) {
+    if (lane < p.B) {
+      pl.first[lane] = first;
+      sc.of[lane] = s;
+    }
+    if (lane == 0) {
+      sc.least_piece = least_piece;
+      pl.first[p.B] = U;
+      pl.n_items = U * p.kv_heads;  // (of a plan without a table)
+      pl.n_cut = 0;
+      pl.share = pl.cut_above = 0x7fffffff;
+    }
+    return;
+  }
   int b = 0;  // the sequence of row job `lane`: the sequences that end at or before it
 #pragma unroll
   for (int step = 16; step >= 1; step >>= 1)
@@ -362,17 +387,7 @@ __device__ __forceinline__ bool plan_small(const VarParams& p, Plan& pl, Item* o
     pl.share = share;
     pl.cut_above = cut_above;
   }
-  return true;
 }
-
-// What plan_build needs for itself.
-constexpr int PLAN_PER = (MAX_TABLE + THREADS - 1) / THREADS;
-struct PlanScratch {
-  int tot[4][THREADS / 32];
-  int sum[THREADS / 32], most[THREADS / 32], least[THREADS / 32], count[THREADS / 32], cut[THREADS / 32];
-  int seq[MAX_TABLE], steps[MAX_TABLE], rank[MAX_TABLE];  // in the order of the sequences
-  int hist[BUCKETS * PLAN_PER * (THREADS / 32)];          // [bucket][round, warp]
-};
 
 // Longest first by bucket, in the sequences' order within one: the rank among a
 // warp's lanes, then a scan over all warps' counts.
@@ -420,17 +435,11 @@ __device__ __noinline__ void plan_sort(Plan& pl, PlanScratch& s, int U, int most
   __syncthreads();
 }
 
-// By all threads; ends with a barrier. The thread that finds item t_own among the listed
-// ones writes it to *own.
-__device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScratch& s, Item* own, int t_own) {
+// The sequences' row jobs, counted by all threads: pl.first, pl.jobs, pl.width; the plan without a table. False
+// where the offsets make no sense; ends with a barrier.
+__device__ __noinline__ bool count_jobs(const VarParams& p, Plan& pl, PlanScratch& s) {
   constexpr int WARPS = THREADS / 32;
   const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
-  if (p.B <= 32) {
-    if (warp == 0) plan_small(p, pl, own, t_own);
-    __syncthreads();
-    if (pl.jobs <= 32) return;
-    __syncthreads();  // (pl.jobs is written again)
-  }
   // row jobs before each sequence
   int before = 0, total, tiles = 0, lk = 0, lq = 0;
   long long all = 0;
@@ -442,25 +451,32 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     lk = max(lk, q.lk);
     lq = max(lq, q.lq);
   }
-  lk = __reduce_max_sync(0xffffffffu, lk);
-  lq = __reduce_max_sync(0xffffffffu, lq);
+  constexpr uint32_t ALL = 0xffffffffu;
+  lk = __reduce_max_sync(ALL, lk);
+  lq = __reduce_max_sync(ALL, lq);
+  tiles = __reduce_add_sync(ALL, tiles);
+  int many = __reduce_add_sync(ALL, static_cast<int>(all >> 12));
   if (lane == 0) {
     s.sum[warp] = lk;
     s.most[warp] = lq;
+    s.count[warp] = tiles;
+    s.cut[warp] = many;
   }
+  __syncthreads();
+  // (lane w of each warp has warp w's)
+  lk = __reduce_max_sync(ALL, lane < WARPS ? s.sum[lane] : 0);
+  lq = __reduce_max_sync(ALL, lane < WARPS ? s.most[lane] : 0);
+  tiles = __reduce_add_sync(ALL, lane < WARPS ? s.count[lane] : 0);
+  many = __reduce_add_sync(ALL, lane < WARPS ? s.cut[lane] : 0);
   // Offsets that fall and rise again can name every row thousands of times, more jobs than an
   // int counts: then there are none. (In order they make at most a tile per row and one per
   // sequence. Counted in 4096s: the threads' sums are below 2^34, what is let through below 2^31.)
-  int many;
-  block_excl_scan(static_cast<int>(all >> 12), s.tot[3], &many);
   if (many > static_cast<int>((static_cast<long long>(p.rows_q) + p.B) >> 12)) {
     if (tid == 0) pl.jobs = pl.n_items = pl.n_cut = 0;
     __syncthreads();
-    return;
+    return false;
   }
-  block_excl_scan(tiles, s.tot[2], &tiles);
-  const int width = job_width(p, tiles, __reduce_max_sync(0xffffffffu, lane < WARPS ? s.sum[lane] : 0));
-  const int least_piece = min_steps(p, __reduce_max_sync(0xffffffffu, lane < WARPS ? s.most[lane] : 0));
+  const int width = job_width(p, tiles, lk), least_piece = min_steps(p, lq);
 #pragma unroll 1
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int b = b0 + tid;
@@ -472,6 +488,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   }
   const int U = before;
   if (tid == 0) {
+    s.least_piece = least_piece;
     pl.first[p.B] = U;
     pl.jobs = U;
     pl.width = width;
@@ -480,7 +497,28 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     pl.share = pl.cut_above = 0x7fffffff;
   }
   __syncthreads();
+  return true;
+}
+
+// By all threads; ends with a barrier. The thread that finds item t_own among the listed
+// ones writes it to *own.
+__device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScratch& s, Item* own, int t_own) {
+  constexpr int WARPS = THREADS / 32;
+  const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
+  bool known = false;  // the sequences' row jobs are counted
+  if (p.B <= 32) {
+    if (warp == 0) plan_small(p, pl, s, own, t_own);
+    __syncthreads();
+    if (pl.jobs <= 32) return;
+    known = pl.jobs < MANY_JOBS;
+  }
+  if (!known) {
+    __syncthreads();  // (pl.jobs is written again)
+    if (!count_jobs(p, pl, s)) return;
+  }
+  const int U = pl.jobs, width = pl.width, least_piece = s.least_piece;
   if (U > MAX_TABLE || U == 0) return;
+  int total;
   // the row jobs' steps
   int sum = 0, most = 0, least = 0x7fffffff;
 #pragma unroll 1
@@ -492,7 +530,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
       else hi = mid;
     }
     const int i = u - pl.first[lo];
-    const Seq q = sequence(p, lo);
+    const Seq q = known ? s.of[lo] : sequence(p, lo);
     const int c = q.steps(p, width, q.tiles(p), i);
     s.seq[u] = lo << 16 | i;
     s.steps[u] = c;

@@ -124,6 +124,9 @@ CASES = [
     # fewer jobs than CTAs, dealt out like many: single tokens, one of them over a long cache
     ([1] * 16, [64, 16000, 1, 300] + [70 + 90 * i for i in range(12)], 16, 8, 64, 1, "bf16"),
     ([1] * 45, [12000] + [1 + 13 * i for i in range(44)], 6, 3, 128, 0, "f16"),
+    # few sequences, more jobs than the table has, and more than one warp plans
+    ([2100], [70], 128, 1, 64, 0, "bf16"),
+    ([700, 0, 90], [300, 5, 200], 64, 1, 128, 1, "f16"),
     ([2500], None, 4, 4, 64, 1, "bf16"),
     ([1500, 700], None, 16, 8, 128, 1, "f16"),
     ([1024, 2048], None, 24, 24, 128, 0, "bf16"),
