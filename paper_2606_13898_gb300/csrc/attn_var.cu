@@ -392,9 +392,12 @@ __device__ __forceinline__ void plan_small(const VarParams& p, Plan& pl, PlanScr
 // Longest first by bucket, in the sequences' order within one: the rank among a
 // warp's lanes, then a scan over all warps' counts.
 __device__ __noinline__ void plan_sort(Plan& pl, PlanScratch& s, int U, int most, int cut_above) {
-  constexpr int WARPS = THREADS / 32, ROWS = PLAN_PER * WARPS;
+  constexpr int WARPS = THREADS / 32;
+  static_assert(BUCKETS * WARPS == THREADS, "a count per thread and round");
   const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
-  for (int i = tid; i < BUCKETS * ROWS; i += THREADS) s.hist[i] = 0;
+  const int rounds = (U + THREADS - 1) / THREADS, rows = rounds * WARPS;
+#pragma unroll 1
+  for (int k = 0; k < rounds; ++k) s.hist[k * THREADS + tid] = 0;
   __syncthreads();
   auto bucket_of = [&](int c) {
     const bool cut = c > cut_above;
@@ -408,19 +411,17 @@ __device__ __noinline__ void plan_sort(Plan& pl, PlanScratch& s, int U, int most
     const uint32_t same = __match_any_sync(0xffffffffu, bucket);
     const int rank = __popc(same & ((1u << lane) - 1u));
     if (u < U) s.rank[u] = rank;
-    if (u < U && rank == 0) s.hist[bucket * ROWS + k * WARPS + warp] = __popc(same);
+    if (u < U && rank == 0) s.hist[bucket * rows + k * WARPS + warp] = __popc(same);
   }
   __syncthreads();
-  constexpr int HPER = (BUCKETS * ROWS + THREADS - 1) / THREADS;
-  int mine = 0, total;
-  for (int i = 0; i < HPER; ++i)
-    if (tid * HPER + i < BUCKETS * ROWS) mine += s.hist[tid * HPER + i];
+  int mine = 0, total;  // thread i has the counts [i * rounds, (i + 1) * rounds)
+#pragma unroll 1
+  for (int i = 0; i < rounds; ++i) mine += s.hist[tid * rounds + i];
   int run = block_excl_scan(mine, s.tot[2], &total);
-  for (int i = 0; i < HPER; ++i) {
-    const int at = tid * HPER + i;
-    if (at >= BUCKETS * ROWS) break;
-    const int h = s.hist[at];
-    s.hist[at] = run;
+#pragma unroll 1
+  for (int i = 0; i < rounds; ++i) {
+    const int h = s.hist[tid * rounds + i];
+    s.hist[tid * rounds + i] = run;
     run += h;
   }
   __syncthreads();
@@ -428,7 +429,7 @@ __device__ __noinline__ void plan_sort(Plan& pl, PlanScratch& s, int U, int most
   for (int k = 0; k * THREADS < U; ++k) {
     const int u = k * THREADS + tid;
     if (u >= U) break;
-    const int at = s.hist[bucket_of(s.steps[u]) * ROWS + k * WARPS + warp] + s.rank[u];
+    const int at = s.hist[bucket_of(s.steps[u]) * rows + k * WARPS + warp] + s.rank[u];
     pl.seq[at] = s.seq[u];
     pl.steps[at] = s.steps[u];
   }
@@ -583,7 +584,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
   // items before each entry
   const int* steps = sorted ? pl.steps : s.steps;
   int mine = 0, cut = 0;
-  const int at0 = tid * PLAN_PER, at1 = min(U, at0 + PLAN_PER);
+  const int per = U <= THREADS ? 1 : PLAN_PER, at0 = tid * per, at1 = min(U, at0 + per);
 #pragma unroll 1
   for (int at = at0; at < at1; ++at) {
     const int c = steps[at], n = pieces_of(c, share, cut_above);
@@ -602,8 +603,8 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
       pl.seq[at] = job;
       pl.steps[at] = c;
     }
-    if (t_own >= run && t_own < run + n * p.kv_heads) 
-      make_item(p, own, sequence(p, job >> 16), width, job & 0xffff, c, n, t_own - run, t_own);
+    if (t_own >= run && t_own < run + n * p.kv_heads)
+      make_item(p, own, known ? s.of[job >> 16] : sequence(p, job >> 16), width, job & 0xffff, c, n, t_own - run, t_own);
     run += n * p.kv_heads;
   }
   cut = __reduce_max_sync(0xffffffffu, lane < WARPS ? s.cut[lane] : 0);
