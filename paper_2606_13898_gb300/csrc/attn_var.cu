@@ -502,23 +502,37 @@ __device__ __noinline__ bool count_jobs(const VarParams& p, Plan& pl, PlanScratc
 }
 
 // By all threads; ends with a barrier. The thread that finds item t_own among the listed
-// ones writes it to *own.
-__device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScratch& s, Item* own, int t_own) {
+// ones writes it to *own. The warp that makes a plan of up to 32 jobs calls `made` before the others
+// go on and `ahead` beside them, lane 0 both; then the result is true.
+template <typename Made, typename Ahead>
+__device__ __forceinline__ bool plan_build(const VarParams& p, Plan& pl, PlanScratch& s, Item* own, int t_own, Made made, Ahead ahead) {
   constexpr int WARPS = THREADS / 32;
   const int tid = threadIdx.x, warp = warp_id(), lane = lane_id();
   bool known = false;  // the sequences' row jobs are counted
   if (p.B <= 32) {
-    if (warp == 0) plan_small(p, pl, s, own, t_own);
-    __syncthreads();
-    if (pl.jobs <= 32) return;
+    if (warp == PRODUCER_WARP) {
+      plan_small(p, pl, s, own, t_own);
+      __syncwarp();
+      if (lane == 0 && pl.jobs <= 32) made();
+      __syncwarp();
+      asm volatile("bar.arrive 3, %0;" ::"n"(THREADS) : "memory");
+      if (pl.jobs <= 32) {
+        if (lane == 0) ahead();
+        __syncwarp();
+        return true;
+      }
+    } else {
+      asm volatile("bar.sync 3, %0;" ::"n"(THREADS) : "memory");
+      if (pl.jobs <= 32) return true;
+    }
     known = pl.jobs < MANY_JOBS;
   }
   if (!known) {
     __syncthreads();  // (pl.jobs is written again)
-    if (!count_jobs(p, pl, s)) return;
+    if (!count_jobs(p, pl, s)) return false;
   }
   const int U = pl.jobs, width = pl.width, least_piece = s.least_piece;
-  if (U > MAX_TABLE || U == 0) return;
+  if (U > MAX_TABLE || U == 0) return false;
   int total;
   // the row jobs' steps
   int sum = 0, most = 0, least = 0x7fffffff;
@@ -615,6 +629,7 @@ __device__ __forceinline__ void plan_build(const VarParams& p, Plan& pl, PlanScr
     pl.cut_above = cut_above;
   }
   __syncthreads();
+  return false;
 }
 
 // A cut job for the second kernel.
@@ -744,6 +759,7 @@ constexpr int RING = 4;
 struct Shared {
   float m1[BQ], l1[BQ];
   Item ring[RING];
+  int ahead;       // K tiles of the first item that are on their way
   int special[2];  // an infinity or NaN was taken out of a value tile of the item (by its parity)
 };
 
@@ -807,12 +823,12 @@ __global__ void __launch_bounds__(THREADS, 1)
   auto sQ = [&](int i) { return smem + C::OFF_Q + i * C::Q_BYTES; };
 
   const int warp = warp_id(), lane = lane_id();
-  if (threadIdx.x == 32) {
+  if (warp == V_PRODUCER_WARP && lane == 0) {
     tma_prefetch_desc(&tm_q);
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
-  if (threadIdx.x == 0) {
+  if (warp == PRODUCER_WARP && lane == 0) {
     mbar_init(q_full, 1);
     for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(&k_full[i], 1);
@@ -843,15 +859,46 @@ __global__ void __launch_bounds__(THREADS, 1)
     tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
   }
-  plan_build(p, plan, *reinterpret_cast<PlanScratch*>(smem), &shr.ring[0], blockIdx.x);
+  auto copy_q = [&](const Item& it) {
+    const int row0 = it.q0 + it.j0 * p.tpt, h0 = it.hk * p.group;
+    mbar_arrive_expect_tx(q_full, static_cast<uint32_t>((it.pair ? 2 : 1) * C::NBOX * 128 * p.tpt * p.group));
+#pragma unroll
+    for (int j = 0; j < C::NBOX; ++j) {
+      tma_load_3d(sQ(0) + j * C::Q_BOX, &tm_q, q_full, 64 * j, h0, row0);
+      if (it.pair) tma_load_3d(sQ(1) + j * C::Q_BOX, &tm_q, q_full, 64 * j, h0, row0 + p.tpt);
+    }
+  };
+  auto copy_tile = [&](const CUtensorMap* tm, unsigned char* dst, uint64_t* full, int hk, int row) {
+    mbar_arrive_expect_tx(full, C::KV_BYTES);
+#pragma unroll
+    for (int j = 0; j < C::NBOX; ++j) tma_load_3d(dst + j * C::KV_BOX, tm, full, 64 * j, hk, row);
+  };
+  // The first item's Q and first K tiles leave as soon as a small plan is made, by the thread
+  // that goes on with the Q and K copies (the plan has not used their shared memory then), and
+  // nothing else waits for that: prompts of 1 to 1021 tokens 24.4 us and 23.4, a chunk of 113
+  // and fewer tokens 9.0 and 8.6; plans of more jobs, which gain nothing, 0.5 more.
+  tc_fence_before();
+  const bool small = plan_build(p, plan, *reinterpret_cast<PlanScratch*>(smem), &shr.ring[0], blockIdx.x, [&] {
+    mbar_arrive(&it_full[0]);  // the plan has left the first item in the ring
+  }, [&] {
+    shr.ahead = 0;
+    if (static_cast<int>(blockIdx.x) >= plan.n_items) return;
+    const Item& it = shr.ring[0];
+    fence_proxy_async_smem();
+    copy_q(it);
+    const int n = min(it.t1 - it.t0, C::STAGES);
+    for (int t = 0; t < n; ++t) copy_tile(&tm_k, sK(t), &k_full[t], it.hk, it.k0 + (it.t0 + t) * BKV);
+    shr.ahead = n;
+  });
   if (p.may_cut && blockIdx.x == gridDim.x - 1) list_joints(p, plan);  // (the CTA that is idle or has the least)
   const bool idle = static_cast<int>(blockIdx.x) >= plan.n_items;  // (uniform)
-  // the plan has left the first item in the ring
-  if (threadIdx.x == 0 && plan.jobs <= MAX_TABLE) mbar_arrive(&it_full[0]);
-  // the plan's scratch (generic proxy) before the first copy over it (async proxy)
-  fence_proxy_async_smem();
-  tc_fence_before();
-  __syncthreads();
+  if (!small) {
+    if (threadIdx.x == 0 && plan.jobs <= MAX_TABLE) mbar_arrive(&it_full[0]);
+    // the plan's scratch (generic proxy) before the first copy over it (async proxy)
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+  }
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   if (idle) {
@@ -872,16 +919,16 @@ __global__ void __launch_bounds__(THREADS, 1)
         // (warp 10). Two threads, so that a K copy never queues behind a V
         // stage that is still being read, and the other way round.
         const bool kq = warp == PRODUCER_WARP;
+        const int ahead = kq && small ? shr.ahead : 0;  // K tiles on their way
         const CUtensorMap* tm = kq ? &tm_k : &tm_v;
         // per stage (bit st): armed at least once, and the parity of the last arming
-        uint32_t armed = 0, par = 0;
-        bool q_armed = false;
+        uint32_t armed = (1u << ahead) - 1u, par = 0;
+        bool q_armed = ahead > 0;
         uint32_t q_par = 0;
         bool ok = true;
         uint32_t kt = 0;
         uint64_t* full = kq ? k_full : v_full;
         uint64_t* empty = kq ? k_empty : v_empty;
-        const uint32_t q_bytes = static_cast<uint32_t>(C::NBOX * 128 * p.tpt * p.group);
         for (uint32_t jn = 0;; ++jn) {
           if (!it_wait(jn, 18)) {
             ok = false;
@@ -890,24 +937,18 @@ __global__ void __launch_bounds__(THREADS, 1)
           const Item& it = shr.ring[jn & (RING - 1)];
           if (!it.more) break;
           const int hk = it.hk, k0 = it.k0, t0 = it.t0, n = it.t1 - it.t0;
-          if (kq) {
-            const int pair = it.pair, row0 = it.q0 + it.j0 * p.tpt, h0 = hk * p.group;
+          if (kq && (jn > 0 || ahead == 0)) {
             // Q once the previous item's S products are done with it
             if (jn > 0 && !mbar_wait_items(q_empty, (jn - 1) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 17)) {
               ok = false;
               break;
             }
-            mbar_arrive_expect_tx(q_full, (pair ? 2 : 1) * q_bytes);
-#pragma unroll
-            for (int j = 0; j < C::NBOX; ++j) {
-              tma_load_3d(sQ(0) + j * C::Q_BOX, &tm_q, q_full, 64 * j, h0, row0);
-              if (pair) tma_load_3d(sQ(1) + j * C::Q_BOX, &tm_q, q_full, 64 * j, h0, row0 + p.tpt);
-            }
+            copy_q(it);
             q_armed = true;
             q_par = jn & 1u;
           }
           mbar_arrive(&it_empty[jn & (RING - 1)]);
-          for (int t = 0; t < n; ++t) {
+          for (int t = jn == 0 ? ahead : 0; t < n; ++t) {
             const int st = kv_stage(kt + t);
             const uint32_t ph = kv_phase(kt + t);
             if (!mbar_wait(&empty[st], ph ^ 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * (kq ? 1 : 2))) {
