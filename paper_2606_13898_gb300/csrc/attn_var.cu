@@ -955,11 +955,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               ok = false;
               break;
             }
-            mbar_arrive_expect_tx(&full[st], C::KV_BYTES);
-            unsigned char* dst = kq ? sK(st) : sV(st);
-#pragma unroll
-            for (int j = 0; j < C::NBOX; ++j)
-              tma_load_3d(dst + j * C::KV_BOX, tm, &full[st], 64 * j, hk, k0 + (t0 + t) * BKV);
+            copy_tile(tm, kq ? sK(st) : sV(st), &full[st], hk, k0 + (t0 + t) * BKV);
             armed |= 1u << st;
             par = (par & ~(1u << st)) | (ph << st);
           }
