@@ -299,7 +299,7 @@ struct PlanScratch {
 };
 
 // The plan of up to 32 row jobs of up to 32 sequences, by one warp without a barrier: a lane per
-// sequence, then per row job. (The CTA's way to the same plan takes 4000 to 5000
+// sequence, then per row job. (The CTA's way to the same plan takes 5000 to 6000
 // cycles of barriers and shared memory, a third of the shortest calls.) More row jobs than
 // that: it leaves what it knows of the sequences.
 constexpr int MANY_JOBS = 1 << 25;  // of a sequence: not counted exactly here
