@@ -1419,7 +1419,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (it.slot >= 0) {
             // a piece: unnormalised rows, their maxima and sums
             const long long at = (static_cast<long long>(it.slot) * 2 + (pair ? i : 0)) * BQ + row;
-            p.part_ml[at] = make_float2(m, l);
+            p.part_ml[at] = make_float2(m, n > 0 ? l : -1.f);  // -1: no rows (a sum is not below 0)
             if (n > 0) {
 #pragma unroll 1
               for (int c = 0; c < HD / 32; ++c) {
@@ -1554,17 +1554,21 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
       float o[COLS] = {}, total = 0.f;
       for (int q0 = 0; q0 < j.pieces; q0 += 32) {
         float a = 0.f;
+        bool there = false;  // the piece left rows; their weight may be 0, which leaves an infinity or a NaN a NaN
         if (q0 + lane < j.pieces) {
           const float2 ml = p.part_ml[row_of(q0 + lane)];
-          // a piece in which the row saw nothing has no rows to read
-          a = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.x == M ? 1.f : ex2(ml.x - M);
-          total = fmaf(a, ml.y, total);
+          there = !(ml.y < 0.f);
+          if (there) {
+            a = ml.x == M ? 1.f : ex2(ml.x - M);
+            total = fmaf(a, ml.y, total);
+          }
         }
+        const uint32_t left = __ballot_sync(0xffffffffu, there);
         const int most = min(32, j.pieces - q0);
 #pragma unroll 4
         for (int q = 0; q < most; ++q) {
           const float f = __shfl_sync(0xffffffffu, a, q);
-          if (f == 0.f) continue;
+          if (!(left >> q & 1u)) continue;
           const float* src = p.part + (row_of(q0 + q) - r) * HD + (lane * COLS / 8 * (8 * BQ) + 8 * r + lane * COLS % 8);
           if (COLS == 4) {
             const float4 v = *reinterpret_cast<const float4*>(src);

@@ -306,3 +306,62 @@ def test_no_keys_at_all(H):
     zero = torch.zeros(2, dtype=torch.int32, device="cuda")
     assert bool((call(H, q, k[:0], v[:0], cu_q, zero, 0) == 0).all())
     assert bool(call(H, q, k, v, zero, zero, 0).isnan().all())
+
+
+def single(hd, lk, low, seed, causal):
+    """One query over lk keys in 2 key heads, the first `low` of them with logits of 200 below the others'."""
+    q, k, v, cu_q, cu_k = make([1], [lk], 8, 2, hd, "bf16", seed=seed)
+    q[:, :, 0], k[:, :, 0] = math.sqrt(hd), 0  # (the logit of channel 0 is k's)
+    k[:low, :, 0] = -200
+    return q, k, v, cu_q, cu_k
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_seen_values_of_no_weight(H, hd, causal):
+    """Infinities and NaNs that a query sees with a probability below the smallest fp32 number: 0 times them is NaN,
+    whether the sequence is cut into pieces, is one job among many, or its steps follow one another."""
+    lk, low, copies = 1300, 700, 200
+    q, k, v, cu_q, cu_k = single(hd, lk, low, hd + causal, causal)
+    clean = reference(q, k, v, cu_q, cu_k, causal)
+    v[10, :, 5], v[300, :, 9], v[650, 1, 33] = math.nan, math.inf, -math.inf
+    bad = torch.zeros(8, hd, dtype=torch.bool, device="cuda")
+    bad[:, 5] = bad[:, 9] = bad[4:, 33] = True
+    cut = call(H, q, k, v, cu_q, cu_k, causal)                      # 2 jobs on 152 CTAs: pieces
+    many = [torch.arange(copies + 1, dtype=torch.int32, device="cuda") * n for n in (1, lk)]
+    whole = call(H, *(x.repeat(copies, 1, 1) for x in (q, k, v)), *many, causal)  # 400 equal jobs: none is cut
+    H.hilo_sync_status()
+    for got in [cut[0], *whole]:
+        assert torch.equal(~got.isfinite(), bad)
+        fine = torch.where(bad, clean[0][0].to(got.dtype), got)[None]
+        check(fine, clean, "bf16")
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("lq,lk,heads", [([300], [300], 2), ([90], [1400], 4), ([1], [500], 4), ([200, 130], [450, 130], 12)])
+def test_infinities_and_nans_of_heads_of_64(H, dtype, causal, lq, lk, heads):
+    """As test_infinities_and_nans_of_unseen_keys; without an order every query sees every key of its sequence."""
+    q, k, v, cu_q, cu_k = make(lq, lk, heads, 2, 64, dtype, first=2, spare=6, seed=15)
+    k[:2], v[:2], k[-6:], v[-6:] = math.nan, math.inf, math.nan, math.nan
+    base = call(H, q, k, v, cu_q, cu_k, causal)
+    sound = [x.clone() for x in (k, v)]
+    for x in sound:
+        x[:2], x[-6:] = 0, 0
+    check(base, reference(q, *sound, cu_q, cu_k, causal), dtype)
+    marks = ((0, 5, math.inf), (1, 40, math.nan), (37, 9, -math.inf), (64, 63, math.inf), (129, 20, math.nan))
+    ends, q_ends = cu_k.tolist()[1:], cu_q.tolist()
+    for end, n in zip(ends, lk):
+        for back, col, value in marks:
+            if back < n:
+                v[end - 1 - back, :, col] = value
+    got = call(H, q, k, v, cu_q, cu_k, causal)
+    H.hilo_sync_status()
+    for b, (n_q, n_k) in enumerate(zip(lq, lk)):
+        for i in range(n_q):
+            hidden = n_q - 1 - i if causal else 0  # keys from the end that query i does not see
+            row, want = got[q_ends[b] + i].float(), base[q_ends[b] + i].float().clone()
+            for back, col, value in marks:
+                if hidden <= back < n_k:
+                    want[:, col] = value
+            assert torch.equal(row.nan_to_num(7e4, 8e4, 9e4), want.nan_to_num(7e4, 8e4, 9e4)), (b, i)
