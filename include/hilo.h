@@ -666,7 +666,9 @@ size_t hilo_attention_workspace_bytes(const hilo_attn_shape* shape);
  *               aligned; nothing in it has to be set. Calls that may overlap
  *               on the device need workspaces of their own.
  * Logits, maxima and sums are fp32; probabilities enter the product with v in
- * the dtype; the result is rounded once. A call repeats itself bit for bit.
+ * the dtype (of HILO_F16 in steps of 2^-31 of the row's largest one where they
+ * are below 2^-21 of it); the result is rounded once. A call repeats itself bit
+ * for bit.
  */
 int hilo_attention(const hilo_attn_shape* shape, const int32_t* cu_q, const int32_t* cu_k, const void* q,
                    const void* k, const void* v, void* out, void* ws, size_t ws_bytes, void* stream);

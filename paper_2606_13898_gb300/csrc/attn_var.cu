@@ -69,6 +69,11 @@ constexpr int ITEM_WARP = 11;
 constexpr uint32_t SOFTMAX_REGS = 232;
 constexpr uint32_t CONTROL_REGS = 40;
 constexpr float RESCALE_LOG2 = 8.0f;
+// Probabilities are 2^(x - m), m the running maximum less this: fp16 ones begin at 2^7, so that
+// with the 2^8 which the maximum may lag behind they end at 2^15, and what is lost below fp16's
+// smallest number is 2^-32 of the largest one, not 2^-25. bf16 has fp32's exponents.
+template <bool F16>
+constexpr float P_ABOVE_LOG2 = F16 ? 7.0f : 0.0f;
 
 struct VarParams {
   const int32_t *cu_q, *cu_k;
@@ -1308,7 +1313,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int u = 0; u < 8; ++u) mx8[u] = fmax3(mx8[u], sv[j + u], sv[j + 8 + u]);
         const float mx = fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]),
                                fmaxf(mx8[6], mx8[7]));
-        const float m_tile = mx * p.scale_log2;
+        const float m_tile = mx * p.scale_log2 - P_ABOVE_LOG2<F16>;
         bool rescale = false;
         float m_use = m;
         if (s == 0) {
@@ -1349,7 +1354,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         rescale_o(rescale, m_use);
         m = m_use;
         l += lsum;
-        // P_i as 16-bit pairs (keys 2c, 2c+1 in column c), the A operand of the PV product
+        // P_i as 16-bit pairs (keys 2c, 2c+1 in column c), the A operand of the PV product: one
+        // rounding each, which the product's operands cannot do without; the sum keeps 32 bits
 #pragma unroll
         for (int h2 = 0; h2 < BKV / 64; ++h2) {
           float pk[32];

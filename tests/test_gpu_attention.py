@@ -365,3 +365,21 @@ def test_infinities_and_nans_of_heads_of_64(H, dtype, causal, lq, lk, heads):
                 if hidden <= back < n_k:
                     want[:, col] = value
             assert torch.equal(row.nan_to_num(7e4, 8e4, 9e4), want.nan_to_num(7e4, 8e4, 9e4)), (b, i)
+
+
+@pytest.mark.parametrize("lq,hd", [(1, 64), (1, 128), (200, 64), (200, 128)])
+def test_small_probabilities_in_f16(H, lq, hd):
+    """Many keys of 2^-26.5 of the largest probability each: below fp16's smallest number, but together all there is of the
+    result. Probabilities are held against 2^7 or more for the largest, so a key is off by at most half of 2^-24 / 2^7."""
+    lk = 512
+    q, k, v, cu_q, cu_k = make([lq], [lk], 4, 2, hd, "f16")
+    q[:], k[:], v[:] = 0, 0, 49152
+    q[:, :, 0] = 1
+    for top in (0, 128):  # the largest in both halves of the keys
+        k[top, :, 0], v[top] = 18.375, 0
+    o, mag, keys = reference(q, k, v, cu_q, cu_k, 0, scale=1.0)
+    got = call(H, q, k, v, cu_q, cu_k, 0, scale=1.0).double()
+    u = 2.0 ** -11
+    tol = (u + 2.0 ** -13) * mag + u * o.abs() + keys * 2.0 ** -32 * 49152
+    assert 0.1 < float(o.min()) and float((tol / o).max()) < 0.05
+    assert bool(((got - o).abs() <= tol).all()), float(got.min())
