@@ -133,7 +133,10 @@ __device__ __forceinline__ Seq sequence(const VarParams& p, int b) {
 // A row job is a job of one sequence for all its key heads. Up to MAX_TABLE
 // row jobs are listed; the items of an entry are its key heads' jobs, or their
 // pieces. More row jobs than that are taken as they come, the last of each
-// sequence first, and never cut: every CTA then has dozens.
+// sequence first: MAX_TABLE * kv_heads / G items per CTA and more, which is 6 with
+// one key head. So of them, too, those that are longer than a share are listed, their pieces
+// ahead of all others (cut_longest: 1100 single tokens, one over 131072 keys and the
+// others over up to 200, 784 us without, 82 so).
 //
 // Cutting: J jobs of T steps together on G CTAs, pieces of at most `share`
 // steps. An item costs about ITEM_STEPS more than its steps (copies to wait for,
@@ -167,11 +170,20 @@ constexpr int BUCKETS = 32;  // 16 of cut jobs, 16 of whole ones
 
 struct Plan {
   int first[MAX_SEQ + 1];  // row jobs before sequence b
-  int seq[MAX_TABLE];      // entry: sequence << 16 | row job of it
+  int seq[MAX_TABLE];      // entry: sequence << 16 | row job of it (of more than MAX_TABLE: counted from its last)
   int steps[MAX_TABLE];
   int items[MAX_TABLE];    // items before the entry
   int width;  // tiles of a job at most
   int jobs, n_items, n_cut, share, cut_above;  // row jobs, items, entries that may be cut (the first ones)
+  // Entries and their items, the first ones. More row jobs than MAX_TABLE: what is listed of them, and behind
+  // it an item for every key head of every row job, nothing to do where that is listed.
+  __device__ __forceinline__ bool whole() const { return jobs <= MAX_TABLE; }
+  __device__ __forceinline__ int entries() const { return whole() ? jobs : n_cut; }
+  __device__ __forceinline__ int entry_items(const VarParams& p) const { return whole() ? n_items : n_items - jobs * p.kv_heads; }
+  __device__ __forceinline__ int row_job(const VarParams& p, const Seq& s, int entry) const {
+    const int i = seq[entry] & 0xffff;
+    return whole() ? i : s.row_jobs(p, width) - 1 - i;
+  }
 };
 static_assert(2 * MIN_STEPS_ROWS >= MIN_STEPS, "may_cut goes by the key tiles of a pair");
 static_assert(MAX_SEQ <= 1 << 15 && MAX_TABLE <= 1 << 16, "an entry's sequence and row job share a word");
@@ -185,7 +197,7 @@ __device__ __forceinline__ int pieces_of(int steps, int share, int cut_above) {
 }
 __device__ __forceinline__ int pieces_of(const Plan& pl, int steps) { return pieces_of(steps, pl.share, pl.cut_above); }
 
-// The plan's larger parts (block_excl_scan, count_jobs, plan_sort, list_joints) are calls of their own,
+// The plan's larger parts (block_excl_scan, count_jobs, cut_longest, plan_sort, list_joints) are calls of their own,
 // made before the warpgroups share out their registers only: setmaxnreg does not know
 // a callee's need.
 
@@ -297,6 +309,7 @@ constexpr int PLAN_PER = (MAX_TABLE + THREADS - 1) / THREADS;
 struct PlanScratch {
   Seq of[32];       // up to 32 sequences
   int least_piece;  // of theirs
+  int lk;           // the longest one's keys
   int tot[4][THREADS / 32];
   int sum[THREADS / 32], most[THREADS / 32], least[THREADS / 32], count[THREADS / 32], cut[THREADS / 32];
   int seq[MAX_TABLE], steps[MAX_TABLE], rank[MAX_TABLE];  // in the order of the sequences
@@ -313,7 +326,8 @@ __device__ __forceinline__ void plan_small(const VarParams& p, Plan& pl, PlanScr
   const int lane = lane_id();
   Seq s = {0, 0, 0, 0};
   if (lane < p.B) s = sequence(p, lane);
-  const int width = job_width(p, __reduce_add_sync(ALL, min(s.tiles(p), MANY_TILES)), __reduce_max_sync(ALL, s.lk));
+  const int lk = __reduce_max_sync(ALL, s.lk);
+  const int width = job_width(p, __reduce_add_sync(ALL, min(s.tiles(p), MANY_TILES)), lk);
   const int least_piece = min_steps(p, __reduce_max_sync(ALL, s.lq));
   const int mine = min(s.row_jobs(p, width), MANY_JOBS), incl = warp_incl_scan(mine), first = incl - mine;
   const int U = __shfl_sync(ALL, incl, 31);
@@ -328,6 +342,7 @@ __device__ __forceinline__ void plan_small(const VarParams& p, Plan& pl, PlanScr
     }
     if (lane == 0) {
       sc.least_piece = least_piece;
+      sc.lk = lk;
       pl.first[p.B] = U;
       pl.n_items = U * p.kv_heads;  // (of a plan without a table)
       pl.n_cut = 0;
@@ -495,6 +510,7 @@ __device__ __noinline__ bool count_jobs(const VarParams& p, Plan& pl, PlanScratc
   const int U = before;
   if (tid == 0) {
     s.least_piece = least_piece;
+    s.lk = lk;
     pl.first[p.B] = U;
     pl.jobs = U;
     pl.width = width;
@@ -504,6 +520,91 @@ __device__ __noinline__ bool count_jobs(const VarParams& p, Plan& pl, PlanScratc
   }
   __syncthreads();
   return true;
+}
+
+// Of more row jobs than MAX_TABLE, those that are longer than a CTA's share by more than
+// ITEM_STEPS: listed with their pieces. A sequence's jobs are of one length, or grow evenly
+// towards its last one, which gives the steps of all of them closely enough for a share; the
+// long ones are looked for from the last (which may be a single of half the steps of the pair
+// before it). By all threads; ends with a barrier.
+__device__ __noinline__ void cut_longest(const VarParams& p, Plan& pl, PlanScratch& s) {
+  constexpr int WARPS = THREADS / 32;
+  constexpr uint32_t ALL = 0xffffffffu;
+  const int tid = threadIdx.x, warp = warp_id(), lane = lane_id(), width = pl.width, G = p.grid;
+  const float J = static_cast<float>(pl.jobs) * static_cast<float>(p.kv_heads);
+  // (what nothing can be longer than, if each had a single step: 1100 tokens over up to 200 keys 39.6 us without, 38.8 so)
+  if ((s.lk + BKV - 1) / BKV <= share_of_many(J, J, G, s.least_piece) + ITEM_STEPS) return;
+  float T = 0.f;
+  int most = 0;
+#pragma unroll 1
+  for (int b = tid; b < p.B; b += THREADS) {
+    const Seq q = sequence(p, b);
+    const int nt = q.tiles(p), n = q.row_jobs(p, width);
+    if (n == 0) continue;
+    const int last = q.steps(p, width, nt, n - 1);
+    most = max(most, last);
+    T += static_cast<float>(last);
+    if (n == 1) continue;
+    const int before = q.steps(p, width, nt, n - 2);
+    most = max(most, before);
+    // (the first ones of more queries than keys see nothing, and are of one step)
+    const int none = p.causal ? min(n - 2, max(0, q.lq - q.lk) / (width * p.tpt)) : 0;
+    T += static_cast<float>(none) + 0.5f * static_cast<float>(n - 1 - none) * static_cast<float>(q.steps(p, width, nt, none) + before);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) T += __shfl_xor_sync(ALL, T, off);
+  most = __reduce_max_sync(ALL, most);
+  if (lane == 0) {
+    s.sum[warp] = __float_as_int(T);
+    s.most[warp] = most;
+  }
+  __syncthreads();
+  T = lane < WARPS ? __int_as_float(s.sum[lane]) : 0.f;
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) T += __shfl_xor_sync(ALL, T, off);
+  T = fminf(__shfl_sync(ALL, T, 0) * static_cast<float>(p.kv_heads), 1e9f * static_cast<float>(G));
+  most = __reduce_max_sync(ALL, lane < WARPS ? s.most[lane] : 0);
+  const int share = share_of_many(T, J, G, s.least_piece), cut_above = share + ITEM_STEPS;
+  if (most <= cut_above) return;  // (the plan is written by no thread, and s by none behind the barrier)
+  int listed = 0, total;
+#pragma unroll 1
+  for (int b0 = 0; b0 < p.B; b0 += THREADS) {
+    const int b = b0 + tid;
+    Seq q = {0, 0, 0, 0};
+    if (b < p.B) q = sequence(p, b);
+    const int nt = q.tiles(p), n = q.row_jobs(p, width);
+    const int skip = n > 0 && q.steps(p, width, nt, n - 1) <= cut_above ? 1 : 0;
+    int longs = 0;
+#pragma unroll 1
+    while (longs + skip < n && longs <= MAX_TABLE && q.steps(p, width, nt, n - 1 - skip - longs) > cut_above) ++longs;
+    const int at = listed + block_excl_scan(longs, s.tot[(b0 / THREADS) & 1], &total);
+    listed += total;
+#pragma unroll 1
+    for (int e = 0; e < longs && at + e < MAX_TABLE; ++e) {
+      pl.seq[at + e] = b << 16 | (skip + e);
+      pl.steps[at + e] = q.steps(p, width, nt, n - 1 - skip - e);
+    }
+  }
+  if (listed > MAX_TABLE) return;
+  __syncthreads();
+  int mine = 0;
+  const int at0 = min(listed, tid * PLAN_PER), at1 = min(listed, at0 + PLAN_PER);
+#pragma unroll 1
+  for (int at = at0; at < at1; ++at) mine += pieces_of(pl.steps[at], share, cut_above) * p.kv_heads;
+  int run = block_excl_scan(mine, s.tot[3], &total);
+#pragma unroll 1
+  for (int at = at0; at < at1; ++at) {
+    pl.items[at] = run;
+    run += pieces_of(pl.steps[at], share, cut_above) * p.kv_heads;
+  }
+  // (as in the table fewer than 2G, T being what it is, but the workspace has no more)
+  if (tid == 0 && total <= SLOTS_PER_CTA * G) {
+    pl.n_items = total + pl.jobs * p.kv_heads;
+    pl.n_cut = listed;
+    pl.share = share;
+    pl.cut_above = cut_above;
+  }
+  __syncthreads();
 }
 
 // By all threads; ends with a barrier. The thread that finds item t_own among the listed
@@ -537,6 +638,7 @@ __device__ __forceinline__ bool plan_build(const VarParams& p, Plan& pl, PlanScr
     if (!count_jobs(p, pl, s)) return false;
   }
   const int U = pl.jobs, width = pl.width, least_piece = s.least_piece;
+  if (U > MAX_TABLE && p.may_cut) cut_longest(p, pl, s);
   if (U > MAX_TABLE || U == 0) return false;
   int total;
   // the row jobs' steps
@@ -658,30 +760,33 @@ __device__ __noinline__ void list_joints(const VarParams& p, const Plan& pl) {
     const int at = e / p.kv_heads, hk = e - at * p.kv_heads, n = pieces_of(pl, pl.steps[at]);
     if (n == 1) continue;
     const Seq s = sequence(p, pl.seq[at] >> 16);
-    p.joints->job[atomicAdd(&p.joints->n, 1)] = {s.q0, s.lq, s.lk, hk, pl.width * (pl.seq[at] & 0xffff) * p.tpt,
+    p.joints->job[atomicAdd(&p.joints->n, 1)] = {s.q0, s.lq, s.lk, hk, pl.width * pl.row_job(p, s, at) * p.tpt,
                                                  pl.items[at] + hk * n, n, pl.width};
   }
 }
 
 // ------------------------------------------------------------------- items --
 
-__device__ __forceinline__ void item_at(const VarParams& p, const Plan& pl, int t, Item* out) {
+// False where item t is nothing to do.
+__device__ __forceinline__ bool item_at(const VarParams& p, const Plan& pl, int t, Item* out) {
   if (t >= pl.n_items) {
     out->more = 0;
-    return;
+    return true;
   }
-  if (pl.jobs <= MAX_TABLE) {
-    int lo = 0, hi = pl.jobs;
+  const int in_entries = pl.entry_items(p);
+  if (t < in_entries) {
+    int lo = 0, hi = pl.entries();
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (pl.items[mid] <= t) lo = mid;
       else hi = mid;
     }
     const int steps = pl.steps[lo];
-    make_item(p, out, sequence(p, pl.seq[lo] >> 16), pl.width, pl.seq[lo] & 0xffff, steps, pieces_of(pl, steps), t - pl.items[lo], t);
-    return;
+    const Seq s = sequence(p, pl.seq[lo] >> 16);
+    make_item(p, out, s, pl.width, pl.row_job(p, s, lo), steps, pieces_of(pl, steps), t - pl.items[lo], t);
+    return true;
   }
-  const int v = t / p.kv_heads, u = pl.jobs - 1 - v;
+  const int r = t - in_entries, v = r / p.kv_heads, u = pl.jobs - 1 - v;
   int lo = 0, hi = p.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -690,7 +795,10 @@ __device__ __forceinline__ void item_at(const VarParams& p, const Plan& pl, int 
   }
   const int i = u - pl.first[lo];
   const Seq s = sequence(p, lo);
-  make_item(p, out, s, pl.width, i, s.steps(p, pl.width, s.tiles(p), i), 1, t - v * p.kv_heads, t);
+  const int steps = s.steps(p, pl.width, s.tiles(p), i);
+  if (steps > pl.cut_above) return false;
+  make_item(p, out, s, pl.width, i, steps, 1, r - v * p.kv_heads, t);
+  return true;
 }
 
 // Item k of CTA x of G, of n: every other round in reverse order; of few rounds the third
@@ -898,7 +1006,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (p.may_cut && blockIdx.x == gridDim.x - 1) list_joints(p, plan);  // (the CTA that is idle or has the least)
   const bool idle = static_cast<int>(blockIdx.x) >= plan.n_items;  // (uniform)
   if (!small) {
-    if (threadIdx.x == 0 && plan.jobs <= MAX_TABLE) mbar_arrive(&it_full[0]);
+    if (threadIdx.x == 0 && plan.whole()) mbar_arrive(&it_full[0]);
     // the plan's scratch (generic proxy) before the first copy over it (async proxy)
     fence_proxy_async_smem();
     tc_fence_before();
@@ -1153,13 +1261,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
     } else if (warp == ITEM_WARP && lane == 0) {
       // ---------------- warp 11, one lane: the CTA's items, ahead of their use
-      for (uint32_t jn = 0;; ++jn) {
+      int k = plan.whole() ? 1 : 0;  // (of a whole table item 0 is there already)
+      for (uint32_t jn = static_cast<uint32_t>(k);; ++jn) {
         const int slot = jn & (RING - 1);
         if (jn >= RING &&
             !mbar_wait_items(&it_empty[slot], ((jn - RING) / RING) & 1u, abort_flag, err, DEV_TIMEOUT_ATTN + 256 * 20))
           break;
-        if (jn == 0 && plan.jobs <= MAX_TABLE) continue;  // there already
-        item_at(p, plan, item_index(static_cast<int>(jn), blockIdx.x, gridDim.x, plan.n_items), &shr.ring[slot]);
+        while (!item_at(p, plan, item_index(k, blockIdx.x, gridDim.x, plan.n_items), &shr.ring[slot])) ++k;
+        ++k;
         mbar_arrive(&it_full[slot]);
         if (!shr.ring[slot].more) break;
       }

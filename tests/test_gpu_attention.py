@@ -383,3 +383,56 @@ def test_small_probabilities_in_f16(H, lq, hd):
     tol = (u + 2.0 ** -13) * mag + u * o.abs() + keys * 2.0 ** -32 * 49152
     assert 0.1 < float(o.min()) and float((tol / o).max()) < 0.05
     assert bool(((got - o).abs() <= tol).all()), float(got.min())
+
+
+def test_one_long_context_among_more_sequences_than_the_table_lists(H):
+    """1100 single tokens, one of them over a long context: that one is cut into pieces as it is among 1000, and not the
+    work of a single CTA. Right in either case, and of about the same time (a tenth more sequences; uncut the long one
+    alone takes some ten times the call)."""
+    def one(n, causal=1):
+        lk = [1 + (37 * i) % 200 for i in range(n)]
+        lk[n // 3] = 131072
+        return make([1] * n, lk, 4, 1, 128, "bf16", seed=n)
+
+    def time(args):
+        ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+        out = torch.full(args[0].shape, math.nan, dtype=torch.bfloat16, device="cuda")
+        best = math.inf
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            call(H, *args, out=out, ws=ws)
+            a.record()
+            for _ in range(5):
+                call(H, *args, out=out, ws=ws)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b) / 5)
+        H.hilo_sync_status()
+        return best, out
+
+    few, many = one(1000), one(1100)
+    t_few, out = time(few)
+    check(out, reference(*few, 1), "bf16")
+    t_many, out = time(many)
+    check(out, reference(*many, 1), "bf16")
+    assert t_many < 3 * t_few, (t_few, t_many)
+
+
+BEYOND = [
+    # lq, lk, heads, kv heads, head_dim, causal, dtype: more than 1024 row jobs, some longer than a CTA's share
+    ([1] * 1500, [90 + i % 300 for i in range(1499)] + [40000], 4, 2, 64, 1, "bf16"),
+    ([1] * 2000, [60000] + [1 + i % 90 for i in range(1998)] + [30000], 3, 1, 128, 0, "f16"),
+    ([1, 0] * 1200, [5 if i % 800 else 20000 for i in range(2400)], 2, 1, 128, 1, "bf16"),
+    ([1200] * 9 + [200, 3], [1200] * 9 + [9000, 70000], 128, 1, 64, 1, "bf16"),   # few sequences of many tiles
+    ([700] * 3 + [261], [90] * 3 + [50000], 128, 1, 64, 0, "f16"),                # a pair and a single at a sequence's end
+    ([2] * 1100 + [64], [3] * 1100 + [30000], 4, 1, 64, 1, "bf16"),
+]
+
+
+@pytest.mark.parametrize("lq,lk,heads,kv,hd,causal,dtype", BEYOND)
+def test_long_jobs_beyond_the_table(H, lq, lk, heads, kv, hd, causal, dtype):
+    q, k, v, cu_q, cu_k = make(lq, lk, heads, kv, hd, dtype, first=3, spare=5, seed=len(lq) + sum(lk))
+    got = call(H, q, k, v, cu_q, cu_k, causal)
+    assert torch.equal(got.view(torch.int16), call(H, q, k, v, cu_q, cu_k, causal).view(torch.int16))
+    H.hilo_sync_status()
+    check(got, reference(q, k, v, cu_q, cu_k, causal), dtype)
