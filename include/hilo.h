@@ -631,7 +631,7 @@ int hilo_gate_norm(const hilo_norm_shape* shape, const hilo_norm_vectors* txt, c
  *                    one before it one key less; 0: every query sees every key
  *   dtype            HILO_BF16 or HILO_F16 (q, k, v and out)
  *   rows_q, rows_k   rows of q and out, of k and v
- *   scale            of the logits, > 0 and finite; 0: 1 / sqrt(head_dim)
+ *   scale            of the logits, > 0 and below 2^127; 0: 1 / sqrt(head_dim)
  *   *_row, *_head    strides in elements between the rows and heads of q, k, v
  *                    and out: positive multiples of 8, below 2^39 (of one head
  *                    or one row the stride does not matter, but must be valid).

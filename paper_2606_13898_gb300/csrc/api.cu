@@ -922,7 +922,8 @@ static int check_attn(const hilo_attn_shape* s) {
     return fail(HILO_ERR_SHAPE, "hilo_attention: head_dim=%d must be 64 or 128", s->head_dim);
   if (s->dtype != HILO_BF16 && s->dtype != HILO_F16) return fail(HILO_ERR_ARG, "hilo_attention: dtype=%d", s->dtype);
   if (s->causal & ~1) return fail(HILO_ERR_ARG, "hilo_attention: causal=%d must be 0 or 1", s->causal);
-  if (!(s->scale >= 0.0f) || !is_finite(s->scale)) return fail(HILO_ERR_ARG, "hilo_attention: scale must be finite and >= 0");
+  // (times log2(e) it is finite, too)
+  if (!(s->scale >= 0.0f && s->scale < 0x1p127f)) return fail(HILO_ERR_ARG, "hilo_attention: scale must be in [0, 2^127)");
   const int most = 1 << 30;
   if (s->rows_q < 0 || s->rows_k < 0 || s->rows_q > most || s->rows_k > most)
     return fail(HILO_ERR_SHAPE, "hilo_attention: rows_q=%d and rows_k=%d must be in [0, 2^30]", s->rows_q, s->rows_k);

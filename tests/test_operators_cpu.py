@@ -87,6 +87,14 @@ def test_attention_workspace(H):
     refused(H, call_attn(H, attn(H, out_row=128, out_head=299 * 128)), ARG)
 
 
+def test_attention_scales_that_overflow_in_base_two(H):
+    """The kernel works with scale * log2(e), which has to be finite as well."""
+    for scale in (3.0e38, 2.0 ** 127):
+        refused(H, call_attn(H, attn(H, scale=scale), n=0), ARG)
+    for scale in (1.7e38, 1e-45, 0.0):
+        refused(H, call_attn(H, attn(H, scale=scale), n=0), WORKSPACE)
+
+
 def test_attention_dense_strides(H):
     s = attn(H)
     assert (s.q_row, s.q_head, s.k_row, s.k_head, s.v_row, s.v_head, s.out_row, s.out_head) == (1024, 128, 256, 128, 256, 128,
