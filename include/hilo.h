@@ -552,7 +552,8 @@ typedef struct {
  *   x       device, 16-byte aligned
  *   pos     fp32 [rows, axes] device, any finite values (pooled rows stand
  *           between tokens); the angle is formed and reduced to one turn with
- *           more than 32 bits, so far positions lose nothing
+ *           more than 32 bits: it is off by less than 2^-21 radians up to
+ *           |pos| = 2^24, by about |pos| * 2^-47 beyond
  *   n_rows  device, or NULL for all: the first min(*n_rows, rows) rows are
  *           rotated, y's others are left as they were
  *   y       device, 16-byte aligned; y == x with x's strides rotates in place

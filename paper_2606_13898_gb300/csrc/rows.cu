@@ -314,8 +314,10 @@ __global__ void __maxnreg__((gn_regs(WARP, YM)))
 // The angle in turns is pos * f, f = theta^-p / 2 pi as the sum of two floats
 // (fh, fl): pos * fh is formed exactly as a product and its error, whole turns
 // are taken off the product (exact), then the error and pos * fl are added.
-// What is left is below one turn with an error of a few 1e-8, however far the
-// position; a plain fp32 product at position 30000 is off by 2e-3 radians.
+// What is left is below one turn, with an error below 2^-24 turns up to |pos| = 2^24, the last
+// whole numbers that fp32 tells apart; a plain fp32 product at position 30000 is off by 2e-3
+// radians. Beyond, the error grows with the position: f is known to 2^-46, and the two
+// terms added are no longer small (1e-6 turns at 2^30, 1e-3 at 1e12).
 
 constexpr int RP_MAX_PAIRS = 128;
 constexpr int RP_THREADS = 128;

@@ -185,6 +185,25 @@ def test_rope(H, rows, heads, hd, dims, dtype, inter, per_axis, theta):
     assert torch.equal(z[:, :rows].transpose(0, 1), y[:rows]) and bool(z[:, rows:].isnan().all())
 
 
+@pytest.mark.parametrize("per_axis,theta", [(0, 1e4), (1, 1e4), (1, 1e6), (0, 1.5), (1, 1e30)])
+@pytest.mark.parametrize("inter", [0, 1])
+def test_rope_at_far_positions(H, inter, per_axis, theta):
+    """Positions up to 2^24: the angle is off by less than 2^-21 radians there, beside sine, cosine, products and sum
+    of a few 2^-24; at 2^30 by 2^30 * 2^-47 = 2^-17."""
+    rows, heads, hd, dims = 64, 2, 128, (64, 32, 32)
+    g = gen(inter + per_axis)
+    x = torch.randn(rows, heads, hd, generator=g, device="cuda")
+    sh = H.RopeShape(rows=rows, heads=heads, head_dim=hd, dtype=F32, axis_dims=dims, theta=theta, interleaved=inter,
+                     per_axis=per_axis)
+    for top, off in ((2.0 ** 24, 2.0 ** -20), (2.0 ** 30, 2.0 ** -16)):
+        pos = top * (2 * torch.rand(rows, 3, generator=g, device="cuda") - 1)
+        pos[0], pos[1], pos[2] = top, -top, 0.75 * top + 0.5
+        y = torch.empty_like(x)
+        H.hilo_rope(sh, x, pos, None, y)
+        want, mag = rope_reference(x, pos, dims, theta, inter, per_axis)
+        assert bool(((y.double() - want).abs() <= mag * off + 2.0 ** -24 * want.abs()).all()), float(((y.double() - want).abs() / mag).max())
+
+
 def test_rope_gradient(H):
     """Rotating by the negated positions undoes the rotation and is its gradient: against differences of
     f(x) = sum(w * rope(x)) in fp32, whose rounding is 2^-24 of f per evaluation."""
