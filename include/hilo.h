@@ -535,9 +535,10 @@ typedef struct {
 
 /*
  * Rows of hilo_rope: x and y are [rows, heads, head_dim] with head_dim (a
- * multiple of 8, at most 256) contiguous and strides in elements between rows
- * and heads: positive multiples of 16 bytes. y's rows and heads must not
- * overlap. dtype HILO_BF16, HILO_F16 or HILO_F32.
+ * multiple of 8, at most 256) contiguous, up to 65536 heads, and strides in
+ * elements between rows and heads: positive multiples of 16 bytes, below 2^39
+ * elements. y's rows and heads must not overlap. dtype HILO_BF16, HILO_F16 or
+ * HILO_F32.
  */
 typedef struct {
   int32_t rows, heads, head_dim, dtype;
@@ -623,15 +624,17 @@ int hilo_gate_norm(const hilo_norm_shape* shape, const hilo_norm_vectors* txt, c
 
 /*
  * Sequences of hilo_attention.
- *   B                sequences (>= 1)
- *   heads, kv_heads  heads of q and of k and v; kv_heads divides heads, query
- *                    head i reads key head i / (heads / kv_heads), and heads /
- *                    kv_heads is at most 128
+ *   B                sequences, 1 to 4096
+ *   heads, kv_heads  heads of q (at most 65536) and of k and v; kv_heads divides
+ *                    heads, query head i reads key head i / (heads / kv_heads),
+ *                    and heads / kv_heads is at most 128
  *   head_dim         64 or 128
  *   causal           1: the last query of a sequence sees all its keys, each
  *                    one before it one key less; 0: every query sees every key
  *   dtype            HILO_BF16 or HILO_F16 (q, k, v and out)
- *   rows_q, rows_k   rows of q and out, of k and v
+ *   rows_q, rows_k   rows of q and out, of k and v, at most 2^30 each; with g =
+ *                    heads / kv_heads, (rows_q / floor(128 / g) + B) * kv_heads
+ *                    is at most 2^30
  *   scale            of the logits, > 0 and below 2^127; 0: 1 / sqrt(head_dim)
  *   *_row, *_head    strides in elements between the rows and heads of q, k, v
  *                    and out: positive multiples of 8, below 2^39 (of one head

@@ -579,7 +579,7 @@ static int block_forward_impl(const hilo_shape* shape, const hilo_block_weights*
 
   if (mod) {
     // Each sub-layer's output goes to the buffer of the norm that is no longer
-    // needed, in bf16, as the attention's inputs are: its rounding is 2^-9 of the
+    // needed, in bf16, as the attention's inputs are: its rounding is 2^-8 of the
     // branch, which joins an fp32 residual once, gated. The norm's output then
     // takes the attention's place.
     void* y = ln;

@@ -307,7 +307,7 @@ __global__ void __maxnreg__((gn_regs(WARP, YM)))
 // interleaved, six pieces and 8 CTAs (four and 10 take 12.4 us for the first rows above);
 // split, two pieces of each half and 9 CTAs (three of each half take 27.4 us for the
 // second rows, one and 16 CTAs 26.4; two and 12 spill, and 1415 rows of 16 heads of 128
-// take 5.3 us instead of 4.7). A thread steps through heads and pieces by addition: one
+// take 5.3 us instead of 4.7; rows of a warp spill a little at 9 already, 4 to 16 bytes). A thread steps through heads and pieces by addition: one
 // division per row and piece took 11.5 us for the first rows, and 5.1 us instead of 2.9
 // for 16 rows of 48 heads of 256.
 //
