@@ -1,0 +1,336 @@
+"""Linear layers and the gated feed-forward in 8 bits, as measurable cases.
+
+Three operators, through the binding's public entry points where `own` is true
+and in elementary torch operations where it is not. All hold e4m3 codes with an
+fp32 scale for each block of 128: of one row's 128 columns for activations, of
+128 rows x 128 columns for weights.
+
+  quant  hilo_quantize_e4m3_128: rows or weights to codes and scales
+  gemm   hilo_gemm_e4m3_128: rows times weights, with bias
+  gated  hilo_gated_e4m3_128: act(rows x gate weights) * (rows x up weights), to
+         16 or 32 bits or to codes and scales again
+
+Values: activations N(0,1) with gains per row (up to 8 either way) and channel
+and a few far larger channels, as behind a norm with a learned gain; weights
+N(0, 1/k) with a gain per output feature; biases N(0, 0.1^2). All drawn on the
+GPU from the seed.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+DEV = "cuda"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+SIZE = {"bf16": 2, "f16": 2, "f32": 4, "e4m3": 1}
+TINY = 2.0 ** -100  # a block's largest magnitude is taken as no less than this, unless all of it is zero
+
+
+# ----------------------------------------------------------------- cases ---
+
+
+def _quant(name=None, **kw):
+    """tile: 0, a scale per row and 128 columns; 1, a scale per 128 x 128. pad: elements between the rows. spare: rows
+    of the buffers behind those that the device counts."""
+    c = dict(op="quant", rows=1, spare=0, cols=4096, pad=0, dtype="bf16", tile=0)
+    c.update(kw)
+    return dict(c, name=name) if name else c
+
+
+def _gemm(name=None, **kw):
+    c = dict(op="gemm", rows=1, spare=0, k=4096, n=4096, bias=0, out="bf16")
+    c.update(kw)
+    return dict(c, name=name) if name else c
+
+
+def _gated(name=None, **kw):
+    c = dict(op="gated", rows=1, spare=0, k=4096, n=10240, bias=0, act="silu", out="e4m3")
+    c.update(kw)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # the row of a single token before its projection: the smallest call, where latency counts
+        _quant("quant_token"),
+        # fp32 rows of a compressed image in a wider buffer, the last block of each row only partly there
+        _quant("quant_rows_f32", rows=2389, spare=107, cols=1168, pad=48, dtype="f32"),
+        # a checkpoint's matrix, at load
+        _quant("quant_weight", rows=10240, cols=4096, tile=1),
+        # q, k and v of a single token
+        _gemm("gemm_token", n=6144, bias=1),
+        # the next tokens of a batch of requests
+        _gemm("gemm_tokens_33", rows=33, k=2048, n=2048, out="f16"),
+        # rows that the device counts, k ending inside a block, features inside a tile
+        _gemm("gemm_ragged", rows=777, spare=247, k=1168, n=4400, out="f32"),
+        # the output projection of the compressed rows of an image with its text
+        _gemm("gemm_rows_2389", rows=2389, bias=1),
+        # the feed-forward's way down for a batch of images
+        _gemm("gemm_rows_8192", rows=8192, k=10240),
+        # the feed-forward's way up for a single token
+        _gated("gated_token", k=2048, n=5504),
+        # for a few short prompts
+        _gated("gated_rows_200", rows=200, act="gelu"),
+        # for narrow rows, with biases, to a 16-bit tensor
+        _gated("gated_rows_1021", rows=1021, spare=3, k=1152, n=4608, bias=1, act="gelu", out="bf16"),
+        # for a batch of images
+        _gated("gated_rows_8192", rows=8192),
+    ]
+
+
+def _log(rng, lo, hi):
+    return math.exp(rng.uniform(math.log(lo), math.log(hi)))
+
+
+def _sixteen(rng, lo, hi):
+    n = 16 * int(_log(rng, lo, hi) / 16)
+    return n if rng.random() < 0.6 else 128 * max(1, n // 128)
+
+
+def draw(rng):
+    op = rng.choice(("quant", "quant", "gemm", "gemm", "gemm", "gated", "gated", "gated"))
+    spare = rng.choice((0, 0, 1, 130))
+    if op == "quant":
+        return _quant(rows=int(_log(rng, 1, 9000)), spare=spare, cols=_sixteen(rng, 16, 8192), pad=rng.choice((0, 0, 16, 64)),
+                      dtype=rng.choice(("bf16", "bf16", "f16", "f32")), tile=rng.choice((0, 0, 1)))
+    rows, k, n = int(_log(rng, 1, 8193)), _sixteen(rng, 64, 8192), _sixteen(rng, 64, 10240)
+    rest = dict(rows=rows, spare=spare, k=k, n=n, bias=rng.choice((0, 1)))
+    if op == "gemm":
+        return _gemm(out=rng.choice(("bf16", "bf16", "f16", "f32")), **rest)
+    while 2 * n * rest["k"] * rows > 2 * 10240 * 4096 * 8192:
+        rest["k"] = 16 * (rest["k"] // 32)
+    return _gated(act=rng.choice(("silu", "gelu")), out=rng.choice(("e4m3", "e4m3", "bf16", "f16", "f32")), **rest)
+
+
+# ---------------------------------------------------------------- inputs ---
+
+
+def _gen(seed, salt):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed) * 1000003 + salt)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+def _activations(g, rows, cols):
+    x = _randn(g, rows, cols)
+    x *= torch.exp2(6 * torch.rand(rows, 1, generator=g, device=DEV) - 3)
+    x *= 0.5 + torch.rand(cols, generator=g, device=DEV)
+    x[:, torch.randint(0, cols, (1 + cols // 500,), generator=g, device=DEV)] *= 20
+    return x
+
+
+def _weights(g, n, k):
+    w = _randn(g, n, k)
+    w *= torch.exp2(2 * torch.rand(n, 1, generator=g, device=DEV) - 1) / math.sqrt(k)
+    return w
+
+
+def _e4m3_rows(x):
+    """Codes of each row's blocks of 128 columns, and their scales [blocks, rows]."""
+    rows, cols = x.shape
+    blocks = -(-cols // 128)
+    x = x.float()
+    y = torch.zeros(rows, blocks * 128, device=DEV)
+    y[:, :cols] = x
+    top = y.view(rows, blocks, 128).abs().amax(2)
+    top = torch.where(top > 0, top.clamp(min=TINY), 448.0)
+    codes = (y.view(rows, blocks, 128) * (448.0 / top)[:, :, None]).view(rows, -1)[:, :cols]
+    return codes.to(torch.float8_e4m3fn), (top / 448.0).t().contiguous()
+
+
+def _e4m3_tiles(x):
+    """Codes of 128 x 128 tiles, and their scales [row blocks, column blocks]."""
+    rows, cols = x.shape
+    down, across = -(-rows // 128), -(-cols // 128)
+    y = torch.zeros(down * 128, across * 128, device=DEV)
+    y[:rows, :cols] = x
+    y = y.view(down, 128, across, 128)
+    top = y.abs().amax(3).amax(1)
+    top = torch.where(top > 0, top.clamp(min=TINY), 448.0)
+    codes = (y * (448.0 / top)[:, None, :, None]).view(down * 128, -1)[:rows, :cols]
+    return codes.to(torch.float8_e4m3fn).contiguous(), top / 448.0
+
+
+def _prepare_quant(c, seed):
+    g = _gen(seed, 1)
+    cap, cols, row = c["rows"] + c["spare"], c["cols"], c["cols"] + c["pad"]
+    x = (_weights if c["tile"] else _activations)(g, cap, row).to(TYPES[c["dtype"]])[:, :cols]
+    across = -(-cols // 128)
+    s = dict(c, x=x, n_rows=torch.tensor([c["rows"]], dtype=torch.int32, device=DEV),
+             codes=torch.zeros(cap, cols, dtype=torch.float8_e4m3fn, device=DEV),
+             scale=torch.zeros(-(-cap // 128), across, device=DEV) if c["tile"] else torch.zeros(across, cap, device=DEV))
+    if own:
+        from paper_2606_13898_gb300 import hilo as H
+        s["shape"] = H.Quant128Shape(rows=cap, cols=cols, dtype=_code(H, c["dtype"]), tile=c["tile"], src_row=row)
+    return s
+
+
+def _code(H, name):
+    return {"bf16": H.HILO_BF16, "f16": H.HILO_F16, "f32": H.HILO_F32, "e4m3": H.HILO_E4M3}[name]
+
+
+def _prepare_gemm(c, seed):
+    g = _gen(seed, 2)
+    cap, k, n, two = c["rows"] + c["spare"], c["k"], c["n"], c["op"] == "gated"
+    a, a_scale = _e4m3_rows(_activations(g, cap, k))
+    w = [_e4m3_tiles(_weights(g, n, k)) for _ in range(1 + two)]
+    bias = [(0.1 * _randn(g, n)).bfloat16() if c["bias"] else None for _ in w]
+    s = dict(c, a=a, a_scale=a_scale, w=[x[0] for x in w], w_scale=[x[1] for x in w], biases=bias,
+             n_rows=torch.tensor([c["rows"]], dtype=torch.int32, device=DEV),
+             y=torch.zeros(cap, n, dtype=TYPES[c["out"]], device=DEV),
+             y_scale=torch.zeros(-(-n // 128), cap, device=DEV) if c["out"] == "e4m3" else None)
+    if own:
+        from paper_2606_13898_gb300 import hilo as H
+        s["shape"] = H.Gemm128Shape(rows=cap, k=k, n=n, out_dtype=_code(H, c["out"]),
+                                    act={"silu": H.HILO_ACT_SILU, "gelu": H.HILO_ACT_GELU}[c["act"]] if two else H.HILO_ACT_NONE)
+    return s
+
+
+def prepare(case, seed):
+    return (_prepare_quant if case["op"] == "quant" else _prepare_gemm)(case, seed)
+
+
+# ------------------------------------------------------------------ plain ---
+
+
+def _plain_quant(s):
+    codes, scale = torch.zeros_like(s["codes"]), torch.zeros_like(s["scale"])
+    x = s["x"][:s["rows"]]
+    if s["tile"]:
+        codes[:s["rows"]], scale[:-(-s["rows"] // 128)] = _e4m3_tiles(x)
+    else:
+        codes[:s["rows"]], scale[:, :s["rows"]] = _e4m3_rows(x)
+    return {"codes": codes, "scale": scale}
+
+
+def _plain_product(s, i):
+    rows, k, n = s["rows"], s["k"], s["n"]
+    a = s["a"][:rows].float() * s["a_scale"][:, :rows].repeat_interleave(128, 0)[:k].t()
+    w = s["w"][i].float() * s["w_scale"][i].repeat_interleave(128, 1)[:, :k].repeat_interleave(128, 0)[:n]
+    y = torch.matmul(a, w.t())
+    return y if s["biases"][i] is None else y + s["biases"][i].float()
+
+
+def _plain_gemm(s):
+    y = _plain_product(s, 0)
+    if s["op"] == "gated":
+        if s["act"] == "silu":
+            y = y / (1 + torch.exp(-y))
+        else:
+            y = 0.5 * y * (1 + torch.tanh(math.sqrt(2 / math.pi) * (y + 0.044715 * y * y * y)))
+        y = y * _plain_product(s, 1)
+    out = {"y": torch.zeros_like(s["y"])}
+    if s["out"] == "e4m3":
+        out["scale"] = torch.zeros_like(s["y_scale"])
+        out["y"][:s["rows"]], out["scale"][:, :s["rows"]] = _e4m3_rows(y)
+    else:
+        out["y"][:s["rows"]] = y.to(out["y"].dtype)
+    return out
+
+
+# --------------------------------------------------------------- one pass ---
+
+
+def run(s):
+    if not own:
+        return (_plain_quant if s["op"] == "quant" else _plain_gemm)(s)
+    from paper_2606_13898_gb300 import hilo as H
+    if s["op"] == "quant":
+        H.hilo_quantize_e4m3_128(s["shape"], s["x"], s["n_rows"], s["codes"], s["scale"])
+        return {"codes": s["codes"], "scale": s["scale"]}
+    if s["op"] == "gemm":
+        H.hilo_gemm_e4m3_128(s["shape"], s["a"], s["a_scale"], s["w"][0], s["w_scale"][0], s["biases"][0], s["n_rows"], s["y"])
+        return {"y": s["y"]}
+    H.hilo_gated_e4m3_128(s["shape"], s["a"], s["a_scale"], s["w"][0], s["w_scale"][0], s["w"][1], s["w_scale"][1],
+                          s["biases"][0], s["biases"][1], s["n_rows"], s["y"], s["y_scale"])
+    return {"y": s["y"]} if s["y_scale"] is None else {"y": s["y"], "scale": s["y_scale"]}
+
+
+def work(c):
+    rows = c["rows"]
+    if c["op"] == "quant":
+        across = -(-c["cols"] // 128)
+        return {"bytes": rows * c["cols"] * (SIZE[c["dtype"]] + 1) + 4 * across * (-(-rows // 128) if c["tile"] else rows),
+                "flops": 2 * rows * c["cols"]}
+    k, n, two = c["k"], c["n"], 1 + (c["op"] == "gated")
+    deep, wide = -(-k // 128), -(-n // 128)
+    out = rows * n * SIZE[c["out"]] + (4 * wide * rows if c["out"] == "e4m3" else 0)
+    return {"bytes": rows * k + 4 * deep * rows + two * (n * k + 4 * deep * wide + 2 * n * c["bias"]) + out,
+            "flops": 2 * two * rows * n * k}
+
+
+# ------------------------------------------------------------------ exact ---
+
+
+def _exact_e4m3(y):
+    """The e4m3 value nearest to each, ties to even, no larger than 448."""
+    m, e = torch.frexp(y.abs().clamp(min=2.0 ** -30))
+    step = torch.exp2((e - 1).clamp(min=-6).double() - 3)
+    return torch.clamp(torch.round(y / step) * step, -448.0, 448.0)
+
+
+def _exact_blocks(x, tall):
+    """Values and scales of blocks of `tall` rows x 128 columns, block by block of columns."""
+    rows, cols = x.shape
+    down = -(-rows // tall)
+    codes, scales = torch.empty_like(x), torch.empty(down, -(-cols // 128), dtype=torch.float64, device=DEV)
+    for b in range(scales.shape[1]):
+        part = x[:, 128 * b:128 * b + 128]
+        most = part.abs().amax(1)
+        most = torch.cat([most, most.new_zeros(down * tall - rows)]).view(down, tall).amax(1)
+        most = torch.where(most == 0, torch.full_like(most, 448.0), most.clamp(min=TINY))
+        codes[:, 128 * b:128 * b + 128] = _exact_e4m3(part / most.repeat_interleave(tall)[:rows, None] * 448.0)
+        scales[:, b] = most / 448.0
+    return codes, scales
+
+
+def _exact_quant(s):
+    rows, cap = s["rows"], s["rows"] + s["spare"]
+    codes, scales = _exact_blocks(s["x"][:rows].double(), 128 if s["tile"] else 1)
+    out = {"codes": torch.zeros(cap, s["cols"], dtype=torch.float64, device=DEV),
+           "scale": torch.zeros(s["scale"].shape, dtype=torch.float64, device=DEV)}
+    out["codes"][:rows] = codes
+    if s["tile"]:
+        out["scale"][:scales.shape[0]] = scales
+    else:
+        out["scale"][:, :rows] = scales.t()
+    return out
+
+
+def _exact_product(s, i):
+    rows, k, n = s["rows"], s["k"], s["n"]
+    y = torch.zeros(rows, n, dtype=torch.float64, device=DEV)
+    if s["biases"][i] is not None:
+        y += s["biases"][i].double()
+    feature = torch.arange(n, device=DEV) // 128
+    for b, k0 in enumerate(range(0, k, 128)):
+        part = s["a"][:rows, k0:k0 + 128].double() @ s["w"][i][:, k0:k0 + 128].double().t()
+        y += part * s["a_scale"][b, :rows].double()[:, None] * s["w_scale"][i][:, b].double()[feature]
+    return y
+
+
+def _exact_gemm(s):
+    rows = s["rows"]
+    y = _exact_product(s, 0)
+    if s["op"] == "gated":
+        z = y if s["act"] == "silu" else 2 * math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3)
+        y = y * torch.sigmoid(z) * _exact_product(s, 1)
+    out = {"y": torch.zeros(s["y"].shape, dtype=torch.float64, device=DEV)}
+    if s["out"] == "e4m3":
+        out["y"][:rows], scales = _exact_blocks(y, 1)
+        out["scale"] = torch.zeros(s["y_scale"].shape, dtype=torch.float64, device=DEV)
+        out["scale"][:, :rows] = scales.t()
+    else:
+        out["y"][:rows] = y
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return (_exact_quant if case["op"] == "quant" else _exact_gemm)(s)
