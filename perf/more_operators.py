@@ -131,6 +131,11 @@ def _weights(g, n, k):
     return w
 
 
+def _most():
+    """448 on the device: divided by a number of the host's, torch rounds twice."""
+    return torch.full((), 448.0, device=DEV)
+
+
 def _e4m3_rows(x):
     """Codes of each row's blocks of 128 columns, and their scales [blocks, rows]."""
     rows, cols = x.shape
@@ -140,8 +145,8 @@ def _e4m3_rows(x):
     y[:, :cols] = x
     top = y.view(rows, blocks, 128).abs().amax(2)
     top = torch.where(top > 0, top.clamp(min=TINY), 448.0)
-    codes = (y.view(rows, blocks, 128) * (448.0 / top)[:, :, None]).view(rows, -1)[:, :cols]
-    return codes.to(torch.float8_e4m3fn), (top / 448.0).t().contiguous()
+    codes = (y.view(rows, blocks, 128) * (_most() / top)[:, :, None]).view(rows, -1)[:, :cols]
+    return codes.to(torch.float8_e4m3fn), (top / _most()).t().contiguous()
 
 
 def _e4m3_tiles(x):
@@ -153,8 +158,8 @@ def _e4m3_tiles(x):
     y = y.view(down, 128, across, 128)
     top = y.abs().amax(3).amax(1)
     top = torch.where(top > 0, top.clamp(min=TINY), 448.0)
-    codes = (y * (448.0 / top)[:, None, :, None]).view(down * 128, -1)[:rows, :cols]
-    return codes.to(torch.float8_e4m3fn).contiguous(), top / 448.0
+    codes = (y * (_most() / top)[:, None, :, None]).view(down * 128, -1)[:rows, :cols]
+    return codes.to(torch.float8_e4m3fn).contiguous(), top / _most()
 
 
 def _prepare_quant(c, seed):
