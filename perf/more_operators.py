@@ -1,16 +1,20 @@
-"""Linear layers and the gated feed-forward in 8 bits, as measurable cases.
+"""Linear layers, the gated feed-forward and group norms in 8 bits, as measurable cases.
 
-Three operators, through the binding's public entry points where `own` is true
-and in elementary torch operations where it is not. All hold e4m3 codes with an
-fp32 scale for each block of 128: of one row's 128 columns for activations, of
-128 rows x 128 columns for weights.
+Four operators, through the binding's public entry points where `own` is true
+and in elementary torch operations where it is not. All hold, write or read e4m3
+codes with an fp32 scale for each block of 128: of one row's 128 columns for
+activations, of 128 rows x 128 columns for weights.
 
   quant  hilo_quantize_e4m3_128: rows or weights to codes and scales
   gemm   hilo_gemm_e4m3_128: rows times weights, with bias
   gated  hilo_gated_e4m3_128: act(rows x gate weights) * (rows x up weights), to
          16 or 32 bits or to codes and scales again
+  norm   hilo_group_norm: group norm of images, channels last, with weights, the
+         time step's scale and shift and an activation, to 16 or 32 bits or to
+         codes and scales
 
-Values: activations N(0,1) with gains per row (up to 8 either way) and channel
+Values: images N(0,1) with an offset and gain per channel, drifting over the
+rows; activations N(0,1) with gains per row (up to 8 either way) and channel
 and a few far larger channels, as behind a norm with a learned gain; weights
 N(0, 1/k) with a gain per output feature; biases N(0, 0.1^2). All drawn on the
 GPU from the seed.
@@ -51,18 +55,22 @@ def _gated(name=None, **kw):
     return dict(c, name=name) if name else c
 
 
+def _norm(name=None, **kw):
+    """cond: a scale and a shift per image, as a time step gives them. pad: elements between the rows of x."""
+    c = dict(op="norm", B=1, rows=1024, d=512, groups=32, cond=0, weights=1, act="silu", dtype="bf16", out="bf16", vec="bf16",
+             pad=0)
+    c.update(kw)
+    return dict(c, name=name) if name else c
+
+
 def listed():
     return [
         # the row of a single token before its projection: the smallest call, where latency counts
         _quant("quant_token"),
-        # fp32 rows of a compressed image in a wider buffer, the last block of each row only partly there
-        _quant("quant_rows_f32", rows=2389, spare=107, cols=1168, pad=48, dtype="f32"),
         # a checkpoint's matrix, at load
         _quant("quant_weight", rows=10240, cols=4096, tile=1),
         # q, k and v of a single token
         _gemm("gemm_token", n=6144, bias=1),
-        # the next tokens of a batch of requests
-        _gemm("gemm_tokens_33", rows=33, k=2048, n=2048, out="f16"),
         # rows that the device counts, k ending inside a block, features inside a tile
         _gemm("gemm_ragged", rows=777, spare=247, k=1168, n=4400, out="f32"),
         # the output projection of the compressed rows of an image with its text
@@ -73,10 +81,14 @@ def listed():
         _gated("gated_token", k=2048, n=5504),
         # for a few short prompts
         _gated("gated_rows_200", rows=200, act="gelu"),
-        # for narrow rows, with biases, to a 16-bit tensor
-        _gated("gated_rows_1021", rows=1021, spare=3, k=1152, n=4608, bias=1, act="gelu", out="bf16"),
         # for a batch of images
         _gated("gated_rows_8192", rows=8192),
+        # the latents of a small image before a 1x1 convolution
+        _norm("norm_32"),
+        # three images of an odd size, conditioned, to the codes that an 8-bit product reads
+        _norm("norm_b3_46x30", B=3, rows=1380, d=1152, groups=36, cond=1, dtype="f16", out="e4m3", vec="f32"),
+        # a decoder's last level: an image of 1024 x 1024 pixels
+        _norm("norm_1024", rows=1 << 20, d=128),
     ]
 
 
@@ -90,7 +102,17 @@ def _sixteen(rng, lo, hi):
 
 
 def draw(rng):
-    op = rng.choice(("quant", "quant", "gemm", "gemm", "gemm", "gated", "gated", "gated"))
+    op = rng.choice(("quant", "gemm", "gemm", "gated", "gated", "norm", "norm"))
+    if op == "norm":
+        groups, per = rng.choice((1, 8, 16, 32, 32, 32, 36)), rng.choice((4, 8, 10, 16, 24, 32, 64))
+        d = groups * per
+        if d % 16:
+            groups, d = 32, 32 * per
+        B = rng.choice((1, 1, 2, 3, 8))
+        return _norm(B=B, rows=int(_log(rng, 1, (1 << 27) // (d * B))), d=d, groups=groups, cond=rng.choice((0, 1)),
+                     weights=rng.choice((0, 1)), act=rng.choice(("none", "silu", "silu", "gelu")),
+                     dtype=rng.choice(("bf16", "bf16", "f16", "f32")), out=rng.choice(("bf16", "f16", "f32", "e4m3")),
+                     vec=rng.choice(("bf16", "f32")), pad=rng.choice((0, 0, 16)))
     spare = rng.choice((0, 0, 1, 130))
     if op == "quant":
         return _quant(rows=int(_log(rng, 1, 9000)), spare=spare, cols=_sixteen(rng, 16, 8192), pad=rng.choice((0, 0, 16, 64)),
@@ -197,8 +219,33 @@ def _prepare_gemm(c, seed):
     return s
 
 
+def _prepare_norm(c, seed):
+    g = _gen(seed, 3)
+    B, n, d, row = c["B"], c["rows"], c["d"], c["d"] + c["pad"]
+    x = _randn(g, B * n, row)
+    x *= torch.exp2(2 * torch.rand(row, generator=g, device=DEV) - 1)
+    x += _randn(g, row) + torch.linspace(-0.5, 0.5, B * n, device=DEV)[:, None]
+    vt = TYPES[c["vec"]]
+    # the time step's vectors: scale | shift of image b in row b
+    cond = (0.3 * _randn(g, B, 2 * d)).to(vt) if c["cond"] else None
+    w = (1 + 0.1 * _randn(g, d)).to(vt) if c["weights"] else None
+    b = (0.1 * _randn(g, d)).to(vt) if c["weights"] else None
+    s = dict(c, x=x.to(TYPES[c["dtype"]])[:, :d], cond_rows=cond, w=w, b=b, y=torch.zeros(B * n, d, dtype=TYPES[c["out"]], device=DEV),
+             y_scale=torch.zeros(-(-d // 128), B * n, device=DEV) if c["out"] == "e4m3" else None)
+    if own:
+        from paper_2606_13898_gb300 import hilo as H
+        s["shape"] = H.GroupNormShape(B=B, rows=n, d=d, groups=c["groups"], eps=1e-5, x_row=row, vec_row=2 * d,
+                                      act={"none": H.HILO_ACT_NONE, "silu": H.HILO_ACT_SILU, "gelu": H.HILO_ACT_GELU}[c["act"]],
+                                      x_dtype=_code(H, c["dtype"]), y_dtype=_code(H, c["out"]), vec_dtype=_code(H, c["vec"]))
+        s["vectors"] = H.NormVectors(scale=cond[:, :d] if c["cond"] else None, shift=cond[:, d:] if c["cond"] else None,
+                                     w_norm=w, b_norm=b)
+        s["ws_bytes"] = H.hilo_group_norm_workspace_bytes(s["shape"])
+        s["ws"] = torch.empty(s["ws_bytes"], dtype=torch.uint8, device=DEV)
+    return s
+
+
 def prepare(case, seed):
-    return (_prepare_quant if case["op"] == "quant" else _prepare_gemm)(case, seed)
+    return {"quant": _prepare_quant, "norm": _prepare_norm}.get(case["op"], _prepare_gemm)(case, seed)
 
 
 # ------------------------------------------------------------------ plain ---
@@ -222,14 +269,34 @@ def _plain_product(s, i):
     return y if s["biases"][i] is None else y + s["biases"][i].float()
 
 
+def _plain_act(y, act):
+    if act == "silu":
+        return y / (1 + torch.exp(-y))
+    if act == "gelu":
+        return 0.5 * y * (1 + torch.tanh(math.sqrt(2 / math.pi) * (y + 0.044715 * y * y * y)))
+    return y
+
+
+def _plain_norm(s):
+    B, n, d = s["B"], s["rows"], s["d"]
+    x = s["x"].float().view(B, n, s["groups"], -1)
+    x = x - x.mean((1, 3), keepdim=True)
+    x = (x * torch.rsqrt(x.square().mean((1, 3), keepdim=True) + 1e-5)).view(B, n, d)
+    if s["weights"]:
+        x = x * s["w"].float() + s["b"].float()
+    if s["cond"]:
+        x = x * (1 + s["cond_rows"][:, None, :d].float()) + s["cond_rows"][:, None, d:].float()
+    y = _plain_act(x, s["act"]).view(B * n, d)
+    if s["out"] != "e4m3":
+        return {"y": y.to(s["y"].dtype)}
+    codes, scale = _e4m3_rows(y)
+    return {"y": codes, "scale": scale}
+
+
 def _plain_gemm(s):
     y = _plain_product(s, 0)
     if s["op"] == "gated":
-        if s["act"] == "silu":
-            y = y / (1 + torch.exp(-y))
-        else:
-            y = 0.5 * y * (1 + torch.tanh(math.sqrt(2 / math.pi) * (y + 0.044715 * y * y * y)))
-        y = y * _plain_product(s, 1)
+        y = _plain_act(y, s["act"]) * _plain_product(s, 1)
     out = {"y": torch.zeros_like(s["y"])}
     if s["out"] == "e4m3":
         out["scale"] = torch.zeros_like(s["y_scale"])
@@ -244,11 +311,14 @@ def _plain_gemm(s):
 
 def run(s):
     if not own:
-        return (_plain_quant if s["op"] == "quant" else _plain_gemm)(s)
+        return {"quant": _plain_quant, "norm": _plain_norm}.get(s["op"], _plain_gemm)(s)
     from paper_2606_13898_gb300 import hilo as H
     if s["op"] == "quant":
         H.hilo_quantize_e4m3_128(s["shape"], s["x"], s["n_rows"], s["codes"], s["scale"])
         return {"codes": s["codes"], "scale": s["scale"]}
+    if s["op"] == "norm":
+        H.hilo_group_norm(s["shape"], s["vectors"], s["x"], s["y"], s["y_scale"], s["ws"], s["ws_bytes"])
+        return {"y": s["y"]} if s["y_scale"] is None else {"y": s["y"], "scale": s["y_scale"]}
     if s["op"] == "gemm":
         H.hilo_gemm_e4m3_128(s["shape"], s["a"], s["a_scale"], s["w"][0], s["w_scale"][0], s["biases"][0], s["n_rows"], s["y"])
         return {"y": s["y"]}
@@ -263,6 +333,10 @@ def work(c):
         across = -(-c["cols"] // 128)
         return {"bytes": rows * c["cols"] * (SIZE[c["dtype"]] + 1) + 4 * across * (-(-rows // 128) if c["tile"] else rows),
                 "flops": 2 * rows * c["cols"]}
+    if c["op"] == "norm":
+        n = c["B"] * c["rows"]
+        return {"bytes": n * c["d"] * (SIZE[c["dtype"]] + SIZE[c["out"]]) + (4 * -(-c["d"] // 128) * n if c["out"] == "e4m3" else 0)
+                + 2 * c["d"] * SIZE[c["vec"]] * (c["weights"] + c["B"] * c["cond"]), "flops": 15 * n * c["d"]}
     k, n, two = c["k"], c["n"], 1 + (c["op"] == "gated")
     deep, wide = -(-k // 128), -(-n // 128)
     out = rows * n * SIZE[c["out"]] + (4 * wide * rows if c["out"] == "e4m3" else 0)
@@ -320,12 +394,39 @@ def _exact_product(s, i):
     return y
 
 
+def _exact_act(y, act):
+    if act == "none":
+        return y
+    return y * torch.sigmoid(y if act == "silu" else 2 * math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3))
+
+
+def _exact_norm(s):
+    B, n, d, per = s["B"], s["rows"], s["d"], s["d"] // s["groups"]
+    y = s["x"].double()
+    for i in range(B):
+        rows = y[i * n:i * n + n]
+        sums, squares = rows.sum(0).view(-1, per).sum(1), torch.zeros(s["groups"], dtype=torch.float64, device=DEV)
+        rows -= (sums / (n * per)).repeat_interleave(per)
+        squares += (rows * rows).sum(0).view(-1, per).sum(1)
+        rows /= torch.sqrt(squares / (n * per) + 1e-5).repeat_interleave(per)
+        if s["weights"]:
+            rows *= s["w"].double()
+            rows += s["b"].double()
+        if s["cond"]:
+            rows *= 1 + s["cond_rows"][i, :d].double()
+            rows += s["cond_rows"][i, d:].double()
+    y = _exact_act(y, s["act"])
+    if s["out"] != "e4m3":
+        return {"y": y}
+    codes, scales = _exact_blocks(y, 1)
+    return {"y": codes, "scale": scales.t().contiguous()}
+
+
 def _exact_gemm(s):
     rows = s["rows"]
     y = _exact_product(s, 0)
     if s["op"] == "gated":
-        z = y if s["act"] == "silu" else 2 * math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3)
-        y = y * torch.sigmoid(z) * _exact_product(s, 1)
+        y = _exact_act(y, s["act"]) * _exact_product(s, 1)
     out = {"y": torch.zeros(s["y"].shape, dtype=torch.float64, device=DEV)}
     if s["out"] == "e4m3":
         out["y"][:rows], scales = _exact_blocks(y, 1)
@@ -338,4 +439,4 @@ def _exact_gemm(s):
 
 def exact(case, seed):
     s = prepare(case, seed)
-    return (_exact_quant if case["op"] == "quant" else _exact_gemm)(s)
+    return {"quant": _exact_quant, "norm": _exact_norm}.get(case["op"], _exact_gemm)(s)
