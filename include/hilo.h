@@ -64,7 +64,7 @@ enum {
 enum { HILO_KEEP = 0, HILO_POOL2 = 1, HILO_POOL4 = 2, HILO_LF = 3 };
 
 /* Input dtypes of hilo_block_forward (HILO_F16: hilo_quantize_rows_e4m3;
- * HILO_E4M3: an output of hilo_gate_norm). */
+ * HILO_E4M3: an output of hilo_gate_norm and hilo_gated_e4m3_128). */
 enum { HILO_BF16 = 0, HILO_F32 = 1, HILO_F16 = 2, HILO_E4M3 = 3 };
 
 /* Norms of hilo_gate_norm and hilo_block_forward_mod, over a row's d channels:
@@ -712,6 +712,106 @@ typedef struct {
 int hilo_block_forward_mod(const hilo_shape* shape, const hilo_block_weights* weights, const hilo_block_mod* mod,
                            const int32_t* cu_img, int32_t cap, const void* in_txt, const void* in_img, int in_dtype,
                            const float* n_img, float* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Linear layers and the gated feed-forward in 8 bits, for the transformer beside
+ * the block (text encoder, refiner). The paper reports FP8 on top of HiLo-Token
+ * (Sec. 3.3) and gives no scheme; here every operand is e4m3 codes with an fp32
+ * scale for each block of 128, so that a large value takes resolution from its
+ * block only, not from its row:
+ *   rows     value(r, c) = code[r * row + c] * scale[(c / 128) * scale_ld + r]
+ *            (block-major: the scales of neighbouring rows are neighbours)
+ *   weights  value(n, k) = code[n * row + k] * scale[(n / 128) * scale_ld + k / 128]
+ * Columns (and features) are multiples of 16; the last block of a row may be
+ * smaller than 128. The operators read `rows` as a capacity: with n_rows (int32,
+ * device) the first min(*n_rows, rows) rows take part, with NULL all; what
+ * belongs to other rows in an output is left as it was.
+ * ---------------------------------------------------------------------------
+ *
+ * Rows of hilo_quantize_e4m3_128: [rows, cols], rows >= 0, cols a positive multiple
+ * of 16.
+ *   dtype     of the source: HILO_BF16, HILO_F16 or HILO_F32
+ *   tile      0: a scale per row and 128 columns; 1: a scale per 128 x 128
+ *   src_row, dst_row   elements between the rows, multiples of 16, at least
+ *             cols, below 2^39
+ *   scale_ld  tile == 0: at least rows; tile == 1: at least ceil(cols / 128);
+ *             below 2^39
+ */
+typedef struct {
+  int32_t rows, cols, dtype, tile;
+  int64_t src_row, dst_row, scale_ld;
+} hilo_quant128_shape;
+
+/*
+ * hilo_quantize_e4m3_128 -- per block: amax = its largest magnitude, code =
+ * e4m3(x * (448 / amax)) and scale = amax / 448 (correctly rounded fp32
+ * divisions, the product rounded to fp32, then to nearest even and saturated at
+ * +-448). A block of zeros has scale 1; amax below 2^-100 counts as 2^-100. A
+ * NaN stays one and does not enter amax; with an infinity the block's values all
+ * become NaN.
+ *   src    device, 16-byte aligned
+ *   dst    uint8 device, 16-byte aligned, overlaps no input
+ *   scale  fp32 device: [ceil(cols / 128)] x scale_ld, or [ceil(rows / 128)] x
+ *          scale_ld
+ * With tile == 1 the last block's rows are those that take part.
+ */
+int hilo_quantize_e4m3_128(const hilo_quant128_shape* shape, const void* src, const int32_t* n_rows, uint8_t* dst,
+                           float* scale, void* stream);
+
+/* Activations of hilo_gated_e4m3_128: SiLU x / (1 + e^-x); GELU in the block's
+ * tanh form. */
+enum { HILO_ACT_NONE = 0, HILO_ACT_SILU = 1, HILO_ACT_GELU = 2 };
+
+/*
+ * Shape of hilo_gemm_e4m3_128 and hilo_gated_e4m3_128: rows [rows, k] times
+ * weights [n, k].
+ *   rows        >= 0; rows * n below 2^47
+ *   k, n        positive multiples of 16
+ *   act         HILO_ACT_NONE (gemm), HILO_ACT_SILU or HILO_ACT_GELU (gated)
+ *   out_dtype   HILO_BF16, HILO_F16 (saturating), HILO_F32; gated: also HILO_E4M3
+ *   a_row, w_row, out_row   elements between rows, multiples of 16, at least k,
+ *               k and n, below 2^39
+ *   a_scale_ld, out_scale_ld   at least rows (out_scale_ld: of HILO_E4M3 only)
+ *   w_scale_ld  at least ceil(k / 128); all three below 2^39
+ */
+typedef struct {
+  int32_t rows, k, n, act, out_dtype;
+  int64_t a_row, w_row, out_row, a_scale_ld, w_scale_ld, out_scale_ld;
+} hilo_gemm128_shape;
+
+/*
+ * hilo_gemm_e4m3_128 -- a linear layer: out = A W^T + bias.
+ *   a, w        uint8 e4m3 codes, device, 16-byte aligned
+ *   a_scale     fp32 [ceil(k / 128)] x a_scale_ld, device; w_scale fp32
+ *               [ceil(n / 128)] x w_scale_ld, device: any finite values, e.g.
+ *               those of hilo_quantize_e4m3_128
+ *   bias        bf16 [n], device, or NULL
+ *   out         [rows, n] of out_dtype, device, 16-byte aligned, overlaps no input
+ * The products of a block are summed by the tensor core in fp32, the blocks,
+ * scaled, in fp32 in a fixed order; the result is rounded once. A call repeats
+ * itself bit for bit. Codes of NaN reach only the row, or the feature, that they
+ * belong to.
+ */
+int hilo_gemm_e4m3_128(const hilo_gemm128_shape* shape, const uint8_t* a, const float* a_scale, const uint8_t* w,
+                       const float* w_scale, const void* bias, const int32_t* n_rows, void* out, void* stream);
+
+/*
+ * hilo_gated_e4m3_128 -- the gated feed-forward's first half in one kernel:
+ *     h = act(A W_gate^T + b_gate) * (A W_up^T + b_up)
+ * with everything between the products and h in fp32.
+ *   w_gate, w_up, s_gate, s_up   [n, k] each, with w_row and w_scale_ld in
+ *               common (halves of one matrix where n is a multiple of 128)
+ *   b_gate, b_up   bf16 [n], device, or NULL
+ *   out, out_scale   [rows, n] of out_dtype; HILO_E4M3: codes, with their scales in
+ *               out_scale fp32 [ceil(n / 128)] x out_scale_ld as by
+ *               hilo_quantize_e4m3_128: what hilo_gemm_e4m3_128 reads for the way
+ *               down (out_scale may be NULL otherwise)
+ * Other arguments and errors as hilo_gemm_e4m3_128.
+ */
+int hilo_gated_e4m3_128(const hilo_gemm128_shape* shape, const uint8_t* a, const float* a_scale, const uint8_t* w_gate,
+                        const float* s_gate, const uint8_t* w_up, const float* s_up, const void* b_gate, const void* b_up,
+                        const int32_t* n_rows, void* out, float* out_scale, void* stream);
 
 /*
  * Instrumentation (no counterpart in the paper; used by the benchmark).

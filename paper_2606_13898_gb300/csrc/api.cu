@@ -304,12 +304,13 @@ int hilo_device_info(int* num_sms, int* is_sm103) {
 int hilo_sync_status(void* stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "hilo_sync_status: stream");
-  const int g = hilo::gemm_take_device_error();
+  const int g1 = hilo::gemm_take_device_error(), g2 = hilo::gemm128_take_device_error();
+  const int g = g1 ? g1 : g2;
   const int a1 = hilo::attn_take_device_error(), a2 = hilo::attn_var_take_device_error();
   const int a = a1 ? a1 : a2;
   const int pr = hilo::probe_take_device_error();
   const int dc = hilo::dcheck_take_bw();
-  if (g < 0 || a1 < 0 || a2 < 0 || pr < 0 || dc < 0)
+  if (g1 < 0 || g2 < 0 || a1 < 0 || a2 < 0 || pr < 0 || dc < 0)
     return fail(HILO_ERR_CUDA, "hilo_sync_status: reading the device error word failed");
   if (g || a || pr)
     return fail(HILO_ERR_TIMEOUT, "device-side wait ran out (gemm=%d, attention=%d, probe=%d)", g, a, pr);
@@ -961,6 +962,90 @@ int hilo_attention(const hilo_attn_shape* s, const int32_t* cu_q, const int32_t*
                                              static_cast<cudaStream_t>(stream));
   count(launches);
   return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_attention");
+}
+
+// Distances between rows or blocks: at least `least`, a multiple of `step`, below 2^39.
+static bool good_ld(int64_t ld, int64_t least, int step) { return ld >= least && ld % step == 0 && ld < (1LL << 39); }
+
+int hilo_quantize_e4m3_128(const hilo_quant128_shape* s, const void* src, const int32_t* n_rows, uint8_t* dst, float* scale,
+                           void* stream) {
+  if (!s) return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: shape is NULL");
+  if (s->dtype != HILO_BF16 && s->dtype != HILO_F16 && s->dtype != HILO_F32)
+    return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: dtype=%d", s->dtype);
+  if (s->tile & ~1) return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: tile=%d must be 0 or 1", s->tile);
+  if (s->rows < 0 || s->cols < 16 || s->cols % 16)
+    return fail(HILO_ERR_SHAPE, "hilo_quantize_e4m3_128: rows=%d must be >= 0, cols=%d a positive multiple of 16", s->rows,
+                s->cols);
+  if (!good_ld(s->src_row, s->cols, 16) || !good_ld(s->dst_row, s->cols, 16) ||
+      !good_ld(s->scale_ld, s->tile ? (s->cols + 127) / 128 : s->rows, 1))
+    return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: src_row=%lld, dst_row=%lld, scale_ld=%lld",
+                static_cast<long long>(s->src_row), static_cast<long long>(s->dst_row), static_cast<long long>(s->scale_ld));
+  // (the grid's size is an int)
+  if (static_cast<int64_t>(s->rows) * ((s->cols + 255) / 256) > (1LL << 33))
+    return fail(HILO_ERR_SHAPE, "hilo_quantize_e4m3_128: %d rows of %d columns", s->rows, s->cols);
+  if (s->rows > 0 && (!src || !dst || !scale)) return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: NULL pointer");
+  if (!aligned16(src, dst)) return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: src and dst must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(scale) | reinterpret_cast<uintptr_t>(n_rows)) & 3)
+    return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: scale and n_rows must be 4-byte aligned");
+  DevInfo dev;
+  int st;
+  if ((st = current_device(&dev))) return st;
+  if (s->rows == 0) return HILO_OK;
+  cudaError_t e = hilo::launch_quant128(*s, src, n_rows, dst, scale, dev.num_sms, static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess) count(1);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_quantize_e4m3_128");
+}
+
+static int gemm128(const char* name, const hilo_gemm128_shape* s, bool two, const uint8_t* a, const float* a_scale,
+                   const uint8_t* w0, const float* s0, const uint8_t* w1, const float* s1, const void* b0, const void* b1,
+                   const int32_t* n_rows, void* out, float* out_scale, void* stream) {
+  if (!s) return fail(HILO_ERR_ARG, "%s: shape is NULL", name);
+  if (two ? s->act != HILO_ACT_SILU && s->act != HILO_ACT_GELU : s->act != HILO_ACT_NONE)
+    return fail(HILO_ERR_ARG, "%s: act=%d", name, s->act);
+  const bool codes = s->out_dtype == HILO_E4M3;
+  if (s->out_dtype != HILO_BF16 && s->out_dtype != HILO_F16 && s->out_dtype != HILO_F32 && !(two && codes))
+    return fail(HILO_ERR_ARG, "%s: out_dtype=%d", name, s->out_dtype);
+  if (s->rows < 0 || s->k < 16 || s->k % 16 || s->n < 16 || s->n % 16)
+    return fail(HILO_ERR_SHAPE, "%s: rows=%d must be >= 0, k=%d and n=%d positive multiples of 16", name, s->rows, s->k, s->n);
+  if (static_cast<int64_t>(s->rows) * s->n >= (1LL << 47))
+    return fail(HILO_ERR_SHAPE, "%s: rows=%d times n=%d must be below 2^47", name, s->rows, s->n);
+  if (!good_ld(s->a_row, s->k, 16) || !good_ld(s->w_row, s->k, 16) || !good_ld(s->out_row, s->n, 16))
+    return fail(HILO_ERR_ARG, "%s: a_row=%lld, w_row=%lld, out_row=%lld", name, static_cast<long long>(s->a_row),
+                static_cast<long long>(s->w_row), static_cast<long long>(s->out_row));
+  if (!good_ld(s->a_scale_ld, s->rows, 1) || !good_ld(s->w_scale_ld, (s->k + 127) / 128, 1) ||
+      (codes && !good_ld(s->out_scale_ld, s->rows, 1)))
+    return fail(HILO_ERR_ARG, "%s: a_scale_ld=%lld, w_scale_ld=%lld, out_scale_ld=%lld", name,
+                static_cast<long long>(s->a_scale_ld), static_cast<long long>(s->w_scale_ld),
+                static_cast<long long>(s->out_scale_ld));
+  if (!w0 || !s0 || (two && (!w1 || !s1)) || (s->rows > 0 && (!a || !a_scale || !out || (codes && !out_scale))))
+    return fail(HILO_ERR_ARG, "%s: NULL pointer", name);
+  if (!aligned16(a, w0, w1, out)) return fail(HILO_ERR_ARG, "%s: codes and out must be 16-byte aligned", name);
+  if ((reinterpret_cast<uintptr_t>(a_scale) | reinterpret_cast<uintptr_t>(s0) | reinterpret_cast<uintptr_t>(s1) |
+       reinterpret_cast<uintptr_t>(out_scale) | reinterpret_cast<uintptr_t>(n_rows)) & 3)
+    return fail(HILO_ERR_ARG, "%s: scales and n_rows must be 4-byte aligned", name);
+  if ((reinterpret_cast<uintptr_t>(b0) | reinterpret_cast<uintptr_t>(b1)) & 1)
+    return fail(HILO_ERR_ARG, "%s: biases must be 2-byte aligned", name);
+  DevInfo dev;
+  int st;
+  if ((st = current_device(&dev))) return st;
+  if (s->rows == 0) return HILO_OK;
+  const hilo::Gemm128Args g = {*s, a, a_scale, {w0, w1}, {s0, s1}, {b0, b1}, n_rows, out, codes ? out_scale : nullptr};
+  cudaError_t e = hilo::launch_gemm128(g, dev.ordinal, dev.num_sms, static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess) count(1);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, name);
+}
+
+int hilo_gemm_e4m3_128(const hilo_gemm128_shape* s, const uint8_t* a, const float* a_scale, const uint8_t* w,
+                       const float* w_scale, const void* bias, const int32_t* n_rows, void* out, void* stream) {
+  return gemm128("hilo_gemm_e4m3_128", s, false, a, a_scale, w, w_scale, nullptr, nullptr, bias, nullptr, n_rows, out, nullptr,
+                 stream);
+}
+
+int hilo_gated_e4m3_128(const hilo_gemm128_shape* s, const uint8_t* a, const float* a_scale, const uint8_t* w_gate,
+                        const float* s_gate, const uint8_t* w_up, const float* s_up, const void* b_gate, const void* b_up,
+                        const int32_t* n_rows, void* out, float* out_scale, void* stream) {
+  return gemm128("hilo_gated_e4m3_128", s, true, a, a_scale, w_gate, s_gate, w_up, s_up, b_gate, b_up, n_rows, out, out_scale,
+                 stream);
 }
 
 int hilo_unpack(const hilo_shape* shape, const float* out_img, const hilo_split_out* split, float* y,

@@ -149,6 +149,23 @@ cudaError_t launch_attention_var(const hilo_attn_shape& s, const int32_t* cu_q, 
                                  const void* k, const void* v, void* out, void* ws, int num_sms, int* launches,
                                  cudaStream_t st);
 int attn_var_take_device_error();
+// ---- 8-bit rows, products and the gated feed-forward with a scale per 128 (quant128.cu, gemm128_tc.cu)
+cudaError_t launch_quant128(const hilo_quant128_shape& s, const void* src, const int32_t* n_rows, uint8_t* dst, float* scale,
+                            int num_sms, cudaStream_t st);
+// Part 1 of w, w_scale and bias (the up projection) where s.act is not HILO_ACT_NONE.
+struct Gemm128Args {
+  hilo_gemm128_shape s;
+  const uint8_t* a;
+  const float* a_scale;
+  const uint8_t* w[2];
+  const float* w_scale[2];
+  const void* bias[2];
+  const int32_t* n_rows;
+  void* out;
+  float* out_scale;
+};
+cudaError_t launch_gemm128(const Gemm128Args& a, int device, int num_sms, cudaStream_t st);
+int gemm128_take_device_error();
 // The wait-timeout probe: one bounded mbarrier wait that runs out; its code
 // is read (and cleared) like the kernels' device error words.
 cudaError_t launch_wait_probe(cudaStream_t st);

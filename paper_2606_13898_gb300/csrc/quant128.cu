@@ -1,0 +1,168 @@
+// Rows and weights to e4m3 codes with an fp32 scale for each block of 128
+// (hilo_quantize_e4m3_128, include/hilo.h; paper Sec. 3.3 reports FP8 on top of
+// HiLo-Token, the scaling scheme is the library's):
+//   m = max |x| over the block,  scale = m / 448,  code = e4m3(x * (448 / m)),
+// the block being 128 columns of one row, or 128 rows x 128 columns.
+//
+// Bound by HBM: each element is read once, stays in registers for both the
+// maximum and the rounding, and leaves as one byte.
+#include "e4m3_128.cuh"
+#include "internal.h"
+
+namespace hilo {
+
+namespace {
+
+constexpr int THREADS = 256;
+
+struct QuantParams {
+  const unsigned char* src;
+  uint8_t* dst;
+  float* scale;
+  const int32_t* n_rows;
+  long long src_row, dst_row, scale_ld;  // src_row in bytes
+  int rows, cols, blocks;                // blocks: of a row, ceil(cols / 128)
+};
+
+// Eight elements from 16-byte aligned memory, as they are there (TYPE 0 bf16, 1 fp16, 2 fp32).
+template <int TYPE>
+struct Eight {
+  uint4 q[TYPE == 2 ? 2 : 1];
+  __device__ __forceinline__ void clear() {
+    for (auto& v : q) v = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ void load(const unsigned char* p) {
+#pragma unroll
+    for (int i = 0; i < (TYPE == 2 ? 2 : 1); ++i) q[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void widen(float* f) const {
+    const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[TYPE == 2 ? 1 : 0].x, q[TYPE == 2 ? 1 : 0].y,
+                           q[TYPE == 2 ? 1 : 0].z, q[TYPE == 2 ? 1 : 0].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (TYPE == 2) f[i] = __uint_as_float(w[i]);
+      else if (TYPE == 0) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+      else f[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu)));
+    }
+  }
+};
+
+__device__ __forceinline__ float amax8(const float* f, float m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
+  return m;
+}
+
+// A scale per row and 128 columns. A half warp has a block, eight columns a lane; a warp has
+// two neighbouring blocks of a row at a time, and U of these on their way at once.
+template <int TYPE, int U>
+__global__ void __launch_bounds__(THREADS) quant128_rows_kernel(const __grid_constant__ QuantParams p) {
+  pdl_wait();
+  pdl_trigger();
+  const int rows = rows_there(p.n_rows, p.rows);
+  const int pairs = (p.blocks + 1) >> 1, lane = lane_id(), half = lane >> 4;
+  const long long total = static_cast<long long>(rows) * pairs;
+  const long long first = (static_cast<long long>(blockIdx.x) * U) * (THREADS / 32) + warp_id();
+  Eight<TYPE> x[U];
+  int row[U], col[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long long c = first + u * (THREADS / 32);
+    row[u] = static_cast<int>(c / pairs);
+    col[u] = static_cast<int>(c - static_cast<long long>(row[u]) * pairs) * 256 + lane * 8;
+    if (c >= total) col[u] = p.cols;
+    x[u].clear();
+    if (col[u] < p.cols) x[u].load(p.src + row[u] * p.src_row + static_cast<long long>(col[u]) * (TYPE == 2 ? 4 : 2));
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float f[8], inv, sc;
+    x[u].widen(f);
+    float m = amax8(f, 0.f);
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    block_scale(m, inv, sc);
+    if (col[u] >= p.cols) continue;
+    *reinterpret_cast<uint2*>(p.dst + row[u] * p.dst_row + col[u]) = block_codes(f, inv);
+    if (lane == 16 * half) p.scale[(col[u] >> 7) * p.scale_ld + row[u]] = sc;
+  }
+}
+
+// A scale per 128 rows x 128 columns: a CTA each, all of the tile in registers.
+template <int TYPE>
+__global__ void __launch_bounds__(THREADS) quant128_tiles_kernel(const __grid_constant__ QuantParams p) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ float most[THREADS / 32];
+  const int rows = rows_there(p.n_rows, p.rows);
+  const int down = blockIdx.x / p.blocks, across = blockIdx.x - down * p.blocks;
+  if (down * QBLOCK >= rows) return;
+  const int col = across * QBLOCK + (threadIdx.x & 15) * 8, row0 = down * QBLOCK + (threadIdx.x >> 4);
+  Eight<TYPE> x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 16 * i;
+    x[i].clear();
+    if (row < rows && col < p.cols) x[i].load(p.src + row * p.src_row + static_cast<long long>(col) * (TYPE == 2 ? 4 : 2));
+  }
+  float m = 0.f, inv, sc;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float f[8];
+    x[i].widen(f);
+    m = amax8(f, m);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  if (lane_id() == 0) most[warp_id()] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) m = fmaxf(m, most[w]);
+  block_scale(m, inv, sc);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 16 * i;
+    float f[8];
+    x[i].widen(f);
+    if (row < rows && col < p.cols) *reinterpret_cast<uint2*>(p.dst + row * p.dst_row + col) = block_codes(f, inv);
+  }
+  if (threadIdx.x == 0) p.scale[down * p.scale_ld + across] = sc;
+}
+
+template <int TYPE>
+cudaError_t launch_type(const QuantParams& p, bool tile, int num_sms, cudaStream_t st) {
+  if (tile) {
+    const long long tiles = static_cast<long long>((p.rows + QBLOCK - 1) / QBLOCK) * p.blocks;
+    if (tiles > 0x7fffffffLL) return cudaErrorInvalidValue;
+    return launch_pdl(quant128_tiles_kernel<TYPE>, dim3(static_cast<unsigned>(tiles)), dim3(THREADS), 0, st, p);
+  }
+  constexpr int WARPS = THREADS / 32;
+  const long long chunks = static_cast<long long>(p.rows) * ((p.blocks + 1) / 2);
+  const bool many = chunks > static_cast<long long>(num_sms) * 8 * WARPS;  // more than the device holds at once
+  const long long per = many ? 4 * WARPS : WARPS, grid = (chunks + per - 1) / per;
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return launch_pdl(many ? quant128_rows_kernel<TYPE, 4> : quant128_rows_kernel<TYPE, 1>, dim3(static_cast<unsigned>(grid)),
+                    dim3(THREADS), 0, st, p);
+}
+
+}  // namespace
+
+cudaError_t launch_quant128(const hilo_quant128_shape& s, const void* src, const int32_t* n_rows, uint8_t* dst, float* scale,
+                            int num_sms, cudaStream_t st) {
+  QuantParams p;
+  p.src = static_cast<const unsigned char*>(src);
+  p.dst = dst;
+  p.scale = scale;
+  p.n_rows = n_rows;
+  p.src_row = s.src_row * (s.dtype == HILO_F32 ? 4 : 2);
+  p.dst_row = s.dst_row;
+  p.scale_ld = s.scale_ld;
+  p.rows = s.rows;
+  p.cols = s.cols;
+  p.blocks = (s.cols + QBLOCK - 1) / QBLOCK;
+  return s.dtype == HILO_BF16 ? launch_type<0>(p, s.tile, num_sms, st)
+         : s.dtype == HILO_F16 ? launch_type<1>(p, s.tile, num_sms, st)
+                               : launch_type<2>(p, s.tile, num_sms, st);
+}
+
+}  // namespace hilo

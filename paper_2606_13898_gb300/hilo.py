@@ -28,6 +28,7 @@ HILO_KEEP, HILO_POOL2, HILO_POOL4 = 0, 1, 2
 HILO_BF16, HILO_F32 = 0, 1
 HILO_E4M3 = 3
 HILO_NORM_NONE, HILO_NORM_LAYER, HILO_NORM_RMS = 0, 1, 2
+HILO_ACT_NONE, HILO_ACT_SILU, HILO_ACT_GELU = 0, 1, 2
 
 
 class HiloError(RuntimeError):
@@ -106,6 +107,17 @@ class hilo_block_mod(ctypes.Structure):
                 + [("pos", ctypes.c_void_p), ("rot", hilo_rotation)])
 
 
+class hilo_quant128_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("rows", "cols", "dtype", "tile")]
+                + [(n, ctypes.c_int64) for n in ("src_row", "dst_row", "scale_ld")])
+
+
+class hilo_gemm128_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("rows", "k", "n", "act", "out_dtype")]
+                + [(n, ctypes.c_int64) for n in ("a_row", "w_row", "out_row", "a_scale_ld", "w_scale_ld",
+                                                 "out_scale_ld")])
+
+
 EXPORTS = ("hilo_status_string", "hilo_last_error", "hilo_sync_status", "hilo_device_info",
            "hilo_score", "hilo_split_workspace_bytes", "hilo_split", "hilo_pack",
            "hilo_block_workspace_bytes", "hilo_block_forward", "hilo_unpack", "hilo_unpack_update",
@@ -115,7 +127,7 @@ EXPORTS = ("hilo_status_string", "hilo_last_error", "hilo_sync_status", "hilo_de
            "hilo_row_capacity", "hilo_quantize_rows_e4m3", "hilo_block_fp8_workspace_bytes",
            "hilo_block_forward_fp8", "hilo_block_forward_fp8_prop", "hilo_debug_wait_timeout",
            "hilo_row_positions", "hilo_rope", "hilo_gate_norm", "hilo_attention_workspace_bytes", "hilo_attention",
-           "hilo_block_forward_mod")
+           "hilo_block_forward_mod", "hilo_quantize_e4m3_128", "hilo_gemm_e4m3_128", "hilo_gated_e4m3_128")
 
 _lib = None
 
@@ -179,6 +191,9 @@ def lib() -> ctypes.CDLL:
         "hilo_attention": (I, [ctypes.POINTER(hilo_attn_shape), P, P, P, P, P, P, P, S, P]),
         "hilo_block_forward_mod": (I, [shp, ctypes.POINTER(hilo_block_weights), ctypes.POINTER(hilo_block_mod), P,
                                        ctypes.c_int32, P, P, I, P, P, P, S, P]),
+        "hilo_quantize_e4m3_128": (I, [ctypes.POINTER(hilo_quant128_shape), P, P, P, P, P]),
+        "hilo_gemm_e4m3_128": (I, [ctypes.POINTER(hilo_gemm128_shape)] + [P] * 8),
+        "hilo_gated_e4m3_128": (I, [ctypes.POINTER(hilo_gemm128_shape)] + [P] * 12),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -504,6 +519,51 @@ class AttnShape:
         return _kept(self, build)
 
 
+@dataclasses.dataclass(frozen=True)
+class Quant128Shape:
+    """Rows of hilo_quantize_e4m3_128 (tile 1: weights). Strides None: dense rows and scales."""
+
+    rows: int
+    cols: int
+    dtype: int = HILO_BF16
+    tile: int = 0
+    src_row: int | None = None
+    dst_row: int | None = None
+    scale_ld: int | None = None
+
+    def c(self) -> hilo_quant128_shape:
+        return self.__dict__.get("_c") or _kept(self, lambda: hilo_quant128_shape(
+            self.rows, self.cols, self.dtype, int(self.tile), self.cols if self.src_row is None else self.src_row,
+            self.cols if self.dst_row is None else self.dst_row,
+            (-(-self.cols // 128) if self.tile else self.rows) if self.scale_ld is None else self.scale_ld))
+
+
+@dataclasses.dataclass(frozen=True)
+class Gemm128Shape:
+    """Rows, weights and output of hilo_gemm_e4m3_128 (act HILO_ACT_NONE) and hilo_gated_e4m3_128. Strides None: dense
+    rows and scales."""
+
+    rows: int
+    k: int
+    n: int
+    act: int = HILO_ACT_NONE
+    out_dtype: int = HILO_BF16
+    a_row: int | None = None
+    w_row: int | None = None
+    out_row: int | None = None
+    a_scale_ld: int | None = None
+    w_scale_ld: int | None = None
+    out_scale_ld: int | None = None
+
+    def c(self) -> hilo_gemm128_shape:
+        def build():
+            given = (self.a_row, self.w_row, self.out_row, self.a_scale_ld, self.w_scale_ld, self.out_scale_ld)
+            dense = (self.k, self.k, self.n, self.rows, -(-self.k // 128), self.rows)
+            return hilo_gemm128_shape(self.rows, self.k, self.n, self.act, self.out_dtype,
+                                      *(d if s is None else s for s, d in zip(given, dense)))
+        return self.__dict__.get("_c") or _kept(self, build)
+
+
 @dataclasses.dataclass
 class BlockMod:
     """Conditioning of one block (hilo_block_forward_mod). axis_dims None: no rotary positions."""
@@ -707,6 +767,24 @@ def hilo_block_forward_mod(shape: Shape, weights: DeviceWeights, mod: BlockMod, 
     _check("hilo_block_forward_mod", lib().hilo_block_forward_mod(
         ctypes.byref(s), ctypes.byref(w), ctypes.byref(m), _ptr(cu_img), cap, _ptr(in_txt), _ptr(in_img), in_dtype,
         _ptr(n_img), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def hilo_quantize_e4m3_128(shape: Quant128Shape, src, n_rows, dst, scale, stream=None) -> None:
+    _check("hilo_quantize_e4m3_128", lib().hilo_quantize_e4m3_128(
+        ctypes.byref(shape.c()), _ptr(src), _ptr(n_rows), _ptr(dst), _ptr(scale), _stream(stream)))
+
+
+def hilo_gemm_e4m3_128(shape: Gemm128Shape, a, a_scale, w, w_scale, bias, n_rows, out, stream=None) -> None:
+    _check("hilo_gemm_e4m3_128", lib().hilo_gemm_e4m3_128(
+        ctypes.byref(shape.c()), _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(n_rows), _ptr(out),
+        _stream(stream)))
+
+
+def hilo_gated_e4m3_128(shape: Gemm128Shape, a, a_scale, w_gate, s_gate, w_up, s_up, b_gate, b_up, n_rows, out,
+                        out_scale=None, stream=None) -> None:
+    _check("hilo_gated_e4m3_128", lib().hilo_gated_e4m3_128(
+        ctypes.byref(shape.c()), _ptr(a), _ptr(a_scale), _ptr(w_gate), _ptr(s_gate), _ptr(w_up), _ptr(s_up),
+        _ptr(b_gate), _ptr(b_up), _ptr(n_rows), _ptr(out), _ptr(out_scale), _stream(stream)))
 
 
 def hilo_block_forward_static_ws(shape: Shape, weights: DeviceWeights, cu_img, cap: int, in_txt, in_img,
