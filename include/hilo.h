@@ -64,7 +64,8 @@ enum {
 enum { HILO_KEEP = 0, HILO_POOL2 = 1, HILO_POOL4 = 2, HILO_LF = 3 };
 
 /* Input dtypes of hilo_block_forward (HILO_F16: hilo_quantize_rows_e4m3;
- * HILO_E4M3: an output of hilo_gate_norm and hilo_gated_e4m3_128). */
+ * HILO_E4M3: an output of hilo_gate_norm, hilo_gated_e4m3_128 and
+ * hilo_group_norm). */
 enum { HILO_BF16 = 0, HILO_F32 = 1, HILO_F16 = 2, HILO_E4M3 = 3 };
 
 /* Norms of hilo_gate_norm and hilo_block_forward_mod, over a row's d channels:
@@ -759,8 +760,8 @@ typedef struct {
 int hilo_quantize_e4m3_128(const hilo_quant128_shape* shape, const void* src, const int32_t* n_rows, uint8_t* dst,
                            float* scale, void* stream);
 
-/* Activations of hilo_gated_e4m3_128: SiLU x / (1 + e^-x); GELU in the block's
- * tanh form. */
+/* Activations of hilo_gated_e4m3_128 and hilo_group_norm: SiLU x / (1 + e^-x); GELU
+ * in the block's tanh form. */
 enum { HILO_ACT_NONE = 0, HILO_ACT_SILU = 1, HILO_ACT_GELU = 2 };
 
 /*
@@ -812,6 +813,54 @@ int hilo_gemm_e4m3_128(const hilo_gemm128_shape* shape, const uint8_t* a, const 
 int hilo_gated_e4m3_128(const hilo_gemm128_shape* shape, const uint8_t* a, const float* a_scale, const uint8_t* w_gate,
                         const float* s_gate, const uint8_t* w_up, const float* s_up, const void* b_gate, const void* b_up,
                         const int32_t* n_rows, void* out, float* out_scale, void* stream);
+
+/*
+ * Images of hilo_group_norm: B images of `rows` positions (H * W, raster order),
+ * d channels each, channels last; image b owns rows b * rows .. of x and y.
+ *   B, rows     B >= 1, rows >= 0, B * rows at most 2^30
+ *   d           a positive multiple of 16, at most 8192
+ *   groups      divides d; group g has channels g * d / groups ..
+ *   act         HILO_ACT_*
+ *   x_dtype     HILO_BF16, HILO_F16 or HILO_F32; y_dtype these (HILO_F16
+ *               saturating) or HILO_E4M3; vec_dtype HILO_BF16 or HILO_F32
+ *   eps         >= 0
+ *   x_row, y_row   elements between rows, multiples of 16, at least d, below 2^39
+ *   vec_row     elements between the images' scale and shift rows, a multiple of
+ *               8 (>= 0; 0: all images share one), below 2^39
+ *   y_scale_ld  of HILO_E4M3: at least B * rows, below 2^39
+ */
+typedef struct {
+  int32_t B, rows, d, groups, act;
+  int32_t x_dtype, y_dtype, vec_dtype;
+  float eps;
+  int64_t x_row, y_row, vec_row, y_scale_ld;
+} hilo_group_norm_shape;
+
+/* Workspace bytes hilo_group_norm needs (0 for an invalid shape). */
+size_t hilo_group_norm_workspace_bytes(const hilo_group_norm_shape* shape);
+
+/*
+ * hilo_group_norm -- group norm of the latents, or of the levels of the image
+ * encoder and decoder around the block (paper Sec. 2.1), with what follows it:
+ *     y = act(((x - mean) / sqrt(var + eps) * w_norm + b_norm) * (1 + scale) + shift)
+ * mean and (biased) variance over an image's rows and a group's channels.
+ *   vectors  scale and shift: a row of d per image; w_norm and b_norm: [d]; each
+ *            16-byte aligned, or NULL for 0, 0, 1 and 0 (gate and w_branch must be
+ *            NULL); or NULL for none of them
+ *   x, y     device, 16-byte aligned; y == x with x's dtype and stride works in
+ *            place, else the two must not overlap
+ *   y_scale  HILO_E4M3: fp32 [ceil(d / 128)] x y_scale_ld, codes and scales as by
+ *            hilo_quantize_e4m3_128 (else may be NULL)
+ *   ws       hilo_group_norm_workspace_bytes of device memory, 16-byte aligned;
+ *            nothing in it has to be set. Calls that may overlap on the device
+ *            need workspaces of their own.
+ * Statistics are fp32: means and squares about them, joined pairwise in a fixed
+ * order, so that an offset far above the deviation costs no more than its own
+ * rounding. A call repeats itself bit for bit. A NaN or an infinity leaves its
+ * image's group NaN.
+ */
+int hilo_group_norm(const hilo_group_norm_shape* shape, const hilo_norm_vectors* vectors, const void* x, void* y,
+                    float* y_scale, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Instrumentation (no counterpart in the paper; used by the benchmark).

@@ -1048,6 +1048,57 @@ int hilo_gated_e4m3_128(const hilo_gemm128_shape* s, const uint8_t* a, const flo
                  stream);
 }
 
+static int check_group_norm(const hilo_group_norm_shape* s) {
+  if (!s) return fail(HILO_ERR_ARG, "hilo_group_norm: shape is NULL");
+  if (s->B < 1 || s->rows < 0 || static_cast<int64_t>(s->B) * s->rows > (1 << 30))
+    return fail(HILO_ERR_SHAPE, "hilo_group_norm: B=%d must be >= 1, rows=%d >= 0, B * rows at most 2^30", s->B, s->rows);
+  if (s->d < 16 || s->d % 16 || s->d > 8192)
+    return fail(HILO_ERR_SHAPE, "hilo_group_norm: d=%d must be a multiple of 16 in [16, 8192]", s->d);
+  if (s->groups < 1 || s->d % s->groups) return fail(HILO_ERR_SHAPE, "hilo_group_norm: groups=%d must divide d=%d", s->groups, s->d);
+  if (s->act != HILO_ACT_NONE && s->act != HILO_ACT_SILU && s->act != HILO_ACT_GELU)
+    return fail(HILO_ERR_ARG, "hilo_group_norm: act=%d", s->act);
+  if ((!is_bf16_or_f32(s->x_dtype) && s->x_dtype != HILO_F16) ||
+      (!is_bf16_or_f32(s->y_dtype) && s->y_dtype != HILO_F16 && s->y_dtype != HILO_E4M3) || !is_bf16_or_f32(s->vec_dtype))
+    return fail(HILO_ERR_ARG, "hilo_group_norm: x_dtype=%d, y_dtype=%d, vec_dtype=%d", s->x_dtype, s->y_dtype, s->vec_dtype);
+  if (!(s->eps >= 0.0f) || !is_finite(s->eps)) return fail(HILO_ERR_ARG, "hilo_group_norm: eps must be finite and >= 0");
+  if (!good_ld(s->x_row, s->d, 16) || !good_ld(s->y_row, s->d, 16) || !good_ld(s->vec_row, 0, 8) ||
+      (s->y_dtype == HILO_E4M3 && !good_ld(s->y_scale_ld, static_cast<int64_t>(s->B) * s->rows, 1)))
+    return fail(HILO_ERR_ARG, "hilo_group_norm: x_row=%lld, y_row=%lld, vec_row=%lld, y_scale_ld=%lld",
+                static_cast<long long>(s->x_row), static_cast<long long>(s->y_row), static_cast<long long>(s->vec_row),
+                static_cast<long long>(s->y_scale_ld));
+  return HILO_OK;
+}
+
+size_t hilo_group_norm_workspace_bytes(const hilo_group_norm_shape* shape) {
+  return check_group_norm(shape) ? 0 : hilo::group_norm_workspace_bytes(*shape);
+}
+
+int hilo_group_norm(const hilo_group_norm_shape* s, const hilo_norm_vectors* vectors, const void* x, void* y, float* y_scale,
+                    void* ws, size_t ws_bytes, void* stream) {
+  int st = check_group_norm(s);
+  if (st) return st;
+  const hilo_norm_vectors none = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+  const hilo_norm_vectors& v = vectors ? *vectors : none;
+  if (v.gate || v.w_branch) return fail(HILO_ERR_ARG, "hilo_group_norm: gate and w_branch must be NULL");
+  if (s->rows > 0 && (!x || !y || (s->y_dtype == HILO_E4M3 && !y_scale))) return fail(HILO_ERR_ARG, "hilo_group_norm: NULL pointer");
+  if (!aligned16(x, y, ws) || !vectors_aligned(v))
+    return fail(HILO_ERR_ARG, "hilo_group_norm: x, y, ws and the vectors must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(y_scale) & 3) return fail(HILO_ERR_ARG, "hilo_group_norm: y_scale must be 4-byte aligned");
+  if (s->rows > 0 && x == y && (s->x_dtype != s->y_dtype || (s->x_row != s->y_row && static_cast<int64_t>(s->B) * s->rows > 1)))
+    return fail(HILO_ERR_ARG, "hilo_group_norm: in place, x and y have the same dtype and stride");
+  const size_t need = hilo::group_norm_workspace_bytes(*s);
+  if (!ws || ws_bytes < need)
+    return fail(HILO_ERR_WORKSPACE, "hilo_group_norm: workspace %zu < %zu bytes", ws ? ws_bytes : 0, need);
+  DevInfo dev;
+  if ((st = current_device(&dev))) return st;
+  if (s->rows == 0) return HILO_OK;
+  const hilo::GroupNormArgs a = {*s, v, x, y, s->y_dtype == HILO_E4M3 ? y_scale : nullptr, ws};
+  int launches = 0;
+  cudaError_t e = hilo::launch_group_norm(a, dev.ordinal, dev.num_sms, &launches, static_cast<cudaStream_t>(stream));
+  count(launches);
+  return e == cudaSuccess ? HILO_OK : cuda_fail(e, "hilo_group_norm");
+}
+
 int hilo_unpack(const hilo_shape* shape, const float* out_img, const hilo_split_out* split, float* y,
                 void* stream) {
   int st = check_shape(shape, false);

@@ -1,5 +1,6 @@
-// e4m3 codes with an fp32 scale for each block of 128 (quant128.cu,
-// gemm128_tc.cu): the block's scale and the codes' values.
+// Device helpers of the 8-bit operators with an fp32 scale for each block of 128
+// (quant128.cu, gemm128_tc.cu, group_norm.cu): the block's scale and codes,
+// eight elements of a row, activations, stores.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -7,7 +8,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "attn_common.cuh"
 #include "common.cuh"
+#include "../../include/hilo.h"
 
 namespace hilo {
 
@@ -26,6 +29,61 @@ __device__ __forceinline__ void block_scale(float amax, float& inv, float& scale
 __device__ __forceinline__ uint2 block_codes(const float* f, float inv) {
   return make_uint2(pack_e4m3x4(__fmul_rn(f[0], inv), __fmul_rn(f[1], inv), __fmul_rn(f[2], inv), __fmul_rn(f[3], inv)),
                     pack_e4m3x4(__fmul_rn(f[4], inv), __fmul_rn(f[5], inv), __fmul_rn(f[6], inv), __fmul_rn(f[7], inv)));
+}
+
+// Eight neighbouring elements in 16-byte aligned memory, as they are there (TYPE 0 bf16, 1 fp16, 2 fp32).
+template <int TYPE>
+struct Eight {
+  uint4 q[TYPE == 2 ? 2 : 1];
+  __device__ __forceinline__ void clear() {
+    for (auto& v : q) v = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ void load(const unsigned char* p) {
+#pragma unroll
+    for (int i = 0; i < (TYPE == 2 ? 2 : 1); ++i) q[i] = *(reinterpret_cast<const uint4*>(p) + i);
+  }
+  // of what is read once
+  __device__ __forceinline__ void load_once(const unsigned char* p) {
+#pragma unroll
+    for (int i = 0; i < (TYPE == 2 ? 2 : 1); ++i) q[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void widen(float* f) const {
+    const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[TYPE == 2 ? 1 : 0].x, q[TYPE == 2 ? 1 : 0].y,
+                           q[TYPE == 2 ? 1 : 0].z, q[TYPE == 2 ? 1 : 0].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (TYPE == 2) f[i] = __uint_as_float(w[i]);
+      else if (TYPE == 0) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+      else f[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu)));
+    }
+  }
+};
+
+__device__ __forceinline__ float amax8(const float* f, float m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
+  return m;
+}
+
+// SiLU z / (1 + e^-z); GELU in its tanh form, z / (1 + 2^(-2u log2(e))) with u = sqrt(2 / pi) (z + 0.044715 z^3),
+// the same function.
+__device__ __forceinline__ float activation(float z, int act) {
+  constexpr float LOG2E = 1.4426950408889634f;
+  if (act == HILO_ACT_NONE) return z;
+  const float t = act == HILO_ACT_SILU ? -LOG2E * z : -2.f * LOG2E * 0.7978845608028654f * (z + 0.044715f * z * z * z);
+  return __fdividef(z, 1.f + ex2(t));
+}
+
+// Four values of a row, rounded once (fp16 saturating), at an element offset that is a multiple of four.
+__device__ __forceinline__ void store4(void* out, int type, long long at, const float* v) {
+  if (type == HILO_F32) {
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    const bool f16 = type == HILO_F16;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
+        f16 ? make_uint2(pack_f16x2_sat(v[0], v[1]), pack_f16x2_sat(v[2], v[3]))
+            : make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
 }
 
 // The first min(*n_rows, rows) rows are there, all where n_rows is null.

@@ -114,28 +114,6 @@ __device__ __forceinline__ void copies_wait() {
 
 constexpr int SCALES_AHEAD = 4;
 
-// ----------------------------------------------------------------- activation --
-
-// act(gate) * up. SiLU g / (1 + e^-g); GELU in its tanh form, z / (1 + 2^(-2u log2(e))) with u = sqrt(2 / pi) (z +
-// 0.044715 z^3), the same function.
-__device__ __forceinline__ float gated(float g, float up, int act) {
-  constexpr float LOG2E = 1.4426950408889634f;
-  const float t = act == HILO_ACT_SILU ? -LOG2E * g : -2.f * LOG2E * 0.7978845608028654f * (g + 0.044715f * g * g * g);
-  return __fdividef(g, 1.f + ex2(t)) * up;
-}
-
-// Four values of a row, rounded once, at an element offset that is a multiple of four.
-__device__ __forceinline__ void store4(void* out, int type, long long at, const float* v) {
-  if (type == HILO_F32) {
-    *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
-  } else {
-    const bool f16 = type == HILO_F16;
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
-        f16 ? make_uint2(pack_f16x2_sat(v[0], v[1]), pack_f16x2_sat(v[2], v[3]))
-            : make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-  }
-}
-
 __device__ __forceinline__ float bias_at(const __nv_bfloat16* b, int n) { return b ? __bfloat162float(__ldg(b + n)) : 0.f; }
 
 // ------------------------------------------------------------------- few rows --
@@ -391,7 +369,7 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       y[0][j] += in ? bias_at(p.bias[0], f + j) : 0.f;
-      if (GATED) y[0][j] = gated(y[0][j], y[C::PARTS - 1][j] + (in ? bias_at(p.bias[1], f + j) : 0.f), p.act);
+      if (GATED) y[0][j] = activation(y[0][j], p.act) * (y[C::PARTS - 1][j] + (in ? bias_at(p.bias[1], f + j) : 0.f));
     }
     if (GATED && p.out_type == HILO_E4M3) {
       float m = 0.f, inv, sc;
@@ -666,8 +644,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
           f2_split(acc[1][j], u0, u1);
           const int f = f1 + 2 * j;
           const bool in = f < p.n;
-          y[2 * j] = in ? gated(g0 + bias_at(p.bias[0], f), u0 + bias_at(p.bias[1], f), p.act) : 0.f;
-          y[2 * j + 1] = in ? gated(g1 + bias_at(p.bias[0], f + 1), u1 + bias_at(p.bias[1], f + 1), p.act) : 0.f;
+          y[2 * j] = in ? activation(g0 + bias_at(p.bias[0], f), p.act) * (u0 + bias_at(p.bias[1], f)) : 0.f;
+          y[2 * j + 1] = in ? activation(g1 + bias_at(p.bias[0], f + 1), p.act) * (u1 + bias_at(p.bias[1], f + 1)) : 0.f;
           m = fmaxf(m, fmaxf(fabsf(y[2 * j]), fabsf(y[2 * j + 1])));
         }
         if (p.out_type == HILO_E4M3) {

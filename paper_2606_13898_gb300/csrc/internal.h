@@ -166,6 +166,18 @@ struct Gemm128Args {
 };
 cudaError_t launch_gemm128(const Gemm128Args& a, int device, int num_sms, cudaStream_t st);
 int gemm128_take_device_error();
+// ---- group norm of images, channels last (group_norm.cu)
+struct GroupNormArgs {
+  hilo_group_norm_shape s;
+  hilo_norm_vectors vec;
+  const void* x;
+  void* y;
+  float* y_scale;
+  void* ws;
+};
+size_t group_norm_workspace_bytes(const hilo_group_norm_shape& s);
+// *launches: kernels launched, also where one of them fails
+cudaError_t launch_group_norm(const GroupNormArgs& a, int device, int num_sms, int* launches, cudaStream_t st);
 // The wait-timeout probe: one bounded mbarrier wait that runs out; its code
 // is read (and cleared) like the kernels' device error words.
 cudaError_t launch_wait_probe(cudaStream_t st);

@@ -24,35 +24,6 @@ struct QuantParams {
   int rows, cols, blocks;                // blocks: of a row, ceil(cols / 128)
 };
 
-// Eight elements from 16-byte aligned memory, as they are there (TYPE 0 bf16, 1 fp16, 2 fp32).
-template <int TYPE>
-struct Eight {
-  uint4 q[TYPE == 2 ? 2 : 1];
-  __device__ __forceinline__ void clear() {
-    for (auto& v : q) v = make_uint4(0u, 0u, 0u, 0u);
-  }
-  __device__ __forceinline__ void load(const unsigned char* p) {
-#pragma unroll
-    for (int i = 0; i < (TYPE == 2 ? 2 : 1); ++i) q[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-  }
-  __device__ __forceinline__ void widen(float* f) const {
-    const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[TYPE == 2 ? 1 : 0].x, q[TYPE == 2 ? 1 : 0].y,
-                           q[TYPE == 2 ? 1 : 0].z, q[TYPE == 2 ? 1 : 0].w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (TYPE == 2) f[i] = __uint_as_float(w[i]);
-      else if (TYPE == 0) f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
-      else f[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu)));
-    }
-  }
-};
-
-__device__ __forceinline__ float amax8(const float* f, float m) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
-  return m;
-}
-
 // A scale per row and 128 columns. A half warp has a block, eight columns a lane; a warp has
 // two neighbouring blocks of a row at a time, and U of these on their way at once.
 template <int TYPE, int U>
@@ -72,7 +43,7 @@ __global__ void __launch_bounds__(THREADS) quant128_rows_kernel(const __grid_con
     col[u] = static_cast<int>(c - static_cast<long long>(row[u]) * pairs) * 256 + lane * 8;
     if (c >= total) col[u] = p.cols;
     x[u].clear();
-    if (col[u] < p.cols) x[u].load(p.src + row[u] * p.src_row + static_cast<long long>(col[u]) * (TYPE == 2 ? 4 : 2));
+    if (col[u] < p.cols) x[u].load_once(p.src + row[u] * p.src_row + static_cast<long long>(col[u]) * (TYPE == 2 ? 4 : 2));
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -103,7 +74,7 @@ __global__ void __launch_bounds__(THREADS) quant128_tiles_kernel(const __grid_co
   for (int i = 0; i < 8; ++i) {
     const int row = row0 + 16 * i;
     x[i].clear();
-    if (row < rows && col < p.cols) x[i].load(p.src + row * p.src_row + static_cast<long long>(col) * (TYPE == 2 ? 4 : 2));
+    if (row < rows && col < p.cols) x[i].load_once(p.src + row * p.src_row + static_cast<long long>(col) * (TYPE == 2 ? 4 : 2));
   }
   float m = 0.f, inv, sc;
 #pragma unroll

@@ -118,6 +118,11 @@ class hilo_gemm128_shape(ctypes.Structure):
                                                  "out_scale_ld")])
 
 
+class hilo_group_norm_shape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "rows", "d", "groups", "act", "x_dtype", "y_dtype", "vec_dtype")]
+                + [("eps", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("x_row", "y_row", "vec_row", "y_scale_ld")])
+
+
 EXPORTS = ("hilo_status_string", "hilo_last_error", "hilo_sync_status", "hilo_device_info",
            "hilo_score", "hilo_split_workspace_bytes", "hilo_split", "hilo_pack",
            "hilo_block_workspace_bytes", "hilo_block_forward", "hilo_unpack", "hilo_unpack_update",
@@ -127,7 +132,8 @@ EXPORTS = ("hilo_status_string", "hilo_last_error", "hilo_sync_status", "hilo_de
            "hilo_row_capacity", "hilo_quantize_rows_e4m3", "hilo_block_fp8_workspace_bytes",
            "hilo_block_forward_fp8", "hilo_block_forward_fp8_prop", "hilo_debug_wait_timeout",
            "hilo_row_positions", "hilo_rope", "hilo_gate_norm", "hilo_attention_workspace_bytes", "hilo_attention",
-           "hilo_block_forward_mod", "hilo_quantize_e4m3_128", "hilo_gemm_e4m3_128", "hilo_gated_e4m3_128")
+           "hilo_block_forward_mod", "hilo_quantize_e4m3_128", "hilo_gemm_e4m3_128", "hilo_gated_e4m3_128",
+           "hilo_group_norm_workspace_bytes", "hilo_group_norm")
 
 _lib = None
 
@@ -193,6 +199,8 @@ def lib() -> ctypes.CDLL:
                                        ctypes.c_int32, P, P, I, P, P, P, S, P]),
         "hilo_quantize_e4m3_128": (I, [ctypes.POINTER(hilo_quant128_shape), P, P, P, P, P]),
         "hilo_gemm_e4m3_128": (I, [ctypes.POINTER(hilo_gemm128_shape)] + [P] * 8),
+        "hilo_group_norm_workspace_bytes": (S, [ctypes.POINTER(hilo_group_norm_shape)]),
+        "hilo_group_norm": (I, [ctypes.POINTER(hilo_group_norm_shape), ctypes.POINTER(hilo_norm_vectors), P, P, P, P, S, P]),
         "hilo_gated_e4m3_128": (I, [ctypes.POINTER(hilo_gemm128_shape)] + [P] * 12),
     }
     for name, (res, args) in sig.items():
@@ -564,6 +572,33 @@ class Gemm128Shape:
         return self.__dict__.get("_c") or _kept(self, build)
 
 
+@dataclasses.dataclass(frozen=True)
+class GroupNormShape:
+    """Images, groups and dtypes of hilo_group_norm. Strides None: dense rows, vectors and scales."""
+
+    B: int
+    rows: int
+    d: int
+    groups: int = 32
+    act: int = HILO_ACT_NONE
+    eps: float = 1e-5
+    x_dtype: int = HILO_BF16
+    y_dtype: int = HILO_BF16
+    vec_dtype: int = HILO_BF16
+    x_row: int | None = None
+    y_row: int | None = None
+    vec_row: int | None = None
+    y_scale_ld: int | None = None
+
+    def c(self) -> hilo_group_norm_shape:
+        def build():
+            given = (self.x_row, self.y_row, self.vec_row, self.y_scale_ld)
+            return hilo_group_norm_shape(self.B, self.rows, self.d, self.groups, self.act, self.x_dtype, self.y_dtype,
+                                         self.vec_dtype, self.eps,
+                                         *(d if s is None else s for s, d in zip(given, (self.d,) * 3 + (self.B * self.rows,))))
+        return self.__dict__.get("_c") or _kept(self, build)
+
+
 @dataclasses.dataclass
 class BlockMod:
     """Conditioning of one block (hilo_block_forward_mod). axis_dims None: no rotary positions."""
@@ -785,6 +820,20 @@ def hilo_gated_e4m3_128(shape: Gemm128Shape, a, a_scale, w_gate, s_gate, w_up, s
     _check("hilo_gated_e4m3_128", lib().hilo_gated_e4m3_128(
         ctypes.byref(shape.c()), _ptr(a), _ptr(a_scale), _ptr(w_gate), _ptr(s_gate), _ptr(w_up), _ptr(s_up),
         _ptr(b_gate), _ptr(b_up), _ptr(n_rows), _ptr(out), _ptr(out_scale), _stream(stream)))
+
+
+def hilo_group_norm_workspace_bytes(shape: GroupNormShape) -> int:
+    n = int(lib().hilo_group_norm_workspace_bytes(ctypes.byref(shape.c())))
+    if n == 0:
+        raise HiloError("hilo_group_norm_workspace_bytes", HILO_ERR_SHAPE, lib().hilo_last_error().decode())
+    return n
+
+
+def hilo_group_norm(shape: GroupNormShape, vectors: NormVectors | None, x, y, y_scale, ws, ws_bytes: int,
+                    stream=None) -> None:
+    _check("hilo_group_norm", lib().hilo_group_norm(
+        ctypes.byref(shape.c()), None if vectors is None else ctypes.byref(vectors.c()), _ptr(x), _ptr(y), _ptr(y_scale),
+        _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def hilo_block_forward_static_ws(shape: Shape, weights: DeviceWeights, cu_img, cap: int, in_txt, in_img,
