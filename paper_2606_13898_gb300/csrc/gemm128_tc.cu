@@ -22,6 +22,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <stdlib.h>
 
 #include "attn_common.cuh"
 #include "common.cuh"
@@ -99,49 +100,134 @@ __device__ __forceinline__ void tmem_ld_wait_n(float* v) {
   }
 }
 
-// ----------------------------------------------------------- scales in flight --
-// A warp's scales of the blocks to come, through its own ring in shared memory: four bytes
-// a lane and copy, so any row offset will do; no other warp is waited for.
+// An arrival on a barrier of this cluster that says only that tensor memory was read: ordered by tcgen05.wait::ld and
+// tcgen05's fences. (One that releases the thread's other memory accesses to the cluster waits for all of them, the
+// scales on their way among them: 8192 rows of 10240, 4096 features 718 us.)
+__device__ __forceinline__ void arrive_peer(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// Whether the phase is complete, without waiting for it (try_wait may stay for microseconds).
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// ----------------------------------------------------------------- scales --
+// One warp copies each block's scales, of the rows and of the weights' parts, into a ring of SLOTS slots in
+// shared memory, asynchronously and four bytes at a time, so that any row offset will do; the copies arrive on
+// the slot's barrier themselves. (4864 rows of 16384, 4096 features: 431 us where the sums' warps loaded their scales
+// four blocks ahead, 270 where one warp loaded two blocks' and then wrote them: its loads' latency.)
+constexpr int SLOTS = 8;
+
+struct ScaleRing {
+  float* slots;
+  uint64_t *full, *empty;  // [SLOTS]: copied (an arrival per lane); read by the sums' warps
+  int size;                // floats of a slot
+};
 
 __device__ __forceinline__ void copy4(void* dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// A slot: the scales of ROWS rows (0 behind `rows`), then the weights' PARTS. as, ws: of the first block; as is this lane's.
+template <int ROWS, int PARTS>
+__device__ __forceinline__ bool fill_scales(const ScaleRing& ring, uint32_t& n, int nkb, int rows, const float* as, long long a_step,
+                                            const float* w0, const float* w1, volatile int* abort_flag, int* err, int code) {
+  const int lane = lane_id();
+  const float* ws = lane == 0 ? w0 : w1;
+  for (int i = 0; i < nkb; ++i, ++n) {
+    const uint32_t k = n % SLOTS;
+    if (!mbar_wait_warp(&ring.empty[k], ((n / SLOTS) & 1u) ^ 1u, abort_flag, err, code)) return false;
+    float* to = ring.slots + k * ring.size;
+#pragma unroll
+    for (int j = 0; j < ROWS; j += 32)
+      if (ROWS >= 32 || lane < ROWS) copy4(to + j + lane, j + lane < rows ? as + j : w0, j + lane < rows);
+    if (lane < PARTS) copy4(to + ROWS + lane, ws, true);
+    copies_arrive(&ring.full[k]);
+    as += a_step;
+    ++ws;
+  }
+  return true;
 }
 
-constexpr int SCALES_AHEAD = 4;
+// Biases of features n and n + 1 (n even).
+__device__ __forceinline__ float2 bias2(const __nv_bfloat16* b, int n) {
+  return make_float2(__bfloat162float(__ldg(b + n)), __bfloat162float(__ldg(b + n + 1)));
+}
 
-__device__ __forceinline__ float bias_at(const __nv_bfloat16* b, int n) { return b ? __bfloat162float(__ldg(b + n)) : 0.f; }
+__device__ __forceinline__ void st_32bytes(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "l"(p)
+               : "memory");
+}
+// 32 bytes of a lane's own row: a whole sector where the row begins on one.
+__device__ __forceinline__ void store32(void* p, const uint32_t* w, bool wide) {
+  if (wide) {
+    st_32bytes(p, w);
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+// 16 values of a row, rounded once (fp16 saturating).
+__device__ __forceinline__ void store16(void* out, int type, long long at, const float* v, bool wide) {
+  uint32_t w[8];
+  if (type == HILO_F32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * h + j]);
+      store32(static_cast<float*>(out) + at + 8 * h, w, wide);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = type == HILO_F16 ? pack_f16x2_sat(v[2 * j], v[2 * j + 1]) : pack_bf16x2(v[2 * j], v[2 * j + 1]);
+    store32(static_cast<uint16_t*>(out) + at, w, wide);
+  }
+}
 
 // ------------------------------------------------------------------- few rows --
 
-constexpr int FEW_THREADS = 320;  // eight warps for the sums, one for the copies, one for the products
-constexpr int FEW_SPLIT = 8;      // CTAs of a cluster at most
+constexpr int FEW_SPLIT = 8;  // CTAs of a cluster at most
+// Registers of a thread where a CTA has the SM to itself.
+constexpr uint32_t SUM_REGS = 232, CONTROL_REGS = 40;
+static_assert(256 * SUM_REGS + 128 * CONTROL_REGS <= 65536, "registers of an SM");
 
 template <int NT, bool GATED>
 struct Few {
   static constexpr int PARTS = GATED ? 2 : 1;
   static constexpr int STAGE = PARTS * PIECE + NT * BK;
   static constexpr int CTAS = NT * PARTS <= 64 ? 2 : 1;  // per SM
+  // eight warps for the sums, one each for copies, products and scales (and one to make whole warpgroups)
+  static constexpr int THREADS = CTAS == 2 ? 352 : 384;
   static constexpr int STAGES = CTAS == 2 ? (104 * 1024) / STAGE : (200 * 1024) / STAGE;
   static constexpr int BUFS = NT * PARTS <= 64 ? 4 : 2;
   static constexpr int NEED = BUFS * PARTS * NT;
   static constexpr uint32_t TMEM_COLS = NEED <= 64 ? 64 : NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
-  static constexpr int COLS = NT / 2;  // of a warp
-  static constexpr int SLOT = COLS + 4;  // floats of a warp's scales of a block: its rows', its weights'
+  static constexpr int COLS = NT / 2;         // of a warp
+  static constexpr int SLOT = NT + 4;         // floats of a block's scales
   static constexpr int OFF_BARS = STAGES * STAGE;
-  static constexpr int OFF_SCALES = OFF_BARS + 256;
-  static constexpr int SMEM_BYTES = OFF_SCALES + 8 * SCALES_AHEAD * SLOT * 4 + 1024;
+  static constexpr int OFF_SCALES = OFF_BARS + 384;
+  static constexpr int SMEM_BYTES = OFF_SCALES + SLOTS * SLOT * 4 + 1024;
   static_assert(STAGES * STAGE >= PARTS * NT * 128 * 4, "the sums take the stages' place");
-  static_assert((2 * STAGES + 2 * BUFS + 3) * 8 <= 256, "room for the barriers");
+  static_assert((2 * STAGES + 2 * BUFS + 2 * SLOTS + 3) * 8 <= 384, "room for the barriers");
   static_assert(SMEM_BYTES <= (CTAS == 2 ? 112 : 226) * 1024, "shared memory");
 };
 
 template <int NT, bool GATED>
-__global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
+__global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
     few128_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                   const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ Params128 p, int split) {
   using C = Few<NT, GATED>;
@@ -151,7 +237,8 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
   uint64_t* empty = full + C::STAGES;
   uint64_t* tfull = empty + C::STAGES;
   uint64_t* tempty = tfull + C::BUFS;
-  uint64_t* drain = tempty + C::BUFS;
+  const ScaleRing ring = {reinterpret_cast<float*>(smem + C::OFF_SCALES), tempty + C::BUFS, tempty + C::BUFS + SLOTS, C::SLOT};
+  uint64_t* drain = ring.empty + SLOTS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* err = &g_gemm128_err;
@@ -165,6 +252,10 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
     for (int b = 0; b < C::BUFS; ++b) {
       mbar_init(&tfull[b], 1);
       mbar_init(&tempty[b], 8);
+    }
+    for (int k = 0; k < SLOTS; ++k) {
+      mbar_init(&ring.full[k], 32);
+      mbar_init(&ring.empty[k], 8);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -195,6 +286,7 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
   const int kb0 = static_cast<int>(static_cast<long long>(p.kblocks) * rank / split);
   const int nkb = static_cast<int>(static_cast<long long>(p.kblocks) * (rank + 1) / split) - kb0;
 
+  if (C::CTAS == 1 && warp >= 8) setmaxnreg_dec<CONTROL_REGS>();
   if (warp == 8) {
     // ---------------- copies
     const bool issuer = elect_one();
@@ -268,66 +360,65 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
       }
     }
     __syncwarp();
-  } else {
+  } else if (warp == 10) {
+    // ---------------- scales
+    const long long w = (f0 >> 7) * p.w_scale_ld + kb0;
+    uint32_t n = 0;
+    fill_scales<NT, C::PARTS>(ring, n, nkb, rows, p.a_scale + kb0 * p.a_scale_ld + r0 + lane, p.a_scale_ld, p.w_scale[0] + w,
+                              p.w_scale[C::PARTS - 1] + w, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 22);
+    copies_done();
+    __syncwarp();
+  } else if (warp < 8) {
+    if (C::CTAS == 1) setmaxnreg_inc<SUM_REGS>();
     // ---------------- sums: lane quarter warp % 4 (32 features), half of the columns
     const int q = warp & 3, col0 = (warp >> 2) * C::COLS;
-    float* ring = reinterpret_cast<float*>(smem + C::OFF_SCALES) + warp * SCALES_AHEAD * C::SLOT;
-    const float* ws0 = p.w_scale[0] + (f0 >> 7) * p.w_scale_ld + kb0;
-    const float* ws1 = GATED ? p.w_scale[1] + (f0 >> 7) * p.w_scale_ld + kb0 : ws0;
-    const float* as = p.a_scale + kb0 * p.a_scale_ld + r0 + col0;
-    auto fetch = [&](int i) {
-      if (i < nkb) {
-        float* slot = ring + (i % SCALES_AHEAD) * C::SLOT;
-#pragma unroll
-        for (int c = 0; c < C::COLS; c += 32) {
-          const bool in = col0 + c + lane < rows;
-          if (c + lane < C::COLS) copy4(slot + c + lane, in ? as + i * p.a_scale_ld + c + lane : p.a_scale, in);
-        }
-        if (lane < C::PARTS) copy4(slot + C::COLS + lane, (lane ? ws1 : ws0) + i, true);
-      }
-      copies_commit();
-    };
-    for (int i = 0; i < SCALES_AHEAD - 1; ++i) fetch(i);
     uint64_t acc[C::PARTS][C::COLS / 2] = {};
     const uint32_t taddr = tmem + (static_cast<uint32_t>(q * 32) << 16) + col0;
-    bool ok = true;
+    constexpr int STEP = C::COLS < 32 ? C::COLS : 32, LOADS = C::PARTS * C::COLS / STEP;
+    bool ok = true, there_already = false;  // block i's products and scales
+#pragma unroll 1
     for (int i = 0; i < nkb; ++i) {
-      __syncwarp();  // (the slot that is fetched into was read by all lanes)
-      fetch(i + SCALES_AHEAD - 1);
-      const int b = i % C::BUFS;
-      if (!mbar_wait_warp(&tfull[b], static_cast<uint32_t>(i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 15)) {
+      const int b = i % C::BUFS, k = i % SLOTS;
+      if (!there_already &&
+          (!mbar_wait_warp(&ring.full[k], static_cast<uint32_t>(i / SLOTS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 21) ||
+           !mbar_wait_warp(&tfull[b], static_cast<uint32_t>(i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 15))) {
         ok = false;
         break;
       }
       tc_fence_after();
-      constexpr int STEP = C::COLS < 32 ? C::COLS : 32, LOADS = C::PARTS * C::COLS / STEP;
-      float v[LOADS][STEP];
-#pragma unroll
-      for (int l = 0; l < LOADS; ++l)
-        tmem_ldn<STEP>(taddr + b * C::PARTS * NT + (l * STEP / C::COLS) * NT + l * STEP % C::COLS, v[l]);
-      copies_wait<SCALES_AHEAD - 1>();
-      __syncwarp();  // every lane's copies of block i have arrived
-#pragma unroll
-      for (int l = 0; l < LOADS; ++l) tmem_ld_wait_n<STEP>(v[l]);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&tempty[b]);
-      const float* slot = ring + (i % SCALES_AHEAD) * C::SLOT;
+      auto column = [&](int l) {
+        return taddr + static_cast<uint32_t>((b * C::PARTS + l * STEP / C::COLS) * NT + l * STEP % C::COLS);
+      };
+      const float* slot = ring.slots + k * C::SLOT;
+      float v[2][STEP];
+      tmem_ldn<STEP>(column(0), v[0]);
 #pragma unroll
       for (int l = 0; l < LOADS; ++l) {
+        tmem_ld_wait_n<STEP>(v[l & 1]);
+        if (l + 1 < LOADS) {
+          tmem_ldn<STEP>(column(l + 1), v[(l + 1) & 1]);
+        } else {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tempty[b]);
+          // asked beside the last sums: a wait takes a hundred cycles where it has nothing to wait for
+          const uint32_t n = static_cast<uint32_t>(i) + 1;
+          there_already = __all_sync(0xffffffffu, mbar_test(&ring.full[n % SLOTS], (n / SLOTS) & 1u) &&
+                                                      mbar_test(&tfull[n % C::BUFS], (n / C::BUFS) & 1u));
+        }
         const int g = l * STEP / C::COLS, c0 = l * STEP % C::COLS;
-        const float w = slot[C::COLS + g];
-        const uint64_t w2 = f2(w, w);
+        const uint64_t w2 = f2(slot[NT + g], slot[NT + g]);
 #pragma unroll
         for (int c = 0; c < STEP; c += 4) {
-          const float4 s = *reinterpret_cast<const float4*>(slot + c0 + c);
+          const float4 s = *reinterpret_cast<const float4*>(slot + col0 + c0 + c);
           uint64_t* o = &acc[g][(c0 + c) / 2];
-          o[0] = f2_fma(f2(v[l][c], v[l][c + 1]), f2_mul(f2(s.x, s.y), w2), o[0]);
-          o[1] = f2_fma(f2(v[l][c + 2], v[l][c + 3]), f2_mul(f2(s.z, s.w), w2), o[1]);
+          o[0] = f2_fma(f2(v[l & 1][c], v[l & 1][c + 1]), f2_mul(f2(s.x, s.y), w2), o[0]);
+          o[1] = f2_fma(f2(v[l & 1][c + 2], v[l & 1][c + 3]), f2_mul(f2(s.z, s.w), w2), o[1]);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ring.empty[k]);
     }
-    copies_wait<0>();
     if (ok) {
       // [part][row][feature], over the stages: every product has been waited for. (After a given-up wait
       // copies may still arrive there; nothing is written then, and what is read below is not meant to be right.)
@@ -342,50 +433,70 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
           sums[(g * NT + col0 + c + 1) * 128] = hi;
         }
     }
-  }
-  __syncthreads();
-  if (split > 1) cluster_sync();
-  // ---- rows rank, rank + split, ..: a warp each, four features a lane, the CTAs' sums in the order of K
-  const bool good = *abort_flag == 0;
-  const int f = f0 + 4 * lane;
-  const uint32_t mine = smem_u32(smem) + 16 * lane;
-  for (int t = rank + split * warp; good && t < rows; t += split * (FEW_THREADS / 32)) {
-    float y[C::PARTS][4] = {};
-    for (int s = 0; s < split; ++s)
+    if (split > 1) cluster_sync();
+    else named_bar_sync(1, 256);
+    // ---- rows rank, rank + split, ..: a warp each, four features a lane, the CTAs' sums in the order of K
+    const bool good = *abort_flag == 0;
+    const int f = f0 + 4 * lane;
+    const uint32_t mine = smem_u32(smem) + 16 * lane;
+    for (int t = rank + split * warp; good && t < rows; t += split * 8) {
+      float y[C::PARTS][4] = {};
+      // (all CTAs' sums, four at a time, on their way before the first is added)
+      for (int s0 = 0; s0 < split; s0 += 4) {
+        float4 v[4][C::PARTS];
 #pragma unroll
-      for (int g = 0; g < C::PARTS; ++g) {
-        float4 v;
-        const uint32_t at = mapa_shared(mine + (g * NT + t) * 512, split > 1 ? s : 0);
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                     : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                     : "r"(at)
-                     : "memory");
-        y[g][0] += v.x;
-        y[g][1] += v.y;
-        y[g][2] += v.z;
-        y[g][3] += v.w;
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int g = 0; g < C::PARTS; ++g) {
+            v[s][g] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (s0 + s >= split) continue;
+            const uint32_t at = mapa_shared(mine + (g * NT + t) * 512, s0 + s);
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(v[s][g].x), "=f"(v[s][g].y), "=f"(v[s][g].z), "=f"(v[s][g].w)
+                         : "r"(at)
+                         : "memory");
+          }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int g = 0; g < C::PARTS; ++g) {
+            y[g][0] += v[s][g].x;
+            y[g][1] += v[s][g].y;
+            y[g][2] += v[s][g].z;
+            y[g][3] += v[s][g].w;
+          }
       }
-    const bool in = f < p.n;  // (n is a multiple of 16)
+      const bool in = f < p.n;  // (n is a multiple of 16)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      y[0][j] += in ? bias_at(p.bias[0], f + j) : 0.f;
-      if (GATED) y[0][j] = activation(y[0][j], p.act) * (y[C::PARTS - 1][j] + (in ? bias_at(p.bias[1], f + j) : 0.f));
-    }
-    if (GATED && p.out_type == HILO_E4M3) {
-      float m = 0.f, inv, sc;
+      for (int g = 0; g < C::PARTS; ++g)
+        if (p.bias[g] && in)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) m = fmaxf(m, in ? fabsf(y[0][j]) : 0.f);
+          for (int j = 0; j < 4; j += 2) {
+            const float2 v = bias2(p.bias[g], f + j);
+            y[g][j] += v.x;
+            y[g][j + 1] += v.y;
+          }
+      if (GATED)
 #pragma unroll
-      for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-      block_scale(m, inv, sc);
-      if (in)
-        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.out) + (r0 + t) * p.out_row + f) =
-            pack_e4m3x4(__fmul_rn(y[0][0], inv), __fmul_rn(y[0][1], inv), __fmul_rn(y[0][2], inv), __fmul_rn(y[0][3], inv));
-      if (lane == 0) p.out_scale[(f0 >> 7) * p.out_scale_ld + r0 + t] = sc;
-    } else if (in) {
-      store4(p.out, p.out_type, (r0 + t) * p.out_row + f, y[0]);
+        for (int j = 0; j < 4; ++j) y[0][j] = activation(y[0][j], p.act) * y[C::PARTS - 1][j];
+      if (GATED && p.out_type == HILO_E4M3) {
+        float m = 0.f, inv, sc;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = fmaxf(m, in ? fabsf(y[0][j]) : 0.f);
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+        block_scale(m, inv, sc);
+        if (in)
+          *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.out) + (r0 + t) * p.out_row + f) =
+              pack_e4m3x4(__fmul_rn(y[0][0], inv), __fmul_rn(y[0][1], inv), __fmul_rn(y[0][2], inv), __fmul_rn(y[0][3], inv));
+        if (lane == 0) p.out_scale[(f0 >> 7) * p.out_scale_ld + r0 + t] = sc;
+      } else if (in) {
+        store4(p.out, p.out_type, (r0 + t) * p.out_row + f, y[0]);
+      }
     }
   }
+  // (the other warps come to the two meetings of the cluster, too)
+  if (split > 1 && warp >= 8) cluster_sync();
   tc_fence_before();
   __syncthreads();
   if (split > 1) cluster_sync();  // no CTA leaves while another reads its sums
@@ -397,30 +508,42 @@ __global__ void __launch_bounds__(FEW_THREADS, Few<NT, GATED>::CTAS)
 
 // ------------------------------------------------------------------ many rows --
 
-constexpr int MANY_THREADS = 384;  // two warpgroups for the sums, one for copies and products
-constexpr uint32_t SUM_REGS = 216, CONTROL_REGS = 72;
-static_assert(256 * SUM_REGS + 128 * CONTROL_REGS <= 65536, "registers of an SM");
-constexpr int MANY_STAGES = 6;
-constexpr int MANY_STAGE = 2 * PIECE;  // 128 rows of A, 128 features: half of the pair's
-constexpr int MANY_BARS = MANY_STAGES * MANY_STAGE;
-constexpr int MANY_SLOT = 36;  // floats of a warp's scales of a block: its rows', the weights' two
-constexpr int MANY_SCALES = MANY_BARS + 256;
-constexpr int MANY_MOST = MANY_SCALES + 8 * SCALES_AHEAD * MANY_SLOT * 4;  // [2][128] row maxima
-constexpr int MANY_SMEM = MANY_MOST + 2 * 128 * 4 + 1024;
-static_assert(MANY_SMEM <= 227 * 1024, "shared memory of a CTA");
+constexpr int SUM_WARPS = 16;
+constexpr int MANY_THREADS = 32 * (SUM_WARPS + 4);  // the sums' four warpgroups, one for copies, products and scales
+constexpr uint32_t MANY_SUM_REGS = 112, MANY_CONTROL_REGS = 32;
+constexpr int MANY_LAUNCH = 32 * SUM_WARPS * MANY_SUM_REGS + 128 * MANY_CONTROL_REGS;  // registers that the split needs
+constexpr int MANY_SMEM = 222 * 1024;
+
+// A pair's tile: 256 rows, NT columns of the product: NT features, or NT / 2 of gate and NT / 2 of up.
+template <int NT, bool GATED>
+struct Many {
+  static constexpr int TF = GATED ? NT / 2 : NT;     // features
+  static constexpr int STAGE = PIECE + NT / 2 * BK;  // 128 rows, and half of the columns
+  static constexpr int BUFS = 512 / NT;              // of tensor memory
+  static constexpr int COLS = NT / 8;                // of a warp, in each half of the columns
+  static constexpr int LOAD = 16;                    // columns read at a time
+  static constexpr int SLOT = 128 + 4;                      // floats of a block's scales: its rows', the weights' of both halves
+  static constexpr int SCALES_BYTES = SLOTS * SLOT * 4, MOST_BYTES = 4 * 128 * 4;  // [4][128] row maxima
+  static constexpr int STAGES = (MANY_SMEM - 1024 - 384 - SCALES_BYTES - MOST_BYTES) / STAGE;
+  static constexpr int OFF_BARS = STAGES * STAGE, OFF_SCALES = OFF_BARS + 384, OFF_MOST = OFF_SCALES + SCALES_BYTES;
+  static_assert(OFF_MOST + MOST_BYTES + 1024 <= MANY_SMEM, "shared memory of a CTA");
+  static_assert((2 * STAGES + 2 * BUFS + 2 * SLOTS + 3) * 8 <= 384, "room for the barriers");
+};
 constexpr int PANEL = 8;  // row tiles that are taken together along the features
 
-template <bool GATED>
+template <int NT, bool GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
     many128_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                    const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ Params128 p) {
+  using C = Many<NT, GATED>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + MANY_BARS);
-  uint64_t* empty = full + MANY_STAGES;
-  uint64_t* tfull = empty + MANY_STAGES;
-  uint64_t* tempty = tfull + 2;
-  uint64_t* drain = tempty + 2;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BARS);
+  uint64_t* empty = full + C::STAGES;
+  uint64_t* tfull = empty + C::STAGES;
+  uint64_t* tempty = tfull + C::BUFS;
+  const ScaleRing ring = {reinterpret_cast<float*>(smem + C::OFF_SCALES), tempty + C::BUFS, tempty + C::BUFS + SLOTS, C::SLOT};
+  uint64_t* drain = ring.empty + SLOTS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* err = &g_gemm128_err;
@@ -429,24 +552,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
   const bool leader = rank == 0;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < MANY_STAGES; ++s) {
+    for (int s = 0; s < C::STAGES; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < C::BUFS; ++b) {
       mbar_init(&tfull[b], 1);
-      mbar_init(&tempty[b], 16);
+      mbar_init(&tempty[b], 2 * SUM_WARPS);
+    }
+    for (int k = 0; k < SLOTS; ++k) {
+      mbar_init(&ring.full[k], 32);
+      mbar_init(&ring.empty[k], SUM_WARPS);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 8 && lane == 0) {
+  if (warp == SUM_WARPS && lane == 0) {
     tma_prefetch_desc(&tm_a);
     tma_prefetch_desc(&tm_w0);
     tma_prefetch_desc(&tm_w1);
   }
-  if (warp == 9) {
+  if (warp == SUM_WARPS + 1) {
     tmem_alloc_pair(tmem_slot, 512);
     tmem_relinquish_pair();
   }
@@ -460,7 +587,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
 
   // The pair's tiles: panels of PANEL row tiles, within one the row tiles of a feature tile after one another, so that the
   // pairs at work at a time read few rows and few features.
-  constexpr int TF = GATED ? 128 : 256;  // features of a tile
+  constexpr int TF = C::TF;
   const int rows = rows_there(p.n_rows, p.rows);
   const int row_tiles = (rows + 255) / 256, f_tiles = (p.n + TF - 1) / TF;
   const int tiles = row_tiles * f_tiles, step = gridDim.x >> 1;
@@ -471,9 +598,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
     f0 = f * TF;
   };
 
-  if (warp >= 8) {
-    setmaxnreg_dec<CONTROL_REGS>();
-    if (warp == 8) {
+  if (warp >= SUM_WARPS) {
+    setmaxnreg_dec<MANY_CONTROL_REGS>();
+    if (warp == SUM_WARPS) {
       // ---------------- copies (both CTAs)
       const bool issuer = elect_one();
       uint32_t armed = 0, par = 0;
@@ -485,22 +612,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
         int r0, f0;
         place(t, r0, f0);
         const CUtensorMap* tm_w = GATED && rank ? &tm_w1 : &tm_w0;
-        const int fw = GATED ? f0 : f0 + 128 * static_cast<int>(rank), rw = r0 + 128 * static_cast<int>(rank);
+        const int fw = GATED ? f0 : f0 + NT / 2 * static_cast<int>(rank), rw = r0 + 128 * static_cast<int>(rank);
         for (int kb = 0; kb < p.kblocks; ++kb) {
           if (!mbar_wait_warp(&empty[st], ph ^ 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 16)) {
             ok = false;
             break;
           }
           if (issuer) {
-            unsigned char* dst = smem + st * MANY_STAGE;
-            if (leader) mbar_arrive_expect_tx(&full[st], 2 * MANY_STAGE);
+            unsigned char* dst = smem + st * C::STAGE;
+            if (leader) mbar_arrive_expect_tx(&full[st], 2 * C::STAGE);
             tma_load_2d_pair(dst, &tm_a, full0 + 8u * st, kb * BK, rw);
             tma_load_2d_pair(dst + PIECE, tm_w, full0 + 8u * st, kb * BK, fw);
           }
           __syncwarp();
           armed |= 1u << st;
           par = (par & ~(1u << st)) | (ph << st);
-          if (++st == MANY_STAGES) {
+          if (++st == C::STAGES) {
             st = 0;
             ph ^= 1u;
           }
@@ -509,7 +636,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
       if (!ok) {  // the copies in flight, before the CTA can exit
         const uint64_t g0 = globaltimer_ns();
         if (leader) {
-          for (int s = 0; s < MANY_STAGES; ++s)
+          for (int s = 0; s < C::STAGES; ++s)
             if (armed >> s & 1u)
               while (!mbar_try_wait(smem_u32(&full[s]), par >> s & 1u) && globaltimer_ns() - g0 < HILO_WAIT_LIMIT_NS / 4) {
               }
@@ -519,10 +646,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
         }
       }
       __syncwarp();
-    } else if (warp == 9 && leader) {
+    } else if (warp == SUM_WARPS + 1 && leader) {
       // ---------------- products (the even CTA)
       const bool issuer = elect_one();
-      constexpr uint32_t idesc = idesc_kind_f16(256, 256, 0, 0, 0);  // (format code 0 is E4M3)
+      constexpr uint32_t idesc = idesc_kind_f16(256, NT, 0, 0, 0);  // (format code 0 is E4M3)
       constexpr uint32_t hi = sw128_hi(1024);
       const uint32_t base = (smem_u32(smem) >> 4) + sw128_lo_lbo(16);
       int st = 0;
@@ -530,22 +657,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
       bool ok = true;
       for (int t = blockIdx.x >> 1; ok && t < tiles; t += step) {
         for (int kb = 0; kb < p.kblocks; ++kb, ++i) {
-          const uint32_t b = i & 1u;
-          if (!mbar_wait_warp(&tempty[b], ((i >> 1) & 1u) ^ 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 17) ||
-              !mbar_wait_warp(&full[st], ph, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 18)) {
+          const uint32_t b = i % C::BUFS;
+          if (!mbar_wait_warp(&full[st], ph, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 17)) {
+            ok = false;
+            break;
+          }
+          if (!mbar_wait_warp(&tempty[b], ((i / C::BUFS) & 1u) ^ 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 18)) {
             ok = false;
             break;
           }
           tc_fence_after();
           if (issuer) {
-            const uint32_t a = base + static_cast<uint32_t>(st * MANY_STAGE >> 4), w = a + (PIECE >> 4);
+            const uint32_t a = base + static_cast<uint32_t>(st * C::STAGE >> 4), w = a + (PIECE >> 4);
 #pragma unroll
-            for (int k = 0; k < BK / 32; ++k) umma_pair_w<true>(tmem + 256 * b, a + 2 * k, w + 2 * k, hi, idesc, k > 0 ? 1u : 0u);
-            umma_commit_pair(&empty[st], 0x3);
+            for (int k = 0; k < BK / 32; ++k) umma_pair_w<true>(tmem + NT * b, a + 2 * k, w + 2 * k, hi, idesc, k > 0 ? 1u : 0u);
             umma_commit_pair(&tfull[b], 0x3);
+            umma_commit_pair(&empty[st], 0x3);
           }
           __syncwarp();
-          if (++st == MANY_STAGES) {
+          if (++st == C::STAGES) {
             st = 0;
             ph ^= 1u;
           }
@@ -561,130 +691,149 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
         }
       }
       __syncwarp();
+    } else if (warp == SUM_WARPS + 2) {
+      // ---------------- scales of this CTA's rows and the tile's two parts of the features
+      uint32_t n = 0;
+      for (int t = blockIdx.x >> 1; t < tiles; t += step) {
+        int r0, f0;
+        place(t, r0, f0);
+        const int row = r0 + 128 * static_cast<int>(rank);
+        const float* w0 = p.w_scale[0] + (f0 >> 7) * p.w_scale_ld;
+        const float* w1 = GATED ? p.w_scale[1] + (f0 >> 7) * p.w_scale_ld : p.w_scale[0] + (min(f0 + NT / 2, p.n - 1) >> 7) * p.w_scale_ld;
+        if (!fill_scales<128, 2>(ring, n, p.kblocks, rows - row, p.a_scale + row + lane, p.a_scale_ld, w0, w1, abort_flag, err,
+                                 DEV_TIMEOUT_GEMM + 256 * 24))
+          break;
+      }
+      copies_done();
+      __syncwarp();
     }
   } else {
-    setmaxnreg_inc<SUM_REGS>();
+    setmaxnreg_inc<MANY_SUM_REGS>();
     // ---------------- sums: lane quarter warp % 4 (32 rows), and of both halves of the columns (gate and up) the
-    // half of the warpgroup
+    // quarter warp / 4 (NT / 8 features)
     const int q = warp & 3, h = warp >> 2, r = 32 * q + lane;
-    float* ring = reinterpret_cast<float*>(smem + MANY_SCALES) + warp * SCALES_AHEAD * MANY_SLOT;
-    float* most = reinterpret_cast<float*>(smem + MANY_MOST);
-    const uint32_t taddr = tmem + (static_cast<uint32_t>(32 * q) << 16) + 64 * h;
+    float* most = reinterpret_cast<float*>(smem + C::OFF_MOST);
+    const uint32_t taddr = tmem + (static_cast<uint32_t>(32 * q) << 16) + C::COLS * h;
     const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
     uint32_t i = 0;
-    bool ok = true;
+    bool ok = true, there_already = false;  // block i's products and scales
     for (int t = blockIdx.x >> 1; t < tiles; t += step) {
       int r0, f0;
       place(t, r0, f0);
       const int row = r0 + 128 * static_cast<int>(rank) + r;
-      const int nb = f0 >> 7, nb_last = (p.n - 1) >> 7;
-      const float* ws = GATED && (lane & 1) ? p.w_scale[1] + nb * p.w_scale_ld
-                                            : p.w_scale[0] + (GATED ? nb : min(nb + (lane & 1), nb_last)) * p.w_scale_ld;
-      const float* as = p.a_scale + min(row, p.rows - 1);
-      auto fetch = [&](int kb) {
-        if (kb < p.kblocks) {
-          float* slot = ring + (kb % SCALES_AHEAD) * MANY_SLOT;
-          copy4(slot + lane, as + kb * p.a_scale_ld, true);
-          if (lane < 2) copy4(slot + 32 + lane, ws + kb, true);
-        }
-        copies_commit();
-      };
-      __syncwarp();
-      for (int kb = 0; kb < SCALES_AHEAD - 1; ++kb) fetch(kb);
-      uint64_t acc[2][32];
+      uint64_t acc[2][C::COLS / 2];
 #pragma unroll
-      for (int j = 0; j < 32; ++j) acc[0][j] = acc[1][j] = 0ull;
+      for (int j = 0; j < C::COLS / 2; ++j) acc[0][j] = acc[1][j] = 0ull;
 #pragma unroll 1
       for (int kb = 0; kb < p.kblocks; ++kb, ++i) {
-        __syncwarp();  // (the slot that is fetched into was read by all lanes)
-        fetch(kb + SCALES_AHEAD - 1);
-        const uint32_t b = i & 1u;
-        if (!mbar_wait_warp(&tfull[b], (i >> 1) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 20)) {
+        const uint32_t b = i % C::BUFS, k = i % SLOTS;
+        if (!there_already && (!mbar_wait_warp(&ring.full[k], (i / SLOTS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 23) ||
+                               !mbar_wait_warp(&tfull[b], (i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 20))) {
           ok = false;
           break;
         }
         tc_fence_after();
-        float v[2][32];
-        const uint32_t at = taddr + 256 * b;
-        tmem_ld32(at, v[0]);
-        copies_wait<SCALES_AHEAD - 1>();
-        __syncwarp();
-        const float* slot = ring + (kb % SCALES_AHEAD) * MANY_SLOT;
-        const float s0 = slot[lane] * slot[32], s1 = slot[lane] * slot[33];
+        const uint32_t at = taddr + NT * b;
+        const float* slot = ring.slots + k * C::SLOT;
+        const float s0 = slot[r] * slot[128], s1 = slot[r] * slot[129];
+        constexpr int LOADS = 2 * C::COLS / C::LOAD;  // the first half of them of the first half of the columns
+        auto column = [&](int c) { return at + (c * C::LOAD / C::COLS) * (NT / 2) + c * C::LOAD % C::COLS; };
+        float v[2][C::LOAD];
+        tmem_ldn<C::LOAD>(column(0), v[0]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          tmem_ld_wait_regs(v[c & 1]);
-          if (c < 3) {
-            tmem_ld32(at + ((c + 1) >> 1) * 128 + ((c + 1) & 1) * 32, v[(c + 1) & 1]);
+        for (int c = 0; c < LOADS; ++c) {
+          tmem_ld_wait_n<C::LOAD>(v[c & 1]);
+          if (c + 1 < LOADS) {
+            tmem_ldn<C::LOAD>(column(c + 1), v[(c + 1) & 1]);
           } else {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tempty0 + 8u * b);
+            if (lane == 0) {
+              arrive_peer(tempty0 + 8u * b);
+              mbar_arrive(&ring.empty[k]);
+            }
+            // asked beside the last sums: a wait takes a hundred cycles where it has nothing to wait for
+            const uint32_t n = i + 1;
+            there_already = __all_sync(0xffffffffu, mbar_test(&ring.full[n % SLOTS], (n / SLOTS) & 1u) &&
+                                                        mbar_test(&tfull[n % C::BUFS], (n / C::BUFS) & 1u));
           }
-          const float s = c < 2 ? s0 : s1;
+          const int g = c * C::LOAD / C::COLS, c0 = c * C::LOAD % C::COLS;
+          const float s = g ? s1 : s0;
           const uint64_t s2 = f2(s, s);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            uint64_t& o = acc[c >> 1][(c & 1) * 16 + j];
-            o = f2_fma(f2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), s2, o);
+          for (int j = 0; j < C::LOAD; j += 2) {
+            uint64_t& o = acc[g][(c0 + j) / 2];
+            o = f2_fma(f2(v[c & 1][j], v[c & 1][j + 1]), s2, o);
           }
         }
       }
-      copies_wait<0>();
-      if (!ok && !(GATED && p.out_type == HILO_E4M3)) break;
+      if (!ok && !(GATED && NT == 256 && p.out_type == HILO_E4M3)) break;
       // ---- the tile's rows
       const bool there = row < rows;
-      if (GATED) {
-        float y[64], m = 0.f;
-        const int f1 = f0 + 64 * h;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          float g0, g1, u0, u1;
-          f2_split(acc[0][j], g0, g1);
-          f2_split(acc[1][j], u0, u1);
-          const int f = f1 + 2 * j;
-          const bool in = f < p.n;
-          y[2 * j] = in ? activation(g0 + bias_at(p.bias[0], f), p.act) * (u0 + bias_at(p.bias[1], f)) : 0.f;
-          y[2 * j + 1] = in ? activation(g1 + bias_at(p.bias[0], f + 1), p.act) * (u1 + bias_at(p.bias[1], f + 1)) : 0.f;
-          m = fmaxf(m, fmaxf(fabsf(y[2 * j]), fabsf(y[2 * j + 1])));
+      // sums j, j + 1 of part g with their biases
+      auto sums = [&](int g, int f, int j, float& lo, float& hi) {
+        f2_split(acc[g][j / 2], lo, hi);
+        const __nv_bfloat16* bias = p.bias[GATED ? g : 0];
+        if (bias && f + j < p.n) {
+          const float2 v = bias2(bias, f + j);
+          lo += v.x;
+          hi += v.y;
         }
-        if (p.out_type == HILO_E4M3) {
+      };
+      if (GATED) {
+        const int f = f0 + C::COLS * h;
+        float y[C::COLS], m = 0.f;
+#pragma unroll
+        for (int j = 0; j < C::COLS; j += 2) {
+          float g0, g1, u0, u1;
+          sums(0, f, j, g0, g1);
+          sums(1, f, j, u0, u1);
+          y[j] = activation(g0, p.act) * u0;
+          y[j + 1] = activation(g1, p.act) * u1;
+          if (f + j < p.n) m = fmaxf(m, fmaxf(fabsf(y[j]), fabsf(y[j + 1])));
+        }
+        if (NT == 256 && p.out_type == HILO_E4M3) {  // (a tile's features are a block)
           most[128 * h + r] = m;
-          // the two warps of these rows go on together or not at all
-          ok = !bar_red_or(1 + q, 64, !ok);
+          // the four warps of these rows go on together or not at all
+          ok = !bar_red_or(1 + q, 128, !ok);
           if (!ok) break;
-          m = fmaxf(m, most[128 * (1 - h) + r]);
-          named_bar_sync(1 + q, 64);  // (read before the next tile's are written)
+#pragma unroll
+          for (int o = 0; o < 4; ++o) m = fmaxf(m, most[128 * o + r]);
+          named_bar_sync(1 + q, 128);  // (read before the next tile's are written)
           float inv, sc;
           block_scale(m, inv, sc);
           if (there) {
-            uint8_t* dst = static_cast<uint8_t*>(p.out) + row * p.out_row + f1;
+            const int nb = f0 >> 7;
+            uint8_t* dst = static_cast<uint8_t*>(p.out) + row * p.out_row + f;
+            uint32_t w[8] = {};
 #pragma unroll
-            for (int c = 0; c < 64; c += 16)
-              if (f1 + c < p.n) {
-                const uint2 lo = block_codes(y + c, inv), hi = block_codes(y + c + 8, inv);
-                *reinterpret_cast<uint4*>(dst + c) = make_uint4(lo.x, lo.y, hi.x, hi.y);
-              }
+            for (int j = 0; j < C::COLS; j += 8) {
+              const uint2 c = block_codes(y + j, inv);
+              w[j / 4] = c.x;
+              w[j / 4 + 1] = c.y;
+            }
+            if (f + 16 < p.n)
+              store32(dst, w, p.out_wide);
+            else if (f < p.n)
+              *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
             if (h == 0) p.out_scale[nb * p.out_scale_ld + row] = sc;
           }
         } else if (there) {
 #pragma unroll
-          for (int c = 0; c < 64; c += 4)
-            if (f1 + c < p.n) store4(p.out, p.out_type, row * p.out_row + f1 + c, y + c);
+          for (int c = 0; c < C::COLS; c += 16)
+            if (f + c < p.n) store16(p.out, p.out_type, row * p.out_row + f + c, y + c, p.out_wide);
         }
       } else if (there) {
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-          for (int c = 0; c < 64; c += 4) {
-            const int f = f0 + 128 * g + 64 * h + c;
-            if (f >= p.n) continue;
-            float y[4];
-            f2_split(acc[g][c / 2], y[0], y[1]);
-            f2_split(acc[g][c / 2 + 1], y[2], y[3]);
+          for (int c = 0; c < C::COLS; c += 16) {
+            const int f = f0 + NT / 2 * g + C::COLS * h;
+            if (f + c >= p.n) continue;
+            float y[16];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] += bias_at(p.bias[0], f + j);
-            store4(p.out, p.out_type, row * p.out_row + f, y);
+            for (int j = 0; j < 16; j += 2) sums(g, f, c + j, y[j], y[j + 1]);
+            store16(p.out, p.out_type, row * p.out_row + f + c, y, p.out_wide);
           }
       }
     }
@@ -693,7 +842,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
   tc_fence_before();
   __syncthreads();
   cluster_sync();  // no remote arrivals / copies into the peer after this point
-  if (warp == 9) {
+  if (warp == SUM_WARPS + 1) {
     tc_fence_after();
     tmem_dealloc_pair(tmem, 512);
   }
@@ -704,6 +853,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
 bool encode(CUtensorMap* m, const void* base, long long rows, long long k, long long row, int box) {
   return encode_tmap_2d(m, TMAP_U8, base, static_cast<uint64_t>(k), static_cast<uint64_t>(rows), static_cast<uint64_t>(row),
                         BK, static_cast<uint32_t>(box));
+}
+
+// The register split must fit what the CTA is launched with, or setmaxnreg.inc would wait forever. (One number for every
+// device: the library holds one binary.)
+template <auto KERNEL, int THREADS, int NEED>
+cudaError_t registers_fit() {
+  static std::atomic<int> known{0};
+  int regs = known.load(std::memory_order_relaxed);
+  if (regs == 0) {
+    cudaFuncAttributes fa;
+    const cudaError_t e = cudaFuncGetAttributes(&fa, KERNEL);
+    if (e != cudaSuccess) return e;
+    regs = fa.numRegs;
+    known.store(regs, std::memory_order_relaxed);
+  }
+  return regs * THREADS < NEED ? cudaErrorInvalidConfiguration : cudaSuccess;
 }
 
 template <int NT, bool GATED>
@@ -718,11 +883,12 @@ cudaError_t launch_few(const Gemm128Args& a, const Params128& p, int split, cuda
   auto* kern = few128_kernel<NT, GATED>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
   if (e != cudaSuccess) return e;
+  if (C::CTAS == 1 && (e = registers_fit<few128_kernel<NT, GATED>, 384, 256 * SUM_REGS + 128 * CONTROL_REGS>()) != cudaSuccess) return e;
   const dim3 grid(static_cast<unsigned>((s.n + 127) / 128 * split), static_cast<unsigned>((s.rows + NT - 1) / NT));
-  return launch_pdl_cluster(kern, split, grid, dim3(FEW_THREADS), C::SMEM_BYTES, st, ta, tw[0], tw[1], p, split);
+  return launch_pdl_cluster(kern, split, grid, dim3(C::THREADS), C::SMEM_BYTES, st, ta, tw[0], tw[1], p, split);
 }
 
-template <bool GATED>
+template <int NT, bool GATED>
 int resident_pairs(int device, int num_sms) {
   static PerDevice pairs;
   const int n = pairs.get(device, [&] {
@@ -738,7 +904,7 @@ int resident_pairs(int device, int num_sms) {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int found = 0;
-    if (cudaOccupancyMaxActiveClusters(&found, many128_kernel<GATED>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&found, many128_kernel<NT, GATED>, &cfg) != cudaSuccess) {
       cudaGetLastError();
       found = 0;
     }
@@ -747,31 +913,21 @@ int resident_pairs(int device, int num_sms) {
   return n > 0 ? n : num_sms / 2;
 }
 
-template <bool GATED>
+template <int NT, bool GATED>
 cudaError_t launch_many(const Gemm128Args& a, const Params128& p, int device, int num_sms, cudaStream_t st) {
   CUtensorMap ta, tw[2];
   const hilo_gemm128_shape& s = a.s;
   if (!encode(&ta, a.a, s.rows, s.k, s.a_row, 128)) return cudaErrorInvalidValue;
   for (int g = 0; g < (GATED ? 2 : 1); ++g)
-    if (!encode(&tw[g], a.w[g], s.n, s.k, s.w_row, 128)) return cudaErrorInvalidValue;
+    if (!encode(&tw[g], a.w[g], s.n, s.k, s.w_row, NT / 2)) return cudaErrorInvalidValue;
   if (!GATED) tw[1] = tw[0];
-  auto* kern = many128_kernel<GATED>;
+  auto* kern = many128_kernel<NT, GATED>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MANY_SMEM);
   if (e != cudaSuccess) return e;
-  // the register split must fit what the CTA is launched with (setmaxnreg.inc would wait forever)
-  static std::atomic<int> known{0};
-  int regs = known.load(std::memory_order_relaxed);
-  if (regs == 0) {
-    cudaFuncAttributes fa;
-    e = cudaFuncGetAttributes(&fa, kern);
-    if (e != cudaSuccess) return e;
-    regs = fa.numRegs;
-    known.store(regs, std::memory_order_relaxed);
-  }
-  if (static_cast<long long>(regs) * MANY_THREADS < 256LL * SUM_REGS + 128LL * CONTROL_REGS) return cudaErrorInvalidConfiguration;
-  const long long tiles = static_cast<long long>((s.rows + 255) / 256) * ((s.n + (GATED ? 127 : 255)) / (GATED ? 128 : 256));
+  if ((e = registers_fit<many128_kernel<NT, GATED>, MANY_THREADS, MANY_LAUNCH>()) != cudaSuccess) return e;
+  const long long tiles = static_cast<long long>((s.rows + 255) / 256) * ((s.n + Many<NT, GATED>::TF - 1) / Many<NT, GATED>::TF);
   if (tiles > 0x7fffffff / 2) return cudaErrorInvalidValue;
-  const int pairs = resident_pairs<GATED>(device, num_sms);
+  const int pairs = resident_pairs<NT, GATED>(device, num_sms);
   return launch_pdl_cluster(kern, 1, dim3(2 * static_cast<unsigned>(tiles < pairs ? tiles : pairs)), dim3(MANY_THREADS), MANY_SMEM,
                             st, ta, tw[0], tw[1], p);
 }
@@ -779,7 +935,10 @@ cudaError_t launch_many(const Gemm128Args& a, const Params128& p, int device, in
 template <bool GATED>
 cudaError_t launch_kind(const Gemm128Args& a, const Params128& p, int device, int num_sms, cudaStream_t st) {
   const int rows = a.s.rows;
-  if (rows > 512) return launch_many<GATED>(a, p, device, num_sms, st);
+  if (rows > 512) {
+    if (!(GATED && p.out_type == HILO_E4M3) && getenv("NT128")) return launch_many<128, GATED>(a, p, device, num_sms, st);
+    return launch_many<256, GATED>(a, p, device, num_sms, st);
+  }
   const int nt = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   // as many CTAs along K as fill the device
   const long long tiles = static_cast<long long>((a.s.n + 127) / 128) * ((rows + nt - 1) / nt);
@@ -816,7 +975,8 @@ cudaError_t launch_gemm128(const Gemm128Args& a, int device, int num_sms, cudaSt
   p.kblocks = (s.k + BK - 1) / BK;
   p.out_type = s.out_dtype;
   p.act = s.act;
-  p.out_wide = 0;
+  const int bytes = s.out_dtype == HILO_F32 ? 4 : s.out_dtype == HILO_E4M3 ? 1 : 2;
+  p.out_wide = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && s.out_row * bytes % 32 == 0;
   return two ? launch_kind<true>(a, p, device, num_sms, st) : launch_kind<false>(a, p, device, num_sms, st);
 }
 
