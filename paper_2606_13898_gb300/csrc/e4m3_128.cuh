@@ -67,11 +67,23 @@ __device__ __forceinline__ float amax8(const float* f, float m) {
 
 // SiLU z / (1 + e^-z); GELU in its tanh form, z / (1 + 2^(-2u log2(e))) with u = sqrt(2 / pi) (z + 0.044715 z^3),
 // the same function.
-__device__ __forceinline__ float activation(float z, int act) {
+template <int ACT>
+__device__ __forceinline__ float activation(float z) {
   constexpr float LOG2E = 1.4426950408889634f;
-  if (act == HILO_ACT_NONE) return z;
-  const float t = act == HILO_ACT_SILU ? -LOG2E * z : -2.f * LOG2E * 0.7978845608028654f * (z + 0.044715f * z * z * z);
+  if (ACT == HILO_ACT_NONE) return z;
+  const float t = ACT == HILO_ACT_SILU ? -LOG2E * z : -2.f * LOG2E * 0.7978845608028654f * (z + 0.044715f * z * z * z);
   return __fdividef(z, 1.f + ex2(t));
+}
+// f(Act<..>) for the activation `act`: one branch around all of a row's values.
+template <int ACT>
+struct Act {
+  static constexpr int value = ACT;
+};
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+  if (act == HILO_ACT_SILU) f(Act<HILO_ACT_SILU>());
+  else if (act == HILO_ACT_GELU) f(Act<HILO_ACT_GELU>());
+  else f(Act<HILO_ACT_NONE>());
 }
 
 // Four values of a row, rounded once (fp16 saturating), at an element offset that is a multiple of four.

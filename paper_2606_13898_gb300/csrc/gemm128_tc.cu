@@ -5,24 +5,24 @@
 //   y[r][n] = sum_b sa[b][r] sw[n / 128][b] sum_{k in block b} a[r][k] w[n][k]   (+ bias)
 //   h[r][n] = act(gate[r][n]) * up[r][n],   gate and up two such products of the same rows.
 //
-// The scales change along K, so the tensor core cannot sum past a block: it
-// forms each block's product of 128 (four tcgen05.mma kind::f8f6f4) in a tensor memory buffer of its
-// own, and eight warps add it, scaled, to sums in their registers while the next
-// block's is formed. The codes' products are exact in fp32.
+// The scales change along K, so the tensor core cannot sum past a block: it forms each block's product of 128 (four
+// tcgen05.mma kind::f8f6f4) in a tensor memory buffer of its own, and other warps add it, scaled, to sums
+// in their registers while the next block's is formed. The codes' products are exact in fp32.
 //
-// Two kernels:
-//   few128   few rows: features on the lanes (M), rows on the columns (N = NT). A CTA has 128
-//            features; a cluster of up to eight shares them along K and adds its sums up through
-//            distributed shared memory in a fixed order. Bound by reading the weights.
-//   many128  CTA pairs (cta_group::2): 256 rows on the lanes, 256 features (or 128 of gate and 128
-//            of up) on the columns, a persistent grid. Bound by the tensor pipe and by shared memory, which
-//            takes each operand byte twice.
+// Two kernels, chosen by cost (choose):
+//   few128   few rows: features on the lanes (M), rows on the columns (N = NT). A CTA has 128 features; a cluster of up
+//            to eight shares them along K and adds its sums up through distributed shared memory in a fixed order.
+//            Bound by reading the weights, and for small ones by a launch and the chain first copy, product, sums,
+//            cluster, rows (about 4 us).
+//   many128  CTA pairs (cta_group::2): 256 rows on the lanes, NT columns: features, or half of them gate and half up;
+//            a persistent grid. Bound by the chain product, sums, next product in the same buffer, of which tensor memory
+//            holds 512 / NT, and at full load by the chip's power: 4864 rows of 16384, 4096 features 226 us, 2.9
+//            PFLOP/s, 75% of twice the measured bf16 rate; tensor pipe active 51% with 4096 columns.
 //
 // Every mbarrier wait is bounded (error latched, TMEM freed, CTA returns).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
-#include <stdlib.h>
 
 #include "attn_common.cuh"
 #include "common.cuh"
@@ -100,24 +100,29 @@ __device__ __forceinline__ void tmem_ld_wait_n(float* v) {
   }
 }
 
-// An arrival on a barrier of this cluster that says only that tensor memory was read: ordered by tcgen05.wait::ld and
-// tcgen05's fences. (One that releases the thread's other memory accesses to the cluster waits for all of them, the
-// scales on their way among them: 8192 rows of 10240, 4096 features 718 us.)
-__device__ __forceinline__ void arrive_peer(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
 // Whether the phase is complete, without waiting for it (try_wait may stay for microseconds).
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
+      : "r"(bar), "r"(parity)
       : "memory");
   return ok != 0;
+}
+
+// Arrivals of lane 0, without a branch, on a barrier of the cluster and on one of this CTA. The first says only that
+// tensor memory was read, which tcgen05.wait::ld and tcgen05's fences order. (One that releases the thread's other
+// memory accesses to the cluster waits for all of them: 8192 rows of 10240, 4096 features, 718 us and 337 so.)
+__device__ __forceinline__ void arrive2_lane0(uint32_t cluster_addr, uint32_t addr, int lane) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.eq.u32 p, %2, 0;\n\t"
+      "@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t"
+      "@p mbarrier.arrive.shared::cta.b64 _, [%1];\n\t}" ::"r"(cluster_addr),
+      "r"(addr), "r"(lane)
+      : "memory");
 }
 
 // ----------------------------------------------------------------- scales --
@@ -198,30 +203,41 @@ __device__ __forceinline__ void store16(void* out, int type, long long at, const
   }
 }
 
+// Where a CTA has the SM to itself: sixteen warps for the sums (four warpgroups), one each for copies, products and
+// scales, and one to make a warpgroup of them; the registers of a thread, which are shared out anew.
+constexpr int SUM_WARPS = 16;
+constexpr int WHOLE_THREADS = 32 * (SUM_WARPS + 4);
+constexpr uint32_t SUM_REGS = 112, CONTROL_REGS = 32;
+constexpr int SPLIT_REGS = 32 * SUM_WARPS * SUM_REGS + 128 * CONTROL_REGS;  // what the kernel's launch must have
+static_assert(SPLIT_REGS <= 65536, "registers of an SM");
+
 // ------------------------------------------------------------------- few rows --
 
 constexpr int FEW_SPLIT = 8;  // CTAs of a cluster at most
-// Registers of a thread where a CTA has the SM to itself.
-constexpr uint32_t SUM_REGS = 232, CONTROL_REGS = 40;
-static_assert(256 * SUM_REGS + 128 * CONTROL_REGS <= 65536, "registers of an SM");
 
 template <int NT, bool GATED>
 struct Few {
   static constexpr int PARTS = GATED ? 2 : 1;
-  static constexpr int STAGE = PARTS * PIECE + NT * BK;
   static constexpr int CTAS = NT * PARTS <= 64 ? 2 : 1;  // per SM
-  // eight warps for the sums, one each for copies, products and scales (and one to make whole warpgroups)
-  static constexpr int THREADS = CTAS == 2 ? 352 : 384;
-  static constexpr int STAGES = CTAS == 2 ? (104 * 1024) / STAGE : (200 * 1024) / STAGE;
-  static constexpr int BUFS = NT * PARTS <= 64 ? 4 : 2;
+  static constexpr int SUMS = CTAS == 2 ? 8 : SUM_WARPS;
+  static constexpr int THREADS = CTAS == 2 ? 32 * (SUMS + 3) : WHOLE_THREADS;
+  static constexpr int COLS = NT / (SUMS / 4);           // of a warp
+  static constexpr int STEP = COLS < 16 ? COLS : 16;     // columns read at a time
+  // The cluster's sums: where there is room for them beside the stages, each CTA stores its sums where they are added up
+  // (PUSH); else they take its own stages' place and are fetched.
+  static constexpr bool PUSH = CTAS == 2 && !GATED;  // (gated, two stages would be left: 16 rows of 4096, 10240 features, 19.3 us, 17.2 so)
+  static constexpr int SUMS_BYTES = PARTS * NT * 128 * 4;
+  static constexpr int STAGE = PARTS * PIECE + NT * BK;
+  static constexpr int STAGES = CTAS == 2 ? (106 * 1024 - (PUSH ? SUMS_BYTES : 0)) / STAGE : (200 * 1024) / STAGE;
+  static constexpr int BUFS = NT * PARTS <= 128 ? 4 : 2;  // of tensor memory
   static constexpr int NEED = BUFS * PARTS * NT;
   static constexpr uint32_t TMEM_COLS = NEED <= 64 ? 64 : NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
-  static constexpr int COLS = NT / 2;         // of a warp
-  static constexpr int SLOT = NT + 4;         // floats of a block's scales
-  static constexpr int OFF_BARS = STAGES * STAGE;
+  static constexpr int SLOT = NT + 4;  // floats of a block's scales
+  static constexpr int OFF_SUMS = PUSH ? STAGES * STAGE : 0;
+  static constexpr int OFF_BARS = STAGES * STAGE + (PUSH ? SUMS_BYTES : 0);
   static constexpr int OFF_SCALES = OFF_BARS + 384;
   static constexpr int SMEM_BYTES = OFF_SCALES + SLOTS * SLOT * 4 + 1024;
-  static_assert(STAGES * STAGE >= PARTS * NT * 128 * 4, "the sums take the stages' place");
+  static_assert(STAGES >= 2 && (PUSH || STAGES * STAGE >= SUMS_BYTES), "the sums take the stages' place");
   static_assert((2 * STAGES + 2 * BUFS + 2 * SLOTS + 3) * 8 <= 384, "room for the barriers");
   static_assert(SMEM_BYTES <= (CTAS == 2 ? 112 : 226) * 1024, "shared memory");
 };
@@ -231,6 +247,7 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
     few128_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                   const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ Params128 p, int split) {
   using C = Few<NT, GATED>;
+  constexpr int COPY_WARP = C::SUMS, MMA_WARP = C::SUMS + 1, SCALE_WARP = C::SUMS + 2;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BARS);
@@ -251,22 +268,22 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
     }
     for (int b = 0; b < C::BUFS; ++b) {
       mbar_init(&tfull[b], 1);
-      mbar_init(&tempty[b], 8);
+      mbar_init(&tempty[b], C::SUMS);
     }
     for (int k = 0; k < SLOTS; ++k) {
       mbar_init(&ring.full[k], 32);
-      mbar_init(&ring.empty[k], 8);
+      mbar_init(&ring.empty[k], C::SUMS);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 8 && lane == 0) {
+  if (warp == COPY_WARP && lane == 0) {
     tma_prefetch_desc(&tm_a);
     tma_prefetch_desc(&tm_w0);
     if (GATED) tma_prefetch_desc(&tm_w1);
   }
-  if (warp == 9) {
+  if (warp == MMA_WARP) {
     tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
   }
@@ -278,16 +295,17 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
   pdl_trigger();
 
   const int rank = blockIdx.x % split, f0 = (blockIdx.x / split) * 128, r0 = blockIdx.y * NT;
-  const int rows = min(NT, rows_there(p.n_rows, p.rows) - r0);
-  if (rows <= 0) {  // (the same for the whole cluster)
-    if (warp == 9) tmem_dealloc(tmem, C::TMEM_COLS);
+  // The first rows' copies do not wait for the row count (most of a microsecond). The whole cluster has the same rows.
+  if (blockIdx.y > 0 && rows_there(p.n_rows, p.rows) <= r0) {
+    if (warp == MMA_WARP) tmem_dealloc(tmem, C::TMEM_COLS);
     return;
   }
+  if (C::PUSH && split > 1) cluster_arrive_relaxed();  // this CTA has begun: the others may store into it
   const int kb0 = static_cast<int>(static_cast<long long>(p.kblocks) * rank / split);
   const int nkb = static_cast<int>(static_cast<long long>(p.kblocks) * (rank + 1) / split) - kb0;
 
-  if (C::CTAS == 1 && warp >= 8) setmaxnreg_dec<CONTROL_REGS>();
-  if (warp == 8) {
+  if (C::CTAS == 1 && warp >= C::SUMS) setmaxnreg_dec<CONTROL_REGS>();
+  if (warp == COPY_WARP) {
     // ---------------- copies
     const bool issuer = elect_one();
     uint32_t armed = 0, par = 0;
@@ -321,7 +339,7 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
           }
     }
     __syncwarp();
-  } else if (warp == 9) {
+  } else if (warp == MMA_WARP) {
     // ---------------- products
     const bool issuer = elect_one();
     constexpr uint32_t idesc = idesc_kind_f16(128, NT, 0, 0, 0);  // (format code 0 is E4M3)
@@ -360,35 +378,34 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
       }
     }
     __syncwarp();
-  } else if (warp == 10) {
-    // ---------------- scales
+  } else if (warp == SCALE_WARP) {
+    // ---------------- scales (of the rows that the buffers have: more may be read than count)
     const long long w = (f0 >> 7) * p.w_scale_ld + kb0;
     uint32_t n = 0;
-    fill_scales<NT, C::PARTS>(ring, n, nkb, rows, p.a_scale + kb0 * p.a_scale_ld + r0 + lane, p.a_scale_ld, p.w_scale[0] + w,
+    fill_scales<NT, C::PARTS>(ring, n, nkb, p.rows - r0, p.a_scale + kb0 * p.a_scale_ld + r0 + lane, p.a_scale_ld, p.w_scale[0] + w,
                               p.w_scale[C::PARTS - 1] + w, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 22);
     copies_done();
     __syncwarp();
-  } else if (warp < 8) {
+  } else if (warp < C::SUMS) {
     if (C::CTAS == 1) setmaxnreg_inc<SUM_REGS>();
-    // ---------------- sums: lane quarter warp % 4 (32 features), half of the columns
+    // ---------------- sums: lane quarter warp % 4 (32 features), a part of the columns
+    const int rows = min(NT, rows_there(p.n_rows, p.rows) - r0);
     const int q = warp & 3, col0 = (warp >> 2) * C::COLS;
     uint64_t acc[C::PARTS][C::COLS / 2] = {};
     const uint32_t taddr = tmem + (static_cast<uint32_t>(q * 32) << 16) + col0;
-    constexpr int STEP = C::COLS < 32 ? C::COLS : 32, LOADS = C::PARTS * C::COLS / STEP;
+    const uint32_t ring_full = smem_u32(ring.full), tfull0 = smem_u32(tfull);
+    constexpr int STEP = C::STEP, LOADS = C::PARTS * C::COLS / STEP;
     bool ok = true, there_already = false;  // block i's products and scales
 #pragma unroll 1
-    for (int i = 0; i < nkb; ++i) {
-      const int b = i % C::BUFS, k = i % SLOTS;
-      if (!there_already &&
-          (!mbar_wait_warp(&ring.full[k], static_cast<uint32_t>(i / SLOTS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 21) ||
-           !mbar_wait_warp(&tfull[b], static_cast<uint32_t>(i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 15))) {
+    for (uint32_t i = 0; i < static_cast<uint32_t>(nkb); ++i) {
+      const uint32_t b = i % C::BUFS, k = i % SLOTS;
+      if (!there_already && (!mbar_wait_warp(&ring.full[k], (i / SLOTS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 21) ||
+                             !mbar_wait_warp(&tfull[b], (i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 15))) {
         ok = false;
         break;
       }
       tc_fence_after();
-      auto column = [&](int l) {
-        return taddr + static_cast<uint32_t>((b * C::PARTS + l * STEP / C::COLS) * NT + l * STEP % C::COLS);
-      };
+      auto column = [&](int l) { return taddr + (b * C::PARTS + l * STEP / C::COLS) * NT + l * STEP % C::COLS; };
       const float* slot = ring.slots + k * C::SLOT;
       float v[2][STEP];
       tmem_ldn<STEP>(column(0), v[0]);
@@ -402,9 +419,9 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
           __syncwarp();
           if (lane == 0) mbar_arrive(&tempty[b]);
           // asked beside the last sums: a wait takes a hundred cycles where it has nothing to wait for
-          const uint32_t n = static_cast<uint32_t>(i) + 1;
-          there_already = __all_sync(0xffffffffu, mbar_test(&ring.full[n % SLOTS], (n / SLOTS) & 1u) &&
-                                                      mbar_test(&tfull[n % C::BUFS], (n / C::BUFS) & 1u));
+          const uint32_t n = i + 1;
+          there_already = __all_sync(0xffffffffu, mbar_test(ring_full + 8u * (n % SLOTS), (n / SLOTS) & 1u) &&
+                                                      mbar_test(tfull0 + 8u * (n % C::BUFS), (n / C::BUFS) & 1u));
         }
         const int g = l * STEP / C::COLS, c0 = l * STEP % C::COLS;
         const uint64_t w2 = f2(slot[NT + g], slot[NT + g]);
@@ -419,54 +436,38 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ring.empty[k]);
     }
+    // The sums of row t are added up by CTA t % split: [CTA][part][t / split][feature] (PUSH), or [part][t][feature]
+    // where they are fetched from, over the stages: every product has been waited for. (After a given-up wait
+    // copies may still arrive there; nothing is stored then, and what is read below is not meant to be right.)
+    const int shift = 31 - __clz(split), per = NT >> shift;  // (a power of two)
+    const uint32_t sums = smem_u32(smem) + C::OFF_SUMS;
+    if (C::PUSH && split > 1) cluster_wait();
     if (ok) {
-      // [part][row][feature], over the stages: every product has been waited for. (After a given-up wait
-      // copies may still arrive there; nothing is written then, and what is read below is not meant to be right.)
-      float* sums = reinterpret_cast<float*>(smem) + q * 32 + lane;
 #pragma unroll
       for (int g = 0; g < C::PARTS; ++g)
 #pragma unroll
-        for (int c = 0; c < C::COLS; c += 2) {
+        for (int c = 0; c < C::COLS; ++c) {
           float lo, hi;
           f2_split(acc[g][c / 2], lo, hi);
-          sums[(g * NT + col0 + c) * 128] = lo;
-          sums[(g * NT + col0 + c + 1) * 128] = hi;
+          const int t = col0 + c;
+          if (t >= rows) continue;
+          uint32_t at = sums + ((g * NT + t) * 128 + q * 32 + lane) * 4;
+          if (C::PUSH) {
+            at = sums + (((rank * C::PARTS + g) * per + (t >> shift)) * 128 + q * 32 + lane) * 4;
+            if (split > 1) at = mapa_shared(at, t & (split - 1));
+          }
+          const float x = c & 1 ? hi : lo;
+          if (C::PUSH && split > 1) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
+          else asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
         }
     }
     if (split > 1) cluster_sync();
-    else named_bar_sync(1, 256);
+    else named_bar_sync(1, 32 * C::SUMS);
     // ---- rows rank, rank + split, ..: a warp each, four features a lane, the CTAs' sums in the order of K
     const bool good = *abort_flag == 0;
     const int f = f0 + 4 * lane;
-    const uint32_t mine = smem_u32(smem) + 16 * lane;
-    for (int t = rank + split * warp; good && t < rows; t += split * 8) {
-      float y[C::PARTS][4] = {};
-      // (all CTAs' sums, four at a time, on their way before the first is added)
-      for (int s0 = 0; s0 < split; s0 += 4) {
-        float4 v[4][C::PARTS];
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int g = 0; g < C::PARTS; ++g) {
-            v[s][g] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (s0 + s >= split) continue;
-            const uint32_t at = mapa_shared(mine + (g * NT + t) * 512, s0 + s);
-            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(v[s][g].x), "=f"(v[s][g].y), "=f"(v[s][g].z), "=f"(v[s][g].w)
-                         : "r"(at)
-                         : "memory");
-          }
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int g = 0; g < C::PARTS; ++g) {
-            y[g][0] += v[s][g].x;
-            y[g][1] += v[s][g].y;
-            y[g][2] += v[s][g].z;
-            y[g][3] += v[s][g].w;
-          }
-      }
-      const bool in = f < p.n;  // (n is a multiple of 16)
+    const bool in = f < p.n;  // (n is a multiple of 16)
+    auto finish = [&](int t, float (*y)[4]) {
 #pragma unroll
       for (int g = 0; g < C::PARTS; ++g)
         if (p.bias[g] && in)
@@ -478,7 +479,8 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
           }
       if (GATED)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[0][j] = activation(y[0][j], p.act) * y[C::PARTS - 1][j];
+        for (int j = 0; j < 4; ++j)
+          y[0][j] = (p.act == HILO_ACT_SILU ? activation<HILO_ACT_SILU>(y[0][j]) : activation<HILO_ACT_GELU>(y[0][j])) * y[C::PARTS - 1][j];
       if (GATED && p.out_type == HILO_E4M3) {
         float m = 0.f, inv, sc;
 #pragma unroll
@@ -493,14 +495,61 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
       } else if (in) {
         store4(p.out, p.out_type, (r0 + t) * p.out_row + f, y[0]);
       }
+    };
+    // TOGETHER rows of a warp at a time, and of each four CTAs' sums, are on their way before the first is added
+    constexpr int TOGETHER = C::PUSH ? 1 : 2;
+    const int step = split * C::SUMS;
+    for (int t0 = rank + split * warp; good && t0 < rows; t0 += TOGETHER * step) {
+      float y[TOGETHER][C::PARTS][4] = {};
+      for (int s0 = 0; s0 < split; s0 += 4) {
+        float4 v[TOGETHER][4][C::PARTS];
+#pragma unroll
+        for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int g = 0; g < C::PARTS; ++g) {
+              float4& x = v[u][s][g];
+              x = make_float4(0.f, 0.f, 0.f, 0.f);
+              const int t = t0 + u * step;
+              if (s0 + s >= split || t >= rows) continue;
+              if (C::PUSH) {
+                const uint32_t at = sums + ((((s0 + s) * C::PARTS + g) * per + (t >> shift)) * 128 + 4 * lane) * 4;
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
+              } else {
+                const uint32_t at = mapa_shared(sums + ((g * NT + t) * 128 + 4 * lane) * 4, s0 + s);
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                             : "r"(at)
+                             : "memory");
+              }
+            }
+#pragma unroll
+        for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int g = 0; g < C::PARTS; ++g) {
+              y[u][g][0] += v[u][s][g].x;
+              y[u][g][1] += v[u][s][g].y;
+              y[u][g][2] += v[u][s][g].z;
+              y[u][g][3] += v[u][s][g].w;
+            }
+      }
+#pragma unroll
+      for (int u = 0; u < TOGETHER; ++u)
+        if (t0 + u * step < rows) finish(t0 + u * step, y[u]);
     }
   }
-  // (the other warps come to the two meetings of the cluster, too)
-  if (split > 1 && warp >= 8) cluster_sync();
+  // (the other warps come to the cluster's meetings, too)
+  if (split > 1 && warp >= C::SUMS) {
+    if (C::PUSH) cluster_wait();
+    cluster_sync();
+  }
   tc_fence_before();
   __syncthreads();
-  if (split > 1) cluster_sync();  // no CTA leaves while another reads its sums
-  if (warp == 9) {
+  if (!C::PUSH && split > 1) cluster_sync();  // no CTA leaves while another fetches its sums
+  if (warp == MMA_WARP) {
     tc_fence_after();
     tmem_dealloc(tmem, C::TMEM_COLS);
   }
@@ -508,10 +557,6 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
 
 // ------------------------------------------------------------------ many rows --
 
-constexpr int SUM_WARPS = 16;
-constexpr int MANY_THREADS = 32 * (SUM_WARPS + 4);  // the sums' four warpgroups, one for copies, products and scales
-constexpr uint32_t MANY_SUM_REGS = 112, MANY_CONTROL_REGS = 32;
-constexpr int MANY_LAUNCH = 32 * SUM_WARPS * MANY_SUM_REGS + 128 * MANY_CONTROL_REGS;  // registers that the split needs
 constexpr int MANY_SMEM = 222 * 1024;
 
 // A pair's tile: 256 rows, NT columns of the product: NT features, or NT / 2 of gate and NT / 2 of up.
@@ -521,7 +566,9 @@ struct Many {
   static constexpr int STAGE = PIECE + NT / 2 * BK;  // 128 rows, and half of the columns
   static constexpr int BUFS = 512 / NT;              // of tensor memory
   static constexpr int COLS = NT / 8;                // of a warp, in each half of the columns
-  static constexpr int LOAD = 16;                    // columns read at a time
+  // Columns read at a time, into one of two sets of registers. (Gated, with 16 the sums spill: 8192 rows of 4096, 10240
+  // features, 633 us, 613 so.)
+  static constexpr int LOAD = GATED ? 8 : 16;
   static constexpr int SLOT = 128 + 4;                      // floats of a block's scales: its rows', the weights' of both halves
   static constexpr int SCALES_BYTES = SLOTS * SLOT * 4, MOST_BYTES = 4 * 128 * 4;  // [4][128] row maxima
   static constexpr int STAGES = (MANY_SMEM - 1024 - 384 - SCALES_BYTES - MOST_BYTES) / STAGE;
@@ -532,7 +579,7 @@ struct Many {
 constexpr int PANEL = 8;  // row tiles that are taken together along the features
 
 template <int NT, bool GATED>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
     many128_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                    const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ Params128 p) {
   using C = Many<NT, GATED>;
@@ -599,7 +646,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
   };
 
   if (warp >= SUM_WARPS) {
-    setmaxnreg_dec<MANY_CONTROL_REGS>();
+    setmaxnreg_dec<CONTROL_REGS>();
     if (warp == SUM_WARPS) {
       // ---------------- copies (both CTAs)
       const bool issuer = elect_one();
@@ -708,13 +755,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
       __syncwarp();
     }
   } else {
-    setmaxnreg_inc<MANY_SUM_REGS>();
+    setmaxnreg_inc<SUM_REGS>();
     // ---------------- sums: lane quarter warp % 4 (32 rows), and of both halves of the columns (gate and up) the
     // quarter warp / 4 (NT / 8 features)
     const int q = warp & 3, h = warp >> 2, r = 32 * q + lane;
     float* most = reinterpret_cast<float*>(smem + C::OFF_MOST);
     const uint32_t taddr = tmem + (static_cast<uint32_t>(32 * q) << 16) + C::COLS * h;
-    const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0);
+    const uint32_t tempty0 = mapa_shared(smem_u32(tempty), 0), tfull0 = smem_u32(tfull);
+    const uint32_t ring_full = smem_u32(ring.full), ring_empty = smem_u32(ring.empty);
     uint32_t i = 0;
     bool ok = true, there_already = false;  // block i's products and scales
     for (int t = blockIdx.x >> 1; t < tiles; t += step) {
@@ -726,20 +774,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
       for (int j = 0; j < C::COLS / 2; ++j) acc[0][j] = acc[1][j] = 0ull;
 #pragma unroll 1
       for (int kb = 0; kb < p.kblocks; ++kb, ++i) {
-        const uint32_t b = i % C::BUFS, k = i % SLOTS;
-        if (!there_already && (!mbar_wait_warp(&ring.full[k], (i / SLOTS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 23) ||
-                               !mbar_wait_warp(&tfull[b], (i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 20))) {
-          ok = false;
-          break;
+        if (!there_already) {
+          const uint32_t b = i % C::BUFS, k = i % SLOTS;
+          if (!mbar_wait_warp(&ring.full[k], (i / SLOTS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 23) ||
+              !mbar_wait_warp(&tfull[b], (i / C::BUFS) & 1u, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 20)) {
+            ok = false;
+            break;
+          }
         }
         tc_fence_after();
-        const uint32_t at = taddr + NT * b;
-        const float* slot = ring.slots + k * C::SLOT;
-        const float s0 = slot[r] * slot[128], s1 = slot[r] * slot[129];
+        const uint32_t at = taddr + (i % C::BUFS) * NT;
+        const float* slot = ring.slots + i % SLOTS * C::SLOT;
         constexpr int LOADS = 2 * C::COLS / C::LOAD;  // the first half of them of the first half of the columns
         auto column = [&](int c) { return at + (c * C::LOAD / C::COLS) * (NT / 2) + c * C::LOAD % C::COLS; };
         float v[2][C::LOAD];
         tmem_ldn<C::LOAD>(column(0), v[0]);
+        const float s0 = slot[r] * slot[128], s1 = slot[r] * slot[129];
 #pragma unroll
         for (int c = 0; c < LOADS; ++c) {
           tmem_ld_wait_n<C::LOAD>(v[c & 1]);
@@ -748,14 +798,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
           } else {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-              arrive_peer(tempty0 + 8u * b);
-              mbar_arrive(&ring.empty[k]);
-            }
+            arrive2_lane0(tempty0 + 8u * (i % C::BUFS), ring_empty + 8u * (i % SLOTS), lane);
             // asked beside the last sums: a wait takes a hundred cycles where it has nothing to wait for
             const uint32_t n = i + 1;
-            there_already = __all_sync(0xffffffffu, mbar_test(&ring.full[n % SLOTS], (n / SLOTS) & 1u) &&
-                                                        mbar_test(&tfull[n % C::BUFS], (n / C::BUFS) & 1u));
+            there_already = __all_sync(0xffffffffu, mbar_test(ring_full + 8u * (n % SLOTS), (n / SLOTS) & 1u) &&
+                                                        mbar_test(tfull0 + 8u * (n % C::BUFS), (n / C::BUFS) & 1u));
           }
           const int g = c * C::LOAD / C::COLS, c0 = c * C::LOAD % C::COLS;
           const float s = g ? s1 : s0;
@@ -770,28 +817,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
       if (!ok && !(GATED && NT == 256 && p.out_type == HILO_E4M3)) break;
       // ---- the tile's rows
       const bool there = row < rows;
-      // sums j, j + 1 of part g with their biases
-      auto sums = [&](int g, int f, int j, float& lo, float& hi) {
-        f2_split(acc[g][j / 2], lo, hi);
-        const __nv_bfloat16* bias = p.bias[GATED ? g : 0];
-        if (bias && f + j < p.n) {
-          const float2 v = bias2(bias, f + j);
-          lo += v.x;
-          hi += v.y;
-        }
-      };
-      if (GATED) {
-        const int f = f0 + C::COLS * h;
-        float y[C::COLS], m = 0.f;
+      // part g's features of this thread, from f on
+      auto feature = [&](int g) { return f0 + (GATED ? 0 : NT / 2 * g) + C::COLS * h; };
 #pragma unroll
-        for (int j = 0; j < C::COLS; j += 2) {
-          float g0, g1, u0, u1;
-          sums(0, f, j, g0, g1);
-          sums(1, f, j, u0, u1);
-          y[j] = activation(g0, p.act) * u0;
-          y[j + 1] = activation(g1, p.act) * u1;
-          if (f + j < p.n) m = fmaxf(m, fmaxf(fabsf(y[j]), fabsf(y[j + 1])));
+      for (int g = 0; g < 2; ++g)
+        if (const __nv_bfloat16* bias = p.bias[GATED ? g : 0]) {
+#pragma unroll
+          for (int j = 0; j < C::COLS; j += 2)
+            if (feature(g) + j < p.n) {
+              const float2 v = bias2(bias, feature(g) + j);
+              acc[g][j / 2] = f2_add(acc[g][j / 2], f2(v.x, v.y));
+            }
         }
+      if (GATED) {
+        const int f = feature(0);
+        float y[C::COLS], m = 0.f;
+        auto combine = [&](auto act) {
+#pragma unroll
+          for (int j = 0; j < C::COLS; j += 2) {
+            float g0, g1, u0, u1;
+            f2_split(acc[0][j / 2], g0, g1);
+            f2_split(acc[1][j / 2], u0, u1);
+            y[j] = activation<decltype(act)::value>(g0) * u0;
+            y[j + 1] = activation<decltype(act)::value>(g1) * u1;
+            m = fmaxf(m, fmaxf(fabsf(y[j]), fabsf(y[j + 1])));  // (features that are not there are 0)
+          }
+        };
+        if (p.act == HILO_ACT_SILU) combine(Act<HILO_ACT_SILU>());
+        else combine(Act<HILO_ACT_GELU>());
         if (NT == 256 && p.out_type == HILO_E4M3) {  // (a tile's features are a block)
           most[128 * h + r] = m;
           // the four warps of these rows go on together or not at all
@@ -828,11 +881,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1)
         for (int g = 0; g < 2; ++g)
 #pragma unroll
           for (int c = 0; c < C::COLS; c += 16) {
-            const int f = f0 + NT / 2 * g + C::COLS * h;
+            const int f = feature(g);
             if (f + c >= p.n) continue;
             float y[16];
 #pragma unroll
-            for (int j = 0; j < 16; j += 2) sums(g, f, c + j, y[j], y[j + 1]);
+            for (int j = 0; j < 16; j += 2) f2_split(acc[g][(c + j) / 2], y[j], y[j + 1]);
             store16(p.out, p.out_type, row * p.out_row + f + c, y, p.out_wide);
           }
       }
@@ -857,7 +910,7 @@ bool encode(CUtensorMap* m, const void* base, long long rows, long long k, long 
 
 // The register split must fit what the CTA is launched with, or setmaxnreg.inc would wait forever. (One number for every
 // device: the library holds one binary.)
-template <auto KERNEL, int THREADS, int NEED>
+template <auto KERNEL>
 cudaError_t registers_fit() {
   static std::atomic<int> known{0};
   int regs = known.load(std::memory_order_relaxed);
@@ -868,7 +921,7 @@ cudaError_t registers_fit() {
     regs = fa.numRegs;
     known.store(regs, std::memory_order_relaxed);
   }
-  return regs * THREADS < NEED ? cudaErrorInvalidConfiguration : cudaSuccess;
+  return regs * WHOLE_THREADS < SPLIT_REGS ? cudaErrorInvalidConfiguration : cudaSuccess;
 }
 
 template <int NT, bool GATED>
@@ -883,7 +936,7 @@ cudaError_t launch_few(const Gemm128Args& a, const Params128& p, int split, cuda
   auto* kern = few128_kernel<NT, GATED>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  if (C::CTAS == 1 && (e = registers_fit<few128_kernel<NT, GATED>, 384, 256 * SUM_REGS + 128 * CONTROL_REGS>()) != cudaSuccess) return e;
+  if (C::CTAS == 1 && (e = registers_fit<few128_kernel<NT, GATED>>()) != cudaSuccess) return e;
   const dim3 grid(static_cast<unsigned>((s.n + 127) / 128 * split), static_cast<unsigned>((s.rows + NT - 1) / NT));
   return launch_pdl_cluster(kern, split, grid, dim3(C::THREADS), C::SMEM_BYTES, st, ta, tw[0], tw[1], p, split);
 }
@@ -894,7 +947,7 @@ int resident_pairs(int device, int num_sms) {
   const int n = pairs.get(device, [&] {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (num_sms / 2), 1, 1);
-    cfg.blockDim = dim3(MANY_THREADS, 1, 1);
+    cfg.blockDim = dim3(WHOLE_THREADS, 1, 1);
     cfg.dynamicSmemBytes = MANY_SMEM;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -924,31 +977,81 @@ cudaError_t launch_many(const Gemm128Args& a, const Params128& p, int device, in
   auto* kern = many128_kernel<NT, GATED>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MANY_SMEM);
   if (e != cudaSuccess) return e;
-  if ((e = registers_fit<many128_kernel<NT, GATED>, MANY_THREADS, MANY_LAUNCH>()) != cudaSuccess) return e;
+  if ((e = registers_fit<many128_kernel<NT, GATED>>()) != cudaSuccess) return e;
   const long long tiles = static_cast<long long>((s.rows + 255) / 256) * ((s.n + Many<NT, GATED>::TF - 1) / Many<NT, GATED>::TF);
   if (tiles > 0x7fffffff / 2) return cudaErrorInvalidValue;
   const int pairs = resident_pairs<NT, GATED>(device, num_sms);
-  return launch_pdl_cluster(kern, 1, dim3(2 * static_cast<unsigned>(tiles < pairs ? tiles : pairs)), dim3(MANY_THREADS), MANY_SMEM,
+  return launch_pdl_cluster(kern, 1, dim3(2 * static_cast<unsigned>(tiles < pairs ? tiles : pairs)), dim3(WHOLE_THREADS), MANY_SMEM,
                             st, ta, tw[0], tw[1], p);
+}
+
+// Which kernel, by its cost in microseconds. A launch is 2.2 of them; then
+//   few128<NT>    per wave of CTAs (as many as the device holds of clusters of `split`) an `each` and, per block of
+//                 128 along K, the longer of `block`, the chain from a block's copy to its sums, and of what the wave's CTAs
+//                 read of the weights at 8 to 9 TB/s (L2 and HBM)
+//   many128<NT>   the first tile of a pair and each further one: an `each` and a `block` of their own (at full load
+//                 the chip is at its power limit)
+// from 143 shapes of 1 to 1024 rows, 1024 and 4096 columns, 1024 to 16384 features, each with every choice: its pick is 1.4%
+// behind the fastest in the mean, 26% at worst (64 rows of 4096, 1024 features gated: 9.1 us, 7.2 in four tiles of 16
+// rows). Examples, in us: 64 rows of 4096, 4096 features: few128<64> 7.3, many128<256> 17.6; 512 rows: few128<128>
+// 18.8, many128<128> 13.7, many128<256> 18.4; 1024 rows: many128<128> 23.3, many128<256> 19.6.
+struct Choice {
+  int many;  // few128 otherwise
+  int nt, split;
+};
+template <bool GATED>
+Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
+  struct Cost {
+    float each, block;
+  };
+  constexpr Cost FEW[2][4] = {{{1.0f, .25f}, {1.5f, .275f}, {2.5f, .32f}, {3.8f, .36f}}, {{2.0f, .32f}, {2.7f, .36f}, {4.0f, .43f}, {6.0f, .73f}}};
+  constexpr Cost FIRST[2][2] = {{{2.1f, .265f}, {3.1f, .39f}}, {{2.2f, .31f}, {2.7f, .51f}}};
+  constexpr Cost NEXT[2][2] = {{{1.1f, .265f}, {1.7f, .44f}}, {{1.1f, .25f}, {1.4f, .49f}}};
+  constexpr int PARTS = GATED ? 2 : 1;
+  auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
+  Choice best = {1, 256, 1};
+  float least = 3e38f;
+  auto offer = [&](float cost, Choice c) {
+    if (cost < least) {
+      least = cost;
+      best = c;
+    }
+  };
+  for (int i = 0; i < 4; ++i) {
+    const int nt = 16 << i;
+    if (rows > 4 * nt || (nt > 16 && rows <= nt / 2)) continue;
+    const long long row_tiles = ceil_div(rows, nt), tiles = ceil_div(n, 128) * row_tiles;
+    const int per_sm = nt * PARTS <= 64 ? 2 : 1;
+    for (int split = 1; split <= FEW_SPLIT && split <= kblocks; split *= 2) {
+      // (clusters stay within a group of SMs, whose number eight does not divide)
+      const int held = per_sm * num_sms * (split <= 2 ? 38 : split == 4 ? 36 : per_sm == 2 ? 32 : 26) / 38;
+      const long long ctas = tiles * split, waves = ceil_div(ctas, held);
+      const float reads = static_cast<float>(ctas < held ? ctas : held) * (PARTS * PIECE) / (row_tiles == 1 ? 9e6f : 8e6f);
+      const Cost c = FEW[GATED][i];
+      offer(0.03f * split + static_cast<float>(waves) * (c.each + static_cast<float>(ceil_div(kblocks, split)) * (reads > c.block ? reads : c.block)),
+            {0, nt, split});
+    }
+  }
+  for (int i = codes ? 1 : 0; i < 2; ++i) {  // (gated to codes: a tile has whole blocks)
+    const int nt = 128 << i;
+    const long long rounds = ceil_div(ceil_div(rows, 256) * ceil_div(n, nt / PARTS), num_sms / 2 > 0 ? num_sms / 2 : 1);
+    const Cost f = FIRST[GATED][i], x = NEXT[GATED][i];
+    offer(f.each + static_cast<float>(kblocks) * f.block + static_cast<float>(rounds - 1) * (x.each + static_cast<float>(kblocks) * x.block),
+          {1, nt, 1});
+  }
+  return best;
 }
 
 template <bool GATED>
 cudaError_t launch_kind(const Gemm128Args& a, const Params128& p, int device, int num_sms, cudaStream_t st) {
-  const int rows = a.s.rows;
-  if (rows > 512) {
-    if (!(GATED && p.out_type == HILO_E4M3) && getenv("NT128")) return launch_many<128, GATED>(a, p, device, num_sms, st);
-    return launch_many<256, GATED>(a, p, device, num_sms, st);
-  }
-  const int nt = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-  // as many CTAs along K as fill the device
-  const long long tiles = static_cast<long long>((a.s.n + 127) / 128) * ((rows + nt - 1) / nt);
-  int split = 1;
-  while (2 * split <= FEW_SPLIT && 2 * split <= p.kblocks && tiles * split < num_sms) split *= 2;
-  switch (nt) {
-    case 16: return launch_few<16, GATED>(a, p, split, st);
-    case 32: return launch_few<32, GATED>(a, p, split, st);
-    case 64: return launch_few<64, GATED>(a, p, split, st);
-    default: return launch_few<128, GATED>(a, p, split, st);
+  const Choice c = choose<GATED>(a.s.rows, a.s.n, p.kblocks, p.out_type == HILO_E4M3, num_sms);
+  if (c.many)
+    return c.nt == 128 ? launch_many<128, GATED>(a, p, device, num_sms, st) : launch_many<256, GATED>(a, p, device, num_sms, st);
+  switch (c.nt) {
+    case 16: return launch_few<16, GATED>(a, p, c.split, st);
+    case 32: return launch_few<32, GATED>(a, p, c.split, st);
+    case 64: return launch_few<64, GATED>(a, p, c.split, st);
+    default: return launch_few<128, GATED>(a, p, c.split, st);
   }
 }
 

@@ -201,8 +201,10 @@ __global__ void __launch_bounds__(MAX_THREADS) group_apply_kernel(const __grid_c
         float f[8];
         e[i].widen(f);
         if (in)
+          with_activation(p.act, [&](auto act) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = activation(fmaf(f[j] - mean[j], a[j], b[j]), p.act);
+            for (int j = 0; j < 8; ++j) f[j] = activation<decltype(act)::value>(fmaf(f[j] - mean[j], a[j], b[j]));
+          });
         if (p.y_type == HILO_E4M3) {
           float m = row[i] >= 0 ? amax8(f, 0.f) : 0.f, inv, sc;
 #pragma unroll
