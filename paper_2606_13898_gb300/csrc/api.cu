@@ -244,6 +244,20 @@ bool encode_tmap_2d(CUtensorMap* map, TmapType type, const void* base, uint64_t 
   return r == CUDA_SUCCESS;
 }
 
+bool encode_tmap_rows_2d(CUtensorMap* map, int esize, const void* base, uint64_t inner, uint64_t outer,
+                         uint64_t row_stride_elems, uint32_t box_inner, uint32_t box_outer) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {inner, outer};
+  cuuint64_t strides[1] = {row_stride_elems * static_cast<uint64_t>(esize)};
+  cuuint32_t box[2] = {box_inner, box_outer};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = fn(map, esize == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base), dims,
+                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 bool encode_tmap_16bit_3d(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, uint64_t n2, uint64_t stride1,
                           uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2) {
   EncodeTiledFn fn = encode_fn();
@@ -304,13 +318,13 @@ int hilo_device_info(int* num_sms, int* is_sm103) {
 int hilo_sync_status(void* stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "hilo_sync_status: stream");
-  const int g1 = hilo::gemm_take_device_error(), g2 = hilo::gemm128_take_device_error();
-  const int g = g1 ? g1 : g2;
+  const int g1 = hilo::gemm_take_device_error(), g2 = hilo::gemm128_take_device_error(), g3 = hilo::group_norm_take_device_error();
+  const int g = g1 ? g1 : g2 ? g2 : g3;
   const int a1 = hilo::attn_take_device_error(), a2 = hilo::attn_var_take_device_error();
   const int a = a1 ? a1 : a2;
   const int pr = hilo::probe_take_device_error();
   const int dc = hilo::dcheck_take_bw();
-  if (g1 < 0 || g2 < 0 || a1 < 0 || a2 < 0 || pr < 0 || dc < 0)
+  if (g1 < 0 || g2 < 0 || g3 < 0 || a1 < 0 || a2 < 0 || pr < 0 || dc < 0)
     return fail(HILO_ERR_CUDA, "hilo_sync_status: reading the device error word failed");
   if (g || a || pr)
     return fail(HILO_ERR_TIMEOUT, "device-side wait ran out (gemm=%d, attention=%d, probe=%d)", g, a, pr);

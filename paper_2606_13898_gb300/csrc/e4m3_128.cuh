@@ -72,7 +72,9 @@ __device__ __forceinline__ float activation(float z) {
   constexpr float LOG2E = 1.4426950408889634f;
   if (ACT == HILO_ACT_NONE) return z;
   const float t = ACT == HILO_ACT_SILU ? -LOG2E * z : -2.f * LOG2E * 0.7978845608028654f * (z + 0.044715f * z * z * z);
-  return __fdividef(z, 1.f + ex2(t));
+  float inv;  // (within 1 ulp; of infinity 0)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(1.f + ex2(t)));
+  return z * inv;
 }
 // f(Act<..>) for the activation `act`: one branch around all of a row's values.
 template <int ACT>
@@ -95,6 +97,20 @@ __device__ __forceinline__ void store4(void* out, int type, long long at, const 
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
         f16 ? make_uint2(pack_f16x2_sat(v[0], v[1]), pack_f16x2_sat(v[2], v[3]))
             : make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
+// Eight values of a row, likewise.
+__device__ __forceinline__ void store8(void* out, int type, long long at, const float* v) {
+  if (type == HILO_F32) {
+    store4(out, type, at, v);
+    store4(out, type, at + 4, v + 4);
+  } else {
+    const bool f16 = type == HILO_F16;
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = f16 ? pack_f16x2_sat(v[2 * j], v[2 * j + 1]) : pack_bf16x2(v[2 * j], v[2 * j + 1]);
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 

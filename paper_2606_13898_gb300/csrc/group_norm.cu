@@ -8,44 +8,41 @@
 //   n = na + nb,  mean = (na ma + nb mb) / n,  M = Ma + Mb + na (ma - mean)^2 + nb (mb - mean)^2,
 // so that no step subtracts large sums from one another. Every order is fixed.
 //
-// Two kernels over the same chunks of rows: the first leaves each chunk's pairs in the
-// workspace, the second joins an image's pairs and writes its chunk, from the last row to the
-// first, as the rows read last are the ones still in L2. Bound by HBM: x is read once, and
-// again as far as it is not in L2, y is written once.
+// Images whose slices of channels (whole groups) fit the shared memory of a cluster: one kernel
+// (group_norm_kernel). A CTA copies its rows of the slice by TMA, finds each group's mean and the squares about it in two
+// passes over them, tells the cluster's other CTAs, and writes. x is read once. 1024 rows of 512 channels take 5.5 us
+// (two kernels: 15.6): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
+// the passes over shared memory and the activation, not by HBM (2 TB/s).
+//
+// Other images: two kernels over chunks of rows. The first leaves the pairs of each cluster's chunks in the workspace, the
+// second joins an image's pairs and writes its chunk, from the last row to the first, as the rows read last are the
+// ones still in L2. Bound by HBM: x is read once, and again as far as it is not in L2, y is written once; 2^20 rows of 128
+// channels in bf16 take 152 us, 5.3 TB/s of three passes.
 #include "e4m3_128.cuh"
 #include "internal.h"
 
 namespace hilo {
 
-namespace {
+__device__ int g_group_norm_err;
 
-constexpr int MAX_THREADS = 512;
-constexpr int MAX_CHUNKS = 320;  // of a call, but for one per image
+namespace {
 
 struct NormParams {
   const unsigned char* x;
   void* y;
   float* y_scale;
-  float2* part;  // [image][chunk][group]: mean, sum of squares about it
+  float2* part;  // [image][group][cluster of chunks]: mean, sum of squares about it
   const void *scale, *shift, *w, *b;
   long long x_row, y_row, vec_row, y_scale_ld;  // x_row in bytes
   int rows, d, groups, per, act;                // per: channels of a group
   int y_type, vec_f32;
-  int across, down;  // threads along the channels (eight each, a multiple of 16 of them), along the rows
-  int passes;        // of the channels: across * passes * 8 >= d
-  int chunks, chunk; // of an image, and rows of each
-  float eps;
+  float eps, inv_rows, inv_count;  // 1 / rows, 1 / (rows per)
 };
 
-// Mean and sum of squares about it of n values.
+// Mean and sum of squares about it.
 struct Pair {
   float mean, sq;
 };
-
-__device__ __forceinline__ float vec_at(const void* v, int f32, long long i, float none) {
-  if (!v) return none;
-  return f32 ? __ldg(static_cast<const float*>(v) + i) : __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(v) + i));
-}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -53,33 +50,210 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Rows of a thread at a time: their mean and squares from registers, joined with what there was.
-constexpr int BATCH = 8;
+// Eight neighbouring elements of a vector, `none` where there is none.
+__device__ __forceinline__ void vec8(const void* v, int f32, long long i, float none, float* f) {
+  if (!v) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = none;
+  } else if (f32) {
+    Eight<2> e;
+    e.load(static_cast<const unsigned char*>(v) + i * 4);
+    e.widen(f);
+  } else {
+    Eight<0> e;
+    e.load(static_cast<const unsigned char*>(v) + i * 2);
+    e.widen(f);
+  }
+}
+
+// What a normalised row's channels c .. c + 7 are multiplied by, and what is added:
+// w (1 + scale) and b (1 + scale) + shift.
+__device__ __forceinline__ void gains(const NormParams& p, int image, int c, float* a, float* b) {
+  float up[8], t[8];
+  vec8(p.w, p.vec_f32, c, 1.f, a);
+  vec8(p.b, p.vec_f32, c, 0.f, b);
+  vec8(p.scale, p.vec_f32, image * p.vec_row + c, 0.f, up);
+  vec8(p.shift, p.vec_f32, image * p.vec_row + c, 0.f, t);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    a[j] *= 1.f + up[j];
+    b[j] = fmaf(b[j], 1.f + up[j], t[j]);
+  }
+}
+
+// ----------------------------------------------------------- a CTA's groups --
+// A CTA has n rows of some channels. Thread (tx, ty) has the channels 8 tx .. of the rows ty, ty + down, .. It leaves its
+// pairs in shared memory: one for all eight channels where groups are whole vectors, one per channel
+// otherwise. Then `lanes` threads a group, as many as there are for all groups at once, join them: the means first, then the squares
+// about the joint mean.
+struct Rows {
+  int n, down;
+  int unit, pitch;  // entries of a group in a thread row, entries of a thread row
+  float weight;     // channels of an entry
+  int base, more;   // rows of a thread: base, and one more of the first `more` thread rows
+  int lanes;        // a power of two
+  int t0, c0, dt, dc;  // a lane's first entry: its thread row and column, and what leads to the next, `lanes` entries on
+  __device__ __forceinline__ Rows(int n, int down, int across, int wide, int per, int groups, int threads) : n(n), down(down) {
+    const bool vectors = per % 8 == 0;
+    unit = vectors ? per / 8 : per;
+    pitch = vectors ? across : wide;
+    weight = vectors ? 8.f : 1.f;
+    base = n / down;
+    more = n - base * down;
+    lanes = 32;
+    while (lanes > 4 && groups * lanes > threads) lanes /= 2;
+    const int l = threadIdx.x & (lanes - 1);
+    t0 = l / unit;
+    c0 = l - t0 * unit;
+    dt = lanes / unit;
+    dc = lanes - dt * unit;
+  }
+  // rows of the threads ty
+  __device__ __forceinline__ int of(int ty) const { return base + (ty < more ? 1 : 0); }
+};
+
+// (8 floats a thread each)
+__device__ __forceinline__ void leave_pairs(const Rows& o, int per, int tx, int ty, int n, const float* mean, const float* sq,
+                                            float* means, float* squares) {
+  if (per % 8 == 0) {
+    float m = 0.f, q = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m += mean[j];
+    m *= 0.125f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q += fmaf(static_cast<float>(n) * (mean[j] - m), mean[j] - m, sq[j]);
+    means[ty * o.pitch + tx] = m;
+    squares[ty * o.pitch + tx] = q;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      means[ty * o.pitch + 8 * tx + j] = mean[j];
+      squares[ty * o.pitch + 8 * tx + j] = sq[j];
+    }
+  }
+}
+
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int off = lanes >> 1; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  return v;
+}
+
+// Every group's pair, to use(group, lane of the group, pair), in whole warps; inv: 1 / (n per).
+template <typename Use>
+__device__ __forceinline__ void join_groups(const Rows& o, int groups, float inv, const float* means, const float* squares, Use use) {
+  const int l = threadIdx.x & (o.lanes - 1), shift = 31 - __clz(o.lanes), threads = blockDim.x;
+  for (int g0 = 0; g0 < groups; g0 += threads >> shift) {
+    const int g = g0 + (threadIdx.x >> shift);
+    const bool there = g < groups && o.n > 0;
+    auto each = [&](auto f) {
+      if (!there) return;
+      for (int t = o.t0, c = o.c0; t < o.down;) {
+        f(o.weight * static_cast<float>(o.of(t)), t * o.pitch + g * o.unit + c);
+        t += o.dt;
+        c += o.dc;
+        if (c >= o.unit) {
+          c -= o.unit;
+          ++t;
+        }
+      }
+    };
+    float sum = 0.f, sq = 0.f;
+    each([&](float n, int at) { sum += n > 0.f ? n * means[at] : 0.f; });
+    const float mean = lanes_sum(sum, o.lanes) * inv;
+    each([&](float n, int at) { sq += n > 0.f ? fmaf(n * (means[at] - mean), means[at] - mean, squares[at]) : 0.f; });
+    sq = lanes_sum(sq, o.lanes);
+    if (g < groups) use(g, l, there ? Pair{mean, sq} : Pair{0.f, 0.f});
+  }
+}
+
+// The pairs of a cluster's CTAs, [CTA][pitch groups], joined by eight lanes a group, to use(group, pair); rows_of(k): rows of
+// CTA k.
+template <typename RowsOf, typename Use>
+__device__ __forceinline__ void join_cluster(const Pair* pairs, int pitch, int parts, int groups, int per, RowsOf rows_of, Use use) {
+  const int k = threadIdx.x & 7, threads = blockDim.x;
+  for (int g0 = 0; g0 < groups; g0 += threads >> 3) {
+    const int g = g0 + (threadIdx.x >> 3);
+    const float m = g < groups && k < parts ? static_cast<float>(rows_of(k)) : 0.f;
+    const Pair q = m > 0.f ? pairs[k * pitch + g] : Pair{0.f, 0.f};
+    const float rows = lanes_sum(m, 8), mean = lanes_sum(m * q.mean, 8) * (rows > 0.f ? __fdividef(1.f, rows) : 0.f);
+    const float sq = lanes_sum(m > 0.f ? fmaf(m * static_cast<float>(per) * (q.mean - mean), q.mean - mean, q.sq) : 0.f, 8);
+    if (g < groups && k == 0) use(g, Pair{mean, sq});
+  }
+}
+
+// Eight values of each of R rows, to the output's type. A half warp's lanes all come here, rows that are not there (below 0)
+// too: its 128 channels are a block of codes.
+template <int R>
+__device__ __forceinline__ void put(const NormParams& p, const long long* row, int c, int tx, const float (*f)[8]) {
+  if (p.y_type == HILO_E4M3) {
+    float m[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) m[i] = row[i] >= 0 ? amax8(f[i], 0.f) : 0.f;
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1)
+#pragma unroll
+      for (int i = 0; i < R; ++i) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], off));
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float inv, sc;
+      block_scale(m[i], inv, sc);
+      if (row[i] < 0) continue;
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + row[i] * p.y_row + c) = block_codes(f[i], inv);
+      if ((tx & 15) == 0) p.y_scale[(c >> 7) * p.y_scale_ld + row[i]] = sc;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (row[i] >= 0) store8(p.y, p.y_type, row[i] * p.y_row + c, f[i]);
+  }
+}
+
+// ------------------------------------------------------------------ two kernels --
+
+constexpr int THREADS = 256;
+constexpr int STATS_CTAS = 3, APPLY_CTAS = 3;  // per SM (four: 64 registers spill, 152 us become 187 and 205)
+constexpr int MAX_CHUNKS = 456;                // of a call's statistics, but for a cluster per image
+constexpr int CHUNKS = 4;                      // of a cluster, whose pairs are joined before they are stored
+constexpr int BATCH = 4;                       // rows of a thread at a time (eight: registers spill, 187 us)
+constexpr int JOINED = MAX_CHUNKS / CHUNKS / 32 + 1;  // pairs of a lane
+
+// The chunks of an image: of its statistics and of its output.
+struct Two {
+  int across, down, passes;  // passes of the channels: across * passes * 8 >= d
+  int chunks, chunk;         // (a multiple of CHUNKS; the last ones may be empty), and rows of each
+  int clusters;
+  int out_chunks, out_chunk;
+};
 
 template <int TYPE>
-__global__ void __launch_bounds__(MAX_THREADS) group_stats_kernel(const __grid_constant__ NormParams p) {
-  extern __shared__ float shared[];  // [down][d] means, then [down][d] squares
+__global__ void __launch_bounds__(THREADS, STATS_CTAS) group_stats_kernel(const __grid_constant__ NormParams p, const __grid_constant__ Two o) {
+  extern __shared__ float shared[];  // means, then squares
   pdl_wait();
   pdl_trigger();
-  const int image = blockIdx.x / p.chunks, chunk = blockIdx.x - image * p.chunks, r0 = chunk * p.chunk, r1 = min(p.rows, r0 + p.chunk);
-  const int tx = threadIdx.x % p.across, ty = threadIdx.x / p.across;
-  const unsigned char* x = p.x + (static_cast<long long>(image) * p.rows) * p.x_row;
+  const int image = blockIdx.x / o.chunks, chunk = blockIdx.x - image * o.chunks, r0 = chunk * o.chunk;
+  cluster_arrive_relaxed();  // this CTA has begun: the others may store into it
+  const Rows rows(max(0, min(p.rows, r0 + o.chunk) - r0), o.down, o.passes * o.across, p.d, p.per, p.groups, THREADS);
+  const int tx = threadIdx.x % o.across, ty = threadIdx.x / o.across;
+  const unsigned char* x = p.x + (static_cast<long long>(image) * p.rows + r0) * p.x_row;
   float* means = shared;
-  float* squares = shared + p.down * p.d;
+  float* squares = shared + o.down * rows.pitch;
+  Pair* pairs = reinterpret_cast<Pair*>(squares + o.down * rows.pitch);  // [chunk of the cluster][group of this CTA]
   constexpr int ESIZE = TYPE == 2 ? 4 : 2;
-  for (int c = tx * 8; c < p.d && ty < p.down; c += p.across * 8) {
+  for (int v = tx; v * 8 < p.d && ty < o.down; v += o.across) {
     float mean[8], sq[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) mean[j] = sq[j] = 0.f;
     int n = 0;
-    for (int r = r0 + ty; r < r1; r += p.down * BATCH) {
+    const int step = o.down * BATCH;
+    for (int r = ty; r < rows.n; r += step) {
       Eight<TYPE> e[BATCH];
-      const int m = min(BATCH, (r1 - r + p.down - 1) / p.down);
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
         e[i].clear();
-        if (i < m) e[i].load(x + (r + i * p.down) * p.x_row + c * ESIZE);
+        if (r + i * o.down < rows.n) e[i].load(x + static_cast<long long>(r + i * o.down) * p.x_row + v * 8 * ESIZE);
       }
+      // a batch's mean and squares from registers, joined with what there was: the mean moves by `part` of the gap
+      const int m = min(BATCH, (rows.n - r + o.down - 1) / o.down);
       float sum[8], two[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] = two[j] = 0.f;
@@ -90,7 +264,7 @@ __global__ void __launch_bounds__(MAX_THREADS) group_stats_kernel(const __grid_c
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += f[j];  // (rows that are not there are zeros)
       }
-      const float inv = __fdividef(1.f, static_cast<float>(m));
+      const float inv = __fdividef(1.f, static_cast<float>(m)), part = __fdividef(static_cast<float>(m), static_cast<float>(n + m));
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] *= inv;
 #pragma unroll
@@ -101,173 +275,399 @@ __global__ void __launch_bounds__(MAX_THREADS) group_stats_kernel(const __grid_c
 #pragma unroll
           for (int j = 0; j < 8; ++j) two[j] = fmaf(f[j] - sum[j], f[j] - sum[j], two[j]);
       }
-      // joined: the new mean lies wb of the way to the batch's
-      const float wb = __fdividef(static_cast<float>(m), static_cast<float>(n + m));
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float gap = sum[j] - mean[j];
-        mean[j] = fmaf(gap, wb, mean[j]);
-        sq[j] += fmaf(gap * gap, wb * static_cast<float>(n), two[j]);
+        mean[j] = fmaf(gap, part, mean[j]);
+        sq[j] += fmaf(gap * gap, part * static_cast<float>(n), two[j]);
       }
       n += m;
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      means[ty * p.d + c + j] = mean[j];
-      squares[ty * p.d + c + j] = sq[j];
-    }
+    leave_pairs(rows, p.per, v, ty, n, mean, sq, means, squares);
   }
   __syncthreads();
-  // a warp per group: the pairs of its channels and of the threads along the rows
-  const int lane = lane_id(), warps = blockDim.x >> 5;
-  for (int g = warp_id(); g < p.groups; g += warps) {
-    const int entries = p.down * p.per;
-    auto each = [&](auto f) {
-      for (int e = lane; e < entries; e += 32) {
-        const int t = e / p.per, at = t * p.d + g * p.per + (e - t * p.per);
-        const int n = max(0, (r1 - r0 - t + p.down - 1) / p.down);  // rows of thread t
-        f(static_cast<float>(n), means[at], squares[at]);
-      }
-    };
-    float sum = 0.f, sq = 0.f;
-    each([&](float n, float m, float) { sum = fmaf(n, m, sum); });
-    const float mean = warp_sum(sum) / (static_cast<float>(r1 - r0) * static_cast<float>(p.per));
-    each([&](float n, float m, float s) { sq += n > 0.f ? fmaf(n * (m - mean), m - mean, s) : 0.f; });
-    sq = warp_sum(sq);
-    if (lane == 0) p.part[(static_cast<long long>(image) * p.chunks + chunk) * p.groups + g] = make_float2(mean, sq);
-  }
+  // group g's pairs to the cluster's CTA g % CHUNKS, which joins them
+  const float inv = rows.n > 0 ? __fdividef(1.f, static_cast<float>(rows.n) * static_cast<float>(p.per)) : 0.f;
+  const int rank = blockIdx.x % CHUNKS, pitch = (p.groups + CHUNKS - 1) / CHUNKS, first = r0 - rank * o.chunk;
+  cluster_wait();
+  join_groups(rows, p.groups, inv, means, squares, [&](int g, int l, Pair q) {
+    if (l == 0)
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa_shared(smem_u32(pairs + rank * pitch + g / CHUNKS), g % CHUNKS)),
+                   "f"(q.mean), "f"(q.sq)
+                   : "memory");
+  });
+  cluster_sync();
+  join_cluster(
+      pairs, pitch, CHUNKS, (p.groups - rank + CHUNKS - 1) / CHUNKS, p.per,
+      [&](int k) { return max(0, min(p.rows, first + (k + 1) * o.chunk) - (first + k * o.chunk)); },
+      [&](int i, Pair q) {
+        p.part[(static_cast<long long>(image) * p.groups + i * CHUNKS + rank) * o.clusters + chunk / CHUNKS] = make_float2(q.mean, q.sq);
+      });
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(MAX_THREADS) group_apply_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const __grid_constant__ NormParams p, const __grid_constant__ Two o) {
   extern __shared__ float shared[];  // [groups] means, then [groups] 1 / deviation
   pdl_wait();
   pdl_trigger();
-  const int image = blockIdx.x / p.chunks, chunk = blockIdx.x - image * p.chunks, r0 = chunk * p.chunk, r1 = min(p.rows, r0 + p.chunk);
+  const int image = blockIdx.x / o.out_chunks, r0 = (blockIdx.x - image * o.out_chunks) * o.out_chunk;
+  const int n = min(p.rows, r0 + o.out_chunk) - r0;
   float* means = shared;
   float* invs = shared + p.groups;
-  // the image's pairs, a warp per group
-  const int lane = lane_id(), warps = blockDim.x >> 5;
-  const float2* part = p.part + static_cast<long long>(image) * p.chunks * p.groups;
-  for (int g = warp_id(); g < p.groups; g += warps) {
+  // the image's pairs, a warp per group, the lanes' in registers
+  const int lane = lane_id();
+#pragma unroll 2
+  for (int g = warp_id(); g < p.groups; g += THREADS / 32) {
+    const float2* part = p.part + (static_cast<long long>(image) * p.groups + g) * o.clusters;
+    const long long each = static_cast<long long>(CHUNKS) * o.chunk;
+    auto rows_of = [&](int k) { return static_cast<float>(min(static_cast<long long>(p.rows), (k + 1) * each) - k * each); };
+    float2 q[JOINED];
     float sum = 0.f, sq = 0.f;
-    auto rows_of = [&](int k) { return static_cast<float>(min(p.rows, (k + 1) * p.chunk) - k * p.chunk); };
-    for (int k = lane; k < p.chunks; k += 32) sum = fmaf(rows_of(k), part[static_cast<long long>(k) * p.groups + g].x, sum);
-    const float mean = warp_sum(sum) / static_cast<float>(p.rows);
-    for (int k = lane; k < p.chunks; k += 32) {
-      const float2 q = part[static_cast<long long>(k) * p.groups + g];
-      sq += fmaf(rows_of(k) * static_cast<float>(p.per) * (q.x - mean), q.x - mean, q.y);
+#pragma unroll
+    for (int i = 0; i < JOINED; ++i) {
+      q[i] = make_float2(0.f, 0.f);
+      if (32 * i + lane < o.clusters) q[i] = __ldg(part + 32 * i + lane);
     }
-    const float var = warp_sum(sq) / (static_cast<float>(p.rows) * static_cast<float>(p.per));
+#pragma unroll
+    for (int i = 0; i < JOINED; ++i)
+      if (32 * i + lane < o.clusters) sum = fmaf(rows_of(32 * i + lane), q[i].x, sum);
+    const float mean = warp_sum(sum) * p.inv_rows;
+#pragma unroll
+    for (int i = 0; i < JOINED; ++i)
+      if (32 * i + lane < o.clusters)
+        sq += fmaf(rows_of(32 * i + lane) * static_cast<float>(p.per) * (q[i].x - mean), q[i].x - mean, q[i].y);
+    const float var = warp_sum(sq) * p.inv_count;
     if (lane == 0) {
       means[g] = mean;
-      invs[g] = 1.f / sqrtf(var + p.eps);
+      invs[g] = rsqrtf(var + p.eps);
     }
   }
   __syncthreads();
-  const int tx = threadIdx.x % p.across, ty = threadIdx.x / p.across;
-  const long long row0 = static_cast<long long>(image) * p.rows;
+  const int tx = threadIdx.x % o.across, ty = threadIdx.x / o.across;
+  const long long row0 = static_cast<long long>(image) * p.rows + r0;
   const unsigned char* x = p.x + row0 * p.x_row;
   constexpr int ESIZE = TYPE == 2 ? 4 : 2;
-  // (all lanes of a half warp stay together: its 128 channels are a block of codes)
-  for (int pass = 0; pass < p.passes; ++pass) {
-    const int c = (tx + pass * p.across) * 8;
-    const bool in = c < p.d && ty < p.down;
+  for (int pass = 0; pass < o.passes; ++pass) {
+    const int c = (tx + pass * o.across) * 8;
+    const bool in = c < p.d && ty < o.down;
     float mean[8], a[8], b[8];
-    if (in)
+    if (in) {
+      gains(p, image, c, a, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int g = (c + j) / p.per;
-        const long long v = image * p.vec_row + c + j;
-        const float up = 1.f + vec_at(p.scale, p.vec_f32, v, 0.f);
         mean[j] = means[g];
-        a[j] = invs[g] * vec_at(p.w, p.vec_f32, c + j, 1.f) * up;
-        b[j] = fmaf(vec_at(p.b, p.vec_f32, c + j, 0.f), up, vec_at(p.shift, p.vec_f32, v, 0.f));
-      }
-    const int n = r1 - r0, steps = (n + p.down - 1) / p.down;
-    constexpr int AHEAD = 4;
-    for (int s = (steps - 1) / AHEAD; s >= 0; --s) {
-      Eight<TYPE> e[AHEAD];
-      int row[AHEAD];
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        row[i] = r0 + ty + (s * AHEAD + i) * p.down;
-        if (!in || row[i] >= r1) row[i] = -1;
-        e[i].clear();
-        if (row[i] >= 0) e[i].load(x + row[i] * p.x_row + c * ESIZE);
-      }
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        float f[8];
-        e[i].widen(f);
-        if (in)
-          with_activation(p.act, [&](auto act) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = activation<decltype(act)::value>(fmaf(f[j] - mean[j], a[j], b[j]));
-          });
-        if (p.y_type == HILO_E4M3) {
-          float m = row[i] >= 0 ? amax8(f, 0.f) : 0.f, inv, sc;
-#pragma unroll
-          for (int off = 8; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-          block_scale(m, inv, sc);
-          if (row[i] < 0) continue;
-          __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y) + (row0 + row[i]) * p.y_row + c), block_codes(f, inv));
-          if ((tx & 15) == 0) p.y_scale[(c >> 7) * p.y_scale_ld + row0 + row[i]] = sc;
-        } else if (row[i] >= 0) {
-          store4(p.y, p.y_type, (row0 + row[i]) * p.y_row + c, f);
-          store4(p.y, p.y_type, (row0 + row[i]) * p.y_row + c + 4, f + 4);
-        }
+        a[j] *= invs[g];
       }
     }
+    const int steps = (n + o.down - 1) / o.down;
+    with_activation(p.act, [&](auto act) {
+      for (int s = (steps - 1) / BATCH; s >= 0; --s) {
+        Eight<TYPE> e[BATCH];
+        long long row[BATCH];  // of all images, -1: not there
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          const int r = ty + (s * BATCH + i) * o.down;
+          const bool there = in && r < n;
+          row[i] = there ? row0 + r : -1;
+          e[i].clear();
+          if (there) e[i].load(x + r * p.x_row + c * ESIZE);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; i += 2) {
+          float f[2][8];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            e[i + u].widen(f[u]);
+            if (in)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[u][j] = activation<decltype(act)::value>(fmaf(f[u][j] - mean[j], a[j], b[j]));
+          }
+          put<2>(p, row + i, c, tx, f);
+        }
+      }
+    });
   }
 }
 
-// Threads and chunks of a shape.
-void lay_out(const hilo_group_norm_shape& s, NormParams& p) {
-  const int vectors = s.d / 8, wide = (vectors + 15) / 16 * 16;
-  p.across = wide < MAX_THREADS ? wide : MAX_THREADS;
-  p.passes = (vectors + p.across - 1) / p.across;
-  p.down = MAX_THREADS / p.across;
-  if (p.down > s.rows && s.rows > 0) p.down = s.rows;
-  const int most = MAX_CHUNKS / s.B > 1 ? MAX_CHUNKS / s.B : 1;
-  const int unit = p.down * BATCH;
-  int chunks = (s.rows + unit - 1) / unit;
-  if (chunks > most) chunks = most;
-  if (chunks < 1) chunks = 1;
-  p.chunk = ((s.rows + chunks - 1) / chunks + p.down - 1) / p.down * p.down;
-  p.chunks = p.chunk ? (s.rows + p.chunk - 1) / p.chunk : 1;
+// ------------------------------------------------------------------ one kernel --
+
+constexpr int ONE_THREADS = 256;
+constexpr int ONE_PARTS = 8;          // CTAs of a cluster at most (four: 3 x 1380 rows of 1152 channels 17.7 us, 14.7 with eight)
+constexpr int ONE_SMEM = 112 * 1024;  // shared memory of a CTA at most: two on an SM (220 KB and one: 4 x 4096 rows of 512 35 us, else 21)
+constexpr int ONE_WIDE = 256;         // channels of a slice at most, and rows of a box (TMA)
+
+// How an image is shared out: `slices` of `wide` channels, each `parts` CTAs of `chunk` rows; a row's `across` vectors of
+// eight channels, `down` rows at a time.
+struct One {
+  int wide, slices, parts, chunk, across, down, box, groups;  // groups: of a slice
+  int tile;                                                   // bytes of x
+  // the tile, means, squares, barrier and flag, the cluster's pairs, the groups' statistics; alignment
+  int smem() const {
+    return tile + ONE_THREADS * 8 * 2 * static_cast<int>(sizeof(float)) + 16 + (parts + 1) * groups * static_cast<int>(sizeof(Pair)) + 16 + 128;
+  }
+};
+
+template <int TYPE>
+__global__ void __launch_bounds__(ONE_THREADS, 2)
+    group_norm_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ NormParams p, const __grid_constant__ One o) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+  constexpr int ESIZE = TYPE == 2 ? 4 : 2;
+  unsigned char* tile = smem;  // [rows][wide]
+  float* means = reinterpret_cast<float*>(smem + o.tile);
+  float* squares = means + ONE_THREADS * 8;
+  uint64_t* bar = reinterpret_cast<uint64_t*>(squares + ONE_THREADS * 8);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar + 1);
+  Pair* pairs = reinterpret_cast<Pair*>(bar + 2);  // [CTA][group]
+  Pair* stats = pairs + o.parts * o.groups;        // [group]: mean, 1 / deviation
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tm);
+  }
+  __syncthreads();
+  pdl_wait();  // all threads
+  pdl_trigger();
+  const int rank = blockIdx.x % o.parts, unit = blockIdx.x / o.parts;
+  const int image = unit / o.slices, c0 = (unit - image * o.slices) * o.wide;
+  const int r0 = rank * o.chunk, n = max(0, min(p.rows, r0 + o.chunk) - r0);
+  const int here = min(o.wide, p.d - c0), groups = here / p.per;
+  const long long row0 = static_cast<long long>(image) * p.rows + r0;
+  if (threadIdx.x == 0 && n > 0) {
+    // (whole boxes: the rows behind the part, and the channels behind the last, are read over or are zeros)
+    const int boxes = (n + o.box - 1) / o.box;
+    mbar_arrive_expect_tx(bar, static_cast<uint32_t>(boxes * o.box * o.wide * ESIZE));
+    for (int i = 0; i < boxes; ++i)
+      tma_load_2d(tile + static_cast<size_t>(i) * o.box * o.wide * ESIZE, &tm, bar, c0, static_cast<int>(row0) + i * o.box);
+  }
+  if (o.parts > 1) cluster_arrive_relaxed();  // this CTA has begun: the others may store into it
+  const int tx = threadIdx.x % o.across, ty = threadIdx.x / o.across, c = tx * 8;
+  const bool on = ty < o.down && c < here;
+  const Rows rows(n, o.down, o.across, o.wide, p.per, groups, ONE_THREADS);
+  const float inv_n = __fdividef(1.f, static_cast<float>(n) * static_cast<float>(p.per));
+  float a[8], b[8];
+  if (on) gains(p, image, c0 + c, a, b);  // beside the copies
+  // (a wait that ran out leaves an error and rows that are not meant to be right)
+  if (n > 0) mbar_wait(bar, 0, abort_flag, &g_group_norm_err, DEV_TIMEOUT_GEMM + 256 * 30);
+  const int pitch = o.wide * ESIZE;
+  auto at = [&](int r) { return tile + r * pitch + c * ESIZE; };
+  // the thread's pairs: its means, then the squares about them
+  if (on) {
+    float mean[8], sq[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mean[j] = sq[j] = 0.f;
+#pragma unroll 4
+    for (int r = ty; r < n; r += o.down) {
+      Eight<TYPE> e;
+      float f[8];
+      e.load(at(r));
+      e.widen(f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mean[j] += f[j];
+    }
+    const int mine = rows.of(ty);
+    const float inv = mine > 0 ? __fdividef(1.f, static_cast<float>(mine)) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mean[j] *= inv;
+#pragma unroll 4
+    for (int r = ty; r < n; r += o.down) {
+      Eight<TYPE> e;
+      float f[8];
+      e.load(at(r));
+      e.widen(f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sq[j] = fmaf(f[j] - mean[j], f[j] - mean[j], sq[j]);
+    }
+    leave_pairs(rows, p.per, tx, ty, mine, mean, sq, means, squares);
+  }
+  __syncthreads();
+  // every CTA gets every CTA's pairs
+  if (o.parts > 1) cluster_wait();
+  join_groups(rows, groups, inv_n, means, squares, [&](int g, int l, Pair q) {
+    for (int k = l; k < o.parts; k += rows.lanes) {
+      const uint32_t to = smem_u32(pairs + rank * groups + g), remote = o.parts > 1 ? mapa_shared(to, k) : to;
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(remote), "f"(q.mean), "f"(q.sq) : "memory");
+    }
+  });
+  if (o.parts > 1) cluster_sync();
+  else __syncthreads();
+  join_cluster(
+      pairs, groups, o.parts, groups, p.per, [&](int k) { return max(0, min(p.rows, (k + 1) * o.chunk) - k * o.chunk); },
+      [&](int g, Pair q) { stats[g] = {q.mean, rsqrtf(fmaf(q.sq, p.inv_count, p.eps))}; });
+  __syncthreads();
+  float mean[8];
+  if (on)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const Pair q = stats[(c + j) / p.per];
+      mean[j] = q.mean;
+      a[j] *= q.sq;
+    }
+  with_activation(p.act, [&](auto act) {
+#pragma unroll 1
+    for (int r1 = ty; r1 - ty < n; r1 += 2 * o.down) {
+      float f[2][8];
+      long long row[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int r = r1 + u * o.down;
+        const bool there = on && r < n;
+        row[u] = there ? row0 + r : -1;
+        if (there) {
+          Eight<TYPE> e;
+          e.load(at(r));
+          e.widen(f[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (row[u] >= 0)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[u][j] = activation<decltype(act)::value>(fmaf(f[u][j] - mean[j], a[j], b[j]));
+      put<2>(p, row, c0 + c, tx, f);
+    }
+  });
+}
+
+// The cheapest way to share an image out, by waves of CTAs: 2.5 us each beside what a CTA reads and writes at its part of
+// HBM's rate. False where no slice fits.
+bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
+  const int per = s.d / s.groups, esize = s.x_dtype == HILO_F32 ? 4 : 2;
+  // whole groups, whole vectors, and of codes whole blocks
+  int unit = per;
+  while (unit % 8) unit += per;
+  if (s.y_dtype == HILO_E4M3 && s.d > 128)
+    while (unit % 128 && unit < s.d) unit += per;
+  const int vectors_most = s.y_dtype == HILO_E4M3 ? 32 : ONE_WIDE / 8;
+  float least = 3e38f;
+  for (int wide = unit; wide <= ONE_WIDE && wide < s.d + unit; wide += unit) {
+    const int w = wide < s.d ? wide : s.d;
+    if (w > ONE_WIDE || w / 8 > vectors_most || (w * esize < 64 && w < s.d)) continue;
+    if (s.y_dtype == HILO_E4M3 && w % 128 && w < s.d) continue;
+    int across = w / 8;
+    if (s.y_dtype == HILO_E4M3) across = (across + 15) / 16 * 16;
+    const int slices = (s.d + w - 1) / w;
+    for (int parts = 1; parts <= ONE_PARTS; parts *= 2) {
+      if (parts > 1 && parts > s.rows) break;
+      const int chunk = (s.rows + parts - 1) / parts;
+      int box = (chunk + 7) / 8 * 8;
+      if (box > ONE_WIDE) box = ONE_WIDE;
+      const long long tile = static_cast<long long>((chunk + box - 1) / box) * box * w * esize;
+      const One one = {w, slices, parts, chunk, across, ONE_THREADS / across, box, w / per, static_cast<int>(tile < ONE_SMEM ? tile : ONE_SMEM)};
+      if (one.smem() > ONE_SMEM) continue;
+      const long long ctas = static_cast<long long>(s.B) * slices * parts;
+      if (ctas > 0x7fffffffLL) continue;
+      const long long waves = (ctas + 2 * num_sms - 1) / (2 * num_sms);
+      const float cost = static_cast<float>(waves) * (2.5f + static_cast<float>(tile) * 2.f / 22e3f) + 0.05f * static_cast<float>(parts);
+      if (cost < least) {
+        least = cost;
+        *best = one;
+      }
+    }
+  }
+  return least < 3e38f;
 }
 
 template <int TYPE>
-cudaError_t launch_type(const NormParams& p, int B, int* launches, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>(p.chunks) * static_cast<unsigned>(B));
-  const dim3 block(static_cast<unsigned>((p.across * p.down + 31) / 32 * 32));
-  const size_t stats = static_cast<size_t>(p.down) * p.d * 2 * sizeof(float);
-  auto* kern = group_stats_kernel<TYPE>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024);
+cudaError_t launch_one(const hilo_group_norm_shape& s, const NormParams& p, const One& o, int* launches, cudaStream_t st) {
+  CUtensorMap tm;
+  const int esize = TYPE == 2 ? 4 : 2;
+  if (!encode_tmap_rows_2d(&tm, esize, p.x, static_cast<uint64_t>(s.d), static_cast<uint64_t>(s.B) * s.rows, static_cast<uint64_t>(s.x_row),
+                           static_cast<uint32_t>(o.wide), static_cast<uint32_t>(o.box)))
+    return cudaErrorInvalidValue;
+  auto* kern = group_norm_kernel<TYPE>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE_SMEM);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kern, grid, block, stats, st, p);
+  e = launch_pdl_cluster(kern, o.parts, dim3(static_cast<unsigned>(s.B) * o.slices * o.parts), dim3(ONE_THREADS), static_cast<size_t>(o.smem()), st, tm, p, o);
+  if (e == cudaSuccess) *launches = 1;
+  return e;
+}
+
+// Threads and chunks of the two kernels; `most` chunks of statistics and `most_out` of output, if each image has one.
+Two plan_two(const hilo_group_norm_shape& s, int most, int most_out) {
+  Two o;
+  const int vectors = s.d / 8, wide = (vectors + 15) / 16 * 16;
+  o.across = wide < THREADS ? wide : THREADS;
+  o.passes = (vectors + o.across - 1) / o.across;
+  o.down = THREADS / o.across;
+  if (o.down > s.rows && s.rows > 0) o.down = s.rows;
+  auto share = [&](int chunks, int* chunk) {  // an image's rows among so many chunks, whole passes each
+    const int unit = o.down * BATCH, full = (s.rows + unit - 1) / unit;
+    if (chunks > full) chunks = full;
+    if (chunks < 1) chunks = 1;
+    *chunk = ((s.rows + chunks - 1) / chunks + o.down - 1) / o.down * o.down;
+    return *chunk ? (s.rows + *chunk - 1) / *chunk : 1;
+  };
+  const int each = most / s.B / CHUNKS * CHUNKS;
+  o.clusters = (share(each > CHUNKS ? each : CHUNKS, &o.chunk) + CHUNKS - 1) / CHUNKS;
+  o.chunks = CHUNKS * o.clusters;
+  o.out_chunks = share(most_out / s.B, &o.out_chunk);
+  return o;
+}
+
+// As many chunks of statistics as the device holds at once: clusters do not fill its groups of SMs. (2^20 rows of
+// 128 channels in bf16: 155 us with the 432 that it holds in clusters of 4, 182 with 448; 164 with the 400 of clusters of 8.)
+template <int TYPE>
+int resident_chunks(int device, int num_sms) {
+  static PerDevice clusters;
+  const int n = clusters.get(device, [&] {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CHUNKS * num_sms, 1, 1);
+    cfg.blockDim = dim3(THREADS, 1, 1);
+    cfg.dynamicSmemBytes = 72 * 1024;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = CHUNKS;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int found = 0;
+    if (cudaOccupancyMaxActiveClusters(&found, group_stats_kernel<TYPE>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      found = 0;
+    }
+    return found;
+  });
+  const int chunks = n > 0 ? CHUNKS * n : num_sms;
+  return chunks < MAX_CHUNKS ? chunks : MAX_CHUNKS;
+}
+
+template <int TYPE>
+cudaError_t launch_two(const hilo_group_norm_shape& s, const NormParams& p, int device, int num_sms, int* launches, cudaStream_t st) {
+  auto* kern = group_stats_kernel<TYPE>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  if (e != cudaSuccess) return e;
+  const Two o = plan_two(s, resident_chunks<TYPE>(device, num_sms), APPLY_CTAS * num_sms);
+  const size_t stats = static_cast<size_t>(o.down) * 2 * sizeof(float) * (p.per % 8 == 0 ? o.across * o.passes : s.d) +
+                       static_cast<size_t>(s.groups + CHUNKS) * sizeof(Pair);
+  e = launch_pdl_cluster(kern, CHUNKS, dim3(static_cast<unsigned>(o.chunks) * static_cast<unsigned>(s.B)), dim3(THREADS), stats, st, p, o);
   if (e != cudaSuccess) return e;
   *launches = 1;
   auto* apply = group_apply_kernel<TYPE>;
   e = cudaFuncSetAttribute(apply, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(apply, grid, block, static_cast<size_t>(p.groups) * 2 * sizeof(float), st, p);
+  e = launch_pdl(apply, dim3(static_cast<unsigned>(o.out_chunks) * static_cast<unsigned>(s.B)), dim3(THREADS),
+                 static_cast<size_t>(p.groups) * 2 * sizeof(float), st, p, o);
   if (e == cudaSuccess) *launches = 2;
   return e;
+}
+
+template <int TYPE>
+cudaError_t launch_type(const hilo_group_norm_shape& s, const NormParams& p, int device, int num_sms, int* launches, cudaStream_t st) {
+  One o;
+  return plan_one(s, num_sms, &o) ? launch_one<TYPE>(s, p, o, launches, st) : launch_two<TYPE>(s, p, device, num_sms, launches, st);
 }
 
 }  // namespace
 
 size_t group_norm_workspace_bytes(const hilo_group_norm_shape& s) {
-  NormParams p;
-  lay_out(s, p);
-  return static_cast<size_t>(s.B) * p.chunks * s.groups * sizeof(float2);
+  return static_cast<size_t>(s.B) * plan_two(s, MAX_CHUNKS, 1).clusters * s.groups * sizeof(float2);
 }
 
 cudaError_t launch_group_norm(const GroupNormArgs& a, int device, int num_sms, int* launches, cudaStream_t st) {
-  (void)device;
-  (void)num_sms;
   *launches = 0;
   const hilo_group_norm_shape& s = a.s;
   NormParams p;
@@ -291,10 +691,18 @@ cudaError_t launch_group_norm(const GroupNormArgs& a, int device, int num_sms, i
   p.y_type = s.y_dtype;
   p.vec_f32 = s.vec_dtype == HILO_F32;
   p.eps = s.eps;
-  lay_out(s, p);
-  return s.x_dtype == HILO_BF16  ? launch_type<0>(p, s.B, launches, st)
-         : s.x_dtype == HILO_F16 ? launch_type<1>(p, s.B, launches, st)
-                                 : launch_type<2>(p, s.B, launches, st);
+  p.inv_rows = 1.0f / static_cast<float>(s.rows);
+  p.inv_count = static_cast<float>(1.0 / (static_cast<double>(s.rows) * p.per));
+  return s.x_dtype == HILO_BF16  ? launch_type<0>(s, p, device, num_sms, launches, st)
+         : s.x_dtype == HILO_F16 ? launch_type<1>(s, p, device, num_sms, launches, st)
+                                 : launch_type<2>(s, p, device, num_sms, launches, st);
+}
+
+int group_norm_take_device_error() {
+  int v = 0, z = 0;
+  if (cudaMemcpyFromSymbol(&v, g_group_norm_err, sizeof(int)) != cudaSuccess) return -1;
+  if (v) cudaMemcpyToSymbol(g_group_norm_err, &z, sizeof(int));
+  return v;
 }
 
 }  // namespace hilo

@@ -178,6 +178,7 @@ struct GroupNormArgs {
 size_t group_norm_workspace_bytes(const hilo_group_norm_shape& s);
 // *launches: kernels launched, also where one of them fails
 cudaError_t launch_group_norm(const GroupNormArgs& a, int device, int num_sms, int* launches, cudaStream_t st);
+int group_norm_take_device_error();
 // The wait-timeout probe: one bounded mbarrier wait that runs out; its code
 // is read (and cleared) like the kernels' device error words.
 cudaError_t launch_wait_probe(cudaStream_t st);
@@ -198,6 +199,9 @@ bool encode_tmap_2d(CUtensorMap* map, TmapType type, const void* base, uint64_t 
 // 16-bit elements over three axes: [n2][n1][n0], strides in elements
 bool encode_tmap_16bit_3d(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, uint64_t n2, uint64_t stride1,
                           uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2);
+// row-major without a swizzle: a box lies in shared memory row after row; esize 2 or 4
+bool encode_tmap_rows_2d(CUtensorMap* map, int esize, const void* base, uint64_t inner, uint64_t outer,
+                         uint64_t row_stride_elems, uint32_t box_inner, uint32_t box_outer);
 bool encode_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                          uint64_t row_stride_elems, uint32_t box_inner, uint32_t box_outer);
 
