@@ -730,8 +730,8 @@ int hilo_block_forward_mod(const hilo_shape* shape, const hilo_block_weights* we
  * belongs to other rows in an output is left as it was.
  * ---------------------------------------------------------------------------
  *
- * Rows of hilo_quantize_e4m3_128: [rows, cols], rows >= 0, cols a positive multiple
- * of 16.
+ * Rows of hilo_quantize_e4m3_128: [rows, cols], rows 0 to 2^30, cols a multiple of
+ * 16, 16 to 2^30, rows * ceil(cols / 256) at most 2^33.
  *   dtype     of the source: HILO_BF16, HILO_F16 or HILO_F32
  *   tile      0: a scale per row and 128 columns; 1: a scale per 128 x 128
  *   src_row, dst_row   elements between the rows, multiples of 16, at least
@@ -767,8 +767,8 @@ enum { HILO_ACT_NONE = 0, HILO_ACT_SILU = 1, HILO_ACT_GELU = 2 };
 /*
  * Shape of hilo_gemm_e4m3_128 and hilo_gated_e4m3_128: rows [rows, k] times
  * weights [n, k].
- *   rows        >= 0; rows * n below 2^47
- *   k, n        positive multiples of 16
+ *   rows        0 to 2^30; rows * n below 2^44
+ *   k, n        multiples of 16, 16 to 2^30
  *   act         HILO_ACT_NONE (gemm), HILO_ACT_SILU or HILO_ACT_GELU (gated)
  *   out_dtype   HILO_BF16, HILO_F16 (saturating), HILO_F32; gated: also HILO_E4M3
  *   a_row, w_row, out_row   elements between rows, multiples of 16, at least k,

@@ -987,9 +987,10 @@ int hilo_quantize_e4m3_128(const hilo_quant128_shape* s, const void* src, const 
   if (s->dtype != HILO_BF16 && s->dtype != HILO_F16 && s->dtype != HILO_F32)
     return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: dtype=%d", s->dtype);
   if (s->tile & ~1) return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: tile=%d must be 0 or 1", s->tile);
-  if (s->rows < 0 || s->cols < 16 || s->cols % 16)
-    return fail(HILO_ERR_SHAPE, "hilo_quantize_e4m3_128: rows=%d must be >= 0, cols=%d a positive multiple of 16", s->rows,
-                s->cols);
+  const int most = 1 << 30;
+  if (s->rows < 0 || s->rows > most || s->cols < 16 || s->cols % 16 || s->cols > most)
+    return fail(HILO_ERR_SHAPE, "hilo_quantize_e4m3_128: rows=%d must be in [0, 2^30], cols=%d a multiple of 16 in [16, 2^30]",
+                s->rows, s->cols);
   if (!good_ld(s->src_row, s->cols, 16) || !good_ld(s->dst_row, s->cols, 16) ||
       !good_ld(s->scale_ld, s->tile ? (s->cols + 127) / 128 : s->rows, 1))
     return fail(HILO_ERR_ARG, "hilo_quantize_e4m3_128: src_row=%lld, dst_row=%lld, scale_ld=%lld",
@@ -1019,10 +1020,12 @@ static int gemm128(const char* name, const hilo_gemm128_shape* s, bool two, cons
   const bool codes = s->out_dtype == HILO_E4M3;
   if (s->out_dtype != HILO_BF16 && s->out_dtype != HILO_F16 && s->out_dtype != HILO_F32 && !(two && codes))
     return fail(HILO_ERR_ARG, "%s: out_dtype=%d", name, s->out_dtype);
-  if (s->rows < 0 || s->k < 16 || s->k % 16 || s->n < 16 || s->n % 16)
-    return fail(HILO_ERR_SHAPE, "%s: rows=%d must be >= 0, k=%d and n=%d positive multiples of 16", name, s->rows, s->k, s->n);
-  if (static_cast<int64_t>(s->rows) * s->n >= (1LL << 47))
-    return fail(HILO_ERR_SHAPE, "%s: rows=%d times n=%d must be below 2^47", name, s->rows, s->n);
+  const int most = 1 << 30;
+  if (s->rows < 0 || s->rows > most || s->k < 16 || s->k % 16 || s->k > most || s->n < 16 || s->n % 16 || s->n > most)
+    return fail(HILO_ERR_SHAPE, "%s: rows=%d must be in [0, 2^30], k=%d and n=%d multiples of 16 in [16, 2^30]", name, s->rows,
+                s->k, s->n);
+  if (static_cast<int64_t>(s->rows) * s->n >= (1LL << 44))
+    return fail(HILO_ERR_SHAPE, "%s: rows=%d times n=%d must be below 2^44", name, s->rows, s->n);
   if (!good_ld(s->a_row, s->k, 16) || !good_ld(s->w_row, s->k, 16) || !good_ld(s->out_row, s->n, 16))
     return fail(HILO_ERR_ARG, "%s: a_row=%lld, w_row=%lld, out_row=%lld", name, static_cast<long long>(s->a_row),
                 static_cast<long long>(s->w_row), static_cast<long long>(s->out_row));

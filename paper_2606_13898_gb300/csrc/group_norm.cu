@@ -532,9 +532,10 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
 }
 
 // The cheapest way to share an image out, by waves of CTAs: 2.5 us each beside what a CTA reads and writes at its part of
-// HBM's rate. False where no slice fits.
+// shared memory's rate, by measurement. False where no slice fits.
 bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
   const int per = s.d / s.groups, esize = s.x_dtype == HILO_F32 ? 4 : 2;
+  if (s.x_row * esize >= (1LL << 40)) return false;  // (TMA's strides)
   // whole groups, whole vectors, and of codes whole blocks
   int unit = per;
   while (unit % 8) unit += per;
@@ -641,6 +642,7 @@ cudaError_t launch_two(const hilo_group_norm_shape& s, const NormParams& p, int 
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
   if (e != cudaSuccess) return e;
   const Two o = plan_two(s, resident_chunks<TYPE>(device, num_sms), APPLY_CTAS * num_sms);
+  if (static_cast<long long>(o.chunks) * s.B > 0x7fffffffLL) return cudaErrorInvalidValue;
   const size_t stats = static_cast<size_t>(o.down) * 2 * sizeof(float) * (p.per % 8 == 0 ? o.across * o.passes : s.d) +
                        static_cast<size_t>(s.groups + CHUNKS) * sizeof(Pair);
   e = launch_pdl_cluster(kern, CHUNKS, dim3(static_cast<unsigned>(o.chunks) * static_cast<unsigned>(s.B)), dim3(THREADS), stats, st, p, o);

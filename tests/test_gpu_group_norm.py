@@ -187,6 +187,18 @@ def test_group_norm_far_rows(H):
     check(big.view(rows, row)[:, :d], want, off, "bf16")
 
 
+def test_group_norm_one_row_of_the_widest_stride(H):
+    p = Images(1, 1, 256, 32, "f32", cond=False)
+    want, off = p.exact("silu", 1e-5)
+    far = (1 << 39) - 16
+    shape = H.GroupNormShape(B=1, rows=1, d=256, groups=32, act=H.HILO_ACT_SILU, x_dtype=H.HILO_F32, y_dtype=H.HILO_F32, x_row=far,
+                             y_row=far, vec_row=far + 8)
+    nb = H.hilo_group_norm_workspace_bytes(shape)
+    y = torch.empty(1, 256, device="cuda")
+    H.hilo_group_norm(shape, p.vectors(H), p.buf, y, None, torch.empty(nb, dtype=torch.uint8, device="cuda"), nb)
+    check(y, want, off, "f32")
+
+
 @pytest.mark.parametrize("B,rows,d", [(1, 600, 512), (2, 40000, 128)])
 def test_group_norm_captured_and_on_two_streams(H, B, rows, d):
     p, q = Images(B, rows, d, 32), Images(B, rows, d, 32, seed=1)
