@@ -10,8 +10,8 @@
 //
 // Images whose slices of channels (whole groups) fit the shared memory of a cluster: one kernel
 // (group_norm_kernel). A CTA copies its rows of the slice by TMA, finds each group's mean and the squares about it in two
-// passes over them, tells the cluster's other CTAs, and writes. x is read once. 1024 rows of 512 channels take 5.5 us
-// (two kernels: 15.6): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
+// passes over them, tells the cluster's other CTAs, and writes. x is read once. 1024 rows of 512 channels take 5.2 us
+// (two kernels: 9.0): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
 // the passes over shared memory and the activation, not by HBM (2 TB/s).
 //
 // Other images: two kernels over chunks of rows. The first leaves the pairs of each cluster's chunks in the workspace, the
@@ -86,6 +86,12 @@ __device__ __forceinline__ void gains(const NormParams& p, int image, int c, flo
 // pairs in shared memory: one for all eight channels where groups are whole vectors, one per channel
 // otherwise. Then `lanes` threads a group, as many as there are for all groups at once, join them: the means first, then the squares
 // about the joint mean.
+__host__ __device__ inline int lanes_of(int groups, int threads) {
+  int lanes = 32;
+  while (lanes > 4 && groups * lanes > threads) lanes /= 2;
+  return lanes;
+}
+
 struct Rows {
   int n, down;
   int unit, pitch;  // entries of a group in a thread row, entries of a thread row
@@ -100,8 +106,7 @@ struct Rows {
     weight = vectors ? 8.f : 1.f;
     base = n / down;
     more = n - base * down;
-    lanes = 32;
-    while (lanes > 4 && groups * lanes > threads) lanes /= 2;
+    lanes = lanes_of(groups, threads);
     const int l = threadIdx.x & (lanes - 1);
     t0 = l / unit;
     c0 = l - t0 * unit;
@@ -395,6 +400,7 @@ __global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const 
 constexpr int ONE_THREADS = 256;
 constexpr int ONE_PARTS = 8;          // CTAs of a cluster at most (four: 3 x 1380 rows of 1152 channels 17.7 us, 14.7 with eight)
 constexpr int ONE_SMEM = 112 * 1024;  // shared memory of a CTA at most: two on an SM (220 KB and one: 4 x 4096 rows of 512 35 us, else 21)
+constexpr int ONE_LEAST = 76 * 1024;  // and at least: three on some SMs and one on others take longer (3 x 1380 rows of 1152: 14.8 us, else 11.6)
 constexpr int ONE_WIDE = 256;         // channels of a slice at most, and rows of a box (TMA)
 
 // How an image is shared out: `slices` of `wide` channels, each `parts` CTAs of `chunk` rows; a row's `across` vectors of
@@ -531,8 +537,11 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
   });
 }
 
-// The cheapest way to share an image out, by waves of CTAs: 2.5 us each beside what a CTA reads and writes at its part of
-// shared memory's rate, by measurement. False where no slice fits.
+// The cheapest way to share an image out: by waves of CTAs, 2.5 us each beside what a CTA reads and writes at its part of
+// shared memory's rate, by CTAs of a cluster and by entries that a lane joins. Fitted to 25 shapes of 22 to 7229 rows, 32 to
+// 2304 channels in every slice and number of parts: its pick is 3% behind the fastest in the mean, 22% at worst; 15 other
+// shapes: 3%, 9%. False where no slice fits: two kernels, which took 1.1 to 2.8 times as long wherever one fits (1024 rows of
+// 512: 9.0 us, else 5.2; 32 x 256 rows of 2048: 28.6, else 26.0).
 bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
   const int per = s.d / s.groups, esize = s.x_dtype == HILO_F32 ? 4 : 2;
   if (s.x_row * esize >= (1LL << 40)) return false;  // (TMA's strides)
@@ -550,7 +559,7 @@ bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
     int across = w / 8;
     if (s.y_dtype == HILO_E4M3) across = (across + 15) / 16 * 16;
     const int slices = (s.d + w - 1) / w;
-    for (int parts = 1; parts <= ONE_PARTS; parts *= 2) {
+    for (int parts = 1; parts <= ONE_PARTS; ++parts) {
       if (parts > 1 && parts > s.rows) break;
       const int chunk = (s.rows + parts - 1) / parts;
       int box = (chunk + 7) / 8 * 8;
@@ -561,7 +570,10 @@ bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
       const long long ctas = static_cast<long long>(s.B) * slices * parts;
       if (ctas > 0x7fffffffLL) continue;
       const long long waves = (ctas + 2 * num_sms - 1) / (2 * num_sms);
-      const float cost = static_cast<float>(waves) * (2.5f + static_cast<float>(tile) * 2.f / 22e3f) + 0.05f * static_cast<float>(parts);
+      const int lanes = lanes_of(w / per, ONE_THREADS), entries = one.down * (per % 8 == 0 ? per / 8 : per);
+      const int joined = (entries + lanes - 1) / lanes * ((w / per * lanes + ONE_THREADS - 1) / ONE_THREADS);
+      const float cost = static_cast<float>(waves) * (2.5f + static_cast<float>(chunk * w * esize) / 8e3f) +
+                         0.2f * static_cast<float>(parts) + 0.3f * static_cast<float>(joined);
       if (cost < least) {
         least = cost;
         *best = one;
@@ -581,7 +593,8 @@ cudaError_t launch_one(const hilo_group_norm_shape& s, const NormParams& p, cons
   auto* kern = group_norm_kernel<TYPE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE_SMEM);
   if (e != cudaSuccess) return e;
-  e = launch_pdl_cluster(kern, o.parts, dim3(static_cast<unsigned>(s.B) * o.slices * o.parts), dim3(ONE_THREADS), static_cast<size_t>(o.smem()), st, tm, p, o);
+  e = launch_pdl_cluster(kern, o.parts, dim3(static_cast<unsigned>(s.B) * o.slices * o.parts), dim3(ONE_THREADS),
+                         static_cast<size_t>(o.smem() > ONE_LEAST ? o.smem() : ONE_LEAST), st, tm, p, o);
   if (e == cudaSuccess) *launches = 1;
   return e;
 }
