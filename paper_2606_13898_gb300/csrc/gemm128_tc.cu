@@ -149,9 +149,10 @@ __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;
 // A slot: the scales of ROWS rows (0 behind `rows`), then the weights' PARTS. as, ws: of the first block; as is this lane's.
 template <int ROWS, int PARTS>
 __device__ __forceinline__ bool fill_scales(const ScaleRing& ring, uint32_t& n, int nkb, int rows, const float* as, long long a_step,
-                                            const float* w0, const float* w1, volatile int* abort_flag, int* err, int code) {
+                                            const float* w0, const float* w1, const float* w2, volatile int* abort_flag, int* err,
+                                            int code) {
   const int lane = lane_id();
-  const float* ws = lane == 0 ? w0 : w1;
+  const float* ws = lane == 0 ? w0 : lane == 1 ? w1 : w2;
   for (int i = 0; i < nkb; ++i, ++n) {
     const uint32_t k = n % SLOTS;
     if (!mbar_wait_warp(&ring.empty[k], ((n / SLOTS) & 1u) ^ 1u, abort_flag, err, code)) return false;
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
     const long long w = (f0 >> 7) * p.w_scale_ld + kb0;
     uint32_t n = 0;
     fill_scales<NT, C::PARTS>(ring, n, nkb, p.rows - r0, p.a_scale + kb0 * p.a_scale_ld + r0 + lane, p.a_scale_ld, p.w_scale[0] + w,
-                              p.w_scale[C::PARTS - 1] + w, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 22);
+                              p.w_scale[C::PARTS - 1] + w, nullptr, abort_flag, err, DEV_TIMEOUT_GEMM + 256 * 22);
     copies_done();
     __syncwarp();
   } else if (warp < C::SUMS) {
@@ -565,11 +566,15 @@ struct Many {
   static constexpr int TF = GATED ? NT / 2 : NT;     // features
   static constexpr int STAGE = PIECE + NT / 2 * BK;  // 128 rows, and half of the columns
   static constexpr int BUFS = 512 / NT;              // of tensor memory
-  static constexpr int COLS = NT / 8;                // of a warp, in each half of the columns
+  // The columns' parts, each with one scale of the weights (gate and up; halves; of 192 columns, whose tiles begin anywhere
+  // on 64, thirds).
+  static constexpr int PARTS = NT == 192 ? 3 : 2, SPAN = NT / PARTS;
+  static constexpr int COLS = SPAN / 4;              // of a warp, in each part
+  static_assert(128 % SPAN == 0 && (!GATED || PARTS == 2), "a scale for each part");
   // Columns read at a time, into one of two sets of registers. (Gated, with 16 the sums spill: 8192 rows of 4096, 10240
   // features, 633 us, 613 so.)
   static constexpr int LOAD = GATED ? 8 : 16;
-  static constexpr int SLOT = 128 + 4;                      // floats of a block's scales: its rows', the weights' of both halves
+  static constexpr int SLOT = 128 + 4;                      // floats of a block's scales: its rows', the weights' parts'
   static constexpr int SCALES_BYTES = SLOTS * SLOT * 4, MOST_BYTES = 4 * 128 * 4;  // [4][128] row maxima
   static constexpr int STAGES = (MANY_SMEM - 1024 - 384 - SCALES_BYTES - MOST_BYTES) / STAGE;
   static constexpr int OFF_BARS = STAGES * STAGE, OFF_SCALES = OFF_BARS + 384, OFF_MOST = OFF_SCALES + SCALES_BYTES;
@@ -746,9 +751,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
         place(t, r0, f0);
         const int row = r0 + 128 * static_cast<int>(rank);
         const float* w0 = p.w_scale[0] + (f0 >> 7) * p.w_scale_ld;
-        const float* w1 = GATED ? p.w_scale[1] + (f0 >> 7) * p.w_scale_ld : p.w_scale[0] + (min(f0 + NT / 2, p.n - 1) >> 7) * p.w_scale_ld;
-        if (!fill_scales<128, 2>(ring, n, p.kblocks, rows - row, p.a_scale + row + lane, p.a_scale_ld, w0, w1, abort_flag, err,
-                                 DEV_TIMEOUT_GEMM + 256 * 24))
+        auto later = [&](int g) { return p.w_scale[0] + (min(f0 + g * C::SPAN, p.n - 1) >> 7) * p.w_scale_ld; };
+        const float* w1 = GATED ? p.w_scale[1] + (f0 >> 7) * p.w_scale_ld : later(1);
+        if (!fill_scales<128, C::PARTS>(ring, n, p.kblocks, rows - row, p.a_scale + row + lane, p.a_scale_ld, w0, w1, later(2), abort_flag,
+                                        err, DEV_TIMEOUT_GEMM + 256 * 24))
           break;
       }
       copies_done();
@@ -756,8 +762,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
     }
   } else {
     setmaxnreg_inc<SUM_REGS>();
-    // ---------------- sums: lane quarter warp % 4 (32 rows), and of both halves of the columns (gate and up) the
-    // quarter warp / 4 (NT / 8 features)
+    // ---------------- sums: lane quarter warp % 4 (32 rows), and of each part of the columns the quarter warp / 4
     const int q = warp & 3, h = warp >> 2, r = 32 * q + lane;
     float* most = reinterpret_cast<float*>(smem + C::OFF_MOST);
     const uint32_t taddr = tmem + (static_cast<uint32_t>(32 * q) << 16) + C::COLS * h;
@@ -769,9 +774,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
       int r0, f0;
       place(t, r0, f0);
       const int row = r0 + 128 * static_cast<int>(rank) + r;
-      uint64_t acc[2][C::COLS / 2];
+      uint64_t acc[C::PARTS][C::COLS / 2];
 #pragma unroll
-      for (int j = 0; j < C::COLS / 2; ++j) acc[0][j] = acc[1][j] = 0ull;
+      for (int j = 0; j < C::PARTS * C::COLS / 2; ++j) acc[j / (C::COLS / 2)][j % (C::COLS / 2)] = 0ull;
 #pragma unroll 1
       for (int kb = 0; kb < p.kblocks; ++kb, ++i) {
         if (!there_already) {
@@ -785,11 +790,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
         tc_fence_after();
         const uint32_t at = taddr + (i % C::BUFS) * NT;
         const float* slot = ring.slots + i % SLOTS * C::SLOT;
-        constexpr int LOADS = 2 * C::COLS / C::LOAD;  // the first half of them of the first half of the columns
-        auto column = [&](int c) { return at + (c * C::LOAD / C::COLS) * (NT / 2) + c * C::LOAD % C::COLS; };
+        constexpr int LOADS = C::PARTS * C::COLS / C::LOAD;  // part by part
+        auto column = [&](int c) { return at + (c * C::LOAD / C::COLS) * C::SPAN + c * C::LOAD % C::COLS; };
         float v[2][C::LOAD];
         tmem_ldn<C::LOAD>(column(0), v[0]);
-        const float s0 = slot[r] * slot[128], s1 = slot[r] * slot[129];
+        float sc[C::PARTS];
+#pragma unroll
+        for (int g = 0; g < C::PARTS; ++g) sc[g] = slot[r] * slot[128 + g];
 #pragma unroll
         for (int c = 0; c < LOADS; ++c) {
           tmem_ld_wait_n<C::LOAD>(v[c & 1]);
@@ -805,8 +812,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
                                                         mbar_test(tfull0 + 8u * (n % C::BUFS), (n / C::BUFS) & 1u));
           }
           const int g = c * C::LOAD / C::COLS, c0 = c * C::LOAD % C::COLS;
-          const float s = g ? s1 : s0;
-          const uint64_t s2 = f2(s, s);
+          const uint64_t s2 = f2(sc[g], sc[g]);
 #pragma unroll
           for (int j = 0; j < C::LOAD; j += 2) {
             uint64_t& o = acc[g][(c0 + j) / 2];
@@ -818,9 +824,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
       // ---- the tile's rows
       const bool there = row < rows;
       // part g's features of this thread, from f on
-      auto feature = [&](int g) { return f0 + (GATED ? 0 : NT / 2 * g) + C::COLS * h; };
+      auto feature = [&](int g) { return f0 + (GATED ? 0 : C::SPAN * g) + C::COLS * h; };
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < C::PARTS; ++g)
         if (const __nv_bfloat16* bias = p.bias[GATED ? g : 0]) {
 #pragma unroll
           for (int j = 0; j < C::COLS; j += 2)
@@ -878,7 +884,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
         }
       } else if (there) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int g = 0; g < C::PARTS; ++g)
 #pragma unroll
           for (int c = 0; c < C::COLS; c += 16) {
             const int f = feature(g);
@@ -994,7 +1000,10 @@ cudaError_t launch_many(const Gemm128Args& a, const Params128& p, int device, in
 // from 143 shapes of 1 to 1024 rows, 1024 and 4096 columns, 1024 to 16384 features, each with every choice: its pick is 1.4%
 // behind the fastest in the mean, 26% at worst (64 rows of 4096, 1024 features gated: 9.1 us, 7.2 in four tiles of 16
 // rows). Examples, in us: 64 rows of 4096, 4096 features: few128<64> 7.3, many128<256> 17.6; 512 rows: few128<128>
-// 18.8, many128<128> 13.7, many128<256> 18.4; 1024 rows: many128<128> 23.3, many128<256> 19.6.
+// 18.8, many128<128> 13.7, many128<256> 18.4; 1024 rows: many128<128> 23.3, many128<256> 19.6. 192 columns are for what
+// fills a round with them and leaves a part of one idle with 256: 700 rows of 4096, 4096 features: 17.2, 128 columns 23.3,
+// 256 19.1; 2389 rows: 42.8, 51.6 and 49.6; 8192 rows: 131, 135 and 110. (Of 18 shapes with all three timed each pick was the
+// fastest.)
 struct Choice {
   int many;  // few128 otherwise
   int nt, split;
@@ -1005,8 +1014,8 @@ Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
     float each, block;
   };
   constexpr Cost FEW[2][4] = {{{1.0f, .25f}, {1.5f, .275f}, {2.5f, .32f}, {3.8f, .36f}}, {{2.0f, .32f}, {2.7f, .36f}, {4.0f, .43f}, {6.0f, .73f}}};
-  constexpr Cost FIRST[2][2] = {{{2.1f, .265f}, {3.1f, .39f}}, {{2.2f, .31f}, {2.7f, .51f}}};
-  constexpr Cost NEXT[2][2] = {{{1.1f, .265f}, {1.7f, .44f}}, {{1.1f, .25f}, {1.4f, .49f}}};
+  constexpr Cost FIRST[2][3] = {{{2.1f, .265f}, {2.6f, .33f}, {3.1f, .39f}}, {{2.2f, .31f}, {}, {2.7f, .51f}}};
+  constexpr Cost NEXT[2][3] = {{{1.1f, .265f}, {1.4f, .35f}, {1.7f, .44f}}, {{1.1f, .25f}, {}, {1.4f, .49f}}};
   constexpr int PARTS = GATED ? 2 : 1;
   auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
   Choice best = {1, 256, 1};
@@ -1032,8 +1041,8 @@ Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
             {0, nt, split});
     }
   }
-  for (int i = codes ? 1 : 0; i < 2; ++i) {  // (gated to codes: a tile has whole blocks)
-    const int nt = 128 << i;
+  for (int i = codes ? 2 : 0; i < 3; i += GATED ? 2 : 1) {  // (gated to codes: a tile has whole blocks)
+    const int nt = 128 + 64 * i;
     const long long rounds = ceil_div(ceil_div(rows, 256) * ceil_div(n, nt / PARTS), num_sms / 2 > 0 ? num_sms / 2 : 1);
     const Cost f = FIRST[GATED][i], x = NEXT[GATED][i];
     offer(f.each + static_cast<float>(kblocks) * f.block + static_cast<float>(rounds - 1) * (x.each + static_cast<float>(kblocks) * x.block),
@@ -1045,8 +1054,11 @@ Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
 template <bool GATED>
 cudaError_t launch_kind(const Gemm128Args& a, const Params128& p, int device, int num_sms, cudaStream_t st) {
   const Choice c = choose<GATED>(a.s.rows, a.s.n, p.kblocks, p.out_type == HILO_E4M3, num_sms);
-  if (c.many)
+  if (c.many) {
+    if constexpr (!GATED)
+      if (c.nt == 192) return launch_many<192, false>(a, p, device, num_sms, st);
     return c.nt == 128 ? launch_many<128, GATED>(a, p, device, num_sms, st) : launch_many<256, GATED>(a, p, device, num_sms, st);
+  }
   switch (c.nt) {
     case 16: return launch_few<16, GATED>(a, p, c.split, st);
     case 32: return launch_few<32, GATED>(a, p, c.split, st);

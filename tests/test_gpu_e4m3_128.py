@@ -224,7 +224,8 @@ def run_gemm(H, p, out="bf16", n_rows=None, opad=0, stream=None, into=None):
 
 SIZES = [(1, 16, 16), (1, 128, 128), (1, 4096, 144), (2, 144, 400), (15, 272, 128), (16, 1168, 256), (17, 128, 272), (31, 640, 144),
          (33, 2048, 128), (64, 272, 144), (65, 400, 272), (127, 128, 16), (129, 1168, 144), (200, 272, 400), (256, 1024, 512),
-         (257, 144, 128), (512, 256, 272), (513, 272, 144), (700, 1168, 272), (1000, 16, 16), (2389, 512, 528)]
+         (257, 144, 128), (512, 256, 272), (513, 272, 144), (700, 1168, 272), (1000, 16, 16), (2389, 512, 528), (1499, 304, 2224),
+         (1300, 1168, 2064), (513, 272, 4752), (2389, 160, 4112), (300, 512, 7200)]
 
 
 @pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
