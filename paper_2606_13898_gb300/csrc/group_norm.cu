@@ -550,34 +550,32 @@ bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
   while (unit % 8) unit += per;
   if (s.y_dtype == HILO_E4M3 && s.d > 128)
     while (unit % 128 && unit < s.d) unit += per;
-  const int vectors_most = s.y_dtype == HILO_E4M3 ? 32 : ONE_WIDE / 8;
   float least = 3e38f;
   for (int wide = unit; wide <= ONE_WIDE && wide < s.d + unit; wide += unit) {
     const int w = wide < s.d ? wide : s.d;
-    if (w > ONE_WIDE || w / 8 > vectors_most || (w * esize < 64 && w < s.d)) continue;
+    if (w > ONE_WIDE || (w * esize < 64 && w < s.d)) continue;
     if (s.y_dtype == HILO_E4M3 && w % 128 && w < s.d) continue;
     int across = w / 8;
     if (s.y_dtype == HILO_E4M3) across = (across + 15) / 16 * 16;
-    const int slices = (s.d + w - 1) / w;
-    for (int parts = 1; parts <= ONE_PARTS; ++parts) {
-      if (parts > 1 && parts > s.rows) break;
+    const int groups = w / per, down = ONE_THREADS / across, lanes = lanes_of(groups, ONE_THREADS);
+    const int entries = (down * (per % 8 == 0 ? per / 8 : per) + lanes - 1) / lanes;  // of a lane, a group
+    const int joined = entries * ((groups * lanes + ONE_THREADS - 1) / ONE_THREADS);
+    const long long slices = (s.d + w - 1) / w, each = s.B * slices;
+    for (int parts = 1; parts <= ONE_PARTS && parts <= (s.rows > 1 ? s.rows : 1); ++parts) {
       const int chunk = (s.rows + parts - 1) / parts;
+      const long long ctas = each * parts, bytes = static_cast<long long>(chunk) * w * esize;
+      if (ctas > 0x7fffffffLL || bytes > ONE_SMEM) continue;
+      const long long waves = ctas <= 2 * num_sms ? 1 : (ctas + 2 * num_sms - 1) / (2 * num_sms);
+      const float cost = static_cast<float>(waves) * (2.5f + static_cast<float>(bytes) * (1 / 8e3f)) + 0.2f * static_cast<float>(parts) +
+                         0.3f * static_cast<float>(joined);
+      if (!(cost < least)) continue;
       int box = (chunk + 7) / 8 * 8;
       if (box > ONE_WIDE) box = ONE_WIDE;
       const long long tile = static_cast<long long>((chunk + box - 1) / box) * box * w * esize;
-      const One one = {w, slices, parts, chunk, across, ONE_THREADS / across, box, w / per, static_cast<int>(tile < ONE_SMEM ? tile : ONE_SMEM)};
+      const One one = {w, static_cast<int>(slices), parts, chunk, across, down, box, groups, static_cast<int>(tile < ONE_SMEM ? tile : ONE_SMEM)};
       if (one.smem() > ONE_SMEM) continue;
-      const long long ctas = static_cast<long long>(s.B) * slices * parts;
-      if (ctas > 0x7fffffffLL) continue;
-      const long long waves = (ctas + 2 * num_sms - 1) / (2 * num_sms);
-      const int lanes = lanes_of(w / per, ONE_THREADS), entries = one.down * (per % 8 == 0 ? per / 8 : per);
-      const int joined = (entries + lanes - 1) / lanes * ((w / per * lanes + ONE_THREADS - 1) / ONE_THREADS);
-      const float cost = static_cast<float>(waves) * (2.5f + static_cast<float>(chunk * w * esize) / 8e3f) +
-                         0.2f * static_cast<float>(parts) + 0.3f * static_cast<float>(joined);
-      if (cost < least) {
-        least = cost;
-        *best = one;
-      }
+      least = cost;
+      *best = one;
     }
   }
   return least < 3e38f;
