@@ -47,6 +47,12 @@ struct Eight {
 #pragma unroll
     for (int i = 0; i < (TYPE == 2 ? 2 : 1); ++i) q[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
   }
+  __device__ __forceinline__ void widen(uint64_t* f) const {
+    float v[8];
+    widen(v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = f2(v[2 * i], v[2 * i + 1]);
+  }
   __device__ __forceinline__ void widen(float* f) const {
     const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[TYPE == 2 ? 1 : 0].x, q[TYPE == 2 ? 1 : 0].y,
                            q[TYPE == 2 ? 1 : 0].z, q[TYPE == 2 ? 1 : 0].w};
@@ -75,6 +81,21 @@ __device__ __forceinline__ float activation(float z) {
   float inv;  // (within 1 ulp; of infinity 0)
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(1.f + ex2(t)));
   return z * inv;
+}
+// Of two values in a register pair: half the instructions.
+template <int ACT>
+__device__ __forceinline__ uint64_t activation2(uint64_t z) {
+  constexpr float LOG2E = 1.4426950408889634f, G = -2.f * LOG2E * 0.7978845608028654f;
+  if (ACT == HILO_ACT_NONE) return z;
+  const uint64_t t = ACT == HILO_ACT_SILU ? f2_mul(z, f2(-LOG2E, -LOG2E))
+                                          : f2_mul(z, f2_fma(f2_mul(z, z), f2(0.044715f * G, 0.044715f * G), f2(G, G)));
+  float lo, hi;
+  f2_split(t, lo, hi);
+  const uint64_t under = f2_add(f2(ex2(lo), ex2(hi)), f2(1.f, 1.f));
+  f2_split(under, lo, hi);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(lo));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(hi));
+  return f2_mul(z, f2(lo, hi));
 }
 // f(Act<..>) for the activation `act`: one branch around all of a row's values.
 template <int ACT>

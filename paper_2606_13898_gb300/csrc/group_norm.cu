@@ -17,7 +17,8 @@
 // Other images: two kernels over chunks of rows. The first leaves the pairs of each cluster's chunks in the workspace, the
 // second joins an image's pairs and writes its chunk, from the last row to the first, as the rows read last are the
 // ones still in L2. Bound by HBM: x is read once, and again as far as it is not in L2, y is written once; 2^20 rows of 128
-// channels in bf16 take 152 us, 5.3 TB/s of three passes.
+// channels in bf16 take 144 us, 5.6 TB/s of three passes (with half as many fp32 instructions as one for each value: pairs in
+// 64-bit registers, full batches without predicates; 152 us with them).
 #include "e4m3_128.cuh"
 #include "internal.h"
 
@@ -80,6 +81,36 @@ __device__ __forceinline__ void gains(const NormParams& p, int image, int c, flo
     b[j] = fmaf(b[j], 1.f + up[j], t[j]);
   }
 }
+
+// A row's channels c .. c + 7, from the elements to the values before rounding.
+struct Affine {
+  uint64_t minus[4], a[4], b[4];
+  // stats(group): mean and 1 / deviation; c0: the first channel among those of the groups
+  template <typename Stats>
+  __device__ __forceinline__ void set(const NormParams& p, int image, int c, int c0, Stats stats) {
+    float u[8], v[8];
+    gains(p, image, c, u, v);
+    set(u, v, p.per, c0, stats);
+  }
+  template <typename Stats>
+  __device__ __forceinline__ void set(const float* u, const float* v, int per, int c0, Stats stats) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      const Pair lo = stats((c0 + j) / per), hi = stats((c0 + j + 1) / per);
+      minus[j / 2] = f2(-lo.mean, -hi.mean);
+      a[j / 2] = f2(u[j] * lo.sq, u[j + 1] * hi.sq);
+      b[j / 2] = f2(v[j], v[j + 1]);
+    }
+  }
+  template <int ACT, int TYPE>
+  __device__ __forceinline__ void apply(const Eight<TYPE>& e, float* f) const {
+    uint64_t x[4];
+    e.widen(x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      f2_split(activation2<ACT>(f2_fma(f2_add(x[j], minus[j]), a[j], b[j])), f[2 * j], f[2 * j + 1]);
+  }
+};
 
 // ----------------------------------------------------------- a CTA's groups --
 // A CTA has n rows of some channels. Thread (tx, ty) has the channels 8 tx .. of the rows ty, ty + down, .. It leaves its
@@ -216,10 +247,10 @@ __device__ __forceinline__ void put(const NormParams& p, const long long* row, i
 // ------------------------------------------------------------------ two kernels --
 
 constexpr int THREADS = 256;
-constexpr int STATS_CTAS = 3, APPLY_CTAS = 3;  // per SM (four: 64 registers spill, 152 us become 187 and 205)
+constexpr int STATS_CTAS = 3, APPLY_CTAS = 3;  // per SM (four: the sums spill, 2^20 rows of 128 took 1.2 and 1.35 times as long)
 constexpr int MAX_CHUNKS = 456;                // of a call's statistics, but for a cluster per image
 constexpr int CHUNKS = 4;                      // of a cluster, whose pairs are joined before they are stored
-constexpr int BATCH = 4;                       // rows of a thread at a time (eight: registers spill, 187 us)
+constexpr int BATCH = 4;                       // rows of a thread at a time (eight: 2^20 rows of 128 148 us, 144 so)
 constexpr int JOINED = MAX_CHUNKS / CHUNKS / 32 + 1;  // pairs of a lane
 
 // The chunks of an image: of its statistics and of its output.
@@ -245,48 +276,61 @@ __global__ void __launch_bounds__(THREADS, STATS_CTAS) group_stats_kernel(const 
   Pair* pairs = reinterpret_cast<Pair*>(squares + o.down * rows.pitch);  // [chunk of the cluster][group of this CTA]
   constexpr int ESIZE = TYPE == 2 ? 4 : 2;
   for (int v = tx; v * 8 < p.d && ty < o.down; v += o.across) {
-    float mean[8], sq[8];
+    uint64_t mean2[4], sq2[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mean[j] = sq[j] = 0.f;
+    for (int j = 0; j < 4; ++j) mean2[j] = sq2[j] = 0ull;
     int n = 0;
-    const int step = o.down * BATCH;
-    for (int r = ty; r < rows.n; r += step) {
+    const unsigned char* at = x + ty * p.x_row + v * 8 * ESIZE;
+    const long long step = o.down * p.x_row;
+    // more rows, of mean -minus and squares `two` about it, `part` of all there are: the mean moves by that of the gap
+    auto join = [&](int j, uint64_t minus, uint64_t two, float part) {
+      const uint64_t gap = f2_add(mean2[j], minus);
+      const float scale = part * static_cast<float>(n);
+      mean2[j] = f2_fma(gap, f2(-part, -part), mean2[j]);
+      sq2[j] = f2_add(sq2[j], f2_fma(f2_mul(gap, gap), f2(scale, scale), two));
+    };
+    int r = ty;
+    for (; r + (BATCH - 1) * o.down < rows.n; r += BATCH * o.down) {
       Eight<TYPE> e[BATCH];
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        e[i].clear();
-        if (r + i * o.down < rows.n) e[i].load(x + static_cast<long long>(r + i * o.down) * p.x_row + v * 8 * ESIZE);
+      for (int i = 0; i < BATCH; ++i) e[i].load(at + i * step);
+      at += BATCH * step;
+      const float part = __fdividef(static_cast<float>(BATCH), static_cast<float>(n + BATCH));
+      uint64_t f[BATCH][4];
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) e[i].widen(f[i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t minus = f2_mul(f2_add(f2_add(f[0][j], f[1][j]), f2_add(f[2][j], f[3][j])), f2(-0.25f, -0.25f));
+        uint64_t two = 0ull;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          const uint64_t d = f2_add(f[i][j], minus);
+          two = i ? f2_fma(d, d, two) : f2_mul(d, d);
+        }
+        join(j, minus, two, part);
       }
-      // a batch's mean and squares from registers, joined with what there was: the mean moves by `part` of the gap
-      const int m = min(BATCH, (rows.n - r + o.down - 1) / o.down);
-      float sum[8], two[8];
+      n += BATCH;
+    }
+    Eight<TYPE> e[BATCH - 1];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] = two[j] = 0.f;
+    for (int i = 0; i < BATCH - 1; ++i)
+      if (r + i * o.down < rows.n) e[i].load(at + i * step);
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        float f[8];
+    for (int i = 0; i < BATCH - 1; ++i)
+      if (r + i * o.down < rows.n) {
+        const float part = __fdividef(1.f, static_cast<float>(n + 1));
+        uint64_t f[4];
         e[i].widen(f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += f[j];  // (rows that are not there are zeros)
+        for (int j = 0; j < 4; ++j) join(j, f2_mul(f[j], f2(-1.f, -1.f)), 0ull, part);
+        ++n;
       }
-      const float inv = __fdividef(1.f, static_cast<float>(m)), part = __fdividef(static_cast<float>(m), static_cast<float>(n + m));
+    float mean[8], sq[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] *= inv;
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        float f[8];
-        e[i].widen(f);
-        if (i < m)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) two[j] = fmaf(f[j] - sum[j], f[j] - sum[j], two[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float gap = sum[j] - mean[j];
-        mean[j] = fmaf(gap, part, mean[j]);
-        sq[j] += fmaf(gap * gap, part * static_cast<float>(n), two[j]);
-      }
-      n += m;
+    for (int j = 0; j < 4; ++j) {
+      f2_split(mean2[j], mean[2 * j], mean[2 * j + 1]);
+      f2_split(sq2[j], sq[2 * j], sq[2 * j + 1]);
     }
     leave_pairs(rows, p.per, v, ty, n, mean, sq, means, squares);
   }
@@ -355,16 +399,8 @@ __global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const 
   for (int pass = 0; pass < o.passes; ++pass) {
     const int c = (tx + pass * o.across) * 8;
     const bool in = c < p.d && ty < o.down;
-    float mean[8], a[8], b[8];
-    if (in) {
-      gains(p, image, c, a, b);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int g = (c + j) / p.per;
-        mean[j] = means[g];
-        a[j] *= invs[g];
-      }
-    }
+    Affine affine;
+    if (in) affine.set(p, image, c, c, [&](int g) { return Pair{means[g], invs[g]}; });
     const int steps = (n + o.down - 1) / o.down;
     with_activation(p.act, [&](auto act) {
       for (int s = (steps - 1) / BATCH; s >= 0; --s) {
@@ -383,10 +419,7 @@ __global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const 
           float f[2][8];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            e[i + u].widen(f[u]);
-            if (in)
-#pragma unroll
-              for (int j = 0; j < 8; ++j) f[u][j] = activation<decltype(act)::value>(fmaf(f[u][j] - mean[j], a[j], b[j]));
+            affine.template apply<decltype(act)::value>(e[i + u], f[u]);
           }
           put<2>(p, row + i, c, tx, f);
         }
@@ -461,31 +494,42 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
   auto at = [&](int r) { return tile + r * pitch + c * ESIZE; };
   // the thread's pairs: its means, then the squares about them
   if (on) {
-    float mean[8], sq[8];
+    uint64_t sum2[4], sq2[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mean[j] = sq[j] = 0.f;
+    for (int j = 0; j < 4; ++j) sum2[j] = sq2[j] = 0ull;
 #pragma unroll 4
     for (int r = ty; r < n; r += o.down) {
       Eight<TYPE> e;
-      float f[8];
+      uint64_t f[4];
       e.load(at(r));
       e.widen(f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mean[j] += f[j];
+      for (int j = 0; j < 4; ++j) sum2[j] = f2_add(sum2[j], f[j]);
     }
     const int mine = rows.of(ty);
     const float inv = mine > 0 ? __fdividef(1.f, static_cast<float>(mine)) : 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mean[j] *= inv;
+    for (int j = 0; j < 4; ++j) sum2[j] = f2_mul(sum2[j], f2(-inv, -inv));
 #pragma unroll 4
     for (int r = ty; r < n; r += o.down) {
       Eight<TYPE> e;
-      float f[8];
+      uint64_t f[4];
       e.load(at(r));
       e.widen(f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sq[j] = fmaf(f[j] - mean[j], f[j] - mean[j], sq[j]);
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t d = f2_add(f[j], sum2[j]);
+        sq2[j] = f2_fma(d, d, sq2[j]);
+      }
     }
+    float mean[8], sq[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f2_split(sum2[j], mean[2 * j], mean[2 * j + 1]);
+      f2_split(sq2[j], sq[2 * j], sq[2 * j + 1]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mean[j] = -mean[j];
     leave_pairs(rows, p.per, tx, ty, mine, mean, sq, means, squares);
   }
   __syncthreads();
@@ -503,14 +547,8 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
       pairs, groups, o.parts, groups, p.per, [&](int k) { return max(0, min(p.rows, (k + 1) * o.chunk) - k * o.chunk); },
       [&](int g, Pair q) { stats[g] = {q.mean, rsqrtf(fmaf(q.sq, p.inv_count, p.eps))}; });
   __syncthreads();
-  float mean[8];
-  if (on)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const Pair q = stats[(c + j) / p.per];
-      mean[j] = q.mean;
-      a[j] *= q.sq;
-    }
+  Affine affine;
+  if (on) affine.set(a, b, p.per, c, [&](int g) { return stats[g]; });
   with_activation(p.act, [&](auto act) {
 #pragma unroll 1
     for (int r1 = ty; r1 - ty < n; r1 += 2 * o.down) {
@@ -521,17 +559,11 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
         const int r = r1 + u * o.down;
         const bool there = on && r < n;
         row[u] = there ? row0 + r : -1;
-        if (there) {
-          Eight<TYPE> e;
-          e.load(at(r));
-          e.widen(f[u]);
-        }
+        Eight<TYPE> e;
+        e.clear();
+        if (there) e.load(at(r));
+        affine.template apply<decltype(act)::value>(e, f[u]);
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (row[u] >= 0)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[u][j] = activation<decltype(act)::value>(fmaf(f[u][j] - mean[j], a[j], b[j]));
       put<2>(p, row, c0 + c, tx, f);
     }
   });
@@ -620,7 +652,8 @@ Two plan_two(const hilo_group_norm_shape& s, int most, int most_out) {
 }
 
 // As many chunks of statistics as the device holds at once: clusters do not fill its groups of SMs. (2^20 rows of
-// 128 channels in bf16: 155 us with the 432 that it holds in clusters of 4, 182 with 448; 164 with the 400 of clusters of 8.)
+// 128 channels in bf16: 155 us with the 432 that it holds in clusters of 4, 182 with 448; 164 with the 400 of clusters of 8; by
+// an earlier form of the loops.)
 template <int TYPE>
 int resident_chunks(int device, int num_sms) {
   static PerDevice clusters;
