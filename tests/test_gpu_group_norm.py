@@ -162,12 +162,13 @@ def test_group_norm_constant_and_eps(H):
     check(y, want, off, "f32")
 
 
-def test_group_norm_specials_stay_in_their_group(H):
-    p = Images(3, 500, 256, 16, "bf16", cond=False, weights=False)
-    p.buf[500 + 77, 40] = float("inf")
-    p.buf[1000 + 3, 255] = float("nan")
+@pytest.mark.parametrize("rows", [500, 40000])
+def test_group_norm_specials_stay_in_their_group(H, rows):
+    p = Images(3, rows, 256, 16, "bf16", cond=False, weights=False)
+    p.buf[rows + 77, 40] = float("inf")
+    p.buf[2 * rows + 3, 255] = float("nan")
     y, _ = p.run(H, "none", "f32")
-    bad = torch.isnan(y).view(3, 500, 16, 16)
+    bad = torch.isnan(y).view(3, rows, 16, 16)
     want = torch.zeros_like(bad)
     want[1, :, 2], want[2, :, 15] = True, True
     assert torch.equal(bad, want)
@@ -222,6 +223,57 @@ def test_group_norm_captured_and_on_two_streams(H, B, rows, d):
     graph.replay()
     torch.cuda.synchronize()
     assert not torch.equal(y, want)
+
+
+FIRST = r"""
+import torch
+from tests.gpu_helpers import lib_ready
+H = lib_ready()
+x = torch.randn(600, 256, device="cuda").bfloat16()
+big = torch.randn(60000, 256, device="cuda").bfloat16()
+w = torch.randn(512, 256, device="cuda").bfloat16()
+E = lambda *s, t=torch.uint8: torch.zeros(*s, dtype=t, device="cuda")
+codes, scale, wc, ws = E(600, 256), E(2, 600, t=torch.float32), E(512, 256), E(4, 2, t=torch.float32)
+h, hs, y = E(600, 256), E(2, 600, t=torch.float32), E(600, 512, t=torch.float32)
+z, work = torch.zeros_like(big), E(1 << 20)
+
+def norm(rows, src, dst, sc, out):
+    s = H.GroupNormShape(B=1, rows=rows, d=256, groups=16, act=H.HILO_ACT_SILU, y_dtype=out)
+    H.hilo_group_norm(s, None, src, dst, sc, work, H.hilo_group_norm_workspace_bytes(s))
+
+def step():
+    norm(60000, big, z, None, H.HILO_BF16)
+    norm(600, x, codes, scale, H.HILO_E4M3)
+    H.hilo_quantize_e4m3_128(H.Quant128Shape(rows=512, cols=256, tile=1), w, None, wc, ws)
+    up = H.Gemm128Shape(rows=600, k=256, n=256, act=H.HILO_ACT_GELU, out_dtype=H.HILO_E4M3)
+    H.hilo_gated_e4m3_128(up, codes, scale, wc, ws, wc[256:], ws[2:], None, None, None, h, hs)
+    for rows in (1, 600):
+        s = H.Gemm128Shape(rows=rows, k=256, n=512, out_dtype=H.HILO_F32, a_scale_ld=600)
+        H.hilo_gemm_e4m3_128(s, h, hs, wc, ws, None, None, y)
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    step()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (z, codes, scale, h, hs, y)]
+for t in (z, codes, scale, h, hs, y):
+    t.zero_()
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (z, codes, scale, h, hs, y))) and y.abs().max() > 0
+print("the same")
+"""
+
+
+def test_first_calls_inside_a_capture(H):
+    """A process whose very first calls are captured: nothing that they set up needs a stream."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "the same" in done.stdout, done.stderr[-3000:]
 
 
 def test_group_norm_into_a_product(H):
