@@ -168,6 +168,10 @@ __device__ __forceinline__ bool fill_scales(const ScaleRing& ring, uint32_t& n, 
   return true;
 }
 
+// The warp's number, known to be the same for its lanes: addresses in tensor memory and of barriers then take one register a
+// warp (8192 rows of 4096, 10240 features gated 619 us, 581 so; one row of 2048, 5504 features 7.3 and 6.9).
+__device__ __forceinline__ int one_warp() { return __shfl_sync(0xffffffffu, warp_id(), 0); }
+
 // Biases of features n and n + 1 (n even).
 __device__ __forceinline__ float2 bias2(const __nv_bfloat16* b, int n) {
   return make_float2(__bfloat162float(__ldg(b + n)), __bfloat162float(__ldg(b + n + 1)));
@@ -260,7 +264,7 @@ __global__ void __launch_bounds__(Few<NT, GATED>::THREADS, Few<NT, GATED>::CTAS)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* err = &g_gemm128_err;
-  const int warp = warp_id(), lane = lane_id();
+  const int warp = one_warp(), lane = lane_id();
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) {
@@ -571,9 +575,7 @@ struct Many {
   static constexpr int PARTS = NT == 192 ? 3 : 2, SPAN = NT / PARTS;
   static constexpr int COLS = SPAN / 4;              // of a warp, in each part
   static_assert(128 % SPAN == 0 && (!GATED || PARTS == 2), "a scale for each part");
-  // Columns read at a time, into one of two sets of registers. (Gated, with 16 the sums spill: 8192 rows of 4096, 10240
-  // features, 633 us, 613 so.)
-  static constexpr int LOAD = GATED ? 8 : 16;
+  static constexpr int LOAD = 16;                    // columns read at a time, into one of two sets of registers
   static constexpr int SLOT = 128 + 4;                      // floats of a block's scales: its rows', the weights' parts'
   static constexpr int SCALES_BYTES = SLOTS * SLOT * 4, MOST_BYTES = 4 * 128 * 4;  // [4][128] row maxima
   static constexpr int STAGES = (MANY_SMEM - 1024 - 384 - SCALES_BYTES - MOST_BYTES) / STAGE;
@@ -599,7 +601,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WHOLE_THREADS, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* err = &g_gemm128_err;
-  const int warp = warp_id(), lane = lane_id();
+  const int warp = one_warp(), lane = lane_id();
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
 
@@ -994,13 +996,13 @@ cudaError_t launch_many(const Gemm128Args& a, const Params128& p, int device, in
 // Which kernel, by its cost in microseconds. A launch is 2.2 of them; then
 //   few128<NT>    per wave of CTAs (as many as the device holds of clusters of `split`) an `each` and, per block of
 //                 128 along K, the longer of `block`, the chain from a block's copy to its sums, and of what the wave's CTAs
-//                 read of the weights at 8 to 9 TB/s (L2 and HBM)
+//                 read of the weights at 7 to 9 TB/s (L2 and HBM)
 //   many128<NT>   the first tile of a pair and each further one: an `each` and a `block` of their own (at full load
 //                 the chip is at its power limit)
-// from 143 shapes of 1 to 1024 rows, 1024 and 4096 columns, 1024 to 16384 features, each with every choice: its pick is 1.4%
-// behind the fastest in the mean, 26% at worst (64 rows of 4096, 1024 features gated: 9.1 us, 7.2 in four tiles of 16
-// rows). Examples, in us: 64 rows of 4096, 4096 features: few128<64> 7.3, many128<256> 17.6; 512 rows: few128<128>
-// 18.8, many128<128> 13.7, many128<256> 18.4; 1024 rows: many128<128> 23.3, many128<256> 19.6. 192 columns are for what
+// from 144 shapes of 1 to 1024 rows, 1024 and 4096 columns, 1024 to 16384 features, each with every choice: its pick is 1.0%
+// behind the fastest in the mean, 29% at worst (64 rows of 4096, 1024 features gated: 8.9 us, 6.9 in four tiles of 16
+// rows). Examples, in us: 64 rows of 4096, 4096 features: few128<64> 6.8, few128<16> 9.1; 512 rows: few128<128>
+// 17.2, many128<128> 13.0, many128<256> 18.0; 1024 rows: many128<128> 22.5, many128<256> 19.5. 192 columns are for what
 // fills a round with them and leaves a part of one idle with 256: 700 rows of 4096, 4096 features: 17.2, 128 columns 23.3,
 // 256 19.1; 2389 rows: 42.8, 51.6 and 49.6; 8192 rows: 131, 135 and 110. (Of 18 shapes with all three timed each pick was the
 // fastest.)
@@ -1013,9 +1015,9 @@ Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
   struct Cost {
     float each, block;
   };
-  constexpr Cost FEW[2][4] = {{{1.0f, .25f}, {1.5f, .275f}, {2.5f, .32f}, {3.8f, .36f}}, {{2.0f, .32f}, {2.7f, .36f}, {4.0f, .43f}, {6.0f, .73f}}};
-  constexpr Cost FIRST[2][3] = {{{2.1f, .265f}, {2.6f, .33f}, {3.1f, .39f}}, {{2.2f, .31f}, {}, {2.7f, .51f}}};
-  constexpr Cost NEXT[2][3] = {{{1.1f, .265f}, {1.4f, .35f}, {1.7f, .44f}}, {{1.1f, .25f}, {}, {1.4f, .49f}}};
+  constexpr Cost FEW[2][4] = {{{1.1f, .21f}, {1.85f, .215f}, {3.05f, .29f}, {3.25f, .385f}}, {{1.4f, .36f}, {2.6f, .36f}, {3.8f, .365f}, {6.0f, .675f}}};
+  constexpr Cost FIRST[2][3] = {{{2.1f, .245f}, {2.6f, .33f}, {3.1f, .405f}}, {{2.0f, .265f}, {}, {3.0f, .38f}}};
+  constexpr Cost NEXT[2][3] = {{{1.15f, .27f}, {1.95f, .345f}, {3.1f, .385f}}, {{.95f, .24f}, {}, {2.05f, .43f}}};
   constexpr int PARTS = GATED ? 2 : 1;
   auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
   Choice best = {1, 256, 1};
@@ -1035,9 +1037,9 @@ Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
       // (clusters stay within a group of SMs, whose number eight does not divide)
       const int held = per_sm * num_sms * (split <= 2 ? 38 : split == 4 ? 36 : per_sm == 2 ? 32 : 26) / 38;
       const long long ctas = tiles * split, waves = ceil_div(ctas, held);
-      const float reads = static_cast<float>(ctas < held ? ctas : held) * (PARTS * PIECE) / (row_tiles == 1 ? 9e6f : 8e6f);
+      const float reads = static_cast<float>(ctas < held ? ctas : held) * (PARTS * PIECE) / (row_tiles == 1 ? 7.4e6f : 9.3e6f);
       const Cost c = FEW[GATED][i];
-      offer(0.03f * split + static_cast<float>(waves) * (c.each + static_cast<float>(ceil_div(kblocks, split)) * (reads > c.block ? reads : c.block)),
+      offer(0.037f * split + static_cast<float>(waves) * (c.each + static_cast<float>(ceil_div(kblocks, split)) * (reads > c.block ? reads : c.block)),
             {0, nt, split});
     }
   }
