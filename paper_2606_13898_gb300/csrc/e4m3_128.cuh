@@ -22,13 +22,19 @@ constexpr int QBLOCK = 128;
 __device__ __forceinline__ void block_scale(float amax, float& inv, float& scale) {
   const float m = amax > 0.f ? fmaxf(amax, 0x1p-100f) : 448.f;
   inv = __fdiv_rn(448.f, m);
-  scale = __fdiv_rn(m, 448.f);
+  // m / 448 by Markstein's correction of a quotient within an ulp by its remainder, which is exact here (IBM J. Res. Dev. 34,
+  // 1990): correctly rounded, as 1 / 448 is. An infinity stays one.
+  constexpr float R = 1.f / 448.f;
+  const float q = __fmul_rn(m, R);
+  scale = m < INFINITY ? __fmaf_rn(__fmaf_rn(-448.f, q, m), R, q) : m;
 }
 
 // Eight codes of eight values.
 __device__ __forceinline__ uint2 block_codes(const float* f, float inv) {
-  return make_uint2(pack_e4m3x4(__fmul_rn(f[0], inv), __fmul_rn(f[1], inv), __fmul_rn(f[2], inv), __fmul_rn(f[3], inv)),
-                    pack_e4m3x4(__fmul_rn(f[4], inv), __fmul_rn(f[5], inv), __fmul_rn(f[6], inv), __fmul_rn(f[7], inv)));
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) f2_split(f2_mul(f2(f[i], f[i + 1]), f2(inv, inv)), v[i], v[i + 1]);
+  return make_uint2(pack_e4m3x4(v[0], v[1], v[2], v[3]), pack_e4m3x4(v[4], v[5], v[6], v[7]));
 }
 
 // Eight neighbouring elements in 16-byte aligned memory, as they are there (TYPE 0 bf16, 1 fp16, 2 fp32).

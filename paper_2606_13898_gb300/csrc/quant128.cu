@@ -5,8 +5,8 @@
 // the block being 128 columns of one row, or 128 rows x 128 columns.
 //
 // Bound by HBM: each element is read once, stays in registers for both the
-// maximum and the rounding, and leaves as one byte. Of bf16 nearly as much by the work of a block, of which the two
-// correctly rounded divisions are a third: 8192 rows of 4096 19.5 us (78% of a copy's rate), of fp32 26.6 (95%); one row 1.5.
+// maximum and the rounding, and leaves as one byte. Of bf16 nearly as much by the work of a block: 8192 rows of
+// 4096 18.8 us (81% of a copy's rate), of fp32 26.5 (95%); one row 1.3 to 1.5.
 #include "e4m3_128.cuh"
 #include "internal.h"
 
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(THREADS) quant128_rows_kernel(const __grid_con
 }
 
 // A scale per 128 rows x 128 columns: a CTA each, all of the tile in registers, three CTAs on an SM. (10240 rows of 4096 in
-// bf16 22.0 us, 5.7 TB/s; two 25.1, four as three, but of fp32 the tile spills: 32.6 us, four 41.6.)
+// bf16 21.6 us, 5.8 TB/s; two 25.1, four as three, but of fp32 the tile spills: 32.6 us, four 41.6.)
 template <int TYPE>
 __global__ void __launch_bounds__(THREADS, 3) quant128_tiles_kernel(const __grid_constant__ QuantParams p) {
   pdl_wait();

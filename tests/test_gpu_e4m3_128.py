@@ -110,6 +110,19 @@ def test_quantise_bit_for_bit(H, dtype, rows, cols, pad, dpad, spare, ld, tile):
     assert (dst[rows:] == 0x55).all() and (dst[:, cols:] == 0x55).all()
 
 
+def test_scales_of_every_mantissa(H):
+    """amax / 448 is correctly rounded: all 2^23 mantissas of an fp32, each at one of 200 exponents."""
+    rows = 1 << 23
+    at = torch.arange(rows, device="cuda", dtype=torch.int32)
+    amax = ((at % 200 + 27) << 23 | at).view(torch.float32)  # from 2^-100
+    x = torch.zeros(rows, 16, device="cuda")
+    x[:, 3] = -amax
+    codes, scale = torch.empty(rows, 16, dtype=torch.uint8, device="cuda"), torch.empty(1, rows, device="cuda")
+    H.hilo_quantize_e4m3_128(H.Quant128Shape(rows=rows, cols=16, dtype=H.HILO_F32), x, None, codes, scale)
+    assert torch.equal(scale[0], amax / torch.full((), 448.0, device="cuda"))
+    assert (codes[:, 3] == 0xFE).all() and (codes[:, :3] == 0).all()
+
+
 @pytest.mark.parametrize("n", [-3, 0, 2, 7, 9, 100])
 @pytest.mark.parametrize("tile", [0, 1])
 def test_quantise_counts_rows_on_the_device(H, n, tile):
