@@ -15,7 +15,7 @@
 // the passes over shared memory and the activation, not by HBM (2 TB/s).
 //
 // Other images: two kernels over chunks of rows. The first leaves the pairs of each cluster's chunks in the workspace, the
-// second joins an image's pairs and writes its chunk, from the last row to the first, as the rows read last are the
+// second joins an image's pairs (of many groups a third kernel between the two does) and writes its chunk, from the last row to the first, as the rows read last are the
 // ones still in L2. Bound by HBM: x is read once, and again as far as it is not in L2, y is written once; 2^20 rows of 128
 // channels in bf16 take 144 us, 5.6 TB/s of three passes (with half as many fp32 instructions as one for each value: pairs in
 // 64-bit registers, full batches without predicates; 152 us with them).
@@ -32,7 +32,8 @@ struct NormParams {
   const unsigned char* x;
   void* y;
   float* y_scale;
-  float2* part;  // [image][group][cluster of chunks]: mean, sum of squares about it
+  float2* part;    // [image][group][cluster of chunks]: mean, sum of squares about it
+  float2* joined;  // [image][group]: mean, 1 / deviation
   const void *scale, *shift, *w, *b;
   long long x_row, y_row, vec_row, y_scale_ld;  // x_row in bytes
   int rows, d, groups, per, act;                // per: channels of a group
@@ -354,41 +355,57 @@ __global__ void __launch_bounds__(THREADS, STATS_CTAS) group_stats_kernel(const 
       });
 }
 
+// A group's mean and 1 / deviation from the pairs of its image's clusters, by a warp, the lanes' pairs in registers.
+__device__ __forceinline__ Pair join_image(const NormParams& p, const Two& o, long long group, int lane) {
+  const float2* part = p.part + group * o.clusters;
+  const long long each = static_cast<long long>(CHUNKS) * o.chunk;
+  auto rows_of = [&](int k) { return static_cast<float>(min(static_cast<long long>(p.rows), (k + 1) * each) - k * each); };
+  float2 q[JOINED];
+  float sum = 0.f, sq = 0.f;
+#pragma unroll
+  for (int i = 0; i < JOINED; ++i) {
+    q[i] = make_float2(0.f, 0.f);
+    if (32 * i + lane < o.clusters) q[i] = __ldg(part + 32 * i + lane);
+  }
+#pragma unroll
+  for (int i = 0; i < JOINED; ++i)
+    if (32 * i + lane < o.clusters) sum = fmaf(rows_of(32 * i + lane), q[i].x, sum);
+  const float mean = warp_sum(sum) * p.inv_rows;
+#pragma unroll
+  for (int i = 0; i < JOINED; ++i)
+    if (32 * i + lane < o.clusters)
+      sq += fmaf(rows_of(32 * i + lane) * static_cast<float>(p.per) * (q[i].x - mean), q[i].x - mean, q[i].y);
+  const float var = warp_sum(sq) * p.inv_count;
+  return {mean, rsqrtf(var + p.eps)};
+}
+
+// More groups than FEW_GROUPS get a warp each in a kernel of their own; few ones each CTA of the output joins for itself.
+// (65536 rows of 512, in us, for itself and by the kernel: 32 groups 43.0 and 47.0, 64 groups 45.5 and 46.3, 128 groups 51.6 and
+// 50.2, 512 groups 81.8 and 56.1; 16384 rows of 2048 channels, a group each, 218 and 79.)
+constexpr int FEW_GROUPS = 64;
+__global__ void __launch_bounds__(THREADS) group_join_kernel(const __grid_constant__ NormParams p, const __grid_constant__ Two o, long long groups) {
+  pdl_wait();
+  pdl_trigger();
+  const long long g = static_cast<long long>(blockIdx.x) * (THREADS / 32) + warp_id();
+  if (g >= groups) return;
+  const Pair q = join_image(p, o, g, lane_id());
+  if (lane_id() == 0) p.joined[g] = make_float2(q.mean, q.sq);
+}
+
 template <int TYPE>
 __global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const __grid_constant__ NormParams p, const __grid_constant__ Two o) {
-  extern __shared__ float shared[];  // [groups] means, then [groups] 1 / deviation
+  __shared__ Pair stats[FEW_GROUPS];  // means and 1 / deviation
   pdl_wait();
   pdl_trigger();
   const int image = blockIdx.x / o.out_chunks, r0 = (blockIdx.x - image * o.out_chunks) * o.out_chunk;
   const int n = min(p.rows, r0 + o.out_chunk) - r0;
-  float* means = shared;
-  float* invs = shared + p.groups;
-  // the image's pairs, a warp per group, the lanes' in registers
-  const int lane = lane_id();
+  const long long group0 = static_cast<long long>(image) * p.groups;
+  if (p.groups <= FEW_GROUPS) {
+    const int lane = lane_id();
 #pragma unroll 2
-  for (int g = warp_id(); g < p.groups; g += THREADS / 32) {
-    const float2* part = p.part + (static_cast<long long>(image) * p.groups + g) * o.clusters;
-    const long long each = static_cast<long long>(CHUNKS) * o.chunk;
-    auto rows_of = [&](int k) { return static_cast<float>(min(static_cast<long long>(p.rows), (k + 1) * each) - k * each); };
-    float2 q[JOINED];
-    float sum = 0.f, sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < JOINED; ++i) {
-      q[i] = make_float2(0.f, 0.f);
-      if (32 * i + lane < o.clusters) q[i] = __ldg(part + 32 * i + lane);
-    }
-#pragma unroll
-    for (int i = 0; i < JOINED; ++i)
-      if (32 * i + lane < o.clusters) sum = fmaf(rows_of(32 * i + lane), q[i].x, sum);
-    const float mean = warp_sum(sum) * p.inv_rows;
-#pragma unroll
-    for (int i = 0; i < JOINED; ++i)
-      if (32 * i + lane < o.clusters)
-        sq += fmaf(rows_of(32 * i + lane) * static_cast<float>(p.per) * (q[i].x - mean), q[i].x - mean, q[i].y);
-    const float var = warp_sum(sq) * p.inv_count;
-    if (lane == 0) {
-      means[g] = mean;
-      invs[g] = rsqrtf(var + p.eps);
+    for (int g = warp_id(); g < p.groups; g += THREADS / 32) {
+      const Pair q = join_image(p, o, group0 + g, lane);
+      if (lane == 0) stats[g] = q;
     }
   }
   __syncthreads();
@@ -400,7 +417,12 @@ __global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const 
     const int c = (tx + pass * o.across) * 8;
     const bool in = c < p.d && ty < o.down;
     Affine affine;
-    if (in) affine.set(p, image, c, c, [&](int g) { return Pair{means[g], invs[g]}; });
+    if (in)
+      affine.set(p, image, c, c, [&](int g) {
+        if (p.groups <= FEW_GROUPS) return stats[g];
+        const float2 q = p.joined[group0 + g];
+        return Pair{q.x, q.y};
+      });
     const int steps = (n + o.down - 1) / o.down;
     with_activation(p.act, [&](auto act) {
       for (int s = (steps - 1) / BATCH; s >= 0; --s) {
@@ -692,12 +714,15 @@ cudaError_t launch_two(const hilo_group_norm_shape& s, const NormParams& p, int 
   e = launch_pdl_cluster(kern, CHUNKS, dim3(static_cast<unsigned>(o.chunks) * static_cast<unsigned>(s.B)), dim3(THREADS), stats, st, p, o);
   if (e != cudaSuccess) return e;
   *launches = 1;
-  auto* apply = group_apply_kernel<TYPE>;
-  e = cudaFuncSetAttribute(apply, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024);
-  if (e != cudaSuccess) return e;
-  e = launch_pdl(apply, dim3(static_cast<unsigned>(o.out_chunks) * static_cast<unsigned>(s.B)), dim3(THREADS),
-                 static_cast<size_t>(p.groups) * 2 * sizeof(float), st, p, o);
-  if (e == cudaSuccess) *launches = 2;
+  if (s.groups > FEW_GROUPS) {
+    const long long groups = static_cast<long long>(s.B) * s.groups, ctas = (groups + THREADS / 32 - 1) / (THREADS / 32);
+    if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
+    e = launch_pdl(group_join_kernel, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), 0, st, p, o, groups);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  e = launch_pdl(group_apply_kernel<TYPE>, dim3(static_cast<unsigned>(o.out_chunks) * static_cast<unsigned>(s.B)), dim3(THREADS), 0, st, p, o);
+  if (e == cudaSuccess) ++*launches;
   return e;
 }
 
@@ -710,7 +735,7 @@ cudaError_t launch_type(const hilo_group_norm_shape& s, const NormParams& p, int
 }  // namespace
 
 size_t group_norm_workspace_bytes(const hilo_group_norm_shape& s) {
-  return static_cast<size_t>(s.B) * plan_two(s, MAX_CHUNKS, 1).clusters * s.groups * sizeof(float2);
+  return static_cast<size_t>(s.B) * (plan_two(s, MAX_CHUNKS, 1).clusters + (s.groups > FEW_GROUPS ? 1 : 0)) * s.groups * sizeof(float2);
 }
 
 cudaError_t launch_group_norm(const GroupNormArgs& a, int device, int num_sms, int* launches, cudaStream_t st) {
@@ -720,7 +745,8 @@ cudaError_t launch_group_norm(const GroupNormArgs& a, int device, int num_sms, i
   p.x = static_cast<const unsigned char*>(a.x);
   p.y = a.y;
   p.y_scale = a.y_scale;
-  p.part = static_cast<float2*>(a.ws);
+  p.joined = static_cast<float2*>(a.ws);
+  p.part = p.joined + (s.groups > FEW_GROUPS ? static_cast<long long>(s.B) * s.groups : 0);
   p.scale = a.vec.scale;
   p.shift = a.vec.shift;
   p.w = a.vec.w_norm;

@@ -100,7 +100,8 @@ class Images:
 SIZES = [(1, 1, 16, 1), (1, 1, 128, 32), (2, 3, 128, 32), (1, 7, 144, 36), (3, 17, 320, 32), (1, 64, 512, 32), (2, 333, 256, 8),
          (1, 1024, 512, 32), (3, 1380, 1152, 36), (1, 900, 2048, 32), (2, 100, 4096, 32), (1, 77, 8192, 16), (1, 50, 4112, 257),
          (5, 4, 48, 48), (1, 20000, 128, 32), (1, 5000, 640, 1), (70, 40, 64, 4), (1, 65536, 64, 8), (1, 9000, 8192, 8192), (2, 3000, 4112, 257),
-         (1, 70000, 320, 32), (3, 30001, 144, 36), (500, 9, 2048, 32)]
+         (1, 70000, 320, 32), (3, 30001, 144, 36), (500, 9, 2048, 32), (2, 20000, 512, 512),
+         (1, 7000, 2048, 128), (1, 16384, 512, 64)]
 
 
 @pytest.mark.parametrize("B,rows,d,groups", SIZES)
