@@ -11,7 +11,7 @@
 // Images whose slices of channels (whole groups) fit the shared memory of a cluster: one kernel
 // (group_norm_kernel). A CTA copies its rows of the slice by TMA, finds each group's mean and the squares about it in two
 // passes over them, tells the cluster's other CTAs, and writes. x is read once. 1024 rows of 512 channels take 5.2 us
-// (two kernels: 9.0): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
+// (two kernels: 8.3): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
 // the passes over shared memory and the activation, not by HBM (2 TB/s).
 //
 // Other images: two kernels over chunks of rows. The first leaves the pairs of each cluster's chunks in the workspace, the
@@ -203,17 +203,17 @@ __device__ __forceinline__ void join_groups(const Rows& o, int groups, float inv
   }
 }
 
-// The pairs of a cluster's CTAs, [CTA][pitch groups], joined by eight lanes a group, to use(group, pair); rows_of(k): rows of
+// The pairs of a cluster's CTAs, [CTA][pitch groups], joined by LANES lanes a group, to use(group, pair); rows_of(k): rows of
 // CTA k.
-template <typename RowsOf, typename Use>
+template <int LANES, typename RowsOf, typename Use>
 __device__ __forceinline__ void join_cluster(const Pair* pairs, int pitch, int parts, int groups, int per, RowsOf rows_of, Use use) {
-  const int k = threadIdx.x & 7, threads = blockDim.x;
-  for (int g0 = 0; g0 < groups; g0 += threads >> 3) {
-    const int g = g0 + (threadIdx.x >> 3);
+  const int k = threadIdx.x & (LANES - 1), threads = blockDim.x;
+  for (int g0 = 0; g0 < groups; g0 += threads / LANES) {
+    const int g = g0 + threadIdx.x / LANES;
     const float m = g < groups && k < parts ? static_cast<float>(rows_of(k)) : 0.f;
     const Pair q = m > 0.f ? pairs[k * pitch + g] : Pair{0.f, 0.f};
-    const float rows = lanes_sum(m, 8), mean = lanes_sum(m * q.mean, 8) * (rows > 0.f ? __fdividef(1.f, rows) : 0.f);
-    const float sq = lanes_sum(m > 0.f ? fmaf(m * static_cast<float>(per) * (q.mean - mean), q.mean - mean, q.sq) : 0.f, 8);
+    const float rows = lanes_sum(m, LANES), mean = lanes_sum(m * q.mean, LANES) * (rows > 0.f ? __fdividef(1.f, rows) : 0.f);
+    const float sq = lanes_sum(m > 0.f ? fmaf(m * static_cast<float>(per) * (q.mean - mean), q.mean - mean, q.sq) : 0.f, LANES);
     if (g < groups && k == 0) use(g, Pair{mean, sq});
   }
 }
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(THREADS, STATS_CTAS) group_stats_kernel(const 
                    : "memory");
   });
   cluster_sync();
-  join_cluster(
+  join_cluster<CHUNKS>(
       pairs, pitch, CHUNKS, (p.groups - rank + CHUNKS - 1) / CHUNKS, p.per,
       [&](int k) { return max(0, min(p.rows, first + (k + 1) * o.chunk) - (first + k * o.chunk)); },
       [&](int i, Pair q) {
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(THREADS, APPLY_CTAS) group_apply_kernel(const 
 // ------------------------------------------------------------------ one kernel --
 
 constexpr int ONE_THREADS = 256;
-constexpr int ONE_PARTS = 8;          // CTAs of a cluster at most (four: 3 x 1380 rows of 1152 channels 17.7 us, 14.7 with eight)
+constexpr int ONE_PARTS = 16;         // CTAs of a cluster at most
 constexpr int ONE_SMEM = 112 * 1024;  // shared memory of a CTA at most: two on an SM (220 KB and one: 4 x 4096 rows of 512 35 us, else 21)
 constexpr int ONE_LEAST = 76 * 1024;  // and at least: three on some SMs and one on others take longer (3 x 1380 rows of 1152: 14.8 us, else 11.6)
 constexpr int ONE_WIDE = 256;         // channels of a slice at most, and rows of a box (TMA)
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
   });
   if (o.parts > 1) cluster_sync();
   else __syncthreads();
-  join_cluster(
+  join_cluster<ONE_PARTS>(
       pairs, groups, o.parts, groups, p.per, [&](int k) { return max(0, min(p.rows, (k + 1) * o.chunk) - k * o.chunk); },
       [&](int g, Pair q) { stats[g] = {q.mean, rsqrtf(fmaf(q.sq, p.inv_count, p.eps))}; });
   __syncthreads();
@@ -591,20 +591,56 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
   });
 }
 
-// The cheapest way to share an image out: by waves of CTAs, 2.5 us each beside what a CTA reads and writes at its part of
-// shared memory's rate, by CTAs of a cluster and by entries that a lane joins. Fitted to 25 shapes of 22 to 7229 rows, 32 to
-// 2304 channels in every slice and number of parts: its pick is 3% behind the fastest in the mean, 22% at worst; 15 other
-// shapes: 3%, 9%. False where no slice fits: two kernels, which took 1.1 to 2.8 times as long wherever one fits (1024 rows of
-// 512: 9.0 us, else 5.2; 32 x 256 rows of 2048: 28.6, else 26.0).
-bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
+// How many clusters of so many CTAs the device holds, two CTAs on an SM: sizes above eight fill its groups of SMs badly or well.
+template <int TYPE>
+int resident_clusters(int parts, int device, int num_sms) {
+  static PerDevice known[ONE_PARTS + 1];
+  const int n = known[parts].get(device, [&] {
+    if (parts > 8 && cudaFuncSetAttribute(group_norm_kernel<TYPE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    cudaFuncSetAttribute(group_norm_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE_SMEM);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(parts * num_sms, 1, 1);
+    cfg.blockDim = dim3(ONE_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = ONE_SMEM;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = parts;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int found = 0;
+    if (cudaOccupancyMaxActiveClusters(&found, group_norm_kernel<TYPE>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      found = 0;
+    }
+    return found;
+  });
+  return n > 0 ? n : parts > 8 ? 0 : num_sms / 8;  // 0: none of this size
+}
+
+// The cheapest way to share an image out, and its cost in us: by waves of clusters, 2.9 us each beside an element's work and
+// a byte's way, more by CTAs of a cluster and by entries that a lane joins. Against the two kernels' 8.2 us and 1.2 for a
+// million elements. Fitted to 34 shapes of 22 to 65536 rows, 32 to 2304 channels in every slice and number of parts: the pick
+// is 1.6% behind the fastest in the mean, 18% at worst (8 x 82 rows of 2048 6.6 us, 5.6 in wider slices). Examples, in us:
+// 1024 rows of 512 5.2, two kernels 8.3; 3 x 1380 rows of 1152 to codes 10.0 in 10 parts, 11.6 in 8, two kernels 17.6; 16384
+// rows of 512 15.4 in 13 parts, 19.8 in 16 (two waves), two kernels 19.0; 4 x 4096 rows of 512 to codes 20.7, two kernels 18.5.
+constexpr float NO_PLAN = 3e38f;
+template <int TYPE>
+float plan_one(const hilo_group_norm_shape& s, int device, int num_sms, One* best) {
   const int per = s.d / s.groups, esize = s.x_dtype == HILO_F32 ? 4 : 2;
-  if (s.x_row * esize >= (1LL << 40)) return false;  // (TMA's strides)
+  if (s.x_row * esize >= (1LL << 40)) return NO_PLAN;  // (TMA's strides)
   // whole groups, whole vectors, and of codes whole blocks
   int unit = per;
   while (unit % 8) unit += per;
   if (s.y_dtype == HILO_E4M3 && s.d > 128)
     while (unit % 128 && unit < s.d) unit += per;
-  float least = 3e38f;
+  int held[ONE_PARTS + 1];
+  for (int parts = 1; parts <= ONE_PARTS; ++parts) held[parts] = resident_clusters<TYPE>(parts, device, num_sms);
+  float least = NO_PLAN;
   for (int wide = unit; wide <= ONE_WIDE && wide < s.d + unit; wide += unit) {
     const int w = wide < s.d ? wide : s.d;
     if (w > ONE_WIDE || (w * esize < 64 && w < s.d)) continue;
@@ -614,14 +650,16 @@ bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
     const int groups = w / per, down = ONE_THREADS / across, lanes = lanes_of(groups, ONE_THREADS);
     const int entries = (down * (per % 8 == 0 ? per / 8 : per) + lanes - 1) / lanes;  // of a lane, a group
     const int joined = entries * ((groups * lanes + ONE_THREADS - 1) / ONE_THREADS);
-    const long long slices = (s.d + w - 1) / w, each = s.B * slices;
+    const long long slices = (s.d + w - 1) / w, clusters = s.B * slices;
     for (int parts = 1; parts <= ONE_PARTS && parts <= (s.rows > 1 ? s.rows : 1); ++parts) {
+      const float fixed = 0.15f * static_cast<float>(parts) + 0.16f * static_cast<float>(joined);
+      if (2.9f + fixed >= least) break;
       const int chunk = (s.rows + parts - 1) / parts;
-      const long long ctas = each * parts, bytes = static_cast<long long>(chunk) * w * esize;
-      if (ctas > 0x7fffffffLL || bytes > ONE_SMEM) continue;
-      const long long waves = ctas <= 2 * num_sms ? 1 : (ctas + 2 * num_sms - 1) / (2 * num_sms);
-      const float cost = static_cast<float>(waves) * (2.5f + static_cast<float>(bytes) * (1 / 8e3f)) + 0.2f * static_cast<float>(parts) +
-                         0.3f * static_cast<float>(joined);
+      const long long ctas = clusters * parts, bytes = static_cast<long long>(chunk) * w * esize;
+      if (ctas > 0x7fffffffLL || bytes > ONE_SMEM || held[parts] == 0) continue;
+      const long long waves = clusters <= held[parts] ? 1 : (clusters + held[parts] - 1) / held[parts];
+      const float work = (0.064e-3f / static_cast<float>(esize) + 0.047e-3f) * static_cast<float>(bytes);
+      const float cost = static_cast<float>(waves) * (2.9f + work * (ctas > num_sms ? 1.26f : 1.f)) + fixed;
       if (!(cost < least)) continue;
       int box = (chunk + 7) / 8 * 8;
       if (box > ONE_WIDE) box = ONE_WIDE;
@@ -632,7 +670,7 @@ bool plan_one(const hilo_group_norm_shape& s, int num_sms, One* best) {
       *best = one;
     }
   }
-  return least < 3e38f;
+  return least;
 }
 
 template <int TYPE>
@@ -645,6 +683,7 @@ cudaError_t launch_one(const hilo_group_norm_shape& s, const NormParams& p, cons
   auto* kern = group_norm_kernel<TYPE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE_SMEM);
   if (e != cudaSuccess) return e;
+  if (o.parts > 8 && (e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
   e = launch_pdl_cluster(kern, o.parts, dim3(static_cast<unsigned>(s.B) * o.slices * o.parts), dim3(ONE_THREADS),
                          static_cast<size_t>(o.smem() > ONE_LEAST ? o.smem() : ONE_LEAST), st, tm, p, o);
   if (e == cudaSuccess) *launches = 1;
@@ -729,7 +768,8 @@ cudaError_t launch_two(const hilo_group_norm_shape& s, const NormParams& p, int 
 template <int TYPE>
 cudaError_t launch_type(const hilo_group_norm_shape& s, const NormParams& p, int device, int num_sms, int* launches, cudaStream_t st) {
   One o;
-  return plan_one(s, num_sms, &o) ? launch_one<TYPE>(s, p, o, launches, st) : launch_two<TYPE>(s, p, device, num_sms, launches, st);
+  const float two = 8.2f + 1.2e-6f * static_cast<float>(s.B) * static_cast<float>(s.rows) * static_cast<float>(s.d);
+  return plan_one<TYPE>(s, device, num_sms, &o) < two ? launch_one<TYPE>(s, p, o, launches, st) : launch_two<TYPE>(s, p, device, num_sms, launches, st);
 }
 
 }  // namespace
