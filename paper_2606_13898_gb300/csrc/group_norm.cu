@@ -288,7 +288,8 @@ __global__ void __launch_bounds__(THREADS, STATS_CTAS) group_stats_kernel(const 
       const uint64_t gap = f2_add(mean2[j], minus);
       const float scale = part * static_cast<float>(n);
       mean2[j] = f2_fma(gap, f2(-part, -part), mean2[j]);
-      sq2[j] = f2_add(sq2[j], f2_fma(f2_mul(gap, gap), f2(scale, scale), two));
+      // (the scale first: of the thread's first rows it is 0, and the gap all of their mean, whose square may leave fp32)
+      sq2[j] = f2_add(sq2[j], f2_fma(f2_mul(gap, f2(scale, scale)), gap, two));
     };
     int r = ty;
     for (; r + (BATCH - 1) * o.down < rows.n; r += BATCH * o.down) {
