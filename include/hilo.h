@@ -855,9 +855,11 @@ size_t hilo_group_norm_workspace_bytes(const hilo_group_norm_shape* shape);
  *            nothing in it has to be set. Calls that may overlap on the device
  *            need workspaces of their own.
  * Statistics are fp32: means and squares about them, joined pairwise in a fixed
- * order, so that an offset far above the deviation costs no more than its own
- * rounding. A call repeats itself bit for bit. A NaN or an infinity leaves its
- * image's group NaN.
+ * order. A mean is off by some roundings of the group's largest magnitude, 2^-24 of
+ * it each; of equal values it is that value, and y what the vectors make of 0. What a
+ * group's magnitudes, and its squares about the mean, add up to must be in fp32's
+ * range. A call repeats itself bit for bit. A NaN or an infinity leaves its image's
+ * group NaN.
  */
 int hilo_group_norm(const hilo_group_norm_shape* shape, const hilo_norm_vectors* vectors, const void* x, void* y,
                     float* y_scale, void* ws, size_t ws_bytes, void* stream);
