@@ -817,9 +817,10 @@ int hilo_gated_e4m3_128(const hilo_gemm128_shape* shape, const uint8_t* a, const
 /*
  * Images of hilo_group_norm: B images of `rows` positions (H * W, raster order),
  * d channels each, channels last; image b owns rows b * rows .. of x and y.
- *   B, rows     B >= 1, rows >= 0, B * rows at most 2^30
+ *   B, rows     B 1 to 2^29 - 1, rows >= 0, B * rows at most 2^30
  *   d           a positive multiple of 16, at most 8192
- *   groups      divides d; group g has channels g * d / groups ..
+ *   groups      divides d; group g has channels g * d / groups ..; B * groups at
+ *               most 2^33
  *   act         HILO_ACT_*
  *   x_dtype     HILO_BF16, HILO_F16 or HILO_F32; y_dtype these (HILO_F16
  *               saturating) or HILO_E4M3; vec_dtype HILO_BF16 or HILO_F32

@@ -1067,11 +1067,15 @@ int hilo_gated_e4m3_128(const hilo_gemm128_shape* s, const uint8_t* a, const flo
 
 static int check_group_norm(const hilo_group_norm_shape* s) {
   if (!s) return fail(HILO_ERR_ARG, "hilo_group_norm: shape is NULL");
-  if (s->B < 1 || s->rows < 0 || static_cast<int64_t>(s->B) * s->rows > (1 << 30))
-    return fail(HILO_ERR_SHAPE, "hilo_group_norm: B=%d must be >= 1, rows=%d >= 0, B * rows at most 2^30", s->B, s->rows);
+  // (a grid's size is an int, and an image takes four CTAs at least where two kernels share it out)
+  if (s->B < 1 || s->B >= 1 << 29 || s->rows < 0 || static_cast<int64_t>(s->B) * s->rows > (1 << 30))
+    return fail(HILO_ERR_SHAPE, "hilo_group_norm: B=%d must be in [1, 2^29), rows=%d >= 0, B * rows at most 2^30", s->B, s->rows);
   if (s->d < 16 || s->d % 16 || s->d > 8192)
     return fail(HILO_ERR_SHAPE, "hilo_group_norm: d=%d must be a multiple of 16 in [16, 8192]", s->d);
   if (s->groups < 1 || s->d % s->groups) return fail(HILO_ERR_SHAPE, "hilo_group_norm: groups=%d must divide d=%d", s->groups, s->d);
+  // (likewise: a warp each joins the groups' pairs)
+  if (static_cast<int64_t>(s->B) * s->groups > (1LL << 33))
+    return fail(HILO_ERR_SHAPE, "hilo_group_norm: B=%d times groups=%d must be at most 2^33", s->B, s->groups);
   if (s->act != HILO_ACT_NONE && s->act != HILO_ACT_SILU && s->act != HILO_ACT_GELU)
     return fail(HILO_ERR_ARG, "hilo_group_norm: act=%d", s->act);
   if ((!is_bf16_or_f32(s->x_dtype) && s->x_dtype != HILO_F16) ||

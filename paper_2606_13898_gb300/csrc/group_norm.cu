@@ -771,7 +771,7 @@ cudaError_t launch_two(const hilo_group_norm_shape& s, const NormParams& p, int 
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
   if (e != cudaSuccess) return e;
   const Two o = plan_two(s, resident_chunks<TYPE>(device, num_sms), APPLY_CTAS * num_sms);
-  if (static_cast<long long>(o.chunks) * s.B > 0x7fffffffLL) return cudaErrorInvalidValue;
+  // (o.chunks is at most what the device holds over B, or CHUNKS: with B below 2^29 the grids are ints)
   const size_t stats = static_cast<size_t>(o.down) * 2 * sizeof(float) * (p.per % 8 == 0 ? o.across * o.passes : s.d) +
                        static_cast<size_t>(s.groups + CHUNKS) * sizeof(Pair);
   e = launch_pdl_cluster(kern, CHUNKS, dim3(static_cast<unsigned>(o.chunks) * static_cast<unsigned>(s.B)), dim3(THREADS), stats, st, p, o);
@@ -779,7 +779,6 @@ cudaError_t launch_two(const hilo_group_norm_shape& s, const NormParams& p, int 
   *launches = 1;
   if (s.groups > FEW_GROUPS) {
     const long long groups = static_cast<long long>(s.B) * s.groups, ctas = (groups + THREADS / 32 - 1) / (THREADS / 32);
-    if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
     e = launch_pdl(group_join_kernel, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), 0, st, p, o, groups);
     if (e != cudaSuccess) return e;
     ++*launches;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from .gpu_helpers import lib_ready
-from .test_gpu_e4m3_128 import check
+from .test_gpu_e4m3_128 import check, check_codes
 from .test_gpu_group_norm import Images, rng
 
 pytestmark = pytest.mark.gpu
@@ -87,3 +87,15 @@ def test_an_offset_costs_its_roundings(H, rows, d, groups, offset):
     want = (x - mean) / root
     off = off_mean / root + want.abs() * rel + off_mean / root * rel
     check(y.view_as(x), want, off, "f32")
+
+
+@pytest.mark.parametrize("B,rows,d,groups,out", [(100003, 16, 64, 4, "f32"), (70001, 1, 16, 1, "e4m3"), (300000, 3, 32, 8, "bf16"),
+                                                 (2000, 40, 1024, 256, "f32")])
+def test_very_many_images(H, B, rows, d, groups, out):
+    p = Images(B, rows, d, groups, "bf16")
+    y, sc = p.run(H, "silu", out)
+    want, off = p.exact("silu", 1e-5)
+    if out == "e4m3":
+        check_codes(y, sc, want, off)
+    else:
+        check(y, want, off, out)
