@@ -9,7 +9,7 @@
 // tcgen05.mma kind::f8f6f4) in a tensor memory buffer of its own, and other warps add it, scaled, to sums
 // in their registers while the next block's is formed. The codes' products are exact in fp32.
 //
-// Two kernels, chosen by cost (choose):
+// Two kernels, chosen by cost (gemm128_choice.h):
 //   few128   few rows: features on the lanes (M), rows on the columns (N = NT). A CTA has 128 features; a cluster of up
 //            to eight shares them along K and adds its sums up through distributed shared memory in a fixed order.
 //            Bound by reading the weights, and for small ones by a launch and the chain first copy, product, sums,
@@ -27,6 +27,7 @@
 #include "attn_common.cuh"
 #include "common.cuh"
 #include "e4m3_128.cuh"
+#include "gemm128_choice.h"
 #include "internal.h"
 
 namespace hilo {
@@ -36,7 +37,7 @@ __device__ int g_gemm128_err;
 namespace {
 
 constexpr int BK = 128;  // K of a stage: a block, a 128-byte swizzled row
-constexpr int PIECE = 128 * BK;  // bytes of 128 rows of a stage
+constexpr int PIECE = GEMM128_PIECE;  // bytes of 128 rows of a stage
 
 struct Params128 {
   const float* a_scale;      // [k / 128][a_scale_ld]
@@ -217,8 +218,6 @@ constexpr int SPLIT_REGS = 32 * SUM_WARPS * SUM_REGS + 128 * CONTROL_REGS;  // w
 static_assert(SPLIT_REGS <= 65536, "registers of an SM");
 
 // ------------------------------------------------------------------- few rows --
-
-constexpr int FEW_SPLIT = 8;  // CTAs of a cluster at most
 
 template <int NT, bool GATED>
 struct Few {
@@ -993,71 +992,9 @@ cudaError_t launch_many(const Gemm128Args& a, const Params128& p, int device, in
                             st, ta, tw[0], tw[1], p);
 }
 
-// Which kernel, by its cost in microseconds. A launch is 2.2 of them; then
-//   few128<NT>    per wave of CTAs (as many as the device holds of clusters of `split`) an `each` and, per block of
-//                 128 along K, the longer of `block`, the chain from a block's copy to its sums, and of what the wave's CTAs
-//                 read of the weights at 8 TB/s (L2 and HBM)
-//   many128<NT>   the first tile of a pair and each further one: an `each` and a `block` of their own (at full load
-//                 the chip is at its power limit)
-// fitted to 252 shapes of 1 to 8192 rows, 512 to 6080 columns, 128 to 16384 features, each with every choice: its pick is 0.5%
-// behind the fastest in the mean, 29% at worst (64 rows of 4096, 1024 features gated: 8.8 us, 6.9 in four tiles of 16
-// rows). Examples, in us: 64 rows of 4096, 4096 features: few128<64> 6.8, few128<16> 9.1; 512 rows: few128<128>
-// 17.2, many128<128> 13.0, many128<256> 18.0; 1024 rows: many128<128> 22.5, many128<256> 19.5; 1300 rows of 6080, 512
-// features: few128<128> 13.9, many128<128> 15.8. 192 columns are for what
-// fills a round with them and leaves a part of one idle with 256: 700 rows of 4096, 4096 features: 17.2, 128 columns 23.3,
-// 256 19.1; 2389 rows: 42.8, 51.6 and 49.6; 8192 rows: 131, 135 and 110. (Of 18 shapes with all three timed each pick was the
-// fastest.)
-struct Choice {
-  int many;  // few128 otherwise
-  int nt, split;
-};
-template <bool GATED>
-Choice choose(int rows, int n, int kblocks, bool codes, int num_sms) {
-  struct Cost {
-    float each, block;
-  };
-  constexpr Cost FEW[2][4] = {{{1.14f, .203f}, {1.78f, .202f}, {3.14f, .263f}, {3.52f, .292f}},
-                              {{1.37f, .325f}, {2.58f, .326f}, {4.27f, .326f}, {6.16f, .655f}}};
-  constexpr Cost FIRST[2][3] = {{{1.92f, .245f}, {2.52f, .327f}, {2.8f, .41f}}, {{1.91f, .244f}, {}, {3.12f, .398f}}};
-  constexpr Cost NEXT[2][3] = {{{1.2f, .274f}, {2.05f, .349f}, {3.24f, .399f}}, {{.77f, .26f}, {}, {2.29f, .416f}}};
-  constexpr int PARTS = GATED ? 2 : 1;
-  auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
-  Choice best = {1, 256, 1};
-  float least = 3e38f;
-  auto offer = [&](float cost, Choice c) {
-    if (cost < least) {
-      least = cost;
-      best = c;
-    }
-  };
-  for (int i = 0; i < 4; ++i) {
-    const int nt = 16 << i;
-    if (rows > 32 * nt || (nt > 16 && rows <= nt / 2)) continue;
-    const long long row_tiles = ceil_div(rows, nt), tiles = ceil_div(n, 128) * row_tiles;
-    const int per_sm = nt * PARTS <= 64 ? 2 : 1;
-    for (int split = 1; split <= FEW_SPLIT && split <= kblocks; split *= 2) {
-      // (clusters stay within a group of SMs, whose number eight does not divide)
-      const int held = per_sm * num_sms * (split <= 2 ? 38 : split == 4 ? 36 : per_sm == 2 ? 32 : 26) / 38;
-      const long long ctas = tiles * split, waves = ceil_div(ctas, held);
-      const float reads = static_cast<float>(ctas < held ? ctas : held) * (PARTS * PIECE) / (row_tiles == 1 ? 8.18e6f : 8.06e6f);
-      const Cost c = FEW[GATED][i];
-      offer(0.05f * split + static_cast<float>(waves) * (c.each + static_cast<float>(ceil_div(kblocks, split)) * (reads > c.block ? reads : c.block)),
-            {0, nt, split});
-    }
-  }
-  for (int i = codes ? 2 : 0; i < 3; i += GATED ? 2 : 1) {  // (gated to codes: a tile has whole blocks)
-    const int nt = 128 + 64 * i;
-    const long long rounds = ceil_div(ceil_div(rows, 256) * ceil_div(n, nt / PARTS), num_sms / 2 > 0 ? num_sms / 2 : 1);
-    const Cost f = FIRST[GATED][i], x = NEXT[GATED][i];
-    offer(f.each + static_cast<float>(kblocks) * f.block + static_cast<float>(rounds - 1) * (x.each + static_cast<float>(kblocks) * x.block),
-          {1, nt, 1});
-  }
-  return best;
-}
-
 template <bool GATED>
 cudaError_t launch_kind(const Gemm128Args& a, const Params128& p, int device, int num_sms, cudaStream_t st) {
-  const Choice c = choose<GATED>(a.s.rows, a.s.n, p.kblocks, p.out_type == HILO_E4M3, num_sms);
+  const Gemm128Choice c = gemm128_choice<GATED>(a.s.rows, a.s.n, p.kblocks, p.out_type == HILO_E4M3, num_sms);
   if (c.many) {
     if constexpr (!GATED)
       if (c.nt == 192) return launch_many<192, false>(a, p, device, num_sms, st);
