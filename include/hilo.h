@@ -785,8 +785,10 @@ typedef struct {
  * hilo_gemm_e4m3_128 -- a linear layer: out = A W^T + bias.
  *   a, w        uint8 e4m3 codes, device, 16-byte aligned
  *   a_scale     fp32 [ceil(k / 128)] x a_scale_ld, device; w_scale fp32
- *               [ceil(n / 128)] x w_scale_ld, device: any finite values, e.g.
- *               those of hilo_quantize_e4m3_128
+ *               [ceil(n / 128)] x w_scale_ld, device: finite values, e.g. those of
+ *               hilo_quantize_e4m3_128. A row's scale and a weight's are multiplied in
+ *               fp32 before a block's sum is: their product has to be 0 or normal
+ *               (a smaller one loses bits, a larger one gives infinities and NaN).
  *   bias        bf16 [n], device, or NULL
  *   out         [rows, n] of out_dtype, device, 16-byte aligned, overlaps no input
  * The products of a block are summed by the tensor core in fp32, the blocks,
