@@ -99,3 +99,30 @@ def test_very_many_images(H, B, rows, d, groups, out):
         check_codes(y, sc, want, off)
     else:
         check(y, want, off, out)
+
+
+@pytest.mark.parametrize("B,rows,d,groups", [(1, 3500, 16, 1), (2, 3000, 16, 4), (1, 1700, 32, 8), (3, 900, 48, 6), (40, 1000, 16, 16)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_narrow_images_to_codes(H, B, rows, d, groups, dtype):
+    """Codes take half a warp a row: of 16 channels a thread has up to 224 rows (what shared memory holds of 16-bit values, 3584
+    rows, by sixteen). Their sum is off by 112 half steps of the mean at most (of fp32, at most 112 rows, what corrects it
+    leaves one); with about ten for what follows that is within ordinary sizes' 66 whole steps."""
+    p = Images(B, rows, d, groups, dtype)
+    y, sc = p.run(H, "silu", "e4m3")
+    want, off = p.exact("silu", 1e-5)
+    check_codes(y, sc, want, off)
+
+
+@pytest.mark.parametrize("rows", [50, 20000])
+def test_images_share_scale_and_shift(H, rows):
+    """vec_row 0: one row of scale and shift for all images."""
+    p = Images(3, rows, 64, 8)
+    one = p.cond[:1].clone()
+    p.cond = one.expand(3, -1).contiguous()
+    want, off = p.exact("silu", 1e-5)
+    shape = H.GroupNormShape(B=3, rows=rows, d=64, groups=8, act=H.HILO_ACT_SILU, y_dtype=H.HILO_F32, vec_row=0)
+    n = H.hilo_group_norm_workspace_bytes(shape)
+    y = torch.empty(3 * rows, 64, device="cuda")
+    vectors = H.NormVectors(scale=one[:, :64], shift=one[:, 64:128], w_norm=p.w, b_norm=p.b)
+    H.hilo_group_norm(shape, vectors, p.buf, y, None, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    check(y, want, off, "f32")
