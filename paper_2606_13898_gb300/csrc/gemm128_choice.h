@@ -14,13 +14,12 @@ constexpr int GEMM128_SPLIT = 8;          // CTAs of a cluster of few128 at most
 //   many128<NT>   the first tile of a pair and each further one: an `each` and a `block` of their own (at full load
 //                 the chip is at its power limit)
 // fitted to 252 shapes of 1 to 8192 rows, 512 to 6080 columns, 128 to 16384 features, each with every choice: its pick is 0.5%
-// behind the fastest in the mean, 29% at worst (64 rows of 4096, 1024 features gated: 8.8 us, 6.9 in four tiles of 16
-// rows). Examples, in us: 64 rows of 4096, 4096 features: few128<64> 6.8, few128<16> 9.1; 512 rows: few128<128>
-// 17.2, many128<128> 13.0, many128<256> 18.0; 1024 rows: many128<128> 22.5, many128<256> 19.5; 1300 rows of 6080, 512
-// features: few128<128> 13.9, many128<128> 15.8. 192 columns are for what
-// fills a round with them and leaves a part of one idle with 256: 700 rows of 4096, 4096 features: 17.2, 128 columns 23.3,
-// 256 19.1; 2389 rows: 42.8, 51.6 and 49.6; 8192 rows: 131, 135 and 110. (Of 18 shapes with all three timed each pick was the
-// fastest.)
+// behind the fastest in the mean, 31% at worst (64 rows of 4096, 1024 features gated: 8.8 us, 6.7 in four tiles of 16
+// rows, cut in four). Examples, in us: 64 rows of 4096, 4096 features: few128<64> cut in four 6.6, few128<16> in two 8.7; 512
+// rows: few128<128> 16.9, many128<128> 12.7, many128<256> 17.6; 1024 rows: many128<128> 22.3, many128<256> 19.4; 1300 rows
+// of 6080, 512 features: few128<128> in two 14.1, many128<128> 15.5. 192 columns are for what fills a round with them and leaves
+// a part of one idle with 256: 700 rows of 4096, 4096 features: 16.6, 128 columns 22.0, 256 18.9; 2389 rows: 41.1, 49.5 and 48.6;
+// 8192 rows: 125, 136 and 109. (Of 18 shapes with all three timed each pick was the fastest.)
 struct Gemm128Choice {
   int many;  // few128 otherwise
   int nt, split;

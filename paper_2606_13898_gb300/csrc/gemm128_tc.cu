@@ -16,8 +16,10 @@
 //            cluster, rows (about 4 us).
 //   many128  CTA pairs (cta_group::2): 256 rows on the lanes, NT columns: features, or half of them gate and half up;
 //            a persistent grid. Bound by the chain product, sums, next product in the same buffer, of which tensor memory
-//            holds 512 / NT, and at full load by the chip's power: 4864 rows of 16384, 4096 features 226 us, 2.9
-//            PFLOP/s, 75% of twice the measured bf16 rate; tensor pipe active 51% with 4096 columns.
+//            holds 512 / NT (a block takes 780 cycles with 256 columns, its product 512), by a tile's rows, which leave while
+//            the tensor core waits (2 to 3 us a tile), and at full load by the chip's power besides: 4864 rows of 16384, 4096
+//            features 224 to 239 us, 2.7 to 2.9 PFLOP/s, 71 to 76% of twice the measured bf16 rate; of 4096 columns the tensor pipe
+//            is active 51% of the time.
 //
 // Every mbarrier wait is bounded (error latched, TMEM freed, CTA returns).
 #include <cuda_bf16.h>

@@ -14,15 +14,16 @@
 //
 // Images whose slices of channels (whole groups) fit the shared memory of a cluster: one kernel
 // (group_norm_kernel). A CTA copies its rows of the slice by TMA, finds each group's mean and the squares about it in two
-// passes over them, tells the cluster's other CTAs, and writes. x is read once. 1024 rows of 512 channels take 5.2 us
-// (two kernels: 8.3): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
+// passes over them, tells the cluster's other CTAs, and writes. x is read once. 1024 rows of 512 channels take 5.3 us
+// (two kernels: 8.2): launch and copy 1.8, means and squares 1, groups and cluster 1.7, rows the rest. More rows: bound by
 // the passes over shared memory and the activation, not by HBM (2 TB/s).
 //
 // Other images: two kernels over chunks of rows. The first leaves the pairs of each cluster's chunks in the workspace, the
 // second joins an image's pairs (of many groups a third kernel between the two does) and writes its chunk, from the last row
 // to the first, as the rows read last are the ones still in L2. Bound by HBM: x is read once, and again as far as it is not
-// in L2, y is written once; 2^20 rows of 128 channels in bf16 take 144 us, 5.6 TB/s of three passes (152 us with sums and
-// activations in single registers instead of pairs).
+// in L2, y is written once; 2^20 rows of 128 channels in bf16 take 142 us, 5.7 TB/s of three passes (152 us with sums and
+// activations in single registers instead of pairs). Of fewer than 128 channels, and of 129 to 255 vectors, a part of the threads
+// has no column (a row's vectors are rounded up to sixteen, and a CTA takes whole rows): 2^21 rows of 64 take 212 us.
 #include "e4m3_128.cuh"
 #include "internal.h"
 
@@ -396,8 +397,8 @@ __device__ __forceinline__ Pair join_image(const NormParams& p, const Two& o, lo
 }
 
 // More groups than FEW_GROUPS get a warp each in a kernel of their own; few ones each CTA of the output joins for itself.
-// (65536 rows of 512, in us, for itself and by the kernel: 32 groups 43.0 and 47.0, 64 groups 45.5 and 46.3, 128 groups 51.6 and
-// 50.2, 512 groups 81.8 and 56.1; 16384 rows of 2048 channels, a group each, 218 and 79.)
+// (65536 rows of 512, in us, for itself and by the kernel: 32 groups 42.8 and 48.5, 64 groups 44.6 and 47.4, 128 groups 50.1 and
+// 49.9, 512 groups 75.4 and 58.5.)
 constexpr int FEW_GROUPS = 64;
 __global__ void __launch_bounds__(THREADS) group_join_kernel(const __grid_constant__ NormParams p, const __grid_constant__ Two o, long long groups) {
   pdl_wait();
@@ -650,8 +651,8 @@ int resident_clusters(int parts, int device, int num_sms) {
 // a byte's way, more by CTAs of a cluster and by entries that a lane joins. Against the two kernels' 8.2 us and 1.2 for a
 // million elements. Fitted to 34 shapes of 22 to 65536 rows, 32 to 2304 channels in every slice and number of parts: the pick
 // is 1.6% behind the fastest in the mean, 18% at worst (8 x 82 rows of 2048 6.6 us, 5.6 in wider slices). Examples, in us:
-// 1024 rows of 512 5.2, two kernels 8.3; 3 x 1380 rows of 1152 to codes 10.0 in 10 parts, 11.6 in 8, two kernels 17.6; 16384
-// rows of 512 15.4 in 13 parts, 19.8 in 16 (two waves), two kernels 19.0; 4 x 4096 rows of 512 to codes 20.7, two kernels 18.5.
+// 1024 rows of 512 5.3, two kernels 8.2; 3 x 1380 rows of 1152 to codes 10.1 in 10 parts, 11.6 in 8, two kernels 17.2; 16384
+// rows of 512 15.4 in 13 parts, 19.8 in 16 (two waves), two kernels 18.2; 4 x 4096 rows of 512 to codes 20.7, two kernels 18.2.
 constexpr float NO_PLAN = 3e38f;
 template <int TYPE>
 float plan_one(const hilo_group_norm_shape& s, int device, int num_sms, One* best) {
