@@ -263,7 +263,7 @@ constexpr int THREADS = 256;
 constexpr int STATS_CTAS = 3, APPLY_CTAS = 3;  // per SM (four: the sums spill, 2^20 rows of 128 took 1.2 and 1.35 times as long)
 constexpr int MAX_CHUNKS = 456;                // of a call's statistics, but for a cluster per image
 constexpr int CHUNKS = 4;                      // of a cluster, whose pairs are joined before they are stored
-constexpr int BATCH = 4;                       // rows of a thread at a time (eight: 2^20 rows of 128 148 us, 144 so)
+constexpr int BATCH = 4;                       // rows of a thread at a time (eight: 2^20 rows of 128 in 3% more)
 constexpr int JOINED = MAX_CHUNKS / CHUNKS / 32 + 1;  // pairs of a lane
 
 // The chunks of an image: of its statistics and of its output.
@@ -527,8 +527,12 @@ __global__ void __launch_bounds__(ONE_THREADS, 2)
   const float inv_n = __fdividef(1.f, static_cast<float>(n) * static_cast<float>(p.per));
   float a[8], b[8];
   if (on) gains(p, image, c0 + c, a, b);  // beside the copies
-  // (a wait that ran out leaves an error and rows that are not meant to be right)
-  if (n > 0) mbar_wait(bar, 0, abort_flag, &g_group_norm_err, DEV_TIMEOUT_GEMM + 256 * 30);
+  // (a wait that ran out leaves an error and rows that are not meant to be right; the copies in flight once more, before the CTA exits)
+  if (n > 0 && !mbar_wait(bar, 0, abort_flag, &g_group_norm_err, DEV_TIMEOUT_GEMM + 256 * 30)) {
+    const uint64_t g0 = globaltimer_ns();
+    while (!mbar_try_wait(smem_u32(bar), 0) && globaltimer_ns() - g0 < HILO_WAIT_LIMIT_NS / 4) {
+    }
+  }
   const int pitch = o.wide * ESIZE;
   auto at = [&](int r) { return tile + r * pitch + c * ESIZE; };
   // the thread's pairs: its means, then the squares about them
